@@ -78,7 +78,8 @@ enum {
                                or a source stride smaller than one slab */
     FC_ERR_ALIGN = -5,      /* pointer or stride not 16-byte aligned */
     FC_ERR_WORKSPACE = -6,  /* workspace NULL or too small */
-    FC_ERR_HIP = -7         /* kernel launch failed; see fc_last_hip_error() */
+    FC_ERR_HIP = -7,        /* kernel launch failed; see fc_last_hip_error() */
+    FC_ERR_TYPE = -8        /* element type, or quantizer, that the call does not take */
 };
 
 /*
@@ -296,6 +297,89 @@ FC_API int fc_dequantize_rot(const void *codes, const float *scales, const float
 FC_API int fc_allreduce_sim_rot(const void *x_f16, int n_src, int64_t tokens, int64_t hidden,
                                 int group, int bits_rs, int bits_ag, int quantizer, void *y_f16,
                                 void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * ---- Attention of a tensor-parallel rank: what runs between its projections, before the all-reduce above ----
+ *
+ * Activations are 16-bit (`type`: FC_TYPE_F16 or FC_TYPE_BF16) tensors [tokens, heads, dim] whose last axis is dense; token and head
+ * strides are in elements, any multiple of 8 (views of a joint projection pass as they are), base pointers are 16-byte
+ * aligned.  Arithmetic and sums are in fp32.
+ *
+ * Sequences are packed: the call's new tokens of sequence b are offsets[b] <= t < offsets[b + 1] (int32 [sequences + 1], offsets[0] = 0,
+ * ascending, offsets[sequences] = tokens; equal neighbours: nothing new).  All index arrays are device memory; the kernels
+ * check what they read from them, and a token, page or position outside its tensor is neither read nor written.
+ */
+#define FC_TYPE_F16 0
+#define FC_TYPE_BF16 1
+
+/*
+ * The table of a rotation: for row r and pair i < rotary / 2, with angle = r * frequencies[i] in 64 bits,
+ *     table[r, i] = magnitude * cos(angle),  table[r, rotary / 2 + i] = magnitude * sin(angle)
+ * frequencies: double [rotary / 2], device memory.  table: float [rows, rotary].
+ */
+FC_API int fc_rotary_table(const double *frequencies, int64_t rows, int rotary, double magnitude, float *table, void *hip_stream);
+
+/*
+ * Rotary positions: of the first `rotary` elements of each head (even, at most dim), pair i turns by row positions[t] of the table,
+ *     a' = a cos - b sin,  b' = b cos + a sin       (inverse != 0: with -sin, which is also the gradient)
+ * a, b = elements i and i + rotary / 2, or interleaved != 0: 2 i and 2 i + 1.  Each product and sum is rounded to fp32, the
+ * result once to the type; other elements are copied.  A position without a row gives NaN.  y == x with equal strides is allowed.
+ * dim: a multiple of 8 up to 4096.
+ */
+FC_API int fc_rotary(const void *x, int64_t x_token_stride, int64_t x_head_stride, const float *table, int64_t table_rows,
+                     const int32_t *positions, int64_t tokens, int heads, int dim, int rotary, int interleaved, int inverse, int type,
+                     void *y, int64_t y_token_stride, int64_t y_head_stride, void *hip_stream);
+
+/*
+ * The paged cache of keys and values in 8-bit codes (quantizer FC_QUANTIZER_SYM: signed bytes, FC_QUANTIZER_FP8: E4M3):
+ *     k_cache, v_cache    bytes [pages, heads, page, dim];  page in {16, 32, 64}, dim in {64, 128, 256}
+ *     k_scales, v_scales  float [pages, heads]: an element is its code's value times its page's scale
+ *     page_table          int32 [sequences, table_width]: page of a sequence's tokens [i * page, (i + 1) * page)
+ *     held                int32 [sequences]: tokens that the sequence holds before this step's.  Negative: the step's first -held
+ *                         tokens have no place and are left out (a padded batch's empty slots: held = -1 and one token)
+ *
+ * fc_cache_append puts the step's tokens behind those held.  Keys turn to their positions on the way if rotary > 0 (table as for
+ * fc_rotary; rotary = 0: table may be NULL).  For every page and head that receives tokens, with x the fp32 key or value and top =
+ * 127 or 448, results are bit-identical to
+ *     s' = max(max|x| / top, FLT_MIN, s)        s: the page's scale, only if it holds tokens of the sequence already and
+ *                                                the scale is a number
+ *     code' = round(code * (s / s'))            of those tokens, where s' > s
+ *     code' = round(x * (1 / s'))               of the new ones; signed codes are clamped to +-127
+ * with IEEE divides, each operation rounded to nearest even.  A token beyond page table or rotation table is left out.
+ * x must be finite.  A page that receives tokens belongs to one sequence.  longest: no sequence gets more new tokens.
+ */
+FC_API int fc_cache_append(const void *k, int64_t k_token_stride, int64_t k_head_stride, const void *v, int64_t v_token_stride,
+                           int64_t v_head_stride, int64_t tokens, int heads, int dim, int type, const float *table, int64_t table_rows,
+                           int rotary, int interleaved, int quantizer, void *k_cache, void *v_cache, float *k_scales, float *v_scales,
+                           int64_t pages, int page, const int32_t *page_table, int table_width, const int32_t *offsets,
+                           const int32_t *held, int sequences, int64_t longest, void *hip_stream);
+
+/*
+ * Attention over that cache, after the step's tokens were appended (same offsets, held, page_table): query i of a sequence sees its
+ * tokens t < held + i + 1,
+ *     o = sum_t w_t v_t,  w = softmax over t of scale * q . k_t
+ * q, out: [tokens, heads * group, dim]; query heads h * group ... use key/value head h.  A query that sees nothing gets zeros;
+ * what the pages hold beyond the tokens of the sequence has no influence.
+ * queries, longest: the most new tokens, and the most tokens in all, of a sequence.  They size the launch and the workspace;
+ * sequences beyond them are computed all the same, more slowly.
+ * workspace: fc_cache_attention_workspace_bytes(...) bytes, 16-byte aligned, contents unspecified; may be NULL if that is 0.
+ */
+FC_API size_t fc_cache_attention_workspace_bytes(int64_t tokens, int sequences, int heads, int group, int dim, int64_t queries, int64_t longest);
+FC_API int fc_cache_attention(const void *q, int64_t q_token_stride, int64_t q_head_stride, int64_t tokens, int heads, int group, int dim,
+                              int type, int quantizer, const void *k_cache, const void *v_cache, const float *k_scales,
+                              const float *v_scales, int64_t pages, int page, const int32_t *page_table, int table_width,
+                              const int32_t *offsets, const int32_t *held, int sequences, int64_t queries, int64_t longest, float scale,
+                              void *out, int64_t out_token_stride, int64_t out_head_stride, void *workspace, size_t workspace_bytes,
+                              void *hip_stream);
+
+/*
+ * Attention of whole prompts to themselves: query i of a sequence sees all its tokens, or causal != 0: those up to i.
+ * q, out: [tokens, heads * group, dim]; k, v: [tokens, heads, dim]; dim in {64, 128}.  longest: no sequence is longer.
+ */
+FC_API int fc_prompt_attention(const void *q, int64_t q_token_stride, int64_t q_head_stride, const void *k, int64_t k_token_stride,
+                               int64_t k_head_stride, const void *v, int64_t v_token_stride, int64_t v_head_stride, int64_t tokens,
+                               int heads, int group, int dim, int type, const int32_t *offsets, int sequences, int64_t longest, int causal,
+                               float scale, void *out, int64_t out_token_stride, int64_t out_head_stride, void *hip_stream);
 
 /* Static, NUL-terminated description of an FC_* code.  Host pointer, never NULL. */
 FC_API const char *fc_strerror(int code);

@@ -43,6 +43,15 @@ from .binding import (  # noqa: F401
     strerror,
     version,
 )
+from .attention import (  # noqa: F401
+    cache_append,
+    cache_attention,
+    cache_attention_workspace_bytes,
+    prompt_attention,
+    rotary,
+    rotary_frequencies,
+    rotary_table,
+)
 
 __all__ = [
     "QUANTIZER_ASYM", "QUANTIZER_FP8", "QUANTIZER_SYM", "allreduce_sim_rot", "dequantize_rot", "quantize_rot",
@@ -51,5 +60,7 @@ __all__ = [
     "dequant_reduce_requant", "dequant_reduce_requant_fp8", "dequant_reduce_requant_sym", "dequantize",
     "dequantize_fp8", "dequantize_sym", "last_hip_error", "lib", "lib_path", "quantize", "quantize_fp8",
     "quantize_sym", "strerror", "version",
+    "cache_append", "cache_attention", "cache_attention_workspace_bytes", "prompt_attention", "rotary",
+    "rotary_frequencies", "rotary_table",
     "allreduce_sim_cmeta", "dequant_reduce_requant_cmeta", "dequantize_cmeta", "quantize_cmeta",
 ]

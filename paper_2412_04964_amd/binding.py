@@ -102,6 +102,22 @@ def lib() -> ctypes.CDLL:
         L.fc_dequantize_rot.restype = i32
         L.fc_allreduce_sim_rot.argtypes = [vp, i32, i64, i64, i32, i32, i32, i32, vp, vp, sz, vp]
         L.fc_allreduce_sim_rot.restype = i32
+        f32, f64 = ctypes.c_float, ctypes.c_double
+        rows = [vp, i64, i64]                            # a tensor [tokens, heads, dim]: address, token stride, head stride
+        L.fc_rotary_table.argtypes = [vp, i64, i32, f64, vp, vp]
+        L.fc_rotary_table.restype = i32
+        L.fc_rotary.argtypes = [*rows, vp, i64, vp, i64, i32, i32, i32, i32, i32, i32, *rows, vp]
+        L.fc_rotary.restype = i32
+        L.fc_cache_append.argtypes = [*rows, *rows, i64, i32, i32, i32, vp, i64, i32, i32, i32, vp, vp, vp, vp, i64, i32, vp, i32,
+                                      vp, vp, i32, i64, vp]
+        L.fc_cache_append.restype = i32
+        L.fc_cache_attention_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i64, i64]
+        L.fc_cache_attention_workspace_bytes.restype = sz
+        L.fc_cache_attention.argtypes = [*rows, i64, i32, i32, i32, i32, i32, vp, vp, vp, vp, i64, i32, vp, i32, vp, vp, i32, i64,
+                                         i64, f32, *rows, vp, sz, vp]
+        L.fc_cache_attention.restype = i32
+        L.fc_prompt_attention.argtypes = [*rows, *rows, *rows, i64, i32, i32, i32, i32, vp, i32, i64, i32, f32, *rows, vp]
+        L.fc_prompt_attention.restype = i32
         L.fc_strerror.argtypes = [i32]
         L.fc_strerror.restype = ctypes.c_char_p
         L.fc_last_hip_error.argtypes = []

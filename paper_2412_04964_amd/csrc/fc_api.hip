@@ -50,12 +50,7 @@ int check_shape(int64_t tokens, int64_t hidden, int group, int bits, int64_t *n_
     return FC_OK;
 }
 
-int hip_result(hipError_t e)
-{
-    if (e == hipSuccess) return FC_OK;
-    g_last_hip_error = (int)e;
-    return FC_ERR_HIP;
-}
+using fc::hip_result;
 
 struct SimLayout {
     size_t codes_rs;     // bytes of one source's codes
@@ -356,6 +351,13 @@ bool rot_steps_apply(int codec, int bits_rs, int n_src, int64_t n_elems, int64_t
 
 }  // namespace
 
+int fc::hip_result(hipError_t e)
+{
+    if (e == hipSuccess) return FC_OK;
+    g_last_hip_error = (int)e;
+    return FC_ERR_HIP;
+}
+
 extern "C" {
 
 int fc_quantize(const void *x_f16, int64_t tokens, int64_t hidden, int group, int bits,
@@ -564,9 +566,10 @@ const char *fc_strerror(int code)
     case FC_ERR_NULL: return "a required pointer is NULL";
     case FC_ERR_BITS: return "bit-width must be 4 or 8";
     case FC_ERR_GROUP: return "group must be a power of two in [32, 16384] that divides hidden";
-    case FC_ERR_SHAPE: return "bad tokens / hidden / n_src / source stride";
+    case FC_ERR_SHAPE: return "bad tokens / hidden / n_src / source stride, or bad heads / head size / rotary part / pages of an attention call";
     case FC_ERR_ALIGN: return "pointers and strides must be 16-byte aligned";
     case FC_ERR_WORKSPACE: return "workspace missing or too small (or volume beyond the static scratch)";
+    case FC_ERR_TYPE: return "element type or quantizer not supported by this call";
     case FC_ERR_HIP: return "HIP launch failed (see fc_last_hip_error)";
     default: return "unknown error code";
     }

@@ -1,0 +1,222 @@
+// fc_attn_api.hip -- the extern "C" boundary of the attention operators declared in include/fc.h: argument checks (no HIP call
+// before they pass) and the choice of a launch.
+#include "fc.h"
+
+#include "fc_attn.hpp"
+
+namespace {
+
+constexpr int kMaxHeads = 1 << 16;
+constexpr int64_t kMaxTokens = 0x7FFFFFFF;
+
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+int check_type(int type) { return type == FC_TYPE_F16 || type == FC_TYPE_BF16 ? FC_OK : FC_ERR_TYPE; }
+int check_code(int quantizer) { return quantizer == FC_QUANTIZER_SYM || quantizer == FC_QUANTIZER_FP8 ? FC_OK : FC_ERR_TYPE; }
+
+// 128-bit accesses: base and strides in whole units of 8 elements
+int check_rows(const void *p, int64_t token_stride, int64_t head_stride)
+{
+    if (!p) return FC_ERR_NULL;
+    return aligned16(p) && token_stride % 8 == 0 && head_stride % 8 == 0 ? FC_OK : FC_ERR_ALIGN;
+}
+
+fc::Rows rows(const void *p, int64_t token_stride, int64_t head_stride) { return {const_cast<void *>(p), token_stride, head_stride}; }
+
+int check_heads(int heads, int64_t tokens, int sequences)
+{
+    if (heads < 1 || heads > kMaxHeads || tokens < 0 || tokens > kMaxTokens || sequences < 0) return FC_ERR_SHAPE;
+    return tokens > 0 && sequences == 0 ? FC_ERR_SHAPE : FC_OK;
+}
+
+int check_rotary(int64_t table_rows, int rotary, int dim)
+{
+    return rotary >= 0 && rotary % 2 == 0 && rotary <= dim && table_rows >= 0 ? FC_OK : FC_ERR_SHAPE;
+}
+
+int check_cache(const void *k, const void *v, const float *k_scales, const float *v_scales, int64_t pages, int page, const int32_t *table,
+                int table_width)
+{
+    if ((page != 16 && page != 32 && page != 64) || pages < 1 || pages > kMaxTokens || table_width < 1) return FC_ERR_SHAPE;
+    if (!k || !v || !k_scales || !v_scales || !table) return FC_ERR_NULL;
+    return aligned16(k) && aligned16(v) ? FC_OK : FC_ERR_ALIGN;
+}
+
+// a launch of this many workgroups of `lanes` is one that the runtime takes
+bool launchable(int64_t workgroups, int lanes) { return workgroups <= ((int64_t)1 << 32) / lanes - 1; }
+
+struct Split { int splits, row_blocks; };
+Split plan(int sequences, int heads, int group, int64_t queries, int64_t longest)
+{
+    Split s;
+    fc::cache_attention_plan(sequences, heads, group, queries, longest, &s.splits, &s.row_blocks);
+    return s;
+}
+
+size_t partial_bytes(int64_t tokens, int query_heads, int dim, int splits)
+{
+    return splits == 1 ? 0 : (size_t)tokens * (size_t)query_heads * (size_t)splits * (size_t)(dim + 2) * sizeof(float);
+}
+
+int check_attention(int64_t tokens, int sequences, int heads, int group, int dim, int64_t queries, int64_t longest)
+{
+    const int rc = check_heads(heads, tokens, sequences);
+    if (rc != FC_OK) return rc;
+    if (group < 1 || (int64_t)heads * group > kMaxHeads || (dim != 64 && dim != 128 && dim != 256)) return FC_ERR_SHAPE;
+    return queries < 1 || queries > kMaxTokens || longest < 1 || longest > kMaxTokens ? FC_ERR_SHAPE : FC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int fc_rotary_table(const double *frequencies, int64_t rows_, int rotary, double magnitude, float *table, void *hip_stream)
+{
+    if (rotary < 2 || rotary % 2 || rotary > 4096 || rows_ < 0 || rows_ > kMaxTokens) return FC_ERR_SHAPE;
+    if (rows_ == 0) return FC_OK;
+    if (!frequencies || !table) return FC_ERR_NULL;
+    if (!launchable((rows_ * (rotary / 2) + 255) / 256, 256)) return FC_ERR_SHAPE;
+    return fc::hip_result(fc::launch_rotary_table(frequencies, rows_, rotary, magnitude, table, static_cast<hipStream_t>(hip_stream)));
+}
+
+int fc_rotary(const void *x, int64_t x_token_stride, int64_t x_head_stride, const float *table, int64_t table_rows,
+              const int32_t *positions, int64_t tokens, int heads, int dim, int rotary, int interleaved, int inverse, int type,
+              void *y, int64_t y_token_stride, int64_t y_head_stride, void *hip_stream)
+{
+    int rc = check_type(type);
+    if (rc != FC_OK) return rc;
+    if ((rc = check_heads(heads, tokens, 1)) != FC_OK) return rc;
+    if (dim < 8 || dim % 8 || dim > 4096 || rotary < 2 || (rc = check_rotary(table_rows, rotary, dim)) != FC_OK) return FC_ERR_SHAPE;
+    if (tokens == 0) return FC_OK;
+    if (!table || !positions) return FC_ERR_NULL;
+    if ((rc = check_rows(x, x_token_stride, x_head_stride)) != FC_OK) return rc;
+    if ((rc = check_rows(y, y_token_stride, y_head_stride)) != FC_OK) return rc;
+    if (!launchable((tokens * heads * dim + 255) / 256, 256)) return FC_ERR_SHAPE;
+    fc::RotaryArgs a;
+    a.x = rows(x, x_token_stride, x_head_stride);
+    a.y = rows(y, y_token_stride, y_head_stride);
+    a.table = table;
+    a.table_rows = table_rows;
+    a.tokens = tokens;
+    a.positions = positions;
+    a.heads = heads;
+    a.dim = dim;
+    a.rotary = rotary;
+    a.interleaved = interleaved != 0;
+    a.inverse = inverse != 0;
+    a.bf16 = type == FC_TYPE_BF16;
+    return fc::hip_result(fc::launch_rotary(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+int fc_cache_append(const void *k, int64_t k_token_stride, int64_t k_head_stride, const void *v, int64_t v_token_stride, int64_t v_head_stride,
+                    int64_t tokens, int heads, int dim, int type, const float *table, int64_t table_rows, int rotary, int interleaved,
+                    int quantizer, void *k_cache, void *v_cache, float *k_scales, float *v_scales, int64_t pages, int page,
+                    const int32_t *page_table, int table_width, const int32_t *offsets, const int32_t *held, int sequences, int64_t longest,
+                    void *hip_stream)
+{
+    int rc = check_type(type);
+    if (rc != FC_OK || (rc = check_code(quantizer)) != FC_OK) return rc;
+    if ((rc = check_heads(heads, tokens, sequences)) != FC_OK) return rc;
+    if ((dim != 64 && dim != 128 && dim != 256) || longest < 1) return FC_ERR_SHAPE;
+    if ((rc = check_rotary(table_rows, rotary, dim)) != FC_OK) return rc;
+    if (tokens == 0) return FC_OK;
+    if ((rc = check_cache(k_cache, v_cache, k_scales, v_scales, pages, page, page_table, table_width)) != FC_OK) return rc;
+    if (!offsets || !held || (rotary && !table)) return FC_ERR_NULL;
+    if ((rc = check_rows(k, k_token_stride, k_head_stride)) != FC_OK) return rc;
+    if ((rc = check_rows(v, v_token_stride, v_head_stride)) != FC_OK) return rc;
+    if (!launchable((tokens / page + 2 * (int64_t)sequences) * 2 * heads, 512)) return FC_ERR_SHAPE;
+    fc::AppendArgs a;
+    a.k = rows(k, k_token_stride, k_head_stride);
+    a.v = rows(v, v_token_stride, v_head_stride);
+    a.step = {offsets, held, sequences, tokens};
+    a.cache = {static_cast<uint8_t *>(k_cache), static_cast<uint8_t *>(v_cache), k_scales, v_scales, page_table, pages, page, table_width};
+    a.table = table;
+    a.table_rows = table_rows;
+    a.longest = longest;
+    a.heads = heads;
+    a.dim = dim;
+    a.rotary = rotary;
+    a.interleaved = interleaved != 0;
+    a.fp8 = quantizer == FC_QUANTIZER_FP8;
+    a.bf16 = type == FC_TYPE_BF16;
+    return fc::hip_result(fc::launch_cache_append(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+size_t fc_cache_attention_workspace_bytes(int64_t tokens, int sequences, int heads, int group, int dim, int64_t queries, int64_t longest)
+{
+    if (check_attention(tokens, sequences, heads, group, dim, queries, longest) != FC_OK) return 0;
+    return partial_bytes(tokens, heads * group, dim, plan(sequences, heads, group, queries, longest).splits);
+}
+
+int fc_cache_attention(const void *q, int64_t q_token_stride, int64_t q_head_stride, int64_t tokens, int heads, int group, int dim, int type,
+                       int quantizer, const void *k_cache, const void *v_cache, const float *k_scales, const float *v_scales, int64_t pages,
+                       int page, const int32_t *page_table, int table_width, const int32_t *offsets, const int32_t *held, int sequences,
+                       int64_t queries, int64_t longest, float scale, void *out, int64_t out_token_stride, int64_t out_head_stride,
+                       void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    int rc = check_type(type);
+    if (rc != FC_OK || (rc = check_code(quantizer)) != FC_OK) return rc;
+    if ((rc = check_attention(tokens, sequences, heads, group, dim, queries, longest)) != FC_OK) return rc;
+    if (tokens == 0) return FC_OK;
+    if ((rc = check_cache(k_cache, v_cache, k_scales, v_scales, pages, page, page_table, table_width)) != FC_OK) return rc;
+    if (!offsets || !held) return FC_ERR_NULL;
+    if ((rc = check_rows(q, q_token_stride, q_head_stride)) != FC_OK) return rc;
+    if ((rc = check_rows(out, out_token_stride, out_head_stride)) != FC_OK) return rc;
+    const Split s = plan(sequences, heads, group, queries, longest);
+    const size_t need = partial_bytes(tokens, heads * group, dim, s.splits);
+    if (need && (!workspace || workspace_bytes < need)) return FC_ERR_WORKSPACE;
+    if (need && !aligned16(workspace)) return FC_ERR_ALIGN;
+    if (!launchable((int64_t)sequences * s.row_blocks * heads * s.splits, 256) || !launchable(tokens * heads * group, 256)) return FC_ERR_SHAPE;
+    fc::CacheAttentionArgs a;
+    a.q = rows(q, q_token_stride, q_head_stride);
+    a.out = rows(out, out_token_stride, out_head_stride);
+    a.step = {offsets, held, sequences, tokens};
+    a.cache = {static_cast<uint8_t *>(const_cast<void *>(k_cache)), static_cast<uint8_t *>(const_cast<void *>(v_cache)),
+               const_cast<float *>(k_scales), const_cast<float *>(v_scales), page_table, pages, page, table_width};
+    a.partial = static_cast<float *>(workspace);
+    a.scale = scale;
+    a.heads = heads;
+    a.group = group;
+    a.dim = dim;
+    a.fp8 = quantizer == FC_QUANTIZER_FP8;
+    a.bf16 = type == FC_TYPE_BF16;
+    a.splits = s.splits;
+    a.row_blocks = s.row_blocks;
+    return fc::hip_result(fc::launch_cache_attention(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+int fc_prompt_attention(const void *q, int64_t q_token_stride, int64_t q_head_stride, const void *k, int64_t k_token_stride,
+                        int64_t k_head_stride, const void *v, int64_t v_token_stride, int64_t v_head_stride, int64_t tokens, int heads,
+                        int group, int dim, int type, const int32_t *offsets, int sequences, int64_t longest, int causal, float scale,
+                        void *out, int64_t out_token_stride, int64_t out_head_stride, void *hip_stream)
+{
+    int rc = check_type(type);
+    if (rc != FC_OK) return rc;
+    if ((rc = check_attention(tokens, sequences, heads, group, dim, 1, longest)) != FC_OK) return rc;
+    if (dim == 256) return FC_ERR_SHAPE;
+    if (tokens == 0) return FC_OK;
+    if (!offsets) return FC_ERR_NULL;
+    if ((rc = check_rows(q, q_token_stride, q_head_stride)) != FC_OK) return rc;
+    if ((rc = check_rows(k, k_token_stride, k_head_stride)) != FC_OK) return rc;
+    if ((rc = check_rows(v, v_token_stride, v_head_stride)) != FC_OK) return rc;
+    if ((rc = check_rows(out, out_token_stride, out_head_stride)) != FC_OK) return rc;
+    if (!launchable((tokens / 64 + sequences) * heads * group, 512)) return FC_ERR_SHAPE;
+    fc::PromptArgs a;
+    a.q = rows(q, q_token_stride, q_head_stride);
+    a.k = rows(k, k_token_stride, k_head_stride);
+    a.v = rows(v, v_token_stride, v_head_stride);
+    a.out = rows(out, out_token_stride, out_head_stride);
+    a.offsets = offsets;
+    a.tokens = tokens;
+    a.longest = longest;
+    a.scale = scale;
+    a.sequences = sequences;
+    a.heads = heads;
+    a.group = group;
+    a.dim = dim;
+    a.causal = causal != 0;
+    a.bf16 = type == FC_TYPE_BF16;
+    return fc::hip_result(fc::launch_prompt_attention(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+}  // extern "C"

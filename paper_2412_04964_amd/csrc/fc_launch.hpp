@@ -48,6 +48,9 @@ inline size_t lds_to_limit(int groups, size_t own)
     return each > own ? each - own : 0;
 }
 
+// A launch's status as an FC_* code; a failure is kept for fc_last_hip_error (fc_api.hip).
+int hip_result(hipError_t e);
+
 // Quantizer: 0 = asymmetric (Eq. 1-2), 1 = symmetric (Eq. 3-4), 2 = FP8 E4M3 (8 bit only),
 // 3 = asymmetric with binary16 metadata (one 32-bit word per group, passed where the other
 // codecs pass `scales`); the values match kAsym / kSym / kFp8 / kAsymH of the device code.

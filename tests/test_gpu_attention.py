@@ -1,0 +1,550 @@
+"""The attention operators on the GPU: rotation and append bit for bit against the formulas of include/fc.h in fp32 on the CPU,
+attention against its definition in 64 bits.
+
+Tolerances of attention, per element, from the roundings the kernels make (u = 2^-11 for float16, 2^-9 for bfloat16, half a unit in
+the last place): one of the result, u |o|; and of each weight, relatively, one to the weights' type, and less than 2^-12 from the
+fp32 score (dims of 256 at most, |score| < 64) and from the sums.  With E = sum_t w_t |v_t| the error is below
+(u_w + 2^-11) E + u |o|, which the tests allow twice, plus the smallest subnormal numbers."""
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+F16, BF16 = torch.float16, torch.bfloat16
+FLT_MIN = 1.1754943508222875e-38
+SYM, FP8 = 1, 2
+TOP = {SYM: 127.0, FP8: 448.0}
+
+
+@pytest.fixture(scope="module")
+def fc():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests selected but no GPU is visible")
+    import paper_2412_04964_amd as m
+    m.lib()
+    return m
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def ints(values):
+    return torch.tensor(values, dtype=torch.int32, device="cuda")
+
+
+def offsets_of(lengths):
+    return ints([0] + list(np.cumsum(lengths)))
+
+
+def bits(t):
+    return t.cpu().contiguous().view(torch.int16 if t.element_size() == 2 else torch.int32)
+
+
+def same(a, b):
+    """equal bits, any NaN equal to any other"""
+    a, b = a.cpu(), b.cpu()
+    nan = torch.isnan(a) & torch.isnan(b)
+    return bool(((bits(a) == bits(b)) | nan).all())
+
+
+def fused(tokens, counts, dim, dtype, seed, spread=1.0):
+    """slices of one joint projection [tokens, sum of counts, dim], on the GPU"""
+    x = (torch.randn((tokens, sum(counts), dim), generator=gen(seed)) * spread).to(dtype).cuda()
+    return x.split(list(counts), dim=1)
+
+
+# ---- rotation ----
+
+def turned(x, table, positions, interleaved, inverse=False):
+    """x float32 [tokens, heads, dim]; each operation rounded to fp32"""
+    rotary = table.shape[1]
+    half = rotary // 2
+    y = x.clone()
+    ok = (positions >= 0) & (positions < table.shape[0])
+    row = table[positions.clamp(0, table.shape[0] - 1).long()]
+    row = torch.where(ok[:, None], row, torch.full_like(row, math.nan))
+    c, s = row[:, None, :half], row[:, None, half:]
+    if inverse:
+        s = -s
+    lo, hi = (slice(0, rotary, 2), slice(1, rotary, 2)) if interleaved else (slice(0, half), slice(half, rotary))
+    a, b = x[..., lo], x[..., hi]
+    y[..., lo] = a * c - b * s
+    y[..., hi] = b * c + a * s
+    return y
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dim,rotary", [(128, 128), (64, 32), (80, 80), (96, 24), (128, 2), (8, 6), (256, 144)])
+def test_rotary_matches_the_formula_bit_for_bit(fc, dtype, interleaved, dim, rotary):
+    for tokens, heads in ((1, 1), (3, 5), (67, 9)):
+        print("rotary", dtype, interleaved, dim, rotary, tokens, heads, flush=True)
+        x, _ = fused(tokens, (heads, 2), dim, dtype, tokens + dim)
+        table = fc.rotary_table(301, fc.rotary_frequencies(rotary))
+        positions = torch.randint(0, 301, (tokens,), generator=gen(tokens)).to(torch.int32)
+        positions[0] = 300
+        if tokens > 3:
+            positions[1], positions[2] = -1, 301                     # no such rows
+        for inverse in (False, True):
+            y = fc.rotary(x, table, positions.cuda(), interleaved, inverse)
+            assert same(y, turned(x.float().cpu(), table.cpu(), positions, interleaved, inverse).to(dtype))
+
+
+def test_rotary_in_place_and_its_inverse(fc):
+    q, rest = fused(33, (6, 3), 128, BF16, 1)
+    table = fc.rotary_table(64, fc.rotary_frequencies(128))
+    positions = torch.arange(33, dtype=torch.int32, device="cuda")
+    before, beside = q.clone(), rest.clone()
+    want = fc.rotary(q, table, positions)
+    assert fc.rotary(q, table, positions, out=q) is q
+    assert same(q, want) and same(rest, beside)
+    back = fc.rotary(q, table, positions, inverse=True)
+    assert (back.float() - before.float()).abs().max() <= 2 * 2.0 ** -8 * before.float().abs().max()
+
+
+def test_inverse_rotation_is_the_gradient(fc):
+    # the rotation is linear: <R x, g> = <x, R' g>, and differences of a linear map are exact up to the two roundings
+    x, g = fused(7, (4, 4), 64, F16, 2)
+    table = fc.rotary_table(16, fc.rotary_frequencies(48))
+    p = torch.arange(7, dtype=torch.int32, device="cuda")
+    for interleaved in (False, True):
+        y, gx = fc.rotary(x, table, p, interleaved), fc.rotary(g, table, p, interleaved, inverse=True)
+        left, right = (y.double() * g.double()).sum(), (x.double() * gx.double()).sum()
+        bound = 2.0 ** -10 * ((y.double() * g.double()).abs().sum() + (x.double() * gx.double()).abs().sum())
+        assert abs(left - right) <= bound
+
+
+def test_rotary_table_has_the_angles_of_64_bits(fc):
+    for method in ("none", "linear", "base", "bands", "ramp"):
+        f = fc.rotary_frequencies(64, method=method, factor=4.0, original=2048, low=1.0, high=32.0 if method == "ramp" else 4.0)
+        table = fc.rotary_table(100001, f, 1.25).cpu()
+        angle = torch.arange(100001, dtype=torch.float64)[:, None] * f
+        want = torch.cat([angle.cos(), angle.sin()], 1) * 1.25
+        assert (table.double() - want).abs().max() <= 2.0 ** -24 * 1.25 * 2
+
+
+# ---- the cache ----
+
+def codes_of(x, quantizer):
+    """fp32 -> codes, nearest even"""
+    if quantizer == SYM:
+        return x.round().clamp(-127, 127).to(torch.int8).view(torch.uint8)
+    return x.to(torch.float8_e4m3fn).view(torch.uint8)
+
+
+def values_of(codes, quantizer, dtype=torch.float32):
+    return codes.view(torch.int8 if quantizer == SYM else torch.float8_e4m3fn).to(dtype)
+
+
+def append_one(codes, scales, table, offsets, held, x, quantizer, limit):
+    """the header's formulas, page by page and token by token; x float32 [tokens, heads, dim], all on the CPU"""
+    page = codes.shape[2]
+    top = torch.tensor(TOP[quantizer])
+    for b in range(len(held)):
+        first = offsets[b]
+        places = [(held[b] + i, first + i) for i in range(offsets[b + 1] - first)]
+        places = [(p, t) for p, t in places if 0 <= p < min(limit, table.shape[1] * page)]
+        for index in sorted({p // page for p, _ in places}):
+            mine = [(p % page, t) for p, t in places if p // page == index]
+            id = int(table[b, index])
+            if not 0 <= id < codes.shape[0]:
+                continue
+            filled = mine[0][0]
+            most = torch.stack([x[t] for _, t in mine]).abs().amax((0, 2))
+            now = torch.maximum(most / top, torch.full_like(most, FLT_MIN))
+            if filled:
+                before = scales[id].clone()
+                now = torch.fmax(now, before)                                    # a NaN scale says nothing
+                for h in range(codes.shape[1]):
+                    if now[h] > before[h]:
+                        codes[id, h, :filled] = codes_of(values_of(codes[id, h, :filled], quantizer) * (before[h] / now[h]), quantizer)
+            inverse = torch.ones_like(now) / now
+            scales[id] = now
+            for slot, t in mine:
+                codes[id, :, slot] = codes_of(x[t] * inverse[:, None], quantizer)
+
+
+def new_cache(pages, heads, page, dim, seed=0, fill=None):
+    """junk: whatever a page held before, NaN codes among it"""
+    c = [torch.randint(0, 256, (pages, heads, page, dim), generator=gen(seed + i), dtype=torch.uint8) if fill is None else
+         torch.full((pages, heads, page, dim), fill, dtype=torch.uint8) for i in range(2)]
+    s = [torch.full((pages, heads), math.nan) for _ in range(2)]
+    return tuple(t.cuda() for t in (*c, *s))
+
+
+def page_table(sequences, width, pages, seed):
+    order = torch.randperm(pages, generator=gen(seed))[:sequences * width]
+    return order.view(sequences, width).to(torch.int32)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("quantizer", [SYM, FP8])
+@pytest.mark.parametrize("page,dim,rotary,interleaved", [(16, 128, 128, False), (32, 64, 32, True), (64, 128, 0, False), (16, 256, 18, False),
+                                                         (64, 256, 256, True), (16, 64, 12, True)])
+def test_append_matches_the_formula_bit_for_bit(fc, dtype, quantizer, page, dim, rotary, interleaved):
+    heads = 3
+    # steps of one cache: prompts (one of them empty), single tokens, uneven ones; the last one finds a full page, an absent slot
+    steps = [[5, 0, page + 1, 2 * page], [1, 1, 1, 1], [1, 2, page, 1], [1, 1, 1, 1], [page - 7, 1, 3, page]]
+    width = 5
+    table = page_table(4, width, 4 * width + 2, 3)
+    cache = new_cache(4 * width + 2, heads, page, dim)
+    want = [t.cpu().clone() for t in cache]
+    angles = fc.rotary_table(width * page, fc.rotary_frequencies(rotary)) if rotary else None
+    held = [0, 0, 0, 0]
+    for n, new in enumerate(steps):
+        print("append", dtype, quantizer, page, dim, rotary, interleaved, "step", n, flush=True)
+        k, v = fused(sum(new), (heads, heads), dim, dtype, n, 1.0 + 2 * n)       # larger every step: scales grow
+        k[:, 1] *= 0                                                                # a head of zeros
+        offsets = [0] + [int(i) for i in np.cumsum(new)]
+        got = fc.cache_append(k, v, cache, table.cuda(), ints(offsets), ints(held), max(new), quantizer, angles, interleaved)
+        assert got is cache
+        positions = torch.cat([torch.arange(h, h + c) for h, c in zip(held, new)])
+        turned_k = turned(k.float().cpu(), angles.cpu(), positions, interleaved) if rotary else k.float().cpu()
+        append_one(want[0], want[2], table, offsets, held, turned_k, quantizer, width * page)
+        append_one(want[1], want[3], table, offsets, held, v.float().cpu(), quantizer, width * page)
+        for name, a, b in zip(("k", "v"), cache[:2], want[:2]):
+            assert torch.equal(a.cpu(), b), name
+        for a, b in zip(cache[2:], want[2:]):
+            assert same(a, b)
+        held = [h + c for h, c in zip(held, new)]
+
+
+def test_append_leaves_out_what_has_no_place(fc):
+    page, heads, dim, quantizer = 16, 2, 64, SYM
+    table = torch.tensor([[0, 1], [2, -1], [9, 4], [5, 6], [7, 8]], dtype=torch.int32)      # no page, a page that is not there
+    new, held = [3, 20, 2, 40, 4], [-2, 0, 0, 10, 30]
+    offsets = [0] + [int(i) for i in np.cumsum(new)]
+    for rows in (32, 13):                                                        # page table, then rotation table ends first
+        cache = new_cache(9, heads, page, dim)
+        want = [t.cpu().clone() for t in cache]
+        k, v = fused(sum(new), (heads, heads), dim, BF16, rows)
+        angles = fc.rotary_table(rows, fc.rotary_frequencies(dim))
+        fc.cache_append(k, v, cache, table.cuda(), ints(offsets), ints(held), 40, quantizer, angles)
+        positions = torch.cat([torch.arange(h, h + c) for h, c in zip(held, new)])
+        append_one(want[0], want[2], table, offsets, held, turned(k.float().cpu(), angles.cpu(), positions, False), quantizer, min(rows, 32))
+        append_one(want[1], want[3], table, offsets, held, v.float().cpu(), quantizer, min(rows, 32))
+        for a, b in zip(cache, want):
+            assert torch.equal(a.cpu().view(torch.uint8), b.view(torch.uint8))
+
+
+def check(got, want, weight, dtype, bf16_weights):
+    """want, weight = sum w |v|: float64"""
+    u = 2.0 ** -9 if dtype == BF16 else 2.0 ** -11
+    uw = 2.0 ** -9 if bf16_weights else 2.0 ** -11
+    bound = 2 * ((uw + 2.0 ** -11) * weight + u * want.abs()) + (0.0 if dtype == BF16 else 2.0 ** -23)
+    got = got.double().cpu()
+    assert bool(torch.isfinite(got).all())
+    worst = ((got - want).abs() / bound.clamp(min=1e-30)).max().item() if got.numel() else 0.0
+    assert bool(((got - want).abs() <= bound).all()), worst
+
+
+def cache_reference(q, cache, table, offsets, held, quantizer, scale):
+    """64 bits; returns the outputs and sum w |v|"""
+    q = q.double().cpu()
+    codes, scales = [t.cpu() for t in cache[:2]], [t.cpu().double() for t in cache[2:]]
+    heads, page, dim = codes[0].shape[1:]
+    group = q.shape[1] // heads
+    out, weight = torch.zeros_like(q), torch.zeros_like(q)
+    for b in range(len(held)):
+        n = offsets[b + 1] - offsets[b]
+        total = min(held[b] + n, table.shape[1] * page)
+        if total <= 0:
+            continue
+        ids = table[b, :-(-total // page)].long()
+        k, v = (((values_of(c[ids], quantizer, torch.float64) * s[ids][..., None, None]).transpose(0, 1).reshape(heads, -1, dim))[:, :total]
+                for c, s in zip(codes, scales))
+        for i in range(n):
+            sees = min(held[b] + i + 1, total)
+            if sees <= 0:
+                continue
+            x = q[offsets[b] + i].view(heads, group, dim)
+            w = torch.softmax(x @ k[:, :sees].transpose(1, 2) * scale, -1)
+            out[offsets[b] + i] = (w @ v[:, :sees]).reshape(-1, dim)
+            weight[offsets[b] + i] = (w @ v[:, :sees].abs()).reshape(-1, dim)
+    return out, weight
+
+
+def filled_cache(pages, heads, page, dim, quantizer, held, new, table, seed):
+    """codes and scales of the tokens there are; beyond them NaN bytes (E4M3), -128 and NaN scales"""
+    cache = [t.cpu() for t in new_cache(pages, heads, page, dim, fill=0xFF if quantizer == FP8 else 0x80)]
+    g = gen(seed)
+    for b in range(len(held)):
+        total = min(held[b] + new[b], table.shape[1] * page)
+        for index in range(-(-max(total, 0) // page)):
+            id, n = int(table[b, index]), min(page, total - index * page)
+            for i in range(2):
+                x = torch.randn((heads, n, dim), generator=g) * (36 if quantizer == SYM else 120)
+                cache[i][id, :, :n] = codes_of(x.clamp(-TOP[quantizer], TOP[quantizer]), quantizer)
+                cache[2 + i][id] = (0.2 + 1.5 * torch.rand(heads, generator=g)) / (36 if quantizer == SYM else 120)
+    return tuple(t.cuda() for t in cache)
+
+
+CACHES = [
+    # heads, group, dim, page, held, new, hints (queries, longest) or None
+    (1, 1, 64, 16, [0], [1], None),
+    (2, 4, 128, 16, [128], [1], None),
+    (2, 8, 128, 64, [1499, 0, 63, 64, 300], [1, 1, 1, 1, 1], None),
+    (1, 5, 128, 32, [7, 700, 31], [3, 5, 1], None),
+    (2, 8, 64, 16, [33, 0, 16], [5, 40, 0], None),                    # several row blocks; a prompt; nothing new
+    (3, 2, 256, 32, [259, 5], [1, 2], None),
+    (1, 4, 128, 16, [-1, 200, -3, 0], [1, 1, 2, 1], None),            # empty slots of a padded batch
+    (1, 3, 128, 64, [5000, 17], [2, 2], None),
+    (1, 8, 128, 16, [900, 40], [9, 2], (1, 50)),                      # more queries and tokens than announced
+    (2, 1, 64, 64, [20000], [1], None),
+]
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("quantizer", [SYM, FP8])
+@pytest.mark.parametrize("case", range(len(CACHES)))
+def test_cache_attention_matches_its_definition(fc, dtype, quantizer, case):
+    heads, group, dim, page, held, new, hints = CACHES[case]
+    print("cache attention", dtype, quantizer, CACHES[case], flush=True)
+    width = max(1, max(-(-(h + n) // page) for h, n in zip(held, new)))
+    pages = len(held) * width + 1
+    table = page_table(len(held), width, pages, case)
+    cache = filled_cache(pages, heads, page, dim, quantizer, held, new, table, case)
+    offsets = [0] + [int(i) for i in np.cumsum(new)]
+    q, _ = fused(sum(new), (heads * group, 1), dim, dtype, 50 + case)
+    queries, longest = hints or (max(new), max(1, max(h + n for h, n in zip(held, new))))
+    got = fc.cache_attention(q, cache, table.cuda(), ints(offsets), ints(held), queries, longest, quantizer)
+    want, weight = cache_reference(q, cache, table, offsets, held, quantizer, dim ** -0.5)
+    check(got, want, weight, dtype, False)
+    again = fc.cache_attention(q, cache, table.cuda(), ints(offsets), ints(held), queries, longest, quantizer)
+    assert same(got, again)
+
+
+@pytest.mark.parametrize("quantizer", [SYM, FP8])
+def test_cache_attention_extremes(fc, quantizer):
+    # queries over bfloat16's range (rows that binary16 could not hold), pages of very different scales, another softmax scale
+    heads, group, dim, page, held, new = 2, 4, 128, 16, [100, 450], [1, 1]
+    table = page_table(2, 29, 60, 1)
+    cache = filled_cache(60, heads, page, dim, quantizer, held, new, table, 5)
+    cache[2].mul_(torch.logspace(-6, 0, 60, device="cuda")[:, None])
+    cache[3].mul_(torch.logspace(-5, 3, 60, device="cuda")[:, None])
+    q, _ = fused(2, (heads * group, 1), dim, BF16, 9)
+    q = (q.float() * torch.logspace(-30, 8, 8, device="cuda")[None, :, None]).to(BF16)
+    scale = 1e-8
+    got = fc.cache_attention(q, cache, table.cuda(), ints([0, 1, 2]), ints(held), 1, 451, quantizer, scale=scale)
+    want, weight = cache_reference(q, cache, table, [0, 1, 2], held, quantizer, scale)
+    check(got, want, weight, BF16, False)
+
+
+def test_cache_attention_beyond_32_bit_offsets(fc):
+    heads, dim, page = 8, 128, 64
+    pages = (1 << 32) // (heads * dim * page) + 40
+    k = torch.empty((pages, heads, page, dim), dtype=torch.uint8, device="cuda")
+    v = torch.empty_like(k)
+    scales = [torch.full((pages, heads), 0.01, device="cuda") for _ in range(2)]
+    table = torch.tensor([[pages - 1, 0, pages - 33], [pages - 2, 5, pages // 2 + 3]], dtype=torch.int32)
+    kv = fused(2 * 150, (heads, heads), dim, F16, 4)
+    cache = (k, v, *scales)
+    fc.cache_append(kv[0], kv[1], cache, table.cuda(), ints([0, 150, 300]), ints([0, 0]), 150)
+    q, _ = fused(2, (16, 1), dim, F16, 6)
+    got = fc.cache_attention(q, cache, table.cuda(), ints([0, 1, 2]), ints([149, 149]), 1, 150)
+    ids = table.flatten().long().cuda()
+    small = tuple(t[ids].contiguous() for t in cache)
+    renamed = torch.arange(6, dtype=torch.int32).view(2, 3)
+    want, weight = cache_reference(q, small, renamed, [0, 1, 2], [149, 149], SYM, dim ** -0.5)
+    check(got, want, weight, F16, False)
+
+
+# ---- prompts ----
+
+def prompt_reference(q, k, v, lengths, causal, scale):
+    q, k, v = (t.double().cpu() for t in (q, k, v))
+    group = q.shape[1] // k.shape[1]
+    out, weight = torch.zeros_like(q), torch.zeros_like(q)
+    at = 0
+    for n in lengths:
+        part = slice(at, at + n)
+        kk, vv = (t[part].transpose(0, 1).repeat_interleave(group, 0) for t in (k, v))
+        s = q[part].transpose(0, 1) @ kk.transpose(1, 2) * scale
+        if causal:
+            s = s.masked_fill(~torch.ones((n, n), dtype=torch.bool).tril(), -math.inf)
+        w = torch.softmax(s, -1)
+        out[part], weight[part] = (w @ vv).transpose(0, 1), (w @ vv.abs()).transpose(0, 1)
+        at += n
+    return out, weight
+
+
+PROMPTS = [
+    # heads, group, dim, lengths
+    (1, 1, 64, [1]),
+    (1, 2, 128, [2, 1, 0, 33]),
+    (2, 4, 128, [130]),
+    (1, 8, 64, [31, 32, 33, 127, 128, 129]),
+    (3, 1, 128, [257, 64, 5, 600]),
+    (2, 5, 64, [191, 0, 0, 320]),
+    (1, 1, 128, [1537]),
+]
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("case", range(len(PROMPTS)))
+def test_prompt_attention_matches_its_definition(fc, dtype, causal, case):
+    heads, group, dim, lengths = PROMPTS[case]
+    print("prompt attention", dtype, causal, PROMPTS[case], flush=True)
+    q, k, v = fused(sum(lengths), (heads * group, heads, heads), dim, dtype, case)
+    got = fc.prompt_attention(q, k, v, offsets_of(lengths), max(lengths), causal)
+    want, weight = prompt_reference(q, k, v, lengths, causal, dim ** -0.5)
+    check(got, want, weight, dtype, dtype == BF16)
+    assert same(got, fc.prompt_attention(q, k, v, offsets_of(lengths), max(lengths), causal))
+
+
+def test_prompt_attention_keeps_sequences_apart(fc):
+    # infinities and NaN of one request change no bit of another's rows
+    lengths = [40, 100, 64, 7]
+    q, k, v = fused(sum(lengths), (4, 2, 2), 128, F16, 3)
+    q, k, v = q.clone(), k.clone(), v.clone()
+    clean = fc.prompt_attention(q, k, v, offsets_of(lengths), 100)
+    for t in (q, k, v):
+        t[40:140:3] = math.nan
+        t[41:140:3] = math.inf
+    got = fc.prompt_attention(q, k, v, offsets_of(lengths), 100)
+    assert same(got[:40], clean[:40]) and same(got[140:], clean[140:])
+
+
+# ---- calls ----
+
+def test_strided_operands_and_results(fc):
+    # heads outside tokens, gaps between both, results into a slice of a larger tensor
+    tokens, heads, dim = 50, 2, 64
+    q = torch.randn((8, tokens, dim), generator=gen(1)).to(F16).cuda().transpose(0, 1)
+    k = torch.randn((tokens, 3, heads, dim + 8), generator=gen(2)).to(F16).cuda()[:, 1, :, :dim]
+    v = torch.randn((tokens, heads, dim), generator=gen(3)).to(F16).cuda()
+    big = torch.full((tokens, 12, dim), 5.0, dtype=F16, device="cuda")
+    out = big[:, 2:10]
+    assert fc.prompt_attention(q, k, v, ints([0, tokens]), tokens, out=out) is out
+    want, weight = prompt_reference(q, k, v, [tokens], True, dim ** -0.5)
+    check(out, want, weight, F16, False)
+    assert bool((big[:, :2] == 5).all()) and bool((big[:, 10:] == 5).all())
+    table = fc.rotary_table(64, fc.rotary_frequencies(dim))
+    p = torch.arange(tokens, dtype=torch.int32, device="cuda")
+    assert same(fc.rotary(q, table, p), fc.rotary(q.contiguous(), table, p))
+    assert same(fc.rotary(k, table, p, out=out[:, :heads]), fc.rotary(k.contiguous(), table, p))
+    cache, twin = new_cache(4, heads, 16, dim, 1), new_cache(4, heads, 16, dim, 1)
+    pages = torch.arange(4, dtype=torch.int32, device="cuda")[None]
+    for c, kk in ((cache, k), (twin, k.contiguous())):
+        fc.cache_append(kk, v, c, pages, ints([0, tokens]), ints([0]), tokens, table=table)
+    for a, b in zip(cache, twin):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    y = fc.cache_attention(q[-3:], cache, pages, ints([0, 3]), ints([47]), 3, 50, out=big[:3, 2:10])
+    assert same(y, fc.cache_attention(q[-3:].contiguous(), cache, pages, ints([0, 3]), ints([47]), 3, 50))
+
+
+def test_a_step_on_another_stream_and_from_a_graph(fc):
+    heads, group, dim, page, width = 2, 4, 128, 16, 40
+    table = page_table(3, width, 3 * width, 0).cuda()
+    angles = fc.rotary_table(width * page, fc.rotary_frequencies(dim))
+    held, offsets = ints([500, 0, 77]), ints([0, 1, 2, 3])
+    qkv = torch.randn((3, heads * (group + 2), dim), generator=gen(0)).to(BF16).cuda()
+    q, k, v = qkv.split([heads * group, heads, heads], 1)
+    start = filled_cache(3 * width, heads, page, dim, SYM, [500, 0, 77], [0, 0, 0], table.cpu(), 1)
+    cache = tuple(t.clone() for t in start)
+    turned_q, out = torch.empty_like(q.contiguous()), torch.empty_like(q.contiguous())
+    space = torch.empty(max(16, fc.cache_attention_workspace_bytes(3, 3, heads, group, dim, 1, 501)), dtype=torch.uint8, device="cuda")
+
+    def step():
+        fc.rotary(q, angles, held, out=turned_q)
+        fc.cache_append(k, v, cache, table, offsets, held, 1, SYM, angles)
+        fc.cache_attention(turned_q, cache, table, offsets, held, 1, 501, SYM, out=out, workspace=space)
+
+    def fresh(seed):
+        qkv.copy_(torch.randn(qkv.shape, generator=gen(seed)))
+        for a, b in zip(cache, start):
+            a.copy_(b)
+        out.fill_(7.0)
+
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        fresh(0)
+        step()
+    side.synchronize()
+    first = out.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        step()
+    for seed in (0, 1, 2, 0, 3):
+        fresh(seed)
+        step()
+        torch.cuda.synchronize()
+        want, kept = out.clone(), [t.clone() for t in cache]
+        fresh(seed)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert same(out, want)
+        for a, b in zip(cache, kept):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+        if seed == 0:
+            assert same(out, first)
+
+
+def test_empty_calls(fc):
+    q, k, v = fused(0, (4, 2, 2), 64, F16, 0)
+    table = fc.rotary_table(4, fc.rotary_frequencies(64))
+    assert fc.rotary(q, table, ints([])).shape == q.shape
+    cache = new_cache(2, 2, 16, 64)
+    before = [t.clone() for t in cache]
+    pages = torch.zeros((1, 1), dtype=torch.int32, device="cuda")
+    fc.cache_append(k, v, cache, pages, ints([0, 0]), ints([3]), 1)
+    assert fc.cache_attention(q, cache, pages, ints([0, 0]), ints([3]), 1, 4).shape == q.shape
+    assert fc.prompt_attention(q, k, v, ints([0, 0]), 1).shape == q.shape
+    torch.cuda.synchronize()
+    for a, b in zip(cache, before):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+def test_refusals(fc):
+    q, k, v = fused(8, (4, 2, 2), 64, F16, 0)
+    o, held, pages = ints([0, 8]), ints([0]), torch.zeros((1, 2), dtype=torch.int32, device="cuda")
+    cache = new_cache(2, 2, 16, 64)
+    table = fc.rotary_table(16, fc.rotary_frequencies(64))
+    p = torch.arange(8, dtype=torch.int32, device="cuda")
+    with pytest.raises(TypeError):
+        fc.rotary(q.float(), table, p)
+    with pytest.raises(TypeError):
+        fc.rotary(q, table, p.long())
+    with pytest.raises(TypeError):
+        fc.rotary(q.cpu(), table, p)
+    with pytest.raises(ValueError):
+        fc.rotary(q, table, p[:5])
+    with pytest.raises(fc.FcError):
+        fc.rotary(q[..., :48], table, p)                                          # more turned than there is
+    with pytest.raises(ValueError):
+        fc.rotary(q[..., 1:57], table[:, :32].contiguous(), p)                    # not aligned
+    with pytest.raises(ValueError):
+        fc.rotary(q, table, p, out=torch.empty((1, 4, 64), dtype=F16, device="cuda").expand(8, 4, 64))
+    with pytest.raises(TypeError):
+        fc.prompt_attention(q, k.bfloat16(), v.bfloat16(), o, 8)
+    with pytest.raises(ValueError):
+        fc.prompt_attention(q[:, :3], k, v, o, 8)                                 # 3 heads over 2
+    with pytest.raises(ValueError):
+        fc.prompt_attention(q, k[:7], v, o, 8)
+    with pytest.raises(fc.FcError):
+        fc.prompt_attention(q[..., :32], k[..., :32], v[..., :32], o, 8)          # head size
+    with pytest.raises(ValueError):
+        fc.cache_append(k, v, cache[:3], pages, o, held, 8)
+    with pytest.raises(ValueError):
+        fc.cache_append(k, v, cache, pages, o, ints([0, 0]), 8)
+    with pytest.raises(ValueError):
+        fc.cache_append(q, q, cache, pages, o, held, 8)                           # 4 heads into a cache of 2
+    with pytest.raises(fc.FcError) as e:
+        fc.cache_append(k, v, cache, pages, o, held, 8, fc.QUANTIZER_ASYM)
+    assert e.value.code == -8
+    with pytest.raises(fc.FcError):
+        fc.cache_append(k, v, new_cache(2, 2, 8, 64), pages, o, held, 8)          # page of 8
+    with pytest.raises(fc.FcError):
+        fc.cache_attention(q, cache, pages, o, held, 0, 8)
+    with pytest.raises(fc.FcError) as e:
+        long = ints([30000])
+        fc.cache_attention(q[:1], cache, pages, ints([0, 1]), long, 1, 30001, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+    assert e.value.code == -6
+    torch.cuda.synchronize()
