@@ -174,6 +174,9 @@ def _table(table):
 def rotary(x, table, positions, interleaved: bool = False, inverse: bool = False, out=None):
     """fc_rotary.  x [tokens, heads, dim] with the first table.shape[1] elements of each head turned to positions (int32 [tokens]);
     out=x turns in place."""
+    done = (binding._native or binding._calls()).rotary(x, table, positions, interleaved, inverse, out)
+    if done is not None:
+        return done
     _rows(x, "x")
     address, rows, turned = _table(table)
     tokens, heads, dim = x.shape
@@ -188,6 +191,9 @@ def cache_append(k, v, cache, pages, offsets, held, longest: int, quantizer: int
                  interleaved: bool = False):
     """fc_cache_append: puts k, v [tokens, heads, dim] behind the tokens that each sequence holds, keys turned to their positions on
     the way if a rotation table is given.  longest: no sequence gets more tokens.  Returns the cache."""
+    done = (binding._native or binding._calls()).cache_append(k, v, cache, pages, offsets, held, longest, quantizer, table, interleaved)
+    if done is not None:
+        return done
     _rows(k, "k")
     _rows(v, "v", k.dtype, tuple(k.shape))
     sequences = _step(offsets, held)
@@ -217,6 +223,9 @@ def cache_attention(q, cache, pages, offsets, held, queries: int, longest: int, 
     """fc_cache_attention: q [tokens, query heads, dim] over the cache that cache_append has put the same step's tokens into; query i
     of a sequence sees its first held + i + 1 tokens.  queries and longest: the most new tokens, and the most in all, that a
     sequence has.  scale: dim^-0.5 unless given."""
+    done = (binding._native or binding._calls()).cache_attention(q, cache, pages, offsets, held, queries, longest, quantizer, scale, out, workspace)
+    if done is not None:
+        return done
     torch = _torch()
     _rows(q, "q")
     sequences = _step(offsets, held)
@@ -242,6 +251,9 @@ def cache_attention(q, cache, pages, offsets, held, queries: int, longest: int, 
 def prompt_attention(q, k, v, offsets, longest: int, causal: bool = True, scale=None, out=None):
     """fc_prompt_attention: every sequence of the packed q [tokens, query heads, dim], k, v [tokens, heads, dim] attends to itself.
     longest: no sequence has more tokens.  scale: dim^-0.5 unless given."""
+    done = (binding._native or binding._calls()).prompt_attention(q, k, v, offsets, longest, causal, scale, out)
+    if done is not None:
+        return done
     _rows(q, "q")
     _rows(k, "k", q.dtype)
     _rows(v, "v", q.dtype, tuple(k.shape))

@@ -27,6 +27,8 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <array>
+#include <cmath>
+#include <utility>
 
 #include "fc.h"
 
@@ -38,7 +40,8 @@ namespace {
     X(fc_dequant_reduce_requant_cmeta)                                                                               \
     X(fc_dequantize) X(fc_dequantize_sym) X(fc_dequantize_fp8) X(fc_dequantize_cmeta) X(fc_dequantize_rot)           \
     X(fc_allreduce_sim) X(fc_allreduce_sim_sym) X(fc_allreduce_sim_fp8) X(fc_allreduce_sim_cmeta)                    \
-    X(fc_allreduce_sim_rot) X(fc_allreduce_sim_workspace_bytes)
+    X(fc_allreduce_sim_rot) X(fc_allreduce_sim_workspace_bytes)                                                      \
+    X(fc_rotary) X(fc_cache_append) X(fc_cache_attention_workspace_bytes) X(fc_cache_attention) X(fc_prompt_attention)
 
 struct Library {
 #define FC_MEMBER(f) decltype(&::f) f = nullptr;
@@ -70,17 +73,22 @@ int device_of(PyObject *o)
     return device == (int)c10::hip::current_device() ? device : -1;
 }
 
+// no functional wrapper or other tensor whose operations something intercepts
+bool ordinary_keys(const at::Tensor &t)
+{
+    static const uint64_t ordinary = c10::DispatchKeySet({c10::DispatchKey::CUDA, c10::DispatchKey::AutogradCUDA,
+                                                          c10::DispatchKey::AutocastCUDA,
+                                                          c10::DispatchKey::ADInplaceOrView}).raw_repr();
+    return (t.key_set().raw_repr() & ~ordinary) == 0;
+}
+
 // The tensor behind `o` if it is a dense, contiguous one of `dtype` on GPU `device` and of no Python subclass or
 // functional wrapper; otherwise null.
 const at::Tensor *plain(PyObject *o, at::ScalarType dtype, int device)
 {
     if (!THPVariable_CheckExact(o)) return nullptr;
     const at::Tensor &t = THPVariable_Unpack(o);
-    if (!t.defined()) return nullptr;
-    static const uint64_t ordinary = c10::DispatchKeySet({c10::DispatchKey::CUDA, c10::DispatchKey::AutogradCUDA,
-                                                          c10::DispatchKey::AutocastCUDA,
-                                                          c10::DispatchKey::ADInplaceOrView}).raw_repr();
-    if ((t.key_set().raw_repr() & ~ordinary) != 0) return nullptr;
+    if (!t.defined() || !ordinary_keys(t)) return nullptr;
     if (!t.is_cuda() || t.scalar_type() != dtype || t.device().index() != device || !t.is_contiguous()) return nullptr;
     return &t;
 }
@@ -456,6 +464,250 @@ PyObject *allreduce(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     END_HANDLE_TH_ERRORS
 }
 
+// ---- attention.py's calls ----
+
+// A [tokens, heads, dim] activation as the C ABI takes it
+struct Activation {
+    const at::Tensor *t = nullptr;
+    void *ptr = nullptr;
+    int64_t token = 0, head = 0;           // strides
+    int64_t tokens() const { return t->size(0); }
+    int64_t heads() const { return t->size(1); }
+    int64_t dim() const { return t->size(2); }
+    bool like(const Activation &o) const { return tokens() == o.tokens() && heads() == o.heads() && dim() == o.dim(); }
+};
+
+bool describe(const at::Tensor &t, Activation &a)
+{
+    if (t.dim() != 3 || t.numel() == 0 || t.stride(2) != 1) return false;
+    a.t = &t;
+    a.ptr = t.data_ptr();
+    a.token = t.size(0) > 1 ? t.stride(0) : 0;
+    a.head = t.size(1) > 1 ? t.stride(1) : 0;
+    return a.token % 8 == 0 && a.head % 8 == 0 && (reinterpret_cast<uintptr_t>(a.ptr) & 15) == 0;
+}
+
+// `o` as one of `dtype` (Undefined: either 16-bit type) on GPU `device`
+bool activation(PyObject *o, at::ScalarType dtype, int device, Activation &a)
+{
+    if (!THPVariable_CheckExact(o)) return false;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (!t.defined() || !ordinary_keys(t) || !t.is_cuda() || t.device().index() != device) return false;
+    if (dtype == at::ScalarType::Undefined ? t.scalar_type() != at::kHalf && t.scalar_type() != at::kBFloat16 : t.scalar_type() != dtype)
+        return false;
+    return describe(t, a);
+}
+
+int type_code(const Activation &a) { return a.t->scalar_type() == at::kBFloat16 ? FC_TYPE_BF16 : FC_TYPE_F16; }
+
+// The caller's result, which must not overlap itself, or a new dense one
+bool result_rows(PyObject *out, const Activation &like, int device, at::Tensor &own, Activation &y)
+{
+    if (out == Py_None) {
+        own = empty({like.tokens(), like.heads(), like.dim()}, like.t->scalar_type(), *like.t);
+        return describe(own, y);
+    }
+    if (!activation(out, like.t->scalar_type(), device, y) || !y.like(like)) return false;
+    constexpr int64_t far = (int64_t)1 << 62;
+    int64_t s0 = y.tokens() > 1 ? y.token : far, n0 = y.tokens(), s1 = y.heads() > 1 ? y.head : far;
+    if (s1 < s0 || (s1 == s0 && y.heads() < n0)) {
+        std::swap(s0, s1);
+        n0 = y.heads();
+    }
+    return s0 >= y.dim() && s1 >= (n0 > 1 ? s0 * (n0 - 1) : 0) + y.dim();
+}
+
+bool truth(PyObject *o, int &v)
+{
+    if (o != Py_True && o != Py_False) return false;
+    v = o == Py_True;
+    return true;
+}
+
+// scale: None is dim^-0.5
+bool softmax_scale(PyObject *o, int64_t dim, float &v)
+{
+    if (o == Py_None) v = (float)(1.0 / std::sqrt((double)dim));
+    else if (PyFloat_CheckExact(o)) v = (float)PyFloat_AS_DOUBLE(o);
+    else return false;
+    return true;
+}
+
+const at::Tensor *vector(PyObject *o, int64_t n, int device)
+{
+    const at::Tensor *t = plain(o, at::kInt, device);
+    return t && t->dim() == 1 && t->size(0) == n ? t : nullptr;
+}
+
+// The cache, its page table and the step's index arrays
+struct PagedStep {
+    const at::Tensor *k, *v, *ks, *vs, *pages, *offsets, *held;
+    int64_t sequences, heads, page, dim, count, width;
+
+    bool take(PyObject *cache, PyObject *table, PyObject *off, PyObject *have, int device)
+    {
+        if (!PyTuple_CheckExact(cache) || PyTuple_GET_SIZE(cache) != 4) return false;
+        k = plain(PyTuple_GET_ITEM(cache, 0), at::kByte, device);
+        v = plain(PyTuple_GET_ITEM(cache, 1), at::kByte, device);
+        ks = plain(PyTuple_GET_ITEM(cache, 2), at::kFloat, device);
+        vs = plain(PyTuple_GET_ITEM(cache, 3), at::kFloat, device);
+        pages = plain(table, at::kInt, device);
+        offsets = plain(off, at::kInt, device);
+        if (!k || !v || !ks || !vs || !pages || !offsets || k->dim() != 4 || pages->dim() != 2 || offsets->dim() != 1) return false;
+        sequences = offsets->size(0) - 1;
+        count = k->size(0);
+        heads = k->size(1);
+        page = k->size(2);
+        dim = k->size(3);
+        width = pages->size(1);
+        held = sequences >= 0 ? vector(have, sequences, device) : nullptr;
+        return held && v->sizes() == k->sizes() && shape2(*ks, count, heads) && shape2(*vs, count, heads) && pages->size(0) == sequences;
+    }
+};
+
+bool table_of(const at::Tensor *t) { return t && t->dim() == 2 && t->size(1) <= 4096; }
+
+// (x, table, positions, interleaved, inverse, out)
+PyObject *rotary(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    HANDLE_TH_ERRORS
+    if (n_args != 6 || !plain_context()) return fallback();
+    const int device = device_of(a[0]);
+    Activation x, y;
+    int interleaved, inverse;
+    if (device < 0 || !activation(a[0], at::ScalarType::Undefined, device, x)) return fallback();
+    const at::Tensor *table = plain(a[1], at::kFloat, device), *positions = vector(a[2], x.tokens(), device);
+    if (!table_of(table) || !positions || !truth(a[3], interleaved) || !truth(a[4], inverse)) return fallback();
+    at::Tensor own;
+    if (!result_rows(a[5], x, device, own, y)) return fallback();
+    const float *angles = (const float *)table->data_ptr();
+    const int32_t *at = (const int32_t *)positions->data_ptr();
+    const int64_t rows = table->size(0), tokens = x.tokens();
+    const int heads = (int)x.heads(), dim = (int)x.dim(), turned = (int)table->size(1), type = type_code(x);
+    void *stream = stream_of(device);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = lib.fc_rotary(x.ptr, x.token, x.head, angles, rows, at, tokens, heads, dim, turned, interleaved, inverse, type, y.ptr, y.token,
+                       y.head, stream);
+    Py_END_ALLOW_THREADS
+    if (!done(rc, "fc_rotary")) return nullptr;
+    return wrapped(a[5], own);
+    END_HANDLE_TH_ERRORS
+}
+
+// (k, v, cache, pages, offsets, held, longest, quantizer, table, interleaved)
+PyObject *cache_append(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    HANDLE_TH_ERRORS
+    if (n_args != 10 || !plain_context()) return fallback();
+    const int device = device_of(a[0]);
+    Activation k, v;
+    PagedStep s;
+    int64_t longest, quantizer;
+    int interleaved;
+    if (device < 0 || !activation(a[0], at::ScalarType::Undefined, device, k) || !activation(a[1], k.t->scalar_type(), device, v) ||
+        !v.like(k) || !s.take(a[2], a[3], a[4], a[5], device) || k.heads() != s.heads || k.dim() != s.dim || !integer(a[6], longest) ||
+        !integer(a[7], quantizer) || !truth(a[9], interleaved))
+        return fallback();
+    const at::Tensor *table = nullptr;
+    if (a[8] != Py_None && !table_of(table = plain(a[8], at::kFloat, device))) return fallback();
+    const float *angles = table ? (const float *)table->data_ptr() : nullptr;
+    const int64_t rows = table ? table->size(0) : 0, tokens = k.tokens();
+    const int turned = table ? (int)table->size(1) : 0, type = type_code(k);
+    void *kc = s.k->data_ptr(), *vc = s.v->data_ptr(), *stream = stream_of(device);
+    float *ks = (float *)s.ks->data_ptr(), *vs = (float *)s.vs->data_ptr();
+    const int32_t *pages = (const int32_t *)s.pages->data_ptr(), *offsets = (const int32_t *)s.offsets->data_ptr(),
+                  *held = (const int32_t *)s.held->data_ptr();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = lib.fc_cache_append(k.ptr, k.token, k.head, v.ptr, v.token, v.head, tokens, (int)s.heads, (int)s.dim, type, angles, rows, turned,
+                             interleaved, (int)quantizer, kc, vc, ks, vs, s.count, (int)s.page, pages, (int)s.width, offsets, held,
+                             (int)s.sequences, longest, stream);
+    Py_END_ALLOW_THREADS
+    if (!done(rc, "fc_cache_append")) return nullptr;
+    Py_INCREF(a[2]);
+    return a[2];
+    END_HANDLE_TH_ERRORS
+}
+
+// (q, cache, pages, offsets, held, queries, longest, quantizer, scale, out, workspace)
+PyObject *cache_attention(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    HANDLE_TH_ERRORS
+    if (n_args != 11 || !plain_context()) return fallback();
+    const int device = device_of(a[0]);
+    Activation q, y;
+    PagedStep s;
+    int64_t queries, longest, quantizer;
+    float scale;
+    if (device < 0 || !activation(a[0], at::ScalarType::Undefined, device, q) || !s.take(a[1], a[2], a[3], a[4], device) || q.dim() != s.dim ||
+        s.heads < 1 || q.heads() % s.heads != 0 || !integer(a[5], queries) || !integer(a[6], longest) || !integer(a[7], quantizer) ||
+        !softmax_scale(a[8], q.dim(), scale))
+        return fallback();
+    const int64_t tokens = q.tokens();
+    const int group = (int)(q.heads() / s.heads), type = type_code(q);
+    const size_t need = lib.fc_cache_attention_workspace_bytes(tokens, (int)s.sequences, (int)s.heads, group, (int)s.dim, queries, longest);
+    const at::Tensor *ws = nullptr;
+    if (a[10] != Py_None) {
+        ws = plain(a[10], at::kByte, device);
+        if (!ws || (size_t)ws->numel() < need) return fallback();
+    }
+    at::Tensor own, own_ws;
+    if (!result_rows(a[9], q, device, own, y)) return fallback();
+    if (need && !ws) {
+        own_ws = empty({(int64_t)need}, at::kByte, *q.t);
+        ws = &own_ws;
+    }
+    void *space = ws ? ws->data_ptr() : nullptr, *stream = stream_of(device);
+    const size_t bytes = ws ? (size_t)ws->numel() : 0;
+    const void *kc = s.k->data_ptr(), *vc = s.v->data_ptr();
+    const float *ks = (const float *)s.ks->data_ptr(), *vs = (const float *)s.vs->data_ptr();
+    const int32_t *pages = (const int32_t *)s.pages->data_ptr(), *offsets = (const int32_t *)s.offsets->data_ptr(),
+                  *held = (const int32_t *)s.held->data_ptr();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = lib.fc_cache_attention(q.ptr, q.token, q.head, tokens, (int)s.heads, group, (int)s.dim, type, (int)quantizer, kc, vc, ks, vs, s.count,
+                                (int)s.page, pages, (int)s.width, offsets, held, (int)s.sequences, queries, longest, scale, y.ptr, y.token,
+                                y.head, space, bytes, stream);
+    Py_END_ALLOW_THREADS
+    if (!done(rc, "fc_cache_attention")) return nullptr;
+    return wrapped(a[9], own);
+    END_HANDLE_TH_ERRORS
+}
+
+// (q, k, v, offsets, longest, causal, scale, out)
+PyObject *prompt_attention(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    HANDLE_TH_ERRORS
+    if (n_args != 8 || !plain_context()) return fallback();
+    const int device = device_of(a[0]);
+    Activation q, k, v, y;
+    int64_t longest;
+    int causal;
+    float scale;
+    if (device < 0 || !activation(a[0], at::ScalarType::Undefined, device, q) || !activation(a[1], q.t->scalar_type(), device, k) ||
+        !activation(a[2], q.t->scalar_type(), device, v) || !v.like(k) || k.tokens() != q.tokens() || k.dim() != q.dim() ||
+        q.heads() % k.heads() != 0 || !integer(a[4], longest) || !truth(a[5], causal) || !softmax_scale(a[6], q.dim(), scale))
+        return fallback();
+    const at::Tensor *offsets = plain(a[3], at::kInt, device);
+    if (!offsets || offsets->dim() != 1 || offsets->size(0) < 1) return fallback();
+    at::Tensor own;
+    if (!result_rows(a[7], q, device, own, y)) return fallback();
+    const int32_t *starts = (const int32_t *)offsets->data_ptr();
+    const int64_t tokens = q.tokens();
+    const int sequences = (int)offsets->size(0) - 1, heads = (int)k.heads(), group = (int)(q.heads() / k.heads()), dim = (int)q.dim(),
+              type = type_code(q);
+    void *stream = stream_of(device);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = lib.fc_prompt_attention(q.ptr, q.token, q.head, k.ptr, k.token, k.head, v.ptr, v.token, v.head, tokens, heads, group, dim, type,
+                                 starts, sequences, longest, causal, scale, y.ptr, y.token, y.head, stream);
+    Py_END_ALLOW_THREADS
+    if (!done(rc, "fc_prompt_attention")) return nullptr;
+    return wrapped(a[7], own);
+    END_HANDLE_TH_ERRORS
+}
+
 // load(path, on_error): the functions of the library that the process already holds under `path`
 PyObject *load(PyObject *, PyObject *args)
 {
@@ -496,6 +748,8 @@ PyMethodDef methods[] = {
     FC_METHOD("allreduce_sim", allreduce<kAsym>), FC_METHOD("allreduce_sim_sym", allreduce<kSym>),
     FC_METHOD("allreduce_sim_fp8", allreduce<kFp8>), FC_METHOD("allreduce_sim_cmeta", allreduce<kCmeta>),
     FC_METHOD("allreduce_sim_rot", allreduce<kRot>),
+    FC_METHOD("rotary", rotary), FC_METHOD("cache_append", cache_append), FC_METHOD("cache_attention", cache_attention),
+    FC_METHOD("prompt_attention", prompt_attention),
     {nullptr, nullptr, 0, nullptr},
 };
 

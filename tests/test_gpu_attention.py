@@ -548,3 +548,28 @@ def test_refusals(fc):
         fc.cache_attention(q[:1], cache, pages, ints([0, 1]), long, 1, 30001, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
     assert e.value.code == -6
     torch.cuda.synchronize()
+
+
+def test_ordinary_calls_are_native(fc):
+    # what the module does not take it returns as None, and the checked path makes the same call
+    native = fc.binding._calls()
+    qkv = fused(20, (4, 2, 2), 64, F16, 0)
+    q, k, v = qkv
+    table, p = fc.rotary_table(32, fc.rotary_frequencies(64)), torch.arange(20, dtype=torch.int32, device="cuda")
+    o, held, pages = ints([0, 20]), ints([0]), torch.arange(2, dtype=torch.int32, device="cuda")[None]
+    cache, twin = new_cache(2, 2, 16, 64), new_cache(2, 2, 16, 64)
+    got = [native.rotary(q, table, p, False, False, None), native.cache_append(k, v, cache, pages, o, held, 20, SYM, table, False),
+           native.cache_attention(q, cache, pages, o, held, 20, 20, SYM, None, None, None), native.prompt_attention(q, k, v, o, 20, True, None, None)]
+    assert all(g is not None for g in got) and got[1] is cache
+    assert native.rotary(q, table, p, 0, False, None) is None and native.prompt_attention(q, k, v, o, 20.0, True, None, None) is None
+    binding, module = fc.binding, fc.binding._native
+    binding._native = binding._NoNativeCalls()
+    try:
+        again = [fc.rotary(q, table, p), fc.cache_append(k, v, twin, pages, o, held, 20, SYM, table), fc.cache_attention(q, twin, pages, o, held, 20, 20),
+                 fc.prompt_attention(q, k, v, o, 20)]
+    finally:
+        binding._native = module
+    for i in (0, 2, 3):
+        assert same(got[i], again[i])
+    for a, b in zip(cache, twin):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
