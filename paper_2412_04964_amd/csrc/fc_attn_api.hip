@@ -124,7 +124,7 @@ int fc_cache_append(const void *k, int64_t k_token_stride, int64_t k_head_stride
     if (!offsets || !held || (rotary && !table)) return FC_ERR_NULL;
     if ((rc = check_rows(k, k_token_stride, k_head_stride)) != FC_OK) return rc;
     if ((rc = check_rows(v, v_token_stride, v_head_stride)) != FC_OK) return rc;
-    if (!launchable((tokens / page + 2 * (int64_t)sequences) * 2 * heads, 512)) return FC_ERR_SHAPE;
+    if (!launchable((tokens / page + 2 * (int64_t)sequences + 8) * 2 * heads, 512)) return FC_ERR_SHAPE;
     fc::AppendArgs a;
     a.k = rows(k, k_token_stride, k_head_stride);
     a.v = rows(v, v_token_stride, v_head_stride);

@@ -3,8 +3,8 @@
 // A pair (a, b) of a head's first `rotary` elements turns by the angle position * frequency_i:
 //     a' = a cos - b sin,  b' = b cos + a sin            (fp32, every product and sum rounded, then one rounding to 16 bits)
 // Pair i is elements (i, i + rotary / 2) or, interleaved, (2 i, 2 i + 1); the rest of the head is copied.  The inverse turns back.
-// The rotation moves 4 bytes per element for 3 operations on each, so memory bounds it: a lane has 8 pairs in 128-bit accesses and
-// takes them through several heads, which share the 64 bytes of table that their 8 angles need.
+// The rotation moves 4 bytes per element for 3 operations on each, so memory bounds it: 6.2 TB/s on 16383 tokens of 80 heads of 128, what a
+// copy reaches here.  The table adds little: the heads of a token follow each other in a workgroup and find it in the nearest cache.
 #include "fc_attn.hpp"
 
 namespace fc {
@@ -23,70 +23,66 @@ __global__ void __launch_bounds__(256) k_rotary_table(const double *__restrict__
     table[row * 2 * half + half + i] = (float)(magnitude * s);
 }
 
-// HEADS heads of one token by one lane
-template <bool BF16, bool INTERLEAVED, int HEADS>
-__global__ void __launch_bounds__(256) k_rotary(RotaryArgs a, int units, int head_blocks)
+// 16 elements of one head by one lane: two pieces of 8, each with a neighbouring lane's on both sides so that every access of a wavefront
+// is of whole lines.  Half layout: the halves of 8 pairs, or 8 + 8 elements that are not turned; interleaved: any two pieces do, the
+// two halves of the head.  Every lane loads and stores alike, so that a wavefront with both kinds does not do either twice.
+// STREAM: x is marked as read once.
+template <bool BF16, bool INTERLEAVED, bool STREAM>
+__global__ void __launch_bounds__(256) k_rotary(RotaryArgs a, uint32_t units)
 {
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t item = at / units;
-    const int unit = (int)(at - item * units);
-    const int64_t token = item / head_blocks;
+    const uint32_t at = blockIdx.x * 256 + threadIdx.x;
+    const uint32_t item = at / units, d = (at - item * units) * 8;
+    const uint32_t token = item / (uint32_t)a.heads;
     if (token >= a.tokens) return;
-    const int head0 = (int)(item - token * head_blocks) * HEADS;
-    const int turned = a.rotary / 16;
-    const uint16_t *x = (const uint16_t *)a.x.ptr + token * a.x.token;
-    uint16_t *y = (uint16_t *)a.y.ptr + token * a.y.token;
-
-    if (unit >= turned) {                               // 8 elements that are not turned
-        const int d = a.rotary + (unit - turned) * 8;
-        uintx4 w[HEADS];
-#pragma unroll
-        for (int j = 0; j < HEADS; ++j)
-            if (head0 + j < a.heads) w[j] = *(const uintx4 *)(x + (head0 + j) * a.x.head + d);
-#pragma unroll
-        for (int j = 0; j < HEADS; ++j)
-            if (head0 + j < a.heads) *(uintx4 *)(y + (head0 + j) * a.y.head + d) = w[j];
-        return;
+    const int head = (int)(item - token * a.heads), half = a.rotary / 2;
+    const uint16_t *x = (const uint16_t *)a.x.ptr + token * a.x.token + head * a.x.head;
+    uint16_t *y = (uint16_t *)a.y.ptr + token * a.y.token + head * a.y.head;
+    const int d0 = INTERLEAVED || (int)d < half ? d : half + d, d1 = INTERLEAVED ? d + a.dim / 2 : (int)d < half ? d + half : d0 + (a.dim - a.rotary) / 2;
+    uintx4 w0, w1;
+    if constexpr (STREAM) {
+        w0 = __builtin_nontemporal_load((const uintx4 *)(x + d0));
+        w1 = __builtin_nontemporal_load((const uintx4 *)(x + d1));
+    } else {
+        w0 = *(const uintx4 *)(x + d0);
+        w1 = *(const uintx4 *)(x + d1);
     }
-    const int half = a.rotary / 2, pair = unit * 8;
-    const int d0 = INTERLEAVED ? 2 * pair : pair, d1 = INTERLEAVED ? d0 + 8 : pair + half;
-    uintx4 w[HEADS][2];
+    if (d0 < a.rotary) {
+        const int position = a.positions[token];
+        // pairs first .. first + 4 and second .. second + 4; interleaved, the second piece may be beyond what is turned
+        const int first = INTERLEAVED ? d0 / 2 : d0, second = INTERLEAVED ? (d1 < a.rotary ? d1 / 2 : first) : d0 + 4;
+        float c[8], s[8];
+        if (position >= 0 && position < a.table_rows) {
+            const float *row = a.table + (int64_t)position * a.rotary;
 #pragma unroll
-    for (int j = 0; j < HEADS; ++j)
-        if (head0 + j < a.heads) {
-            w[j][0] = *(const uintx4 *)(x + (head0 + j) * a.x.head + d0);
-            w[j][1] = *(const uintx4 *)(x + (head0 + j) * a.x.head + d1);
+            for (int i = 0; i < 4; ++i) {
+                c[i] = row[first + i];
+                c[4 + i] = row[second + i];
+                s[i] = row[half + first + i];
+                s[4 + i] = row[half + second + i];
+            }
+        } else {                                        // there is no such angle
+#pragma unroll
+            for (int i = 0; i < 8; ++i) c[i] = s[i] = __builtin_nanf("");
         }
-    const int position = a.positions[token];
-    float c[8], s[8];
-    if (position >= 0 && position < a.table_rows) {
-        const float *row = a.table + (int64_t)position * a.rotary + pair;
+        if (a.inverse)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[i] = -s[i];
+        float u[8], v[8];
+        widen8<BF16>(w0, u);
+        widen8<BF16>(w1, v);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            c[i] = row[i];
-            s[i] = a.inverse ? -row[half + i] : row[half + i];
+            float &p = INTERLEAVED ? (i < 4 ? u[2 * i] : v[2 * i - 8]) : u[i];
+            float &q = INTERLEAVED ? (i < 4 ? u[2 * i + 1] : v[2 * i - 7]) : v[i];
+            const float p2 = p * c[i] - q * s[i];
+            q = q * c[i] + p * s[i];
+            p = p2;
         }
-    } else {                                            // there is no such angle
-#pragma unroll
-        for (int i = 0; i < 8; ++i) c[i] = s[i] = __builtin_nanf("");
+        w0 = narrow8<BF16>(u);
+        if (!INTERLEAVED || d1 < a.rotary) w1 = narrow8<BF16>(v);
     }
-#pragma unroll
-    for (int j = 0; j < HEADS; ++j)
-        if (head0 + j < a.heads) {
-            float u[8], v[8];
-            widen8<BF16>(w[j][0], u);
-            widen8<BF16>(w[j][1], v);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float &p = INTERLEAVED ? (i < 4 ? u[2 * i] : v[2 * i - 8]) : u[i];
-                float &q = INTERLEAVED ? (i < 4 ? u[2 * i + 1] : v[2 * i - 7]) : v[i];
-                const float p2 = p * c[i] - q * s[i];
-                q = q * c[i] + p * s[i];
-                p = p2;
-            }
-            *(uintx4 *)(y + (head0 + j) * a.y.head + d0) = narrow8<BF16>(u);
-            *(uintx4 *)(y + (head0 + j) * a.y.head + d1) = narrow8<BF16>(v);
-        }
+    __builtin_nontemporal_store(w0, (uintx4 *)(y + d0));
+    __builtin_nontemporal_store(w1, (uintx4 *)(y + d1));
 }
 
 // any even part of a head: one pair, or one element that is not turned, per lane
@@ -120,14 +116,17 @@ __global__ void __launch_bounds__(256) k_rotary_any(RotaryArgs a)
     y[d1] = (uint16_t)(w >> 16);
 }
 
+// x beyond the memory-side cache is read as a stream: 335 MB of it (16383 x 80 heads of 128) 108 us so,
+// 111 us with ordinary loads; 42 MB (2048 tokens), which a projection has just written there, 16.7 and 13.9 us.  Where only a part
+// of each head turns, its halves' pieces are not whole lines and ordinary loads are faster in any case (131 and 119 us).
 template <bool BF16, bool INTERLEAVED>
-hipError_t rotary_heads(const RotaryArgs &a, hipStream_t stream)
+hipError_t rotary_pieces(const RotaryArgs &a, hipStream_t stream)
 {
-    const int units = a.rotary / 16 + (a.dim - a.rotary) / 8;
-    constexpr int HEADS = 4;
-    const int blocks = (a.heads + HEADS - 1) / HEADS;
-    const int64_t lanes = a.tokens * blocks * units;
-    return launch_kernel(k_rotary<BF16, INTERLEAVED, HEADS>, dim3((uint32_t)((lanes + 255) / 256)), dim3(256), stream, a, units, blocks);
+    const int64_t lanes = a.tokens * a.heads * (a.dim / 16);
+    const dim3 grid((uint32_t)((lanes + 255) / 256));
+    const bool stream_x = beyond_cache(lanes * 32) && (INTERLEAVED || a.rotary == a.dim);
+    return stream_x ? launch_kernel(k_rotary<BF16, INTERLEAVED, true>, grid, dim3(256), stream, a, a.dim / 16)
+                    : launch_kernel(k_rotary<BF16, INTERLEAVED, false>, grid, dim3(256), stream, a, a.dim / 16);
 }
 
 }  // namespace
@@ -140,9 +139,9 @@ hipError_t launch_rotary_table(const double *frequencies, int64_t rows, int rota
 
 hipError_t launch_rotary(const RotaryArgs &a, hipStream_t stream)
 {
-    if (a.rotary % 16 == 0) {                           // whole 128-bit accesses, and each pair's two halves in two of them
-        if (a.bf16) return a.interleaved ? rotary_heads<true, true>(a, stream) : rotary_heads<true, false>(a, stream);
-        return a.interleaved ? rotary_heads<false, true>(a, stream) : rotary_heads<false, false>(a, stream);
+    if (a.rotary % 16 == 0 && a.dim % 16 == 0) {        // whole 128-bit accesses, and each pair's two halves in two of them
+        if (a.bf16) return a.interleaved ? rotary_pieces<true, true>(a, stream) : rotary_pieces<true, false>(a, stream);
+        return a.interleaved ? rotary_pieces<false, true>(a, stream) : rotary_pieces<false, false>(a, stream);
     }
     const int64_t lanes = a.tokens * a.heads * (a.dim - a.rotary / 2);
     const dim3 grid((uint32_t)((lanes + 255) / 256));
