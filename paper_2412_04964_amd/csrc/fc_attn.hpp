@@ -60,12 +60,16 @@ struct CacheAttentionArgs {
     Rows q, out;
     Step step;
     Cache cache;
-    float *partial;            // [tokens * query heads, splits, dim] sums, then [tokens * query heads, splits, 2] maxima and weights
+    float *partial;            // [workgroups, 2, rows, dim] sums, then [workgroups, 2, rows, 2] maxima and weights
     float scale;
-    int heads, group, dim, fp8, bf16, splits, row_blocks;
+    int heads, group, dim, fp8, bf16;
+    // cache_attention_plan's: 16-row tiles that a workgroup takes; workgroups that share all sequences' contexts evenly, or 0: one for each
+    // head and sequence, and for each of `row_blocks` of its rows; whether codes are read once
+    int row_tiles, row_blocks, workgroups, stream;
+    uint32_t *plan;            // how many units there are, and where each sequence's begin
 };
-// how a call is split: pieces of the context that workgroups take, and workgroups over a sequence's rows
-void cache_attention_plan(int sequences, int heads, int group, int64_t queries, int64_t longest, int *splits, int *row_blocks);
+void cache_attention_plan(int sequences, int heads, int group, int dim, int64_t queries, int64_t longest, CacheAttentionArgs *a);
+size_t cache_attention_workspace(const CacheAttentionArgs &a, int sequences, int dim);
 hipError_t launch_cache_attention(const CacheAttentionArgs &a, hipStream_t stream);
 
 struct PromptArgs {
@@ -149,6 +153,25 @@ __device__ __forceinline__ floatx16 mma32(uintx4 a, uintx4 b, floatx16 c)
 __device__ __forceinline__ floatx4 mma16(uintx4 a, uintx4 b, floatx4 c)
 {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), c, 0, 0, 0);
+}
+
+// 16 bytes per lane from memory to lds + 16 lane.  Not the builtin: the compiler would make LDS reads of what has arrived wait for what is
+// on its way.  Who reads it waits for vmcnt himself, and has read what was there before.  (A wait state between the write of m0, which
+// nothing else in these kernels has a value in, and its use.)  STREAM: marked as read once.
+template <bool STREAM>
+__device__ __forceinline__ void load_to_lds(uintx4 rsrc, int offset, uint32_t lds)
+{
+    if constexpr (STREAM) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(lds), "v"(offset), "s"(rsrc) : "memory");
+    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(rsrc) : "memory");
+}
+
+__device__ __forceinline__ uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p; }
+
+// A buffer resource of `bytes` from `base` on, which all lanes share; beyond them reads are zero
+__device__ __forceinline__ uintx4 resource(const void *base, uint32_t bytes)
+{
+    const uint64_t at = (uint64_t)base;
+    return uintx4{(uint32_t)at, (uint32_t)(at >> 32) & 0xFFFFu, bytes, 0x00020000u};
 }
 
 // Which sequence has work unit u, where sequence b has at most (tokens of b) / 2^shift + extra units and therefore owns the numbers

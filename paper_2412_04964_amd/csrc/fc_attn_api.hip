@@ -45,19 +45,6 @@ int check_cache(const void *k, const void *v, const float *k_scales, const float
 // a launch of this many workgroups of `lanes` is one that the runtime takes
 bool launchable(int64_t workgroups, int lanes) { return workgroups <= ((int64_t)1 << 32) / lanes - 1; }
 
-struct Split { int splits, row_blocks; };
-Split plan(int sequences, int heads, int group, int64_t queries, int64_t longest)
-{
-    Split s;
-    fc::cache_attention_plan(sequences, heads, group, queries, longest, &s.splits, &s.row_blocks);
-    return s;
-}
-
-size_t partial_bytes(int64_t tokens, int query_heads, int dim, int splits)
-{
-    return splits == 1 ? 0 : (size_t)tokens * (size_t)query_heads * (size_t)splits * (size_t)(dim + 2) * sizeof(float);
-}
-
 int check_attention(int64_t tokens, int sequences, int heads, int group, int dim, int64_t queries, int64_t longest)
 {
     const int rc = check_heads(heads, tokens, sequences);
@@ -145,7 +132,9 @@ int fc_cache_append(const void *k, int64_t k_token_stride, int64_t k_head_stride
 size_t fc_cache_attention_workspace_bytes(int64_t tokens, int sequences, int heads, int group, int dim, int64_t queries, int64_t longest)
 {
     if (check_attention(tokens, sequences, heads, group, dim, queries, longest) != FC_OK) return 0;
-    return partial_bytes(tokens, heads * group, dim, plan(sequences, heads, group, queries, longest).splits);
+    fc::CacheAttentionArgs a;
+    fc::cache_attention_plan(sequences, heads, group, dim, queries, longest, &a);
+    return fc::cache_attention_workspace(a, sequences, dim);
 }
 
 int fc_cache_attention(const void *q, int64_t q_token_stride, int64_t q_head_stride, int64_t tokens, int heads, int group, int dim, int type,
@@ -162,26 +151,28 @@ int fc_cache_attention(const void *q, int64_t q_token_stride, int64_t q_head_str
     if (!offsets || !held) return FC_ERR_NULL;
     if ((rc = check_rows(q, q_token_stride, q_head_stride)) != FC_OK) return rc;
     if ((rc = check_rows(out, out_token_stride, out_head_stride)) != FC_OK) return rc;
-    const Split s = plan(sequences, heads, group, queries, longest);
-    const size_t need = partial_bytes(tokens, heads * group, dim, s.splits);
+    fc::CacheAttentionArgs a;
+    fc::cache_attention_plan(sequences, heads, group, dim, queries, longest, &a);
+    // ranges are counted in 32 bits: up to this many units, whatever the arrays say
+    const double units = ((double)table_width * page / 32 + 1) * heads * ((double)tokens * group / 16 + sequences);
+    if (units >= 2147483648.0) a.workgroups = 0;
+    const size_t need = fc::cache_attention_workspace(a, sequences, dim);
     if (need && (!workspace || workspace_bytes < need)) return FC_ERR_WORKSPACE;
     if (need && !aligned16(workspace)) return FC_ERR_ALIGN;
-    if (!launchable((int64_t)sequences * s.row_blocks * heads * s.splits, 256) || !launchable(tokens * heads * group, 256)) return FC_ERR_SHAPE;
-    fc::CacheAttentionArgs a;
+    if (!launchable((int64_t)sequences * a.row_blocks * heads, 512) || !launchable(tokens * heads * group, 256)) return FC_ERR_SHAPE;
     a.q = rows(q, q_token_stride, q_head_stride);
     a.out = rows(out, out_token_stride, out_head_stride);
     a.step = {offsets, held, sequences, tokens};
     a.cache = {static_cast<uint8_t *>(const_cast<void *>(k_cache)), static_cast<uint8_t *>(const_cast<void *>(v_cache)),
                const_cast<float *>(k_scales), const_cast<float *>(v_scales), page_table, pages, page, table_width};
-    a.partial = static_cast<float *>(workspace);
+    a.plan = static_cast<uint32_t *>(workspace);       // the partials behind it, on a 16-byte boundary
+    a.partial = reinterpret_cast<float *>(static_cast<char *>(workspace) + (((size_t)sequences + 1) * sizeof(uint32_t) + 15) / 16 * 16);
     a.scale = scale;
     a.heads = heads;
     a.group = group;
     a.dim = dim;
     a.fp8 = quantizer == FC_QUANTIZER_FP8;
     a.bf16 = type == FC_TYPE_BF16;
-    a.splits = s.splits;
-    a.row_blocks = s.row_blocks;
     return fc::hip_result(fc::launch_cache_attention(a, static_cast<hipStream_t>(hip_stream)));
 }
 

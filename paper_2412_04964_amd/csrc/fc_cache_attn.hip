@@ -17,9 +17,12 @@
 namespace fc {
 namespace {
 
-constexpr int kWaves = 4;
+constexpr int64_t kMaxContext = 0x7FFF0000;
 constexpr float kSlack = 8.0f;          // in powers of two
-constexpr float kMost = 256.0f, kLeast = 1e-30f;
+constexpr float kMost = 256.0f, kTiny = 1e-30f;
+constexpr int kLeast = 8;               // units of a range
+
+constexpr int waves_of(int dim, int row_tiles) { return dim < 256 && row_tiles == 1 ? 8 : 4; }      // of a workgroup for a whole context
 constexpr int kTile = 16;               // tokens of a matrix instruction; a page holds whole tiles
 
 // 4 codes of a word -> binary16
@@ -66,311 +69,601 @@ __device__ __forceinline__ void load_words(const uint8_t *p, uint32_t (&w)[4])
     for (int i = 0; i < 4; ++i) w[i] = x[i];
 }
 
+// until no more than N of this wavefront's loads are on their way
+template <int N>
+__device__ __forceinline__ void wait_vm()
+{
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
 // over the four lanes that share l % 16
 __device__ __forceinline__ float max4(float v) { v = fmaxf(v, __shfl_xor(v, 16)); return fmaxf(v, __shfl_xor(v, 32)); }
 __device__ __forceinline__ float sum4(float v) { v += __shfl_xor(v, 16); return v + __shfl_xor(v, 32); }
 
-// pieces that a sequence of `tiles` tiles is cut into, of at most `splits`: no piece below kWaves tiles' pairs
-__host__ __device__ __forceinline__ int pieces_of(int64_t tiles, int splits)
+// What there is to do for one sequence: its queries and context, and in units of a pair of tiles for each head and block of rows.  A
+// sequence without context has one unit, which writes zeros.
+struct Job {
+    int64_t off, held;
+    int queries, context, units, blocks;                 // blocks: of rows
+};
+
+__device__ __forceinline__ Job job_of(const CacheAttentionArgs &a, int off, int next, int held, int page_shift, int block_rows)
 {
-    const int64_t most = (tiles + 2 * kWaves - 1) / (2 * kWaves);
-    return most < 1 ? 1 : most < splits ? (int)most : splits;
+    Job j;
+    j.off = off;
+    j.held = held;
+    j.queries = off < 0 || next < off || next > a.step.tokens ? 0 : next - off;
+    const int64_t room = (int64_t)a.cache.table_width << page_shift, all = j.held + j.queries;
+    const int64_t seen = all < room ? all : room;
+    j.context = (int)(seen < 0 ? 0 : seen < kMaxContext ? seen : kMaxContext);
+    j.units = j.context > 0 ? (int)(((int64_t)j.context + 2 * kTile - 1) / (2 * kTile)) : 1;
+    j.blocks = (int)(((int64_t)j.queries * a.group + block_rows - 1) / block_rows);
+    return j;
 }
 
-template <int DIM, bool FP8, bool BF16>
-__global__ void __launch_bounds__(64 * kWaves) k_cache_attention(CacheAttentionArgs a, int page_shift)
+// The units of all sequences, one behind the other, are cut into ranges that differ by one unit at most, one for a workgroup.  Fewer ranges
+// than workgroups where they would have less than `least` units.
+struct Ranges {
+    uint32_t count, each, longer;                        // the first `longer` of them have one more than `each`
+    __device__ __forceinline__ Ranges(uint32_t total, uint32_t workgroups, uint32_t least)
+    {
+        const uint32_t most = (total + least - 1) / least;
+        count = most < workgroups ? most : workgroups;
+        each = count ? total / count : 0;
+        longer = total - count * each;
+    }
+    __device__ __forceinline__ uint32_t begin(uint32_t r) const { return r * each + (r < longer ? r : longer); }
+    __device__ __forceinline__ uint32_t of(uint32_t unit) const
+    {
+        const uint32_t split = longer * (each + 1);
+        return unit < split ? unit / (each + 1) : longer + (unit - split) / each;
+    }
+};
+
+// sums of the lanes up to this one
+__device__ __forceinline__ uint32_t running_sum(uint32_t v, int lane)
+{
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        const uint32_t u = __shfl_up(v, m);
+        if (lane >= m) v += u;
+    }
+    return v;
+}
+
+// A wavefront's part of LDS: two tiles of K and two of V, 16 tokens of DIM bytes each, which come straight from memory: those of K for the
+// next step while this one's weights are made and V is read, those of V while the next step reads K.  The 16-byte units of a row are
+// exchanged (unit ^ swizzle of its row): K's operand reads one unit of all 16 rows at a time, without a conflict.
+template <int DIM> constexpr int kTileBytes = kTile * DIM;
+template <int DIM> __device__ __forceinline__ constexpr int swizzle(int row) { return row / (256 / DIM) & (DIM / 16 - 1); }
+
+// The rows of a sequence's queries and the heads that share K and V, 16 ROW_TILES of them at a time.  RANGES: a workgroup has a range of
+// all units, as described at ranges_of; else a block of rows of one sequence and head, from its first token to its last.
+template <int DIM, bool FP8, bool BF16, int ROW_TILES, int WAVES, bool RANGES, bool STREAM>
+__global__ void __launch_bounds__(64 * WAVES, DIM == 256 ? 2 : ROW_TILES == 1 ? 4 : 2) k_cache_attention(CacheAttentionArgs a, int page_shift)
 {
     constexpr int kSteps = DIM / 32;                    // matrix instructions over the head's elements
     constexpr int kOut = DIM / 16;                      // result tiles
     constexpr int kWords = DIM / 64;                    // 4-byte words of V that a lane has of a token
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quad = lane >> 4;
-    uint32_t at = blockIdx.x;
-    const int piece = at % a.splits;
-    at /= a.splits;
-    const int head = at % a.heads;
-    at /= a.heads;
-    const int row_block = at % a.row_blocks, b = at / a.row_blocks;
+    constexpr int kRows = 16 * ROW_TILES;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
 
-    const int64_t off = a.step.offsets[b], held = a.step.held[b];
-    int64_t queries = (int64_t)a.step.offsets[b + 1] - off;
-    if (off < 0 || queries < 0 || off + queries > a.step.tokens) return;
-    const int64_t room = (int64_t)a.cache.table_width << page_shift;
-    const int64_t context = held + queries < room ? held + queries : room;     // may be negative
-    const int64_t tiles = context > 0 ? (context + kTile - 1) / kTile : 0;
-    const int pieces = pieces_of(tiles, a.splits);
-    if (piece >= pieces) return;
-    // this workgroup's tiles, in pairs, then this wavefront's
-    const int64_t pairs = (tiles + 1) / 2;
-    const int64_t pair0 = pairs * piece / pieces, pair1 = pairs * (piece + 1) / pieces;
-    const int64_t begin = 2 * (pair0 + (pair1 - pair0) * wave / kWaves), stop = 2 * (pair0 + (pair1 - pair0) * (wave + 1) / kWaves);
-    const int64_t end_token = stop * kTile < context ? stop * kTile : context;  // of this wavefront
+    int b, head, block;                                 // what the workgroup is at
+    uint32_t at = 0, end = 0, begins = 0;               // RANGES: its place in all units and where it ends; where the sequence's begin
+    Job job;
+    if constexpr (RANGES) {
+        int off = 0, next = 0, held = 0;
+        uint32_t sum = 0, work = 0;
+        for (int c = 0; c < a.step.sequences; c += 64)
+            if (c + lane < a.step.sequences) {
+                off = a.step.offsets[c + lane];
+                next = a.step.offsets[c + lane + 1];
+                held = a.step.held[c + lane];
+                const Job j = job_of(a, off, next, held, page_shift, kRows);
+                work = j.units * j.blocks * a.heads;
+                sum += work;
+            }
+        uint32_t upto = running_sum(sum, lane);
+        const uint32_t total = __builtin_amdgcn_readlane(upto, 63);
+        const Ranges ranges(total, gridDim.x, kLeast);
+        if (blockIdx.x == 0 && threadIdx.x == 0) a.plan[0] = total;
+        if (blockIdx.x >= ranges.count) return;
+        at = ranges.begin(blockIdx.x);
+        end = ranges.begin(blockIdx.x + 1);
+        b = -1;
+        uint32_t run = 0;
+        for (int c = 0; c < a.step.sequences; c += 64) {
+            if (a.step.sequences > 64) {                // else the lanes have them still
+                work = 0;
+                if (c + lane < a.step.sequences) {
+                    off = a.step.offsets[c + lane];
+                    next = a.step.offsets[c + lane + 1];
+                    held = a.step.held[c + lane];
+                    const Job j = job_of(a, off, next, held, page_shift, kRows);
+                    work = j.units * j.blocks * a.heads;
+                }
+                upto = run + running_sum(work, lane);
+            }
+            if (blockIdx.x == 0 && wave == 0 && c + lane < a.step.sequences) a.plan[1 + c + lane] = upto - work;
+            const uint64_t past = __ballot(upto > at);
+            if (b < 0 && past) {
+                const int l = __builtin_ctzll(past);
+                b = c + l;
+                begins = __builtin_amdgcn_readlane(upto - work, l);
+                job = job_of(a, __builtin_amdgcn_readlane(off, l), __builtin_amdgcn_readlane(next, l), __builtin_amdgcn_readlane(held, l), page_shift, kRows);
+                if (blockIdx.x) break;                  // the first one writes where every sequence begins
+            }
+            run = __builtin_amdgcn_readlane(upto, 63);
+        }
+    } else {
+        uint32_t id = blockIdx.x;
+        head = id % a.heads;
+        id /= a.heads;
+        block = id % a.row_blocks;
+        b = id / a.row_blocks;
+        job = job_of(a, a.step.offsets[b], a.step.offsets[b + 1], a.step.held[b], page_shift, kRows);
+    }
 
-    __shared__ float join[kWaves][16][DIM + 4];
-    __shared__ float join_max[kWaves][16], join_sum[kWaves][16];
+    __shared__ __attribute__((aligned(1024))) uint8_t stages[WAVES][4 * kTileBytes<DIM>];
+    __shared__ float join_max[WAVES][16], join_sum[WAVES][16];
+    float(*join)[16][DIM + 4] = reinterpret_cast<float(*)[16][DIM + 4]>(stages);       // [WAVES / 2], when the stages are done with
+    static_assert(sizeof(stages) >= sizeof(float) * WAVES / 2 * 16 * (DIM + 4), "the wavefronts' sums fit the stages");
+    static_assert(sizeof(stages) <= 65536, "m0 has 16 bits of an LDS address");
+    // this lane's places: of the pieces that it brings to a tile, and of its operands in one
+    constexpr int kPieces = kTileBytes<DIM> / 1024, kPieceRows = 1024 / DIM;
+    int bring_at[kPieces];
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+        const int row = i * kPieceRows + lane / (DIM / 16);
+        bring_at[i] = row * DIM + ((lane % (DIM / 16)) ^ swizzle<DIM>(row)) * 16;
+    }
+    const int at_k = col * DIM + (quad ^ swizzle<DIM>(col)) * 16;
+    const int at_v = quad * 4 * DIM + ((col * DIM / 256) ^ swizzle<DIM>(quad * 4)) * 16 + col * (DIM / 16) % 16;
+    const uint32_t lds = lds_address(&stages[wave][0]);
+    const uint8_t *const tile_k = &stages[wave][0], *const tile_v = tile_k + 2 * kTileBytes<DIM>;
 
-    const int64_t rows = queries * a.group;
-    for (int64_t row0 = (int64_t)row_block * 16; row0 < rows; row0 += (int64_t)a.row_blocks * 16) {
-        const int64_t row = row0 + col;
-        const int64_t query = row < rows ? row / a.group : queries - 1;
-        const int64_t token = off + query;
-        const int query_head = head * a.group + (int)(row - query * a.group);
-        int64_t sees = held + query + 1;
-        if (sees > end_token) sees = end_token;
-        if (row >= rows) sees = 0;
-        const int64_t all_see = held + row0 / a.group + 1 < end_token ? held + row0 / a.group + 1 : end_token;    // what every row of the block sees
+    while (RANGES ? at < end : block < job.blocks) {
+        int pair0 = 0, pair1 = job.units;               // of the sequence
+        if constexpr (RANGES) {
+            const uint32_t work = job.units * job.blocks * a.heads;
+            if (at >= begins + work) {
+                begins += work;
+                ++b;
+                job = job_of(a, a.step.offsets[b], a.step.offsets[b + 1], a.step.held[b], page_shift, kRows);
+                continue;
+            }
+            const uint32_t item = (at - begins) / job.units, item0 = begins + item * job.units;
+            head = (int)(item / job.blocks);
+            block = (int)(item - (uint32_t)head * job.blocks);
+            pair0 = at - item0;
+            if (end - item0 < (uint32_t)pair1) pair1 = end - item0;
+            at = item0 + pair1;
+        }
+        const bool whole = pair0 == 0 && pair1 == job.units;
+        const int64_t off = job.off, held = job.held, rows = (int64_t)job.queries * a.group, row0 = (int64_t)block * kRows;
+        const int context = job.context;
+        const int begin = 2 * (pair0 + (pair1 - pair0) * wave / WAVES), stop = 2 * (pair0 + (pair1 - pair0) * (wave + 1) / WAVES);
+        const int end_token = stop * kTile < context ? stop * kTile : context;  // of this wavefront
 
-        // the row's elements quad * DIM / 4 .., scaled into binary16
-        uintx4 qf[kSteps];
-        float factor;
-        {
-            float f[kSteps][8], most = 0.0f;
-            const uint16_t *q = (const uint16_t *)a.q.ptr + token * a.q.token + query_head * a.q.head + quad * (DIM / 4);
+        // the rows: elements 64 j + 16 quad + 8 s for step 2 j + s
+        uintx4 qf[ROW_TILES][kSteps];
+#pragma unroll
+        for (int x = 0; x < ROW_TILES; ++x) {
+            const int64_t row = row0 + 16 * x + col, query = row < rows ? row / a.group : 0;
+            const int query_head = head * a.group + (int)(row - query * a.group);
+            const uint16_t *q = (const uint16_t *)a.q.ptr + (off + query) * a.q.token + query_head * a.q.head + quad * 16;
 #pragma unroll
             for (int j = 0; j < kSteps; ++j) {
-                if (row < rows) widen8<BF16>(*(const uintx4 *)(q + 8 * j), f[j]);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    if (row >= rows) f[j][i] = 0.0f;
-                    most = fmaxf(most, fabsf(f[j][i]));
+                qf[x][j] = uintx4{0, 0, 0, 0};
+                if (row < rows) qf[x][j] = *(const uintx4 *)(q + 64 * (j / 2) + 8 * (j & 1));
+            }
+        }
+        const int64_t least_seen = held + row0 / a.group + 1;
+        const int all_see = least_seen < 0 ? 0 : least_seen < end_token ? (int)least_seen : end_token;     // what every row of the block sees
+
+        // page and scales of 64 tiles from `base` on, one a lane
+        int page = 0;
+        float ks = 0.0f, vs = 0.0f;
+        const auto look_up = [&](int base) {
+            page = 0;
+            ks = vs = 0.0f;
+            if (base + lane < stop && (base + lane) * kTile < context) {
+                const int id = a.cache.table[(int64_t)b * a.cache.table_width + ((base + lane) * kTile >> page_shift)];
+                if (id >= 0 && id < a.cache.pages) {
+                    page = id;
+                    ks = a.cache.k_scales[(int64_t)id * a.heads + head];
+                    vs = a.cache.v_scales[(int64_t)id * a.heads + head];
                 }
             }
-            factor = 1.0f;
+        };
+        // the pair of tiles of lanes i and i + 1, from base + i on; what the place held before has been read
+        const auto bring = [&](const uint8_t *from, uint32_t to, int base, int i) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const int slot = ((base + i + t) * kTile) & ((1 << page_shift) - 1);
+                const int64_t place = ((((int64_t)__builtin_amdgcn_readlane(page, i + t) * a.heads + head) << page_shift) + slot) * DIM;
+                const uintx4 tile = resource(from + place, kTileBytes<DIM>);
+#pragma unroll
+                for (int j = 0; j < kPieces; ++j) load_to_lds<STREAM>(tile, bring_at[j], to + t * kTileBytes<DIM> + j * 1024);
+            }
+        };
+        const uint32_t to_k = lds, to_v = lds + 2 * kTileBytes<DIM>;
+        if (begin < stop) {
+            look_up(begin);
+            bring(a.cache.k, to_k, begin, 0);
+            bring(a.cache.v, to_v, begin, 0);
+        }
+
+        float factor[ROW_TILES];                        // scores in powers of two
+#pragma unroll
+        for (int x = 0; x < ROW_TILES; ++x) {
+            factor[x] = a.scale * 1.4426950408889634f;
             if constexpr (BF16) {
+                // into binary16, the largest magnitude times 2^e in [2^13, 2^14)
+                float most = 0.0f;
+#pragma unroll
+                for (int j = 0; j < kSteps; ++j) {
+                    float f[8];
+                    widen8<BF16>(qf[x][j], f);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(f[i]));
+                }
                 most = max4(most);
                 int e = 0;
-                if (most > 0.0f && most < __builtin_inff()) e = 14 - __builtin_amdgcn_frexp_expf(most);      // most * 2^e in [2^13, 2^14)
-                factor = __builtin_amdgcn_ldexpf(1.0f, -e);
+                if (most > 0.0f && most < __builtin_inff()) e = 14 - __builtin_amdgcn_frexp_expf(most);
 #pragma unroll
-                for (int j = 0; j < kSteps; ++j)
+                for (int j = 0; j < kSteps; ++j) {
+                    float f[8];
+                    widen8<BF16>(qf[x][j], f);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) f[j][i] = __builtin_amdgcn_ldexpf(f[j][i], e);
+                    for (int i = 0; i < 8; ++i) f[i] = __builtin_amdgcn_ldexpf(f[i], e);
+                    qf[x][j] = narrow8<false>(f);
+                }
+                factor[x] = __builtin_amdgcn_ldexpf(factor[x], -e);
             }
-#pragma unroll
-            for (int j = 0; j < kSteps; ++j) qf[j] = narrow8<false>(f[j]);
-            factor *= a.scale * 1.4426950408889634f;    // scores in powers of two
         }
 
-        floatx4 acc[kOut];
+        floatx4 acc[ROW_TILES][kOut];
+        float top[ROW_TILES], total[ROW_TILES], ref[ROW_TILES];
 #pragma unroll
-        for (int i = 0; i < kOut; ++i) acc[i] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-        float top = -FLT_MAX, total = 0.0f, ref = kLeast, inv_ref = 1.0f / kLeast;
+        for (int x = 0; x < ROW_TILES; ++x) {
+#pragma unroll
+            for (int o = 0; o < kOut; ++o) acc[x][o] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+            top[x] = -FLT_MAX;
+            total[x] = 0.0f;
+            ref[x] = kTiny;
+        }
         // the sums' unit: they are acc * was, and are acc * ref afterwards
-        const auto rebase = [&](float was, float least) {
-            ref = fmaxf(was, least);
-            inv_ref = 1.0f / ref;
-            const float change = was * inv_ref;
+        const auto rebase = [&](int x, float was, float least) {
+            ref[x] = fmaxf(was, least);
+            const float change = was / ref[x];
 #pragma unroll
-            for (int o = 0; o < kOut; ++o) acc[o] *= change;
+            for (int o = 0; o < kOut; ++o) acc[x][o] *= change;
         };
 
-        for (int64_t base = begin; base < stop; base += 64) {
-            // page and scales of the next 64 tiles, one a lane
-            int page = 0;
-            float ks = 0.0f, vs = 0.0f;
-            {
-                const int64_t index = (base + lane) * kTile >> page_shift;
-                if (base + lane < stop && (base + lane) * kTile < context) {
-                    const int id = a.cache.table[(int64_t)b * a.cache.table_width + index];
-                    if (id >= 0 && id < a.cache.pages) {
-                        page = id;
-                        ks = a.cache.k_scales[(int64_t)id * a.heads + head];
-                        vs = a.cache.v_scales[(int64_t)id * a.heads + head];
-                    }
-                }
+        for (int base = begin; base < stop; base += 64) {
+            const int n = stop - base < 64 ? stop - base : 64;
+            if (base != begin) {
+                look_up(base);
+                bring(a.cache.k, to_k, base, 0);
+                bring(a.cache.v, to_v, base, 0);
             }
-            const int n = stop - base < 64 ? (int)(stop - base) : 64;
+            // the scales are here before the loop, where waiting for them would wait for all that is on its way
+            asm volatile("" : "+v"(ks), "+v"(vs));
             for (int i = 0; i < n; i += 2) {
-                const int64_t first = (base + i) * kTile;
-                if (first >= end_token) break;
-                uintx4 kf[2][kSteps / 2];
-                uint32_t vf[2][4][kWords];
-                float ksc[2], vsc[2];
+                const int first = (base + i) * kTile;
+                wait_vm<2 * kPieces>();                 // K is here, V may be on its way
+                floatx4 s[ROW_TILES][2];
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    const int64_t slot = ((base + i + t) * kTile) & ((1 << page_shift) - 1);
-                    const int64_t place = ((((int64_t)__builtin_amdgcn_readlane(page, i + t) * a.heads + head) << page_shift) + slot) * DIM;
-                    ksc[t] = lane_f(ks, i + t);
-                    vsc[t] = lane_f(vs, i + t);
-                    const uint8_t *k = a.cache.k + place + col * DIM + quad * (DIM / 4);
 #pragma unroll
-                    for (int j = 0; j < kSteps / 2; ++j) kf[t][j] = *(const uintx4 *)(k + 16 * j);
-                    const uint8_t *v = a.cache.v + place + quad * 4 * DIM + col * (DIM / 16);
+                    for (int x = 0; x < ROW_TILES; ++x) s[x][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) load_words(v + r * DIM, vf[t][r]);
-                }
-                floatx4 s[2];
+                    for (int j = 0; j < kWords; ++j) {
+                        const uintx4 w = *(const uintx4 *)(tile_k + t * kTileBytes<DIM> + (at_k ^ (j << 6)));
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    s[t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+                        for (int h = 0; h < 2; ++h) {
+                            const uintx2 lo = halves<FP8>(w[2 * h]), hi = halves<FP8>(w[2 * h + 1]);
 #pragma unroll
-                    for (int j = 0; j < kSteps; ++j) {
-                        const uintx2 lo = halves<FP8>(kf[t][j / 2][(j & 1) * 2]), hi = halves<FP8>(kf[t][j / 2][(j & 1) * 2 + 1]);
-                        s[t] = mma16(uintx4{lo[0], lo[1], hi[0], hi[1]}, qf[j], s[t]);
-                    }
-                    const float scale = factor * ksc[t];
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) s[t][r] *= scale;
-                }
-                if (first + 2 * kTile > all_see) {
-                    // tokens that a row does not see: whatever the cache holds there
-#pragma unroll
-                    for (int t = 0; t < 2; ++t)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const int64_t tok = first + t * kTile + quad * 4 + r;
-                            if (tok >= sees) s[t][r] = -__builtin_inff();
-                            if (tok >= end_token)
-#pragma unroll
-                                for (int w = 0; w < kWords; ++w) vf[t][r][w] = 0;
+                            for (int x = 0; x < ROW_TILES; ++x) s[x][t] = mma16(uintx4{lo[0], lo[1], hi[0], hi[1]}, qf[x][2 * j + h], s[x][t]);
                         }
+                    }
                 }
-                float most = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-                if (__any(most > top + kSlack)) {
-                    const float now = fmaxf(top, max4(most)), shrink = __builtin_amdgcn_exp2f(top - now);
-                    top = now;
-                    total *= shrink;
-                    rebase(ref * shrink, kLeast);
-                }
-                float p[8];
+                const bool more = i + 2 < n;
+                if (more) bring(a.cache.k, to_k, base, i + 2);
+                const float ksc[2] = {lane_f(ks, i), lane_f(ks, i + 1)}, vsc[2] = {lane_f(vs, i), lane_f(vs, i + 1)};
+                const bool masked = first + 2 * kTile > all_see;
+                uintx4 pf[ROW_TILES];
 #pragma unroll
-                for (int r = 0; r < 8; ++r) {
-                    p[r] = __builtin_amdgcn_exp2f(s[r / 4][r % 4] - top);
-                    total += p[r];
-                    p[r] *= vsc[r / 4];
-                }
-                const float weight = fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7])));
-                if (__any(weight * inv_ref > kMost)) rebase(ref, max4(weight));
-                uintx4 pf;
+                for (int x = 0; x < ROW_TILES; ++x) {
+                    float scale[2], most = -__builtin_inff();
 #pragma unroll
-                for (int r = 0; r < 4; ++r) pf[r] = narrow2<false>(p[2 * r] * inv_ref, p[2 * r + 1] * inv_ref);
+                    for (int t = 0; t < 2; ++t) {
+                        scale[t] = factor[x] * ksc[t];
+                        if (masked) {                   // (a scale of 0 would make NaN of a masked score)
+                            const int64_t row = row0 + 16 * x + col, seen = held + row / a.group + 1;
+                            const int sees = row >= rows || seen < 0 ? 0 : seen < end_token ? (int)seen : end_token;
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) s[x][t][r] = first + t * kTile + quad * 4 + r < sees ? s[x][t][r] * scale[t] : -__builtin_inff();
+                            scale[t] = 1.0f;
+                        }
+                        most = fmaxf(most, fmaxf(fmaxf(s[x][t][0], s[x][t][1]), fmaxf(s[x][t][2], s[x][t][3])) * scale[t]);
+                    }
+                    if (__any(most > top[x] + kSlack)) {
+                        const float now = fmaxf(top[x], max4(most)), shrink = __builtin_amdgcn_exp2f(top[x] - now);
+                        top[x] = now;
+                        total[x] *= shrink;
+                        rebase(x, ref[x] * shrink, kTiny);
+                    }
+                    float p[8], w[8];
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) {
+                        p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][r / 4][r % 4], scale[r / 4], -top[x]));
+                        total[x] += p[r];
+                    }
+                    const auto weigh = [&] {
+                        const float inv = __builtin_amdgcn_rcpf(ref[x]), unit[2] = {vsc[0] * inv, vsc[1] * inv};
+#pragma unroll
+                        for (int r = 0; r < 8; ++r) w[r] = p[r] * unit[r / 4];
+                        return fmaxf(fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3])), fmaxf(fmaxf(w[4], w[5]), fmaxf(w[6], w[7])));
+                    };
+                    const float weight = weigh();
+                    if (__any(weight > kMost)) {
+                        rebase(x, ref[x], max4(weight) * ref[x]);
+                        weigh();
+                    }
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) pf[x][r] = narrow2<false>(w[2 * r], w[2 * r + 1]);
+                }
+                if (more) wait_vm<2 * kPieces>();       // V is here, the next K may be on its way
+                else wait_vm<0>();
+                uint32_t vf[2][4][kWords];
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        load_words(tile_v + t * kTileBytes<DIM> + r * DIM + (at_v ^ (swizzle<DIM>(r) << 4)), vf[t][r]);
+                        // codes beyond the context: whatever the cache holds there
+                        if (masked && first + t * kTile + quad * 4 + r >= end_token)
+#pragma unroll
+                            for (int w = 0; w < kWords; ++w) vf[t][r][w] = 0;
+                    }
 #pragma unroll
                 for (int w = 0; w < kWords; ++w) {
-                    uint32_t x[2][4];
+                    uint32_t y[2][4];
 #pragma unroll
-                    for (int t = 0; t < 2; ++t) transpose4(vf[t][0][w], vf[t][1][w], vf[t][2][w], vf[t][3][w], x[t]);
+                    for (int t = 0; t < 2; ++t) transpose4(vf[t][0][w], vf[t][1][w], vf[t][2][w], vf[t][3][w], y[t]);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const uintx2 lo = halves<FP8>(x[0][e]), hi = halves<FP8>(x[1][e]);
-                        acc[w * 4 + e] = mma16(uintx4{lo[0], lo[1], hi[0], hi[1]}, pf, acc[w * 4 + e]);
+                        const uintx2 lo = halves<FP8>(y[0][e]), hi = halves<FP8>(y[1][e]);
+#pragma unroll
+                        for (int x = 0; x < ROW_TILES; ++x) acc[x][w * 4 + e] = mma16(uintx4{lo[0], lo[1], hi[0], hi[1]}, pf[x], acc[x][w * 4 + e]);
                     }
                 }
+                if (more) bring(a.cache.v, to_v, base, i + 2);
             }
         }
-        total = sum4(total);
 
-        // join the wavefronts
-        if (quad == 0) {
-            join_max[wave][col] = top;
-            join_sum[wave][col] = total;
-        }
-        __syncthreads();
-        float best = join_max[0][col];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) best = fmaxf(best, join_max[w][col]);
-        const float mine = __builtin_amdgcn_exp2f(top - best) * ref;
+        for (int x = 0; x < ROW_TILES; ++x) {
+            if (16 * x >= rows - row0) break;
+            __syncthreads();                            // the stages, or the row tile before, are done with
+            // join the wavefronts: all in the unit of the largest maximum, then halves of them added to the other half
+            const float sum = sum4(total[x]);
+            if (quad == 0) {
+                join_max[wave][col] = top[x];
+                join_sum[wave][col] = sum;
+            }
+            __syncthreads();
+            float best = join_max[0][col], all = 0.0f;
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+            for (int w = 1; w < WAVES; ++w) best = fmaxf(best, join_max[w][col]);
 #pragma unroll
-            for (int o = 0; o < kOut; ++o) join[wave][col][(quad * 4 + r) * kOut + o] = acc[o][r] * mine;
-        __syncthreads();
-        // 16 lanes a row, each DIM / 16 neighbouring elements
-        const int out_row = threadIdx.x >> 4, d = (threadIdx.x & 15) * kOut;
-        float best_row = join_max[0][out_row], sum_row = 0.0f, o[kOut];
+            for (int w = 0; w < WAVES; ++w) all += join_sum[w][col] * __builtin_amdgcn_exp2f(join_max[w][col] - best);
+            const float mine = __builtin_amdgcn_exp2f(top[x] - best) * ref[x];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) best_row = fmaxf(best_row, join_max[w][out_row]);
+            for (int o = 0; o < kOut; ++o) acc[x][o] *= mine;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) sum_row += join_sum[w][out_row] * __builtin_amdgcn_exp2f(join_max[w][out_row] - best_row);
+            for (int half = WAVES / 2; half; half >>= 1) {
+                if (wave >= half && wave < 2 * half)
 #pragma unroll
-        for (int i = 0; i < kOut; ++i) {
-            o[i] = join[0][out_row][d + i];
+                    for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int w = 1; w < kWaves; ++w) o[i] += join[w][out_row][d + i];
-        }
-        if (row0 + out_row < rows) {
-            const int64_t q = (row0 + out_row) / a.group;
-            const int h = head * a.group + (int)(row0 + out_row - q * a.group);
-            if (pieces == 1) {
-                const float inv = sum_row == 0.0f ? 0.0f : 1.0f / sum_row;      // a row that sees nothing is zero
-                uint16_t *y = (uint16_t *)a.out.ptr + (off + q) * a.out.token + h * a.out.head + d;
+                        for (int o = 0; o < kOut; o += 4)
+                            *(floatx4 *)&join[wave - half][col][(quad * 4 + r) * kOut + o] = floatx4{acc[x][o][r], acc[x][o + 1][r], acc[x][o + 2][r], acc[x][o + 3][r]};
+                __syncthreads();
+                if (wave < half)
 #pragma unroll
-                for (int i = 0; i < kOut; i += 2) *(uint32_t *)(y + i) = narrow2<BF16>(o[i] * inv, o[i + 1] * inv);
-            } else {
-                const int64_t at_row = ((off + q) * a.heads * a.group + h) * a.splits + piece;
-                float *y = a.partial + at_row * DIM + d;
+                    for (int r = 0; r < 4; ++r)
 #pragma unroll
-                for (int i = 0; i < kOut; i += 4) *(floatx4 *)(y + i) = floatx4{o[i], o[i + 1], o[i + 2], o[i + 3]};
-                if ((threadIdx.x & 15) == 0) {
-                    float *m = a.partial + (int64_t)a.step.tokens * a.heads * a.group * a.splits * DIM + at_row * 2;
-                    m[0] = best_row;
-                    m[1] = sum_row;
+                        for (int o = 0; o < kOut; o += 4) {
+                            const floatx4 y = *(const floatx4 *)&join[wave][col][(quad * 4 + r) * kOut + o];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) acc[x][o + i][r] += y[i];
+                        }
+                __syncthreads();
+            }
+            const int64_t row = row0 + 16 * x + col;
+            if (wave == 0 && row < rows) {
+                const int64_t q = row / a.group;
+                const int h = head * a.group + (int)(row - q * a.group);
+                if (whole) {
+                    const float inv = all == 0.0f ? 0.0f : 1.0f / all;          // a row that sees nothing is zero
+                    uint16_t *y = (uint16_t *)a.out.ptr + (off + q) * a.out.token + h * a.out.head + quad * 4 * kOut;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+#pragma unroll
+                        for (int o = 0; o < kOut; o += 4)
+                            *(uintx2 *)(y + r * kOut + o) = uintx2{narrow2<BF16>(acc[x][o][r] * inv, acc[x][o + 1][r] * inv), narrow2<BF16>(acc[x][o + 2][r] * inv, acc[x][o + 3][r] * inv)};
+                } else {
+                    const int64_t place = ((int64_t)blockIdx.x * 2 + (pair0 == 0)) * kRows + 16 * x + col;
+                    float *y = a.partial + place * DIM + quad * 4 * kOut;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+#pragma unroll
+                        for (int o = 0; o < kOut; o += 4)
+                            *(floatx4 *)(y + r * kOut + o) = floatx4{acc[x][o][r], acc[x][o + 1][r], acc[x][o + 2][r], acc[x][o + 3][r]};
+                    if (quad == 0) *(floatx2 *)(a.partial + (int64_t)gridDim.x * 2 * kRows * DIM + place * 2) = floatx2{best, all};
                 }
             }
         }
-        __syncthreads();
+        if constexpr (!RANGES) block += a.row_blocks;
     }
 }
 
-// joins the pieces of a row: DIM / 4 lanes, 4 elements each
-template <int DIM, bool BF16>
+// Joins the pieces of the rows that were cut.  A range has two places for them: 1 for an item that it begins and does not end, 0 for one
+// that began before.  WAVES wavefronts for a token's row; in one, DIM / 4 lanes have 4 elements each.
+template <int DIM, bool BF16, int WAVES>
 __global__ void __launch_bounds__(256) k_cache_attention_join(CacheAttentionArgs a, int page_shift)
 {
-    constexpr int kLanes = DIM / 4;
-    const int64_t row = (int64_t)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes;
-    const int d = threadIdx.x % kLanes * 4, query_heads = a.heads * a.group;
-    if (row >= a.step.tokens * query_heads) return;
-    const int64_t token = row / query_heads;
-    const int head = (int)(row - token * query_heads);
-    const int b = find_sequence(a.step.offsets, a.step.sequences, 0, 0, token);
-    const int64_t off = a.step.offsets[b], next = a.step.offsets[b + 1], room = (int64_t)a.cache.table_width << page_shift;
-    if (token < off || token >= next || next > a.step.tokens) return;
-    int64_t context = a.step.held[b] + (next - off);
-    if (context > room) context = room;
-    const int pieces = pieces_of(context > 0 ? (context + kTile - 1) / kTile : 0, a.splits);
-    if (pieces == 1) return;                            // written already
-    const float *o = a.partial + row * a.splits * DIM + d;
-    const float *m = a.partial + (int64_t)a.step.tokens * query_heads * a.splits * DIM + row * a.splits * 2;
+    constexpr int kLanes = DIM / 4, kSets = 64 * WAVES / kLanes;          // every kSets-th piece is one set of lanes'
+    const int block_rows = 16 * a.row_tiles, query_heads = a.heads * a.group;
+    const int64_t row_id = (int64_t)blockIdx.x * (4 / WAVES) + (WAVES == 4 ? 0 : threadIdx.x / (64 * WAVES));
+    if (row_id >= a.step.tokens * query_heads) return;
+    const int64_t token = row_id / query_heads;
+    const int h = (int)(row_id - token * query_heads), head = h / a.group;
+    // single tokens: the sequence is the token's, or else it is looked for
+    const int guess = token < a.step.sequences ? (int)token : a.step.sequences - 1;
+    int off = a.step.offsets[guess], next = a.step.offsets[guess + 1], held = a.step.held[guess];
+    uint32_t begins = a.plan[1 + guess];
+    const uint32_t total = a.plan[0];
+    if (off != token || next != token + 1) {
+        const int b = find_sequence(a.step.offsets, a.step.sequences, 0, 0, token);
+        off = a.step.offsets[b];
+        next = a.step.offsets[b + 1];
+        held = a.step.held[b];
+        begins = a.plan[1 + b];
+    }
+    const Job job = job_of(a, off, next, held, page_shift, block_rows);
+    if (token < off || token >= off + job.queries) return;
+    const Ranges ranges(total, a.workgroups, kLeast);
+    const int64_t row = (token - off) * a.group + (h - head * a.group);
+    const int block = (int)(row / block_rows), row_at = (int)(row - (int64_t)block * block_rows);
+    const uint32_t item0 = begins + ((uint32_t)head * job.blocks + block) * job.units;
+    const uint32_t first = ranges.of(item0), last = ranges.of(item0 + job.units - 1);
+    if (first == last) return;                          // written already
+    const int pieces = (int)(last - first) + 1;
+    const auto place = [&](int p) { return ((int64_t)(first + p) * 2 + (p == 0)) * block_rows + row_at; };
+
+    const floatx2 *m = (const floatx2 *)(a.partial + (int64_t)a.workgroups * 2 * block_rows * DIM);
+    const int lane = threadIdx.x & 63, d = threadIdx.x % kLanes * 4, set = threadIdx.x % (64 * WAVES) / kLanes;
     float best = -FLT_MAX, sum = 0.0f;
     floatx4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int p = 0; p < pieces; ++p) best = fmaxf(best, m[2 * p]);
-    for (int p = 0; p < pieces; ++p) {
-        const float w = __builtin_amdgcn_exp2f(m[2 * p] - best);
-        sum += w * m[2 * p + 1];
-        x += *(const floatx4 *)(o + (int64_t)p * DIM) * w;
+    for (int p0 = 0; p0 < pieces; p0 += 64) {
+        const int n = pieces - p0 < 64 ? pieces - p0 : 64;
+        floatx2 mine = {-FLT_MAX, 0.0f};
+        if (lane < n) mine = m[place(p0 + lane)];
+        // the first pieces' sums are on their way meanwhile
+        floatx4 early = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (set < n) early = *(const floatx4 *)(a.partial + place(p0 + set) * DIM + d);
+        float top = mine[0];
+#pragma unroll
+        for (int w = 1; w < 64; w <<= 1) top = fmaxf(top, __shfl_xor(top, w));
+        const float now = fmaxf(best, top), shrink = __builtin_amdgcn_exp2f(best - now);
+        best = now;
+        const float weight = __builtin_amdgcn_exp2f(mine[0] - now);
+        sum = sum * shrink + weight * mine[1];          // a part of it in each lane
+        x *= shrink;
+        x += early * __shfl(weight, set < n ? set : 0);
+        for (int p = kSets; p < n; p += kSets) {
+            const float w = __shfl(weight, p + set < 64 ? p + set : 63);
+            if (p + set < n) x += *(const floatx4 *)(a.partial + place(p0 + p + set) * DIM + d) * w;
+        }
+    }
+#pragma unroll
+    for (int w = 1; w < 64; w <<= 1) sum += __shfl_xor(sum, w);
+    if constexpr (WAVES > 1) {
+        __shared__ floatx4 sets[kSets][kLanes];
+        sets[set][threadIdx.x % kLanes] = x;
+        __syncthreads();
+        if (set) return;
+#pragma unroll
+        for (int i = 1; i < kSets; ++i) x += sets[i][threadIdx.x];
+    } else {
+#pragma unroll
+        for (int w = kLanes; w < 64; w <<= 1)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] += __shfl_xor(x[i], w);
+        if (set) return;
     }
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    uint16_t *y = (uint16_t *)a.out.ptr + token * a.out.token + head * a.out.head + d;
+    uint16_t *y = (uint16_t *)a.out.ptr + token * a.out.token + h * a.out.head + d;
     *(uintx2 *)y = uintx2{narrow2<BF16>(x[0] * inv, x[1] * inv), narrow2<BF16>(x[2] * inv, x[3] * inv)};
 }
 
-template <int DIM, bool BF16>
-hipError_t attend(const CacheAttentionArgs &a, hipStream_t stream)
+template <int DIM, bool FP8, bool BF16, int ROW_TILES>
+hipError_t attend_rows(const CacheAttentionArgs &a, hipStream_t stream)
 {
     const int shift = log2_int(a.cache.page);
-    const dim3 grid((uint32_t)((int64_t)a.step.sequences * a.row_blocks * a.heads * a.splits));
-    const hipError_t e = a.fp8 ? launch_kernel(k_cache_attention<DIM, true, BF16>, grid, dim3(64 * kWaves), stream, a, shift)
-                               : launch_kernel(k_cache_attention<DIM, false, BF16>, grid, dim3(64 * kWaves), stream, a, shift);
-    if (e != hipSuccess || a.splits == 1) return e;
-    const int64_t rows = a.step.tokens * a.heads * a.group, per = 256 / (DIM / 4);
-    return launch_kernel(k_cache_attention_join<DIM, BF16>, dim3((uint32_t)((rows + per - 1) / per)), dim3(256), stream, a, shift);
+    hipError_t e;
+    if (!a.workgroups) {
+        constexpr int kWaves = waves_of(DIM, ROW_TILES);
+        const dim3 grid((uint32_t)((int64_t)a.step.sequences * a.row_blocks * a.heads)), block(64 * kWaves);
+        return a.stream ? launch_kernel(k_cache_attention<DIM, FP8, BF16, ROW_TILES, kWaves, false, true>, grid, block, stream, a, shift)
+                        : launch_kernel(k_cache_attention<DIM, FP8, BF16, ROW_TILES, kWaves, false, false>, grid, block, stream, a, shift);
+    }
+    e = a.stream ? launch_kernel(k_cache_attention<DIM, FP8, BF16, ROW_TILES, 4, true, true>, dim3(a.workgroups), dim3(256), stream, a, shift)
+                 : launch_kernel(k_cache_attention<DIM, FP8, BF16, ROW_TILES, 4, true, false>, dim3(a.workgroups), dim3(256), stream, a, shift);
+    if (e != hipSuccess) return e;
+    const int64_t rows = a.step.tokens * a.heads * a.group;
+    // where there are many rows, there are few pieces of each
+    return rows < 1024 ? launch_kernel(k_cache_attention_join<DIM, BF16, 4>, dim3((uint32_t)rows), dim3(256), stream, a, shift)
+                       : launch_kernel(k_cache_attention_join<DIM, BF16, 1>, dim3((uint32_t)((rows + 3) / 4)), dim3(256), stream, a, shift);
+}
+
+template <int DIM, bool FP8, bool BF16>
+hipError_t attend(const CacheAttentionArgs &a, hipStream_t stream)
+{
+    if constexpr (DIM != 256) {
+        if (a.row_tiles == 2) return attend_rows<DIM, FP8, BF16, 2>(a, stream);
+        if (a.row_tiles == 3) return attend_rows<DIM, FP8, BF16, 3>(a, stream);
+    }
+    return attend_rows<DIM, FP8, BF16, 1>(a, stream);
+}
+
+template <int DIM>
+hipError_t attend_types(const CacheAttentionArgs &a, hipStream_t stream)
+{
+    if (a.fp8) return a.bf16 ? attend<DIM, true, true>(a, stream) : attend<DIM, true, false>(a, stream);
+    return a.bf16 ? attend<DIM, false, true>(a, stream) : attend<DIM, false, false>(a, stream);
 }
 
 }  // namespace
 
-void cache_attention_plan(int sequences, int heads, int group, int64_t queries, int64_t longest, int *splits, int *row_blocks)
+void cache_attention_plan(int sequences, int heads, int group, int dim, int64_t queries, int64_t longest, CacheAttentionArgs *a)
 {
-    const int64_t blocks = (queries * group + 15) / 16;
-    *row_blocks = blocks < 1 ? 1 : blocks > 4096 ? 4096 : (int)blocks;
-    const int64_t groups = (int64_t)sequences * heads * *row_blocks;
-    const int64_t want = groups ? 1024 / groups : 1, most = pieces_of((longest + kTile - 1) / kTile, 64);
-    *splits = (int)(want < 1 ? 1 : want < most ? want : most);
+    const int64_t tiles = (queries * group + 15) / 16, pairs = (longest + 2 * kTile - 1) / (2 * kTile), contexts = (int64_t)sequences * heads;
+    // Three tiles of rows at a time read the context once for 48 rows, but leave fewer workgroups; us for 40 rows of 8 heads by context with
+    // two and three: 4000 tokens 21.6 / 28.0, 16000 28.7 / 34.0, 131071 73.8 / 62.2
+    a->row_tiles = dim == 256 || tiles == 1 ? 1 : tiles == 2 || contexts * pairs < 16384 ? 2 : 3;
+    const int64_t blocks = (tiles + a->row_tiles - 1) / a->row_tiles;
+    a->row_blocks = blocks > 4096 ? 4096 : (int)blocks;
+    const int64_t groups = contexts * blocks;
+    // One workgroup for a whole context needs no second launch and no sharing out, which cost 8 to 15 us, but its time goes with the
+    // longest one; us whole / shared: 16 contexts of 700 tokens 10.3 / 15.7, 1536 14.6 / 16.3, 3000 22.2 / 17.5; 512 contexts of up to
+    // 1000 24.5 / 31.8, 2048 41.5 / 46.7, 4096 82.8 / 77.2; 16 with 40 rows of 2000 29.7 / 19.1
+    const int64_t whole = waves_of(dim, a->row_tiles) * (groups >= 256 ? 12 : 6);
+    // Two workgroups of four wavefronts a compute unit hold enough loads in flight; 512 / 1024 / 2048 of them for 64 x 8 contexts of 8192:
+    // 142 / 143 / 147 us
+    const int64_t want = (groups * pairs + kLeast - 1) / kLeast;
+    a->workgroups = pairs <= whole ? 0 : want < 512 ? (int)want : 512;
+    // what one workgroup reads and the memory-side cache does not hold is marked as read once (157 -> 143 us there)
+    a->stream = blocks == 1 && beyond_cache(contexts * longest * 2 * dim);
+}
+
+size_t cache_attention_workspace(const CacheAttentionArgs &a, int sequences, int dim)
+{
+    if (!a.workgroups) return 0;
+    return (size_t)a.workgroups * 2 * 16 * a.row_tiles * (dim + 2) * sizeof(float) + ((size_t)sequences + 5) * sizeof(uint32_t);
 }
 
 hipError_t launch_cache_attention(const CacheAttentionArgs &a, hipStream_t stream)
 {
     switch (a.dim) {
-    case 64: return a.bf16 ? attend<64, true>(a, stream) : attend<64, false>(a, stream);
-    case 128: return a.bf16 ? attend<128, true>(a, stream) : attend<128, false>(a, stream);
-    default: return a.bf16 ? attend<256, true>(a, stream) : attend<256, false>(a, stream);
+    case 64: return attend_types<64>(a, stream);
+    case 128: return attend_types<128>(a, stream);
+    default: return attend_types<256>(a, stream);
     }
 }
 

@@ -29,19 +29,8 @@ __device__ __forceinline__ uintx4 tile_rows(const uint16_t *base, int64_t stride
 {
     int64_t bytes = ((left - 1) * stride + dim) * 2;
     if (left <= 0) bytes = 0;
-    const uint64_t at = (uint64_t)base;
-    return uintx4{(uint32_t)at, (uint32_t)(at >> 32) & 0xFFFFu, bytes > 0x7FFFFFF0 ? 0x7FFFFFF0u : (uint32_t)bytes, 0x00020000u};
+    return resource(base, bytes > 0x7FFFFFF0 ? 0x7FFFFFF0u : (uint32_t)bytes);
 }
-
-// 16 bytes per lane from memory to lds + 16 lane.  Not the builtin: the compiler would make LDS reads of the other tile wait for it.
-// Who reads what has arrived waits for vmcnt himself.  (A wait state between the write
-// of m0, which nothing else in these kernels has a value in, and its use.)
-__device__ __forceinline__ void load_to_lds(uintx4 rsrc, int offset, uint32_t lds)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(rsrc) : "memory");
-}
-
-__device__ __forceinline__ uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p; }
 
 // tile positions of this lane's pieces: kPieces times 16 bytes, which land at lds + piece * 1024 + 16 lane of the wavefront's part
 template <int DIM>
@@ -60,7 +49,7 @@ struct Staging {
     __device__ __forceinline__ void load(uintx4 rsrc, const uint8_t *lds, int wave) const
     {
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) load_to_lds(rsrc, offset[i], lds_address(lds) + (wave * kPieces + i) * 1024);
+        for (int i = 0; i < kPieces; ++i) load_to_lds<false>(rsrc, offset[i], lds_address(lds) + (wave * kPieces + i) * 1024);
     }
 };
 
