@@ -5,8 +5,7 @@
 // matrix instructions, which leaves a lane with weights of the very tokens that it needs as operand of O^T = V^T P^T, and keeps the
 // running maximum and sum of its column: one pass over K and V, and nothing but K and V goes through LDS.
 //   K and V tiles go from memory straight to LDS, one tile ahead of the arithmetic; beyond the sequence's end they are zeros.
-//   Rows of a tile lie as in memory, their 16-byte units exchanged (unit ^ 2 k, k a function of the row) so that neither the rows that
-//   K's operand reads together nor the four that V's transposing reads take share a bank.
+//   Rows of a tile lie as in memory, their 16-byte units exchanged (unit ^ swizzle of the row) so that reads find every bank once.
 //   The running maximum is raised only when a score passes it by kSlack; the sums carry the same factor either way.
 // Matrix instructions and the exponentials between them bound it.
 #include "fc_attn.hpp"
@@ -21,8 +20,13 @@ constexpr int kRows = 32 * kWaves;      // queries of a workgroup
 constexpr int kTokens = 64;             // of a tile
 constexpr float kSlack = 8.0f;          // in powers of two
 
-// what a 16-byte unit's number is exchanged by, halved, in row t of a tile
-template <int DIM> __device__ __forceinline__ int swizzle(int t) { return DIM == 128 ? t & 7 : (t >> 1) & 3; }
+// what the number of a 16-byte unit is exchanged by in row t of a tile: 16 rows of K, read one unit each, and four of V, read 64 bytes
+// each, take every bank once
+template <int DIM, bool K> __device__ __forceinline__ int swizzle(int t)
+{
+    if (K) return DIM == 128 ? t & 15 : (t >> 1) & 7;
+    return DIM == 128 ? 4 * (t & 3) : 4 * ((t >> 1) & 1);
+}
 
 // buffer resource of rows [0, left) of a tile; everything else reads as zero
 __device__ __forceinline__ uintx4 tile_rows(const uint16_t *base, int64_t stride, int64_t left, int dim)
@@ -33,7 +37,7 @@ __device__ __forceinline__ uintx4 tile_rows(const uint16_t *base, int64_t stride
 }
 
 // tile positions of this lane's pieces: kPieces times 16 bytes, which land at lds + piece * 1024 + 16 lane of the wavefront's part
-template <int DIM>
+template <int DIM, bool K>
 struct Staging {
     static constexpr int kPieces = kTokens * DIM * 2 / 1024 / kWaves;
     int offset[kPieces];
@@ -43,7 +47,7 @@ struct Staging {
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
             const int at = (wave * kPieces + i) * 1024 + lane * 16, row = at / (2 * DIM), unit = at % (2 * DIM) / 16;
-            offset[i] = row * (int)stride * 2 + (unit ^ (2 * swizzle<DIM>(row))) * 16;
+            offset[i] = row * (int)stride * 2 + (unit ^ swizzle<DIM, K>(row)) * 16;
         }
     }
     __device__ __forceinline__ void load(uintx4 rsrc, const uint8_t *lds, int wave) const
@@ -96,11 +100,12 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_prompt_attention(PromptArgs 
     const uint16_t *v = (const uint16_t *)a.v.ptr + off * a.v.token + kv_head * a.v.head;
     const float factor = a.scale * 1.4426950408889634f;       // scores in powers of two
 
-    const Staging<DIM> stage_k(wave, lane, a.k.token), stage_v(wave, lane, a.v.token);
+    const Staging<DIM, true> stage_k(wave, lane, a.k.token);
+    const Staging<DIM, false> stage_v(wave, lane, a.v.token);
     // operand addresses in a tile: K by row lane % 32, V by the row and the 8 bytes that this lane contributes to a transposing read
-    const int at_k = col * kRow + side * 16 + swizzle<DIM>(col) * 32;
+    const int at_k = col * kRow + (side ^ swizzle<DIM, true>(col)) * 16;
     const int v_row = 4 * side + (lane & 15) / 4;
-    const int at_v = v_row * kRow + ((((lane >> 4) & 1) ^ swizzle<DIM>(v_row)) * 2 + ((lane & 3) >> 1)) * 16 + (lane & 1) * 8;
+    const int at_v = v_row * kRow + ((((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) ^ swizzle<DIM, false>(v_row)) * 16 + (lane & 1) * 8;
 
     floatx16 acc[kOut];
 #pragma unroll
