@@ -1,7 +1,7 @@
 // fc_prompt.hip -- attention over whole prompts, packed one behind the other.
 //
 // Query i of a sequence sees all its tokens, or (causal) those up to i:  o = sum_t softmax_t(scale q . k_t) v_t.
-// A wavefront has 32 queries of one head and takes 64 tokens at a time.  It forms the transposed score S^T = K Q^T with 32 x 32 x 16
+// A wavefront has 32 queries of one head and takes 64 (or 32) tokens at a time.  It forms the transposed score S^T = K Q^T with 32 x 32 x 16
 // matrix instructions, which leaves a lane with weights of the very tokens that it needs as operand of O^T = V^T P^T, and keeps the
 // running maximum and sum of its column: one pass over K and V, and nothing but K and V goes through LDS.
 //   K and V tiles go from memory straight to LDS, one tile ahead of the arithmetic; beyond the sequence's end they are zeros.
@@ -15,9 +15,6 @@ namespace {
 
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 
-constexpr int kWaves = 4;
-constexpr int kRows = 32 * kWaves;      // queries of a workgroup
-constexpr int kTokens = 64;             // of a tile
 constexpr float kSlack = 8.0f;          // in powers of two
 
 // what the number of a 16-byte unit is exchanged by in row t of a tile: 16 rows of K, read one unit each, and four of V, read 64 bytes
@@ -36,24 +33,24 @@ __device__ __forceinline__ uintx4 tile_rows(const uint16_t *base, int64_t stride
     return resource(base, bytes > 0x7FFFFFF0 ? 0x7FFFFFF0u : (uint32_t)bytes);
 }
 
-// tile positions of this lane's pieces: kPieces times 16 bytes, which land at lds + piece * 1024 + 16 lane of the wavefront's part
+// How a wavefront brings 16 rows of a tile to LDS, 1 KB at a time: where in memory each lane finds its 16 bytes
 template <int DIM, bool K>
-struct Staging {
-    static constexpr int kPieces = kTokens * DIM * 2 / 1024 / kWaves;
+struct Rows16 {
+    static constexpr int kPieces = 16 * DIM * 2 / 1024;
     int offset[kPieces];
 
-    __device__ __forceinline__ Staging(int wave, int lane, int64_t stride)
+    __device__ __forceinline__ Rows16(int lane, int64_t stride)
     {
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
-            const int at = (wave * kPieces + i) * 1024 + lane * 16, row = at / (2 * DIM), unit = at % (2 * DIM) / 16;
+            const int at = i * 1024 + lane * 16, row = at / (2 * DIM), unit = at % (2 * DIM) / 16;
             offset[i] = row * (int)stride * 2 + (unit ^ swizzle<DIM, K>(row)) * 16;
         }
     }
-    __device__ __forceinline__ void load(uintx4 rsrc, const uint8_t *lds, int wave) const
+    __device__ __forceinline__ void load(uintx4 rsrc, const uint8_t *lds) const
     {
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) load_to_lds<false>(rsrc, offset[i], lds_address(lds) + (wave * kPieces + i) * 1024);
+        for (int i = 0; i < kPieces; ++i) load_to_lds<false>(rsrc, offset[i], lds_address(lds) + i * 1024);
     }
 };
 
@@ -62,12 +59,41 @@ __device__ __forceinline__ uintx2 transposed(const uint8_t *p)
     return __builtin_bit_cast(uintx2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4 *)p));
 }
 
-template <int DIM, bool BF16>
-__global__ void __launch_bounds__(64 * kWaves, 2) k_prompt_attention(PromptArgs a, int64_t units)
+template <int N>
+__device__ __forceinline__ void wait_vm()
 {
-    constexpr int kSteps = DIM / 16, kOut = DIM / 32, kRow = 2 * DIM;
-    __shared__ __attribute__((aligned(1024))) uint8_t tile_k0[kTokens * kRow], tile_v0[kTokens * kRow];
-    __shared__ __attribute__((aligned(1024))) uint8_t tile_k1[kTokens * kRow], tile_v1[kTokens * kRow];
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+// The sequence that has work unit u (see find_sequence), its first token and the next one's.  One read for 64 sequences instead of one
+// behind the other.
+struct Found {
+    int b, off, next;
+};
+__device__ __forceinline__ Found find_sequence_wide(const int32_t *__restrict__ offsets, int sequences, int shift, int64_t u, int lane)
+{
+    for (int c = 0;; c += 63) {
+        const int i = c + lane < sequences ? c + lane : sequences;
+        const int off = offsets[i];
+        // lanes up to the last sequence that begins at or before u
+        const uint64_t before = __ballot(c + lane < sequences && (int64_t)(off >> shift) + i <= u);
+        const int count = __builtin_popcountll(before);
+        if (count < 64) {
+            const int l = count ? count - 1 : 0;
+            return {c + l, __builtin_amdgcn_readlane(off, l), __builtin_amdgcn_readlane(off, l + 1)};
+        }
+    }
+}
+
+// SPLIT: the wavefronts have the same 32 rows and take their tiles in turn, each with a K and a V tile of its own in LDS; they are joined
+// at the end.  Else each has 32 rows and all work on the same tiles, two of each in LDS.
+template <int DIM, bool BF16, bool SPLIT>
+__global__ void __launch_bounds__(SPLIT ? 512 : 256, 2) k_prompt_attention(PromptArgs a, int64_t units)
+{
+    constexpr int kWaves = SPLIT ? 8 : 4, kTokens = SPLIT ? 32 : 64;            // tokens of a tile
+    constexpr int kSteps = DIM / 16, kOut = DIM / 32, kRow = 2 * DIM, kTile = kTokens * kRow, kHalves = kTokens / 32, kGroups = kTokens / 16;
+    constexpr int kShift = SPLIT ? 5 : 7, kRows = 1 << kShift;                 // queries of a workgroup
+    __shared__ __attribute__((aligned(1024))) uint8_t tiles[SPLIT ? 2 * kWaves : 4][kTile];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, side = lane >> 5;
     const int query_heads = a.heads * a.group;
     // workgroups go to the 8 XCDs in turn: where heads can be dealt to them, an XCD's L2 has few heads' K and V
@@ -82,13 +108,12 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_prompt_attention(PromptArgs 
         unit = units - 1 - blockIdx.x / query_heads;
     }
     const int kv_head = head / a.group;
-    const int b = find_sequence(a.offsets, a.sequences, 7, 1, unit);
-    const int64_t off = a.offsets[b];
-    const int64_t n = (int64_t)a.offsets[b + 1] - off;
+    const Found at = find_sequence_wide(a.offsets, a.sequences, kShift, unit, lane);
+    const int64_t off = at.off, n = (int64_t)at.next - off;
     if (off < 0 || n <= 0 || off + n > a.tokens) return;
-    const int64_t first = (unit - ((off >> 7) + b)) * kRows;
+    const int64_t first = (unit - ((off >> kShift) + at.b)) * kRows;
     if (first >= n) return;
-    const int64_t row0 = first + wave * 32, row = row0 + col;
+    const int64_t row0 = SPLIT ? first : first + wave * 32, row = row0 + col;
 
     uintx4 qf[kSteps];
     {
@@ -100,8 +125,8 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_prompt_attention(PromptArgs 
     const uint16_t *v = (const uint16_t *)a.v.ptr + off * a.v.token + kv_head * a.v.head;
     const float factor = a.scale * 1.4426950408889634f;       // scores in powers of two
 
-    const Staging<DIM, true> stage_k(wave, lane, a.k.token);
-    const Staging<DIM, false> stage_v(wave, lane, a.v.token);
+    const Rows16<DIM, true> rows_k(lane, a.k.token);
+    const Rows16<DIM, false> rows_v(lane, a.v.token);
     // operand addresses in a tile: K by row lane % 32, V by the row and the 8 bytes that this lane contributes to a transposing read
     const int at_k = col * kRow + (side ^ swizzle<DIM, true>(col)) * 16;
     const int v_row = 4 * side + (lane & 15) / 4;
@@ -118,33 +143,40 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_prompt_attention(PromptArgs 
     const int64_t my_end = a.causal && row0 + 32 < n ? row0 + 32 : n;
     const int64_t clear = a.causal && row0 < n ? row0 + 1 : n;                  // tokens that every row sees
 
-    const auto load = [&](int64_t t0, uint8_t *lds_k, uint8_t *lds_v) {
-        stage_k.load(tile_rows(k + t0 * a.k.token, a.k.token, n - t0, DIM), lds_k, wave);
-        stage_v.load(tile_rows(v + t0 * a.v.token, a.v.token, n - t0, DIM), lds_v, wave);
+    // 16 rows of a tile from token t0 on
+    const auto load_k = [&](int64_t t0, int group, const uint8_t *tile) {
+        t0 += 16 * group;
+        rows_k.load(tile_rows(k + t0 * a.k.token, a.k.token, n - t0, DIM), tile + group * 16 * kRow);
     };
-    const auto compute = [&](int64_t t0, const uint8_t *lds_k, const uint8_t *lds_v) {
-        if (t0 >= my_end) return;
-        floatx16 s[2];
+    const auto load_v = [&](int64_t t0, int group, const uint8_t *tile) {
+        t0 += 16 * group;
+        rows_v.load(tile_rows(v + t0 * a.v.token, a.v.token, n - t0, DIM), tile + group * 16 * kRow);
+    };
+    floatx16 s[kHalves];
+    const auto scores = [&](const uint8_t *lds_k) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < kHalves; ++h)
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[h][r] = 0.0f;
 #pragma unroll
         for (int j = 0; j < kSteps; ++j)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < kHalves; ++h)
                 s[h] = mma32<BF16>(*(const uintx4 *)(lds_k + (at_k ^ (j << 5)) + h * 32 * kRow), qf[j], s[h]);
+    };
+    uintx4 pf[2 * kHalves];
+    const auto weights = [&](int64_t t0) {
         if (t0 + kTokens > clear) {
             const int64_t sees = a.causal && row < n - 1 ? row + 1 : n;
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < kHalves; ++h)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     if (t0 + h * 32 + 8 * (r / 4) + 4 * side + r % 4 >= sees) s[h][r] = -__builtin_inff();
         }
         float most = s[0][0];
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < kHalves; ++h)
 #pragma unroll
             for (int r = 0; r < 16; ++r) most = fmaxf(most, s[h][r]);
         most *= factor;
@@ -156,9 +188,8 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_prompt_attention(PromptArgs 
 #pragma unroll
             for (int o = 0; o < kOut; ++o) acc[o] *= shrink;
         }
-        uintx4 pf[4];
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < kHalves; ++h)
 #pragma unroll
             for (int r = 0; r < 16; r += 2) {
                 const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h][r], factor, -top));
@@ -167,8 +198,10 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_prompt_attention(PromptArgs 
                 total += p1;
                 pf[2 * h + r / 8][r % 8 / 2] = narrow2<BF16>(p0, p1);
             }
+    };
+    const auto add_values = [&](const uint8_t *lds_v) {
 #pragma unroll
-        for (int m = 0; m < 4; ++m)
+        for (int m = 0; m < 2 * kHalves; ++m)
 #pragma unroll
             for (int o = 0; o < kOut; ++o) {
                 const uint8_t *p = lds_v + (at_v ^ (o << 6)) + m * 16 * kRow;
@@ -176,47 +209,156 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_prompt_attention(PromptArgs 
                 acc[o] = mma32<BF16>(uintx4{lo[0], lo[1], hi[0], hi[1]}, pf[m], acc[o]);
             }
     };
-    const auto arrived = [] {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    };
-
-    load(0, tile_k0, tile_v0);
     // the queries are here before the loop, where waiting for them would wait for the tiles that are loaded ahead
+    const auto queries_here = [&] {
 #pragma unroll
-    for (int j = 0; j < kSteps; ++j) asm volatile("" : "+v"(qf[j]));
-    arrived();
-    for (int64_t t0 = 0; t0 < end; t0 += 2 * kTokens) {
-        if (t0 + kTokens < end) load(t0 + kTokens, tile_k1, tile_v1);
-        compute(t0, tile_k0, tile_v0);
+        for (int j = 0; j < kSteps; ++j) asm volatile("" : "+v"(qf[j]));
+    };
+    if constexpr (SPLIT) {
+        constexpr int kLoads = kGroups * Rows16<DIM, true>::kPieces;
+        const uint8_t *const tile_k = tiles[2 * wave], *const tile_v = tiles[2 * wave + 1];
+        int64_t t0 = wave * kTokens;
+        if (t0 < end) {
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) load_k(t0, g, tile_k);
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) load_v(t0, g, tile_v);
+        }
+        queries_here();
+        for (; t0 < end; t0 += kWaves * kTokens) {
+            const bool more = t0 + kWaves * kTokens < end;
+            wait_vm<kLoads>();                           // K is here, V may be on its way
+            scores(tile_k);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (more)
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g) load_k(t0 + kWaves * kTokens, g, tile_k);
+            weights(t0);
+            if (more) wait_vm<kLoads>();                 // V is here, the next K may be on its way
+            else wait_vm<0>();
+            add_values(tile_v);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (more)
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g) load_v(t0 + kWaves * kTokens, g, tile_v);
+        }
+    } else {
+        const auto load = [&](int64_t t0, int to) {
+            load_k(t0, wave, tiles[to]);
+            load_v(t0, wave, tiles[to + 1]);
+        };
+        const auto compute = [&](int64_t t0, int from) {
+            if (t0 >= my_end) return;
+            scores(tiles[from]);
+            weights(t0);
+            add_values(tiles[from + 1]);
+        };
+        const auto arrived = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+        load(0, 0);
+        queries_here();
         arrived();
-        if (t0 + kTokens >= end) break;
-        if (t0 + 2 * kTokens < end) load(t0 + 2 * kTokens, tile_k0, tile_v0);
-        compute(t0 + kTokens, tile_k1, tile_v1);
-        arrived();
+        for (int64_t t0 = 0; t0 < end; t0 += 2 * kTokens) {
+            if (t0 + kTokens < end) load(t0 + kTokens, 2);
+            compute(t0, 0);
+            arrived();
+            if (t0 + kTokens >= end) break;
+            if (t0 + 2 * kTokens < end) load(t0 + 2 * kTokens, 0);
+            compute(t0 + kTokens, 2);
+            arrived();
+        }
     }
 
     total += __shfl_xor(total, 32);
-    if (row >= n) return;
+    if constexpr (SPLIT) {
+        // all in the unit of the largest maximum, then halves of the wavefronts added to the other half
+        __shared__ float join_max[kWaves][32], join_sum[kWaves][32];
+        float(*join)[32][DIM + 4] = reinterpret_cast<float(*)[32][DIM + 4]>(tiles);        // [kWaves / 2], when the tiles are done with
+        static_assert(sizeof(tiles) >= sizeof(float) * kWaves / 2 * 32 * (DIM + 4), "the wavefronts' sums fit the tiles");
+        if (side == 0) {
+            join_max[wave][col] = top;
+            join_sum[wave][col] = total;
+        }
+        __syncthreads();
+        float best = join_max[0][col];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) best = fmaxf(best, join_max[w][col]);
+        total = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) total += join_sum[w][col] * __builtin_amdgcn_exp2f(join_max[w][col] - best);
+        const float mine = __builtin_amdgcn_exp2f(top - best);
+#pragma unroll
+        for (int o = 0; o < kOut; ++o) acc[o] *= mine;
+#pragma unroll
+        for (int half = kWaves / 2; half; half >>= 1) {
+            if (wave >= half && wave < 2 * half)
+#pragma unroll
+                for (int o = 0; o < kOut; ++o)
+#pragma unroll
+                    for (int r = 0; r < 16; r += 4)
+                        *(floatx4 *)&join[wave - half][col][o * 32 + 2 * r + 4 * side] = floatx4{acc[o][r], acc[o][r + 1], acc[o][r + 2], acc[o][r + 3]};
+            __syncthreads();
+            if (wave < half)
+#pragma unroll
+                for (int o = 0; o < kOut; ++o)
+#pragma unroll
+                    for (int r = 0; r < 16; r += 4) {
+                        const floatx4 x = *(const floatx4 *)&join[wave][col][o * 32 + 2 * r + 4 * side];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[o][r + i] += x[i];
+                    }
+            __syncthreads();
+        }
+        if (wave) return;
+    }
+    // through LDS, where the tiles are done with, so that a wavefront stores whole rows (a lane has 4 elements of a row at a time)
     const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-    uint16_t *y = (uint16_t *)a.out.ptr + (off + row) * a.out.token + head * a.out.head;
+    constexpr int kOutRow = kRow + 16;                   // bytes; neighbouring rows begin 4 banks apart
+    static_assert(sizeof(tiles) >= (SPLIT ? 1 : kWaves) * 32 * kOutRow, "the results fit the tiles");
+    uint8_t *const mine = &tiles[0][0] + (SPLIT ? 0 : wave) * 32 * kOutRow;
 #pragma unroll
     for (int o = 0; o < kOut; ++o)
 #pragma unroll
         for (int r = 0; r < 16; r += 4)
-            *(uintx2 *)(y + o * 32 + 2 * r + 4 * side) = uintx2{narrow2<BF16>(acc[o][r] * inv, acc[o][r + 1] * inv), narrow2<BF16>(acc[o][r + 2] * inv, acc[o][r + 3] * inv)};
+            *(uintx2 *)(mine + col * kOutRow + (o * 32 + 2 * r + 4 * side) * 2) = uintx2{narrow2<BF16>(acc[o][r] * inv, acc[o][r + 1] * inv), narrow2<BF16>(acc[o][r + 2] * inv, acc[o][r + 3] * inv)};
+    constexpr int kLanes = DIM / 8;                      // of a row
+#pragma unroll
+    for (int i = 0; i < 32 * kLanes / 64; ++i) {
+        const int out_row = i * (64 / kLanes) + lane / kLanes, d = lane % kLanes * 8;
+        const uintx4 w = *(const uintx4 *)(mine + out_row * kOutRow + d * 2);
+        if (row0 + out_row < n) *(uintx4 *)((uint16_t *)a.out.ptr + (off + row0 + out_row) * a.out.token + head * a.out.head + d) = w;
+    }
 }
 
-template <bool BF16>
+// Whether workgroups of 32 rows whose wavefronts split the tokens are faster than those of 128 rows, by what both were measured to take
+// in tenths of a microsecond.  128 rows: as long as the longest sequence's last rows, 1.1 us (0.8 with heads of 64) for 64 tokens, while
+// no more than two workgroups share a compute unit.  32 rows: rounds of one workgroup (two) a compute unit, 3.2 us and 1.5 us for 256
+// tokens each.  us, 8 heads of 128, causal, 128 / 32 rows: 1024 tokens 24.2 / 12.8, 2048 41.9 / 25.5, 4096 77.2 / 68.7, 8192 172 / 219;
+// 16 heads, 2048 tokens 42.9 / 48.6; 8 sequences of 1024 tokens 47.0 / 87.3.
+bool split_is_faster(const PromptArgs &a, int64_t wide, int64_t narrow)
+{
+    const int64_t heads = a.heads * a.group, longest = a.longest < a.tokens ? a.longest : a.tokens;
+    if (wide * heads > 512) return false;
+    const int64_t slots = a.dim == 64 ? 512 : 256, rounds = (narrow * heads + slots - 1) / slots;
+    const int64_t half_steps = a.causal ? longest / 256 + 1 : longest / 128;
+    return rounds * (32 + 15 * half_steps / 2) < (a.dim == 64 ? 8 : 11) * ((longest + 63) / 64);
+}
+
+template <int DIM, bool BF16>
 hipError_t prompt(const PromptArgs &a, hipStream_t stream)
 {
-    const int64_t units = (a.tokens >> 7) + a.sequences;
-    const dim3 grid((uint32_t)(units * a.heads * a.group));
-    return a.dim == 64 ? launch_kernel(k_prompt_attention<64, BF16>, grid, dim3(64 * kWaves), stream, a, units)
-                       : launch_kernel(k_prompt_attention<128, BF16>, grid, dim3(64 * kWaves), stream, a, units);
+    const int query_heads = a.heads * a.group;
+    const int64_t wide = (a.tokens >> 7) + a.sequences, narrow = (a.tokens >> 5) + a.sequences;
+    if (split_is_faster(a, wide, narrow))
+        return launch_kernel(k_prompt_attention<DIM, BF16, true>, dim3((uint32_t)(narrow * query_heads)), dim3(512), stream, a, narrow);
+    return launch_kernel(k_prompt_attention<DIM, BF16, false>, dim3((uint32_t)(wide * query_heads)), dim3(256), stream, a, wide);
 }
 
 }  // namespace
 
-hipError_t launch_prompt_attention(const PromptArgs &a, hipStream_t stream) { return a.bf16 ? prompt<true>(a, stream) : prompt<false>(a, stream); }
+hipError_t launch_prompt_attention(const PromptArgs &a, hipStream_t stream)
+{
+    if (a.dim == 64) return a.bf16 ? prompt<64, true>(a, stream) : prompt<64, false>(a, stream);
+    return a.bf16 ? prompt<128, true>(a, stream) : prompt<128, false>(a, stream);
+}
 
 }  // namespace fc
