@@ -191,7 +191,9 @@ int fc_prompt_attention(const void *q, int64_t q_token_stride, int64_t q_head_st
     if ((rc = check_rows(k, k_token_stride, k_head_stride)) != FC_OK) return rc;
     if ((rc = check_rows(v, v_token_stride, v_head_stride)) != FC_OK) return rc;
     if ((rc = check_rows(out, out_token_stride, out_head_stride)) != FC_OK) return rc;
-    if (!launchable((tokens / 64 + sequences) * heads * group, 512)) return FC_ERR_SHAPE;
+    // 32-bit offsets in a tile; a grid of 32-row workgroups at most
+    if (k_token_stride >= 1 << 25 || v_token_stride >= 1 << 25 || k_token_stride < 0 || v_token_stride < 0) return FC_ERR_SHAPE;
+    if (!launchable((tokens / 32 + sequences) * heads * group, 512)) return FC_ERR_SHAPE;
     fc::PromptArgs a;
     a.q = rows(q, q_token_stride, q_head_stride);
     a.k = rows(k, k_token_stride, k_head_stride);

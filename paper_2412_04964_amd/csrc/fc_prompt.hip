@@ -25,12 +25,11 @@ template <int DIM, bool K> __device__ __forceinline__ int swizzle(int t)
     return DIM == 128 ? 4 * (t & 3) : 4 * ((t >> 1) & 1);
 }
 
-// buffer resource of rows [0, left) of a tile; everything else reads as zero
-__device__ __forceinline__ uintx4 tile_rows(const uint16_t *base, int64_t stride, int64_t left, int dim)
+// buffer resource of 16 rows, of which [0, left) are there; everything else reads as zero
+__device__ __forceinline__ uintx4 rows16(const uint16_t *base, int stride, int left, int dim)
 {
-    int64_t bytes = ((left - 1) * stride + dim) * 2;
-    if (left <= 0) bytes = 0;
-    return resource(base, bytes > 0x7FFFFFF0 ? 0x7FFFFFF0u : (uint32_t)bytes);
+    const int last = left < 16 ? left - 1 : 15;
+    return resource(base, last < 0 ? 0u : (uint32_t)(last * stride + dim) * 2u);
 }
 
 // How a wavefront brings 16 rows of a tile to LDS, 1 KB at a time: where in memory each lane finds its 16 bytes
@@ -39,12 +38,12 @@ struct Rows16 {
     static constexpr int kPieces = 16 * DIM * 2 / 1024;
     int offset[kPieces];
 
-    __device__ __forceinline__ Rows16(int lane, int64_t stride)
+    __device__ __forceinline__ Rows16(int lane, int stride)
     {
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
             const int at = i * 1024 + lane * 16, row = at / (2 * DIM), unit = at % (2 * DIM) / 16;
-            offset[i] = row * (int)stride * 2 + (unit ^ swizzle<DIM, K>(row)) * 16;
+            offset[i] = row * stride * 2 + (unit ^ swizzle<DIM, K>(row)) * 16;
         }
     }
     __device__ __forceinline__ void load(uintx4 rsrc, const uint8_t *lds) const
@@ -88,7 +87,7 @@ __device__ __forceinline__ Found find_sequence_wide(const int32_t *__restrict__ 
 // SPLIT: the wavefronts have the same 32 rows and take their tiles in turn, each with a K and a V tile of its own in LDS; they are joined
 // at the end.  Else each has 32 rows and all work on the same tiles, two of each in LDS.
 template <int DIM, bool BF16, bool SPLIT>
-__global__ void __launch_bounds__(SPLIT ? 512 : 256, 2) k_prompt_attention(PromptArgs a, int64_t units)
+__global__ void __launch_bounds__(SPLIT ? 512 : 256, 2) k_prompt_attention(PromptArgs a, int units)
 {
     constexpr int kWaves = SPLIT ? 8 : 4, kTokens = SPLIT ? 32 : 64;            // tokens of a tile
     constexpr int kSteps = DIM / 16, kOut = DIM / 32, kRow = 2 * DIM, kTile = kTokens * kRow, kHalves = kTokens / 32, kGroups = kTokens / 16;
@@ -97,8 +96,7 @@ __global__ void __launch_bounds__(SPLIT ? 512 : 256, 2) k_prompt_attention(Promp
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, side = lane >> 5;
     const int query_heads = a.heads * a.group;
     // workgroups go to the 8 XCDs in turn: where heads can be dealt to them, an XCD's L2 has few heads' K and V
-    int head;
-    int64_t unit;
+    int head, unit;
     if (query_heads % 8 == 0) {
         const uint32_t per = query_heads / 8, j = blockIdx.x >> 3;
         head = (blockIdx.x & 7) * per + j % per;
@@ -109,11 +107,12 @@ __global__ void __launch_bounds__(SPLIT ? 512 : 256, 2) k_prompt_attention(Promp
     }
     const int kv_head = head / a.group;
     const Found at = find_sequence_wide(a.offsets, a.sequences, kShift, unit, lane);
-    const int64_t off = at.off, n = (int64_t)at.next - off;
-    if (off < 0 || n <= 0 || off + n > a.tokens) return;
-    const int64_t first = (unit - ((off >> kShift) + at.b)) * kRows;
-    if (first >= n) return;
-    const int64_t row0 = SPLIT ? first : first + wave * 32, row = row0 + col;
+    const int64_t off = at.off;
+    const int n = at.next - at.off;
+    if (at.off < 0 || at.next <= at.off || at.next > a.tokens) return;
+    const int place = unit - ((at.off >> kShift) + at.b);
+    if (place > (n - 1) >> kShift) return;
+    const int first = place * kRows, row0 = SPLIT ? first : first + wave * 32, row = row0 + col;
 
     uintx4 qf[kSteps];
     {
@@ -121,12 +120,13 @@ __global__ void __launch_bounds__(SPLIT ? 512 : 256, 2) k_prompt_attention(Promp
 #pragma unroll
         for (int j = 0; j < kSteps; ++j) qf[j] = *(const uintx4 *)(q + 16 * j);
     }
+    const int stride_k = (int)a.k.token, stride_v = (int)a.v.token;
     const uint16_t *k = (const uint16_t *)a.k.ptr + off * a.k.token + kv_head * a.k.head;
     const uint16_t *v = (const uint16_t *)a.v.ptr + off * a.v.token + kv_head * a.v.head;
     const float factor = a.scale * 1.4426950408889634f;       // scores in powers of two
 
-    const Rows16<DIM, true> rows_k(lane, a.k.token);
-    const Rows16<DIM, false> rows_v(lane, a.v.token);
+    const Rows16<DIM, true> rows_k(lane, stride_k);
+    const Rows16<DIM, false> rows_v(lane, stride_v);
     // operand addresses in a tile: K by row lane % 32, V by the row and the 8 bytes that this lane contributes to a transposing read
     const int at_k = col * kRow + (side ^ swizzle<DIM, true>(col)) * 16;
     const int v_row = 4 * side + (lane & 15) / 4;
@@ -139,18 +139,18 @@ __global__ void __launch_bounds__(SPLIT ? 512 : 256, 2) k_prompt_attention(Promp
         for (int r = 0; r < 16; ++r) acc[o][r] = 0.0f;
     float top = -FLT_MAX, total = 0.0f;
 
-    const int64_t end = a.causal && first + kRows < n ? first + kRows : n;      // of the workgroup
-    const int64_t my_end = a.causal && row0 + 32 < n ? row0 + 32 : n;
-    const int64_t clear = a.causal && row0 < n ? row0 + 1 : n;                  // tokens that every row sees
+    const int end = a.causal && first + kRows < n ? first + kRows : n;      // of the workgroup
+    const int my_end = a.causal && row0 + 32 < n ? row0 + 32 : n;
+    const int clear = a.causal && row0 < n ? row0 + 1 : n;                  // tokens that every row sees
 
     // 16 rows of a tile from token t0 on
-    const auto load_k = [&](int64_t t0, int group, const uint8_t *tile) {
+    const auto load_k = [&](int t0, int group, const uint8_t *tile) {
         t0 += 16 * group;
-        rows_k.load(tile_rows(k + t0 * a.k.token, a.k.token, n - t0, DIM), tile + group * 16 * kRow);
+        rows_k.load(rows16(k + (int64_t)t0 * stride_k, stride_k, n - t0, DIM), tile + group * 16 * kRow);
     };
-    const auto load_v = [&](int64_t t0, int group, const uint8_t *tile) {
+    const auto load_v = [&](int t0, int group, const uint8_t *tile) {
         t0 += 16 * group;
-        rows_v.load(tile_rows(v + t0 * a.v.token, a.v.token, n - t0, DIM), tile + group * 16 * kRow);
+        rows_v.load(rows16(v + (int64_t)t0 * stride_v, stride_v, n - t0, DIM), tile + group * 16 * kRow);
     };
     floatx16 s[kHalves];
     const auto scores = [&](const uint8_t *lds_k) {
@@ -165,14 +165,14 @@ __global__ void __launch_bounds__(SPLIT ? 512 : 256, 2) k_prompt_attention(Promp
                 s[h] = mma32<BF16>(*(const uintx4 *)(lds_k + (at_k ^ (j << 5)) + h * 32 * kRow), qf[j], s[h]);
     };
     uintx4 pf[2 * kHalves];
-    const auto weights = [&](int64_t t0) {
+    const auto weights = [&](int t0) {
         if (t0 + kTokens > clear) {
-            const int64_t sees = a.causal && row < n - 1 ? row + 1 : n;
+            const int sees = (a.causal && row < n - 1 ? row + 1 : n) - t0 - 4 * side;
 #pragma unroll
             for (int h = 0; h < kHalves; ++h)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    if (t0 + h * 32 + 8 * (r / 4) + 4 * side + r % 4 >= sees) s[h][r] = -__builtin_inff();
+                    if (h * 32 + 8 * (r / 4) + r % 4 >= sees) s[h][r] = -__builtin_inff();
         }
         float most = s[0][0];
 #pragma unroll
@@ -217,7 +217,7 @@ __global__ void __launch_bounds__(SPLIT ? 512 : 256, 2) k_prompt_attention(Promp
     if constexpr (SPLIT) {
         constexpr int kLoads = kGroups * Rows16<DIM, true>::kPieces;
         const uint8_t *const tile_k = tiles[2 * wave], *const tile_v = tiles[2 * wave + 1];
-        int64_t t0 = wave * kTokens;
+        int t0 = wave * kTokens;
         if (t0 < end) {
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) load_k(t0, g, tile_k);
@@ -243,11 +243,11 @@ __global__ void __launch_bounds__(SPLIT ? 512 : 256, 2) k_prompt_attention(Promp
                 for (int g = 0; g < kGroups; ++g) load_v(t0 + kWaves * kTokens, g, tile_v);
         }
     } else {
-        const auto load = [&](int64_t t0, int to) {
+        const auto load = [&](int t0, int to) {
             load_k(t0, wave, tiles[to]);
             load_v(t0, wave, tiles[to + 1]);
         };
-        const auto compute = [&](int64_t t0, int from) {
+        const auto compute = [&](int t0, int from) {
             if (t0 >= my_end) return;
             scores(tiles[from]);
             weights(t0);
@@ -257,7 +257,7 @@ __global__ void __launch_bounds__(SPLIT ? 512 : 256, 2) k_prompt_attention(Promp
         load(0, 0);
         queries_here();
         arrived();
-        for (int64_t t0 = 0; t0 < end; t0 += 2 * kTokens) {
+        for (int t0 = 0; t0 < end; t0 += 2 * kTokens) {
             if (t0 + kTokens < end) load(t0 + kTokens, 2);
             compute(t0, 0);
             arrived();
@@ -310,6 +310,46 @@ __global__ void __launch_bounds__(SPLIT ? 512 : 256, 2) k_prompt_attention(Promp
         }
         if (wave) return;
     }
+    // An infinity or NaN among the values of a token that a row does not see, but another row of its tile does, is NaN times its weight of
+    // zero.  Rows with such results are computed again, one token after the other, by what each row sees.
+    float finite = 0.0f;
+#pragma unroll
+    for (int o = 0; o < kOut; ++o)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) finite = __builtin_fmaf(acc[o][r], 0.0f, finite);
+    if (a.causal && __any(finite != 0.0f)) {
+        top = -FLT_MAX;
+        total = 0.0f;
+#pragma unroll
+        for (int o = 0; o < kOut; ++o)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[o][r] = 0.0f;
+        const uint16_t *again = (const uint16_t *)a.q.ptr + (off + (row < n ? row : n - 1)) * a.q.token + head * a.q.head + side * 8;
+        for (int t = 0; t < my_end; ++t) {
+            float dot = 0.0f;
+#pragma unroll
+            for (int j = 0; j < kSteps; ++j) {
+                float x[8], y[8];
+                widen8<BF16>(*(const uintx4 *)(again + 16 * j), x);
+                widen8<BF16>(*(const uintx4 *)(k + (int64_t)t * stride_k + 16 * j + side * 8), y);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) dot = __builtin_fmaf(x[i], y[i], dot);
+            }
+            dot = (dot + __shfl_xor(dot, 32)) * factor;
+            if (t > row) continue;
+            const float now = fmaxf(top, dot), shrink = __builtin_amdgcn_exp2f(top - now), p = __builtin_amdgcn_exp2f(dot - now);
+            top = now;
+            total = total * shrink + p;
+#pragma unroll
+            for (int o = 0; o < kOut; ++o)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    const uintx2 w = *(const uintx2 *)(v + (int64_t)t * stride_v + o * 32 + 2 * r + 4 * side);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[o][r + i] = __builtin_fmaf(p, widen<BF16>(i & 1 ? w[i / 2] >> 16 : w[i / 2] & 0xFFFFu), acc[o][r + i] * shrink);
+                }
+        }
+    }
     // through LDS, where the tiles are done with, so that a wavefront stores whole rows (a lane has 4 elements of a row at a time)
     const float inv = total == 0.0f ? 0.0f : 1.0f / total;
     constexpr int kOutRow = kRow + 16;                   // bytes; neighbouring rows begin 4 banks apart
@@ -349,8 +389,8 @@ hipError_t prompt(const PromptArgs &a, hipStream_t stream)
     const int query_heads = a.heads * a.group;
     const int64_t wide = (a.tokens >> 7) + a.sequences, narrow = (a.tokens >> 5) + a.sequences;
     if (split_is_faster(a, wide, narrow))
-        return launch_kernel(k_prompt_attention<DIM, BF16, true>, dim3((uint32_t)(narrow * query_heads)), dim3(512), stream, a, narrow);
-    return launch_kernel(k_prompt_attention<DIM, BF16, false>, dim3((uint32_t)(wide * query_heads)), dim3(256), stream, a, wide);
+        return launch_kernel(k_prompt_attention<DIM, BF16, true>, dim3((uint32_t)(narrow * query_heads)), dim3(512), stream, a, (int)narrow);
+    return launch_kernel(k_prompt_attention<DIM, BF16, false>, dim3((uint32_t)(wide * query_heads)), dim3(256), stream, a, (int)wide);
 }
 
 }  // namespace

@@ -411,6 +411,30 @@ def test_prompt_attention_keeps_sequences_apart(fc):
     assert same(got[:40], clean[:40]) and same(got[140:], clean[140:])
 
 
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("dim,lengths", [(128, [70, 300]), (64, [513])])
+def test_prompt_attention_sees_nothing_of_later_tokens(fc, dtype, dim, lengths):
+    # infinities and NaN among later tokens, in the same tile and in others: rows before them are what they would be without
+    tokens, heads, group = sum(lengths), 2, 2
+    q, k, v = (t.clone() for t in fused(tokens, (heads * group, heads, heads), dim, dtype, 7))
+    bad = 50                                                      # in the first sequence; 45 and 200 in the second
+    places = [bad] if len(lengths) == 1 else [bad, lengths[0] + 45, lengths[0] + 200]
+    want, weight = prompt_reference(q, k, v, lengths, True, dim ** -0.5)
+    for i, p in enumerate(places):
+        v[p, 0, 3 + i] = (math.nan, math.inf, -math.inf)[i]
+        k[p, 1, 5] = math.nan
+    got = fc.prompt_attention(q, k, v, offsets_of(lengths), max(lengths))
+    at = 0
+    for n in lengths:
+        first = min(p for p in places if at <= p < at + n)
+        check(got[at:first], want[at:first], weight[at:first], dtype, dtype == BF16)
+        assert not bool(torch.isfinite(got[first:at + n, :group, 3:6]).all(-1).any())     # heads of the first key/value head
+        assert bool(torch.isnan(got[first:at + n, group:]).all())
+        clean = got[first:at + n, :group, 8:].double().cpu()
+        assert bool(((clean - want[first:at + n, :group, 8:]).abs() <= 2.0 ** -6 * weight[first:at + n, :group, 8:] + 2.0 ** -6 * clean.abs()).all())
+        at += n
+
+
 # ---- calls ----
 
 def test_strided_operands_and_results(fc):
