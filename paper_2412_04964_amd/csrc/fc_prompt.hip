@@ -194,8 +194,7 @@ __global__ void __launch_bounds__(SPLIT ? 512 : 256, 2) k_prompt_attention(Promp
             for (int r = 0; r < 16; r += 2) {
                 const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h][r], factor, -top));
                 const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h][r + 1], factor, -top));
-                total += p0;
-                total += p1;
+                total += p0 + p1;
                 pf[2 * h + r / 8][r % 8 / 2] = narrow2<BF16>(p0, p1);
             }
     };
