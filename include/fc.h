@@ -346,7 +346,8 @@ FC_API int fc_rotary(const void *x, int64_t x_token_stride, int64_t x_head_strid
  *     code' = round(code * (s / s'))            of those tokens, where s' > s
  *     code' = round(x * (1 / s'))               of the new ones; signed codes are clamped to +-127
  * with IEEE divides, each operation rounded to nearest even.  A token beyond page table or rotation table is left out.
- * x must be finite.  A page that receives tokens belongs to one sequence.  longest: no sequence gets more new tokens.
+ * x must be finite.  A page that receives tokens belongs to one sequence.  longest: no sequence gets more new tokens (1: only the
+ * first one of each is appended).
  */
 FC_API int fc_cache_append(const void *k, int64_t k_token_stride, int64_t k_head_stride, const void *v, int64_t v_token_stride,
                            int64_t v_head_stride, int64_t tokens, int heads, int dim, int type, const float *table, int64_t table_rows,
@@ -357,11 +358,12 @@ FC_API int fc_cache_append(const void *k, int64_t k_token_stride, int64_t k_head
 /*
  * Attention over that cache, after the step's tokens were appended (same offsets, held, page_table): query i of a sequence sees its
  * tokens t < held + i + 1,
- *     o = sum_t w_t v_t,  w = softmax over t of scale * q . k_t
+ *     o = sum_t w_t v_t,  w = softmax over t of scale * q . k_t          (scale positive and finite)
  * q, out: [tokens, heads * group, dim]; query heads h * group ... use key/value head h.  A query that sees nothing gets zeros;
  * what the pages hold beyond the tokens of the sequence has no influence.
  * queries, longest: the most new tokens, and the most tokens in all, of a sequence.  They size the launch and the workspace;
- * sequences beyond them are computed all the same, more slowly.
+ * sequences beyond them are computed all the same, more slowly.  Entries of the page table that the context uses must be pages of
+ * the cache (others are not followed; what such a sequence gets is unspecified).
  * workspace: fc_cache_attention_workspace_bytes(...) bytes, 16-byte aligned, contents unspecified; may be NULL if that is 0.
  */
 FC_API size_t fc_cache_attention_workspace_bytes(int64_t tokens, int sequences, int heads, int group, int dim, int64_t queries, int64_t longest);
@@ -374,7 +376,9 @@ FC_API int fc_cache_attention(const void *q, int64_t q_token_stride, int64_t q_h
 
 /*
  * Attention of whole prompts to themselves: query i of a sequence sees all its tokens, or causal != 0: those up to i.
- * q, out: [tokens, heads * group, dim]; k, v: [tokens, heads, dim]; dim in {64, 128}.  longest: no sequence is longer.
+ * q, out: [tokens, heads * group, dim]; k, v: [tokens, heads, dim]; dim in {64, 128}; token strides of k and v below 2^25.
+ * longest: the most tokens of a sequence; it only chooses the form of the launch.  Causal rows depend on nothing of later tokens,
+ * infinities and NaN among them included.
  */
 FC_API int fc_prompt_attention(const void *q, int64_t q_token_stride, int64_t q_head_stride, const void *k, int64_t k_token_stride,
                                int64_t k_head_stride, const void *v, int64_t v_token_stride, int64_t v_head_stride, int64_t tokens,

@@ -577,6 +577,6 @@ const char *fc_strerror(int code)
 
 int fc_last_hip_error(void) { return g_last_hip_error; }
 
-int fc_version(void) { return 100; }
+int fc_version(void) { return 200; }
 
 }  // extern "C"

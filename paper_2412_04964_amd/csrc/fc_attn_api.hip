@@ -2,6 +2,8 @@
 // before they pass) and the choice of a launch.
 #include "fc.h"
 
+#include <float.h>
+
 #include "fc_attn.hpp"
 
 namespace {
@@ -44,6 +46,9 @@ int check_cache(const void *k, const void *v, const float *k_scales, const float
 
 // a launch of this many workgroups of `lanes` is one that the runtime takes
 bool launchable(int64_t workgroups, int lanes) { return workgroups <= ((int64_t)1 << 32) / lanes - 1; }
+
+// a softmax of a finite, positive multiple of the scores: the largest one stays the largest
+int check_scale(float scale) { return scale > 0.0f && scale <= FLT_MAX ? FC_OK : FC_ERR_SHAPE; }
 
 int check_attention(int64_t tokens, int sequences, int heads, int group, int dim, int64_t queries, int64_t longest)
 {
@@ -145,7 +150,7 @@ int fc_cache_attention(const void *q, int64_t q_token_stride, int64_t q_head_str
 {
     int rc = check_type(type);
     if (rc != FC_OK || (rc = check_code(quantizer)) != FC_OK) return rc;
-    if ((rc = check_attention(tokens, sequences, heads, group, dim, queries, longest)) != FC_OK) return rc;
+    if ((rc = check_attention(tokens, sequences, heads, group, dim, queries, longest)) != FC_OK || (rc = check_scale(scale)) != FC_OK) return rc;
     if (tokens == 0) return FC_OK;
     if ((rc = check_cache(k_cache, v_cache, k_scales, v_scales, pages, page, page_table, table_width)) != FC_OK) return rc;
     if (!offsets || !held) return FC_ERR_NULL;
@@ -185,6 +190,7 @@ int fc_prompt_attention(const void *q, int64_t q_token_stride, int64_t q_head_st
     if (rc != FC_OK) return rc;
     if ((rc = check_attention(tokens, sequences, heads, group, dim, 1, longest)) != FC_OK) return rc;
     if (dim == 256) return FC_ERR_SHAPE;
+    if ((rc = check_scale(scale)) != FC_OK) return rc;
     if (tokens == 0) return FC_OK;
     if (!offsets) return FC_ERR_NULL;
     if ((rc = check_rows(q, q_token_stride, q_head_stride)) != FC_OK) return rc;

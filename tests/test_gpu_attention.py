@@ -567,6 +567,14 @@ def test_refusals(fc):
         fc.cache_append(k, v, new_cache(2, 2, 8, 64), pages, o, held, 8)          # page of 8
     with pytest.raises(fc.FcError):
         fc.cache_attention(q, cache, pages, o, held, 0, 8)
+    for scale in (0.0, -1.0, math.inf, math.nan):
+        with pytest.raises(fc.FcError):
+            fc.cache_attention(q, cache, pages, o, held, 8, 8, scale=scale)
+        with pytest.raises(fc.FcError):
+            fc.prompt_attention(q, k, v, o, 8, scale=scale)
+    far = torch.empty(((1 << 26) + 128,), dtype=F16, device="cuda").as_strided((2, 2, 64), (1 << 26, 64, 1))
+    with pytest.raises(fc.FcError):
+        fc.prompt_attention(q[:2], far, far, ints([0, 2]), 2)            # token stride
     with pytest.raises(fc.FcError) as e:
         long = ints([30000])
         fc.cache_attention(q[:1], cache, pages, ints([0, 1]), long, 1, 30001, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
@@ -597,3 +605,17 @@ def test_ordinary_calls_are_native(fc):
         assert same(got[i], again[i])
     for a, b in zip(cache, twin):
         assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+# ---- the layer ----
+
+@pytest.mark.parametrize("quantizer,bound", [(SYM, 0.06), (FP8, 0.09)])
+def test_attention_layer_of_four_ranks(fc, quantizer, bound):
+    # Prompts see no cache: binary16 activations and one INT8 all-reduce, whose groups of 128 span about six standard deviations in 255 steps,
+    # twice: 6 / 255 / 12^0.5 * 2^0.5 = 0.010.  A decode step's keys and values are codes: signed ones have steps of 4.5 deviations / 127
+    # (0.010 of each value, and the all-reduce's again; a page's growing scale rounds its first codes a few times more), E4M3 has 3
+    # fraction bits (0.026).  The scores' errors move the weights by about as much again.  Together below 0.03 and 0.06; allowed 1.5 times.
+    from paper_2412_04964_amd import attention_block
+    errors, _, _ = attention_block.run(ranks=4, hidden=1024, query_heads=16, kv_heads=4, dim=64, prompts=3, length=150, steps=20, quantizer=quantizer)
+    assert errors[0] < 0.02
+    assert max(errors[1:]) < bound, errors
