@@ -140,7 +140,7 @@ template <int DIM> __device__ __forceinline__ constexpr int swizzle(int row) { r
 // The rows of a sequence's queries and the heads that share K and V, 16 ROW_TILES of them at a time.  RANGES: a workgroup has a range of
 // all units, as described at ranges_of; else a block of rows of one sequence and head, from its first token to its last.
 template <int DIM, bool FP8, bool BF16, int ROW_TILES, int WAVES, bool RANGES, bool STREAM>
-__global__ void __launch_bounds__(64 * WAVES, DIM == 256 ? 2 : ROW_TILES == 1 ? 4 : 2) k_cache_attention(CacheAttentionArgs a, int page_shift)
+__global__ void __launch_bounds__(64 * WAVES, RANGES || DIM == 256 || ROW_TILES > 1 ? 2 : 4) k_cache_attention(CacheAttentionArgs a, int page_shift)
 {
     constexpr int kSteps = DIM / 32;                    // matrix instructions over the head's elements
     constexpr int kOut = DIM / 16;                      // result tiles
