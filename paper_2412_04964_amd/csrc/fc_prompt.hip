@@ -84,15 +84,19 @@ __device__ __forceinline__ Found find_sequence_wide(const int32_t *__restrict__ 
     }
 }
 
-// SPLIT: the wavefronts have the same 32 rows and take their tiles in turn, each with a K and a V tile of its own in LDS; they are joined
-// at the end.  Else each has 32 rows and all work on the same tiles, two of each in LDS.
-template <int DIM, bool BF16, bool SPLIT>
-__global__ void __launch_bounds__(SPLIT ? 512 : 256, 2) k_prompt_attention(PromptArgs a, int units)
+// SPLIT: eight wavefronts have the same 32 rows and take their tiles in turn, each with a K and a V tile of its own in LDS; they are joined
+// at the end.  Else four have 32 rows each and all work on the same tiles, two of each in LDS: of 64 tokens, or of 32, which leaves registers
+// and LDS for three workgroups on a compute unit.
+template <int DIM, bool BF16, bool SPLIT, int TOKENS>
+__global__ void __launch_bounds__(SPLIT ? 512 : 256, SPLIT || TOKENS == 64 ? 2 : 3) k_prompt_attention(PromptArgs a, int units)
 {
-    constexpr int kWaves = SPLIT ? 8 : 4, kTokens = SPLIT ? 32 : 64;            // tokens of a tile
+    constexpr int kWaves = SPLIT ? 8 : 4, kTokens = TOKENS;                     // tokens of a tile
     constexpr int kSteps = DIM / 16, kOut = DIM / 32, kRow = 2 * DIM, kTile = kTokens * kRow, kHalves = kTokens / 32, kGroups = kTokens / 16;
     constexpr int kShift = SPLIT ? 5 : 7, kRows = 1 << kShift;                 // queries of a workgroup
-    __shared__ __attribute__((aligned(1024))) uint8_t tiles[SPLIT ? 2 * kWaves : 4][kTile];
+    constexpr int kOutRow = kRow + 16, kOutBytes = (SPLIT ? 1 : kWaves) * 32 * kOutRow;         // of the results on their way out
+    constexpr int kTiles = SPLIT ? 2 * kWaves : 4;
+    static_assert(TOKENS == 64 || TOKENS == 32, "whole matrix instructions");
+    __shared__ __attribute__((aligned(1024))) uint8_t tiles[kTiles * kTile > kOutBytes ? kTiles : (kOutBytes + kTile - 1) / kTile][kTile];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, side = lane >> 5;
     const int query_heads = a.heads * a.group;
     // workgroups go to the 8 XCDs in turn: where heads can be dealt to them, an XCD's L2 has few heads' K and V
@@ -104,6 +108,12 @@ __global__ void __launch_bounds__(SPLIT ? 512 : 256, 2) k_prompt_attention(Promp
     } else {
         head = blockIdx.x % query_heads;
         unit = units - 1 - blockIdx.x / query_heads;
+    }
+    // late rows, which see most, come first; where all workgroups are on the chip at once, the second ones on a compute unit go from early rows
+    // to late ones, so that the longest run beside the shortest (8192 tokens of 8 heads 165 -> 157 us)
+    if (!SPLIT && units * query_heads > 256 && units * query_heads <= 640) {
+        const int u = units - 1 - unit, once = 256 / query_heads;
+        if (u >= once) unit = u - once;
     }
     const int kv_head = head / a.group;
     const Found at = find_sequence_wide(a.offsets, a.sequences, kShift, unit, lane);
@@ -243,8 +253,13 @@ __global__ void __launch_bounds__(SPLIT ? 512 : 256, 2) k_prompt_attention(Promp
         }
     } else {
         const auto load = [&](int t0, int to) {
-            load_k(t0, wave, tiles[to]);
-            load_v(t0, wave, tiles[to + 1]);
+            if constexpr (kGroups == kWaves) {
+                load_k(t0, wave, tiles[to]);
+                load_v(t0, wave, tiles[to + 1]);
+            } else {                                     // half of the wavefronts bring K, half V
+                if (wave < kGroups) load_k(t0, wave, tiles[to]);
+                else load_v(t0, wave - kGroups, tiles[to + 1]);
+            }
         };
         const auto compute = [&](int t0, int from) {
             if (t0 >= my_end) return;
@@ -284,9 +299,9 @@ __global__ void __launch_bounds__(SPLIT ? 512 : 256, 2) k_prompt_attention(Promp
         total = 0.0f;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) total += join_sum[w][col] * __builtin_amdgcn_exp2f(join_max[w][col] - best);
-        const float mine = __builtin_amdgcn_exp2f(top - best);
+        const float unit = __builtin_amdgcn_exp2f(top - best);
 #pragma unroll
-        for (int o = 0; o < kOut; ++o) acc[o] *= mine;
+        for (int o = 0; o < kOut; ++o) acc[o] *= unit;
 #pragma unroll
         for (int half = kWaves / 2; half; half >>= 1) {
             if (wave >= half && wave < 2 * half)
@@ -351,9 +366,7 @@ __global__ void __launch_bounds__(SPLIT ? 512 : 256, 2) k_prompt_attention(Promp
     }
     // through LDS, where the tiles are done with, so that a wavefront stores whole rows (a lane has 4 elements of a row at a time)
     const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-    constexpr int kOutRow = kRow + 16;                   // bytes; neighbouring rows begin 4 banks apart
-    static_assert(sizeof(tiles) >= (SPLIT ? 1 : kWaves) * 32 * kOutRow, "the results fit the tiles");
-    uint8_t *const mine = &tiles[0][0] + (SPLIT ? 0 : wave) * 32 * kOutRow;
+    uint8_t *const mine = &tiles[0][0] + (SPLIT ? 0 : wave) * 32 * kOutRow;                     // neighbouring rows begin 4 banks apart
 #pragma unroll
     for (int o = 0; o < kOut; ++o)
 #pragma unroll
@@ -388,8 +401,15 @@ hipError_t prompt(const PromptArgs &a, hipStream_t stream)
     const int query_heads = a.heads * a.group;
     const int64_t wide = (a.tokens >> 7) + a.sequences, narrow = (a.tokens >> 5) + a.sequences;
     if (split_is_faster(a, wide, narrow))
-        return launch_kernel(k_prompt_attention<DIM, BF16, true>, dim3((uint32_t)(narrow * query_heads)), dim3(512), stream, a, (int)narrow);
-    return launch_kernel(k_prompt_attention<DIM, BF16, false>, dim3((uint32_t)(wide * query_heads)), dim3(256), stream, a, (int)wide);
+        return launch_kernel(k_prompt_attention<DIM, BF16, true, 32>, dim3((uint32_t)(narrow * query_heads)), dim3(512), stream, a, (int)narrow);
+    const dim3 grid((uint32_t)(wide * query_heads));
+    // Three workgroups on a compute unit, where there are two rounds of them and more; us for tiles of 64 / 32 tokens: 16384 tokens of 16 heads
+    // of 128 (2064 workgroups) 966 / 951, 8191 packed ones of 40 heads (3000) 136 / 126, but 8 x 512 tokens of 32 heads (1280) 41.4 / 42.7, 8192 of
+    // 8 heads (520) 164 / 197, 4096 (264) 72 / 94.  Heads of 64 have four workgroups with 64 tokens: 548 / 559.
+    if constexpr (DIM == 128) {
+        if (wide * query_heads > 1536) return launch_kernel(k_prompt_attention<DIM, BF16, false, 32>, grid, dim3(256), stream, a, (int)wide);
+    }
+    return launch_kernel(k_prompt_attention<DIM, BF16, false, 64>, grid, dim3(256), stream, a, (int)wide);
 }
 
 }  // namespace
