@@ -65,11 +65,11 @@ struct CacheAttentionArgs {
     int heads, group, dim, fp8, bf16;
     // cache_attention_plan's: 16-row tiles that a workgroup takes; workgroups that share all sequences' contexts evenly, or 0: one for each
     // head and sequence, and for each of `row_blocks` of its rows; whether codes are read once
-    int row_tiles, row_blocks, workgroups, stream;
+    int row_tiles, row_blocks, workgroups, splits, stream;
     uint32_t *plan;            // how many units there are, and where each sequence's begin
 };
 void cache_attention_plan(int sequences, int heads, int group, int dim, int64_t queries, int64_t longest, CacheAttentionArgs *a);
-size_t cache_attention_workspace(const CacheAttentionArgs &a, int sequences, int dim);
+size_t cache_attention_workspace(const CacheAttentionArgs &a, int64_t tokens, int sequences, int query_heads, int dim);
 hipError_t launch_cache_attention(const CacheAttentionArgs &a, hipStream_t stream);
 
 struct PromptArgs {

@@ -139,7 +139,7 @@ size_t fc_cache_attention_workspace_bytes(int64_t tokens, int sequences, int hea
     if (check_attention(tokens, sequences, heads, group, dim, queries, longest) != FC_OK) return 0;
     fc::CacheAttentionArgs a;
     fc::cache_attention_plan(sequences, heads, group, dim, queries, longest, &a);
-    return fc::cache_attention_workspace(a, sequences, dim);
+    return fc::cache_attention_workspace(a, tokens, sequences, heads * group, dim);
 }
 
 int fc_cache_attention(const void *q, int64_t q_token_stride, int64_t q_head_stride, int64_t tokens, int heads, int group, int dim, int type,
@@ -160,11 +160,14 @@ int fc_cache_attention(const void *q, int64_t q_token_stride, int64_t q_head_str
     fc::cache_attention_plan(sequences, heads, group, dim, queries, longest, &a);
     // ranges are counted in 32 bits: up to this many units, whatever the arrays say
     const double units = ((double)table_width * page / 32 + 1) * heads * ((double)tokens * group / 16 + sequences);
-    if (units >= 2147483648.0) a.workgroups = 0;
-    const size_t need = fc::cache_attention_workspace(a, sequences, dim);
+    if (units >= 2147483648.0) {
+        a.workgroups = 0;
+        a.splits = 1;
+    }
+    const size_t need = fc::cache_attention_workspace(a, tokens, sequences, heads * group, dim);
     if (need && (!workspace || workspace_bytes < need)) return FC_ERR_WORKSPACE;
     if (need && !aligned16(workspace)) return FC_ERR_ALIGN;
-    if (!launchable((int64_t)sequences * a.row_blocks * heads, 512) || !launchable(tokens * heads * group, 256)) return FC_ERR_SHAPE;
+    if (!launchable((int64_t)sequences * a.row_blocks * heads * a.splits, 512) || !launchable(tokens * heads * group, 256)) return FC_ERR_SHAPE;
     a.q = rows(q, q_token_stride, q_head_stride);
     a.out = rows(out, out_token_stride, out_head_stride);
     a.step = {offsets, held, sequences, tokens};

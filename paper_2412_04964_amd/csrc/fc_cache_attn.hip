@@ -5,13 +5,15 @@
 // with the scales sk, sv of t's page and head.  Codes of either kind are exact in binary16, so the products run on codes: sk multiplies
 // the score and sv the weight.  Rows of the matrix products are the queries of a sequence times the query heads that share a
 // key/value head (16 rows); the transposed score S^T = K Q^T leaves a lane with the weights of the tokens that it needs again as the
-// operand of O^T = V^T P^T, so nothing goes through LDS before the end.
+// operand of O^T = V^T P^T, so scores and weights never leave the registers.
 //   Queries are scaled by a power of two per row so that they fit binary16 (bfloat16's 8 bits stay exact over 2^28 below a row's largest).
 //   Weights are rounded to binary16 as p sv / ref, where ref is the row's largest p sv so far or less by kMost: 11 bits.
 //   The running maximum is raised only when a score passes it by kSlack, and ref by kMost: the sums carry the same factors either way.
 // The context is split over workgroups and their wavefronts, each with its own maximum and sums; wavefronts are joined in LDS,
-// workgroups by a second kernel through the workspace.  Memory bounds it: 2 bytes per token, head and element against one multiply-add
-// for each query head.
+// workgroups by a second kernel through the workspace (cache_attention_plan says which contexts are, and how).
+// Memory bounds large batches: 2 bytes per token, head and element against 2 multiply-adds for each query head.  64 x 8 contexts of up to
+// 8192 tokens, 807 MB: 138 us, 5.9 TB/s, where a bare stream of such pieces reaches 6.8.  Few requests are bound by latency: 8 of 1536 tokens
+// 11.7 us, two launches and in each a chain of three reads; a lone step of a wavefront takes 1.2 us for its 250 to 340 vector instructions.
 #include "fc_attn.hpp"
 
 namespace fc {
@@ -21,6 +23,7 @@ constexpr int64_t kMaxContext = 0x7FFF0000;
 constexpr float kSlack = 8.0f;          // in powers of two
 constexpr float kMost = 256.0f, kTiny = 1e-30f;
 constexpr int kLeast = 8;               // units of a range
+constexpr int kPiece = 4;               // of a piece, at least (8: 16 contexts of 1536 tokens 12.4 us instead of 11.7)
 
 constexpr int waves_of(int dim, int row_tiles) { return dim < 256 && row_tiles == 1 ? 8 : 4; }      // of a workgroup for a whole context
 constexpr int kTile = 16;               // tokens of a matrix instruction; a page holds whole tiles
@@ -131,6 +134,17 @@ __device__ __forceinline__ uint32_t running_sum(uint32_t v, int lane)
     return v;
 }
 
+// How a call shares out its work: one workgroup for a whole context (of a sequence, head and block of rows); contexts cut into pieces, one
+// workgroup each; equal ranges of all contexts
+enum { kByContext, kByPiece, kByRange };
+
+// pieces of a context of `units`, up to `splits`
+__device__ __forceinline__ int pieces_of(int units, int splits)
+{
+    const int most = units / kPiece;
+    return most < 1 ? 1 : most < splits ? most : splits;
+}
+
 // A wavefront's part of LDS: two tiles of K and two of V, 16 tokens of DIM bytes each, which come straight from memory: those of K for the
 // next step while this one's weights are made and V is read, those of V while the next step reads K.  The 16-byte units of a row are
 // exchanged (unit ^ swizzle of its row): K's operand reads one unit of all 16 rows at a time, without a conflict.
@@ -139,8 +153,8 @@ template <int DIM> __device__ __forceinline__ constexpr int swizzle(int row) { r
 
 // The rows of a sequence's queries and the heads that share K and V, 16 ROW_TILES of them at a time.  RANGES: a workgroup has a range of
 // all units, as described at ranges_of; else a block of rows of one sequence and head, from its first token to its last.
-template <int DIM, bool FP8, bool BF16, int ROW_TILES, int WAVES, bool RANGES, bool STREAM>
-__global__ void __launch_bounds__(64 * WAVES, RANGES || DIM == 256 || ROW_TILES > 1 ? 2 : 4) k_cache_attention(CacheAttentionArgs a, int page_shift)
+template <int DIM, bool FP8, bool BF16, int ROW_TILES, int WAVES, int FORM, bool STREAM>
+__global__ void __launch_bounds__(64 * WAVES, FORM != kByContext || DIM == 256 || ROW_TILES > 1 ? 2 : 4) k_cache_attention(CacheAttentionArgs a, int page_shift)
 {
     constexpr int kSteps = DIM / 32;                    // matrix instructions over the head's elements
     constexpr int kOut = DIM / 16;                      // result tiles
@@ -148,7 +162,8 @@ __global__ void __launch_bounds__(64 * WAVES, RANGES || DIM == 256 || ROW_TILES 
     constexpr int kRows = 16 * ROW_TILES;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
 
-    int b, head, block;                                 // what the workgroup is at
+    constexpr bool RANGES = FORM == kByRange;
+    int b, head, block, piece = 0;                      // what the workgroup is at
     uint32_t at = 0, end = 0, begins = 0;               // RANGES: its place in all units and where it ends; where the sequence's begin
     Job job;
     if constexpr (RANGES) {
@@ -197,6 +212,10 @@ __global__ void __launch_bounds__(64 * WAVES, RANGES || DIM == 256 || ROW_TILES 
         }
     } else {
         uint32_t id = blockIdx.x;
+        if constexpr (FORM == kByPiece) {
+            piece = id % a.splits;
+            id /= a.splits;
+        }
         head = id % a.heads;
         id /= a.heads;
         block = id % a.row_blocks;
@@ -238,6 +257,11 @@ __global__ void __launch_bounds__(64 * WAVES, RANGES || DIM == 256 || ROW_TILES 
             pair0 = at - item0;
             if (end - item0 < (uint32_t)pair1) pair1 = end - item0;
             at = item0 + pair1;
+        } else if constexpr (FORM == kByPiece) {
+            const int pieces = pieces_of(job.units, a.splits);
+            if (piece >= pieces) return;
+            pair0 = (int)((int64_t)job.units * piece / pieces);
+            pair1 = (int)((int64_t)job.units * (piece + 1) / pieces);
         }
         const bool whole = pair0 == 0 && pair1 == job.units;
         const int64_t off = job.off, held = job.held, rows = (int64_t)job.queries * a.group, row0 = (int64_t)block * kRows;
@@ -497,14 +521,17 @@ __global__ void __launch_bounds__(64 * WAVES, RANGES || DIM == 256 || ROW_TILES 
                         for (int o = 0; o < kOut; o += 4)
                             *(uintx2 *)(y + r * kOut + o) = uintx2{narrow2<BF16>(acc[x][o][r] * inv, acc[x][o + 1][r] * inv), narrow2<BF16>(acc[x][o + 2][r] * inv, acc[x][o + 3][r] * inv)};
                 } else {
-                    const int64_t place = ((int64_t)blockIdx.x * 2 + (pair0 == 0)) * kRows + 16 * x + col;
+                    const int64_t tokens_rows = a.step.tokens * a.heads * a.group;
+                    const int64_t place = RANGES ? ((int64_t)blockIdx.x * 2 + (pair0 == 0)) * kRows + 16 * x + col
+                                                 : ((off + q) * a.heads * a.group + h) * a.splits + piece;
+                    const int64_t places = RANGES ? (int64_t)gridDim.x * 2 * kRows : tokens_rows * a.splits;
                     float *y = a.partial + place * DIM + quad * 4 * kOut;
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
 #pragma unroll
                         for (int o = 0; o < kOut; o += 4)
                             *(floatx4 *)(y + r * kOut + o) = floatx4{acc[x][o][r], acc[x][o + 1][r], acc[x][o + 2][r], acc[x][o + 3][r]};
-                    if (quad == 0) *(floatx2 *)(a.partial + (int64_t)gridDim.x * 2 * kRows * DIM + place * 2) = floatx2{best, all};
+                    if (quad == 0) *(floatx2 *)(a.partial + places * DIM + place * 2) = floatx2{best, all};
                 }
             }
         }
@@ -514,7 +541,7 @@ __global__ void __launch_bounds__(64 * WAVES, RANGES || DIM == 256 || ROW_TILES 
 
 // Joins the pieces of the rows that were cut.  A range has two places for them: 1 for an item that it begins and does not end, 0 for one
 // that began before.  WAVES wavefronts for a token's row; in one, DIM / 4 lanes have 4 elements each.
-template <int DIM, bool BF16, int WAVES>
+template <int DIM, bool BF16, int WAVES, bool RANGES>
 __global__ void __launch_bounds__(256) k_cache_attention_join(CacheAttentionArgs a, int page_shift)
 {
     constexpr int kLanes = DIM / 4, kSets = 64 * WAVES / kLanes;          // every kSets-th piece is one set of lanes'
@@ -526,27 +553,43 @@ __global__ void __launch_bounds__(256) k_cache_attention_join(CacheAttentionArgs
     // single tokens: the sequence is the token's, or else it is looked for
     const int guess = token < a.step.sequences ? (int)token : a.step.sequences - 1;
     int off = a.step.offsets[guess], next = a.step.offsets[guess + 1], held = a.step.held[guess];
-    uint32_t begins = a.plan[1 + guess];
-    const uint32_t total = a.plan[0];
+    uint32_t begins = 0, total = 0;
+    if constexpr (RANGES) {
+        begins = a.plan[1 + guess];
+        total = a.plan[0];
+    }
     if (off != token || next != token + 1) {
         const int b = find_sequence(a.step.offsets, a.step.sequences, 0, 0, token);
         off = a.step.offsets[b];
         next = a.step.offsets[b + 1];
         held = a.step.held[b];
-        begins = a.plan[1 + b];
+        if constexpr (RANGES) begins = a.plan[1 + b];
     }
     const Job job = job_of(a, off, next, held, page_shift, block_rows);
     if (token < off || token >= off + job.queries) return;
-    const Ranges ranges(total, a.workgroups, kLeast);
-    const int64_t row = (token - off) * a.group + (h - head * a.group);
-    const int block = (int)(row / block_rows), row_at = (int)(row - (int64_t)block * block_rows);
-    const uint32_t item0 = begins + ((uint32_t)head * job.blocks + block) * job.units;
-    const uint32_t first = ranges.of(item0), last = ranges.of(item0 + job.units - 1);
-    if (first == last) return;                          // written already
-    const int pieces = (int)(last - first) + 1;
-    const auto place = [&](int p) { return ((int64_t)(first + p) * 2 + (p == 0)) * block_rows + row_at; };
+    int64_t place0, step, places;                       // of the first piece and of the others behind it
+    int pieces;
+    if constexpr (RANGES) {
+        const Ranges ranges(total, a.workgroups, kLeast);
+        const int64_t row = (token - off) * a.group + (h - head * a.group);
+        const int block = (int)(row / block_rows), row_at = (int)(row - (int64_t)block * block_rows);
+        const uint32_t item0 = begins + ((uint32_t)head * job.blocks + block) * job.units;
+        const uint32_t first = ranges.of(item0), last = ranges.of(item0 + job.units - 1);
+        pieces = (int)(last - first) + 1;
+        place0 = ((int64_t)first * 2 + 1) * block_rows + row_at;
+        step = 2 * block_rows;
+        places = (int64_t)a.workgroups * step;
+    } else {
+        pieces = pieces_of(job.units, a.splits);
+        place0 = row_id * a.splits;
+        step = 1;
+        places = a.step.tokens * query_heads * a.splits;
+    }
+    if (pieces == 1) return;                            // written already
+    // ranges: the first piece is in the second place of its range, the others are in the first ones
+    const auto place = [&](int p) { return place0 + p * step - (RANGES && p ? block_rows : 0); };
 
-    const floatx2 *m = (const floatx2 *)(a.partial + (int64_t)a.workgroups * 2 * block_rows * DIM);
+    const floatx2 *m = (const floatx2 *)(a.partial + places * DIM);
     const int lane = threadIdx.x & 63, d = threadIdx.x % kLanes * 4, set = threadIdx.x % (64 * WAVES) / kLanes;
     float best = -FLT_MAX, sum = 0.0f;
     floatx4 x = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -596,20 +639,24 @@ template <int DIM, bool FP8, bool BF16, int ROW_TILES>
 hipError_t attend_rows(const CacheAttentionArgs &a, hipStream_t stream)
 {
     const int shift = log2_int(a.cache.page);
-    hipError_t e;
-    if (!a.workgroups) {
-        constexpr int kWaves = waves_of(DIM, ROW_TILES);
-        const dim3 grid((uint32_t)((int64_t)a.step.sequences * a.row_blocks * a.heads)), block(64 * kWaves);
-        return a.stream ? launch_kernel(k_cache_attention<DIM, FP8, BF16, ROW_TILES, kWaves, false, true>, grid, block, stream, a, shift)
-                        : launch_kernel(k_cache_attention<DIM, FP8, BF16, ROW_TILES, kWaves, false, false>, grid, block, stream, a, shift);
-    }
-    e = a.stream ? launch_kernel(k_cache_attention<DIM, FP8, BF16, ROW_TILES, 4, true, true>, dim3(a.workgroups), dim3(256), stream, a, shift)
-                 : launch_kernel(k_cache_attention<DIM, FP8, BF16, ROW_TILES, 4, true, false>, dim3(a.workgroups), dim3(256), stream, a, shift);
+    constexpr int kWaves = waves_of(DIM, ROW_TILES);
+    const int64_t groups = (int64_t)a.step.sequences * a.row_blocks * a.heads;
+    const auto go = [&](auto *kernel, int64_t grid, int waves) { return launch_kernel(kernel, dim3((uint32_t)grid), dim3(64 * waves), stream, a, shift); };
+    if (!a.workgroups && a.splits == 1)
+        return a.stream ? go(k_cache_attention<DIM, FP8, BF16, ROW_TILES, kWaves, kByContext, true>, groups, kWaves)
+                        : go(k_cache_attention<DIM, FP8, BF16, ROW_TILES, kWaves, kByContext, false>, groups, kWaves);
+    hipError_t e = hipErrorInvalidValue;
+    if (a.workgroups)
+        e = a.stream ? go(k_cache_attention<DIM, FP8, BF16, ROW_TILES, 4, kByRange, true>, a.workgroups, 4)
+                     : go(k_cache_attention<DIM, FP8, BF16, ROW_TILES, 4, kByRange, false>, a.workgroups, 4);
+    else if constexpr (ROW_TILES < 3)                   // three tiles go with much more work than pieces
+        e = go(k_cache_attention<DIM, FP8, BF16, ROW_TILES, 4, kByPiece, false>, groups * a.splits, 4);
     if (e != hipSuccess) return e;
     const int64_t rows = a.step.tokens * a.heads * a.group;
     // where there are many rows, there are few pieces of each
-    return rows < 1024 ? launch_kernel(k_cache_attention_join<DIM, BF16, 4>, dim3((uint32_t)rows), dim3(256), stream, a, shift)
-                       : launch_kernel(k_cache_attention_join<DIM, BF16, 1>, dim3((uint32_t)((rows + 3) / 4)), dim3(256), stream, a, shift);
+    if (rows < 1024)
+        return a.workgroups ? go(k_cache_attention_join<DIM, BF16, 4, true>, rows, 4) : go(k_cache_attention_join<DIM, BF16, 4, false>, rows, 4);
+    return a.workgroups ? go(k_cache_attention_join<DIM, BF16, 1, true>, (rows + 3) / 4, 4) : go(k_cache_attention_join<DIM, BF16, 1, false>, (rows + 3) / 4, 4);
 }
 
 template <int DIM, bool FP8, bool BF16>
@@ -639,23 +686,33 @@ void cache_attention_plan(int sequences, int heads, int group, int dim, int64_t 
     a->row_tiles = dim == 256 || tiles == 1 ? 1 : tiles == 2 || contexts * pairs < 16384 ? 2 : 3;
     const int64_t blocks = (tiles + a->row_tiles - 1) / a->row_tiles;
     a->row_blocks = blocks > 4096 ? 4096 : (int)blocks;
-    const int64_t groups = contexts * blocks;
-    // One workgroup for a whole context needs no second launch and no sharing out, which cost 8 to 15 us, but its time goes with the
-    // longest one; us whole / shared: 16 contexts of 700 tokens 10.3 / 15.7, 1536 14.6 / 16.3, 3000 22.2 / 17.5; 512 contexts of up to
-    // 1000 24.5 / 31.8, 2048 41.5 / 46.7, 4096 82.8 / 77.2; 16 with 40 rows of 2000 29.7 / 19.1
-    const int64_t whole = waves_of(dim, a->row_tiles) * (groups >= 256 ? 12 : 6);
-    // Two workgroups of four wavefronts a compute unit hold enough loads in flight; 512 / 1024 / 2048 of them for 64 x 8 contexts of 8192:
-    // 142 / 143 / 147 us
-    const int64_t want = (groups * pairs + kLeast - 1) / kLeast;
-    a->workgroups = pairs <= whole ? 0 : want < 512 ? (int)want : 512;
+    const int64_t groups = contexts * blocks, units = groups * pairs;
+    a->splits = 1;
+    a->workgroups = 0;
+    if (pairs <= waves_of(dim, a->row_tiles) * (groups >= 192 ? 12 : 3)) {
+        // One workgroup for a whole context: no second launch, but the time of the longest context on one compute unit.  us whole / in
+        // pieces: 16 contexts of 700 tokens 10.5 / 11.2, 1536 14.7 / 11.7; 128 of 1500 17.5 / 16.4; 240 of 1500 18.6 / 21.7
+    } else if (units <= 16384 && a->row_tiles < 3) {
+        // Pieces, a workgroup each: as many as one or two for every compute unit, and few enough to be joined quickly.  us in pieces / in equal
+        // ranges, which have to be found first: 16 contexts of 3000 tokens 12.3 / 17.1, 64 of 4000 18.0 / 22.6, 8 of 40000 23.1 / 26.4;
+        // 256 / 512 pieces: 16 of 3000 12.3 / 13.5, 64 of 4000 20.0 / 18.0; 2 of 32000 with 125 and 250 each 17.1 / 23.2
+        const int64_t fit = (units > 4096 ? 512 : 256) / groups, most = pairs / kPiece, splits = fit < most ? fit : most;
+        a->splits = (int)(splits < 1 ? 1 : splits < 128 ? splits : 128);
+    } else {
+        // Two workgroups of four wavefronts a compute unit hold enough loads in flight; 512 / 1024 / 2048 of them for 64 x 8 contexts of up to
+        // 8192: 142 / 143 / 147 us.  160 contexts of up to 8192 in ranges / in pieces 52.5 / 58.2
+        const int64_t want = (units + kLeast - 1) / kLeast;
+        a->workgroups = want < 512 ? (int)want : 512;
+    }
     // what one workgroup reads and the memory-side cache does not hold is marked as read once (157 -> 143 us there)
     a->stream = blocks == 1 && beyond_cache(contexts * longest * 2 * dim);
 }
 
-size_t cache_attention_workspace(const CacheAttentionArgs &a, int sequences, int dim)
+size_t cache_attention_workspace(const CacheAttentionArgs &a, int64_t tokens, int sequences, int query_heads, int dim)
 {
-    if (!a.workgroups) return 0;
-    return (size_t)a.workgroups * 2 * 16 * a.row_tiles * (dim + 2) * sizeof(float) + ((size_t)sequences + 5) * sizeof(uint32_t);
+    const size_t each = (size_t)(dim + 2) * sizeof(float);
+    if (a.workgroups) return (size_t)a.workgroups * 2 * 16 * a.row_tiles * each + ((size_t)sequences + 5) * sizeof(uint32_t);
+    return a.splits == 1 ? 0 : (size_t)tokens * query_heads * a.splits * each + ((size_t)sequences + 5) * sizeof(uint32_t);
 }
 
 hipError_t launch_cache_attention(const CacheAttentionArgs &a, hipStream_t stream)
