@@ -296,6 +296,11 @@ CACHES = [
     (1, 3, 128, 64, [5000, 17], [2, 2], None),
     (1, 8, 128, 16, [900, 40], [9, 2], (1, 50)),                      # more queries and tokens than announced
     (2, 1, 64, 64, [20000], [1], None),
+    (1, 5, 256, 64, [3000, 900], [1, 4], None),
+    # contexts shared out evenly, cut anywhere; some of them empty, short, or with several queries
+    (8, 2, 64, 64, [25000, 3, 24000, -1, 700, 8, 15999], [1, 1, 1, 1, 2, 0, 3], None),
+    (8, 5, 128, 32, [24000, 21007, 22000, 0], [8, 1, 9, 20], None),   # three tiles of rows at a time
+    (2, 4, 256, 16, [131070, 130000], [1, 1], None),
 ]
 
 
@@ -382,6 +387,10 @@ PROMPTS = [
     (3, 1, 128, [257, 64, 5, 600]),
     (2, 5, 64, [191, 0, 0, 320]),
     (1, 1, 128, [1537]),
+    # more rows than fit the chip once, and than fit it twice
+    (8, 4, 128, [400, 397, 700, 1, 502]),
+    (8, 4, 64, [400, 397, 700, 1, 502]),
+    (16, 4, 128, [300, 321, 330, 64, 500, 129, 31, 640, 444, 441]),
 ]
 
 
@@ -604,6 +613,31 @@ def test_ordinary_calls_are_native(fc):
     for i in (0, 2, 3):
         assert same(got[i], again[i])
     for a, b in zip(cache, twin):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+def test_large_calls_equal_their_parts(fc):
+    # inputs beyond the memory-side cache are read in another way
+    tokens, heads, dim = 8200, 66, 128
+    x = (torch.rand((tokens, heads, dim), device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)) - 0.5).half()
+    assert x.numel() * 2 > 128 << 20
+    table = fc.rotary_table(tokens, fc.rotary_frequencies(dim))
+    positions = torch.arange(tokens, dtype=torch.int32, device="cuda")
+    for interleaved in (False, True):
+        whole = fc.rotary(x, table, positions, interleaved)
+        for part in (slice(0, 3000), slice(3000, tokens)):
+            assert torch.equal(whole[part], fc.rotary(x[part], table, positions[part], interleaved))
+    kv_heads, page, lengths = 33, 32, [4100, 100, 4000]
+    width = -(-max(lengths) // page)
+    pages = torch.randperm(3 * width, generator=gen(1)).view(3, width).to(torch.int32)
+    whole, parts = new_cache(3 * width, kv_heads, page, dim, fill=1), new_cache(3 * width, kv_heads, page, dim, fill=1)
+    k, v = x[:, :kv_heads], x[:, kv_heads:]
+    fc.cache_append(k, v, whole, pages.cuda(), offsets_of(lengths), ints([0, 0, 0]), max(lengths), FP8, table)
+    at = 0
+    for b, n in enumerate(lengths):
+        fc.cache_append(k[at:at + n], v[at:at + n], parts, pages[b:b + 1].cuda(), ints([0, n]), ints([0]), n, FP8, table)
+        at += n
+    for a, b in zip(whole, parts):
         assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
 
 
