@@ -7,6 +7,7 @@
  *     FinegrainedQuantize  ->  [All2All]  ->  Dequantize x N, ReduceSum,
  *     FinegrainedQuantize  ->  [All-Gather]  ->  Dequantize
  *
+ * and, further down, the attention of a tensor-parallel rank that such all-reduces follow.
  * The exchanges themselves are not part of this library: the N partial tensors
  * (or their quantized slices) are simply N slabs in this GPU's memory.
  *

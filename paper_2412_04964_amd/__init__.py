@@ -1,4 +1,4 @@
-"""MI355X-native Flash Communication quantization path (arXiv 2412.04964).
+"""MI355X-native Flash Communication quantization path (arXiv 2412.04964), and the attention of a tensor-parallel rank before it.
 
 Thin binding over ``libfc.so`` (the C ABI in ``include/fc.h``): a native module
 for the ordinary call, checks in Python and ctypes for the rest.  The
