@@ -7,7 +7,9 @@
 //   K and V tiles go from memory straight to LDS, one tile ahead of the arithmetic; beyond the sequence's end they are zeros.
 //   Rows of a tile lie as in memory, their 16-byte units exchanged (unit ^ swizzle of the row) so that reads find every bank once.
 //   The running maximum is raised only when a score passes it by kSlack; the sums carry the same factor either way.
-// Matrix instructions and the exponentials between them bound it.
+// Matrix instructions and the exponentials between them bound it, at a clock that falls under this load (1.4 to 1.7 GHz counted):
+// 16384 tokens, 16 heads, causal, bfloat16: 941 to 1013 us, 1.17 to 1.09 PFLOP/s, where a library's 16384^3 product reaches 1.31.
+// 11 ragged prompts, 8191 tokens, 40 heads, binary16: 126 to 133 us; edges take 137 vector instructions for 32 x 32 scores, not 87.
 #include "fc_attn.hpp"
 
 namespace fc {
