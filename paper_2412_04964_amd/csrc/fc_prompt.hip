@@ -8,8 +8,8 @@
 //   Rows of a tile lie as in memory, their 16-byte units exchanged (unit ^ swizzle of the row) so that reads find every bank once.
 //   The running maximum is raised only when a score passes it by kSlack; the sums carry the same factor either way.
 // Matrix instructions and the exponentials between them bound it, at a clock that falls under this load (1.4 to 1.7 GHz counted):
-// 16384 tokens, 16 heads, causal, bfloat16: 941 to 1013 us, 1.17 to 1.09 PFLOP/s, where a library's 16384^3 product reaches 1.31.
-// 11 ragged prompts, 8191 tokens, 40 heads, binary16: 126 to 133 us; edges take 137 vector instructions for 32 x 32 scores, not 87.
+// 16384 tokens, 16 heads, causal, bfloat16: 941 to 1021 us, 1.17 to 1.08 PFLOP/s, where a library's 16384^3 product reaches 1.31.
+// 11 ragged prompts, 8191 tokens, 40 heads, binary16: 126 us, where edges and what surrounds the loop weigh more.
 #include "fc_attn.hpp"
 
 namespace fc {
@@ -152,7 +152,8 @@ __global__ void __launch_bounds__(SPLIT ? 512 : 256, SPLIT || TOKENS == 64 ? 2 :
     float top = -FLT_MAX, total = 0.0f;
 
     const int end = a.causal && first + kRows < n ? first + kRows : n;      // of the workgroup
-    const int my_end = a.causal && row0 + 32 < n ? row0 + 32 : n;
+    // a wavefront without rows takes no tokens (11 ragged prompts, 8191 tokens, 40 heads: 128.9 -> 125.6 us)
+    const int my_end = !SPLIT && row0 >= n ? 0 : a.causal && row0 + 32 < n ? row0 + 32 : n;
     const int clear = a.causal && row0 < n ? row0 + 1 : n;                  // tokens that every row sees
 
     // 16 rows of a tile from token t0 on
