@@ -123,7 +123,7 @@ __global__ void __launch_bounds__(SPLIT ? 512 : 256, SPLIT || TOKENS == 64 ? 2 :
     const int n = at.next - at.off;
     if (at.off < 0 || at.next <= at.off || at.next > a.tokens) return;
     const int place = unit - ((at.off >> kShift) + at.b);
-    if (place > (n - 1) >> kShift) return;
+    if (place < 0 || place > (n - 1) >> kShift) return;    // (negative: tokens before the first sequence, or offsets that do not ascend)
     const int first = place * kRows, row0 = SPLIT ? first : first + wave * 32, row = row0 + col;
 
     uintx4 qf[kSteps];

@@ -444,6 +444,26 @@ def test_prompt_attention_sees_nothing_of_later_tokens(fc, dtype, dim, lengths):
         at += n
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("heads,group,dim", [(1, 2, 64), (16, 4, 128)])         # tokens split over wavefronts, and not
+def test_prompt_attention_stays_in_its_tensors(fc, causal, heads, group, dim):
+    # whatever the offsets are, only rows of q's tokens are written; tokens of no sequence are left alone
+    tokens, guard = 2000, 200
+    q, k, v = fused(tokens, (heads * group, heads, heads), dim, F16, 8)
+    for offsets in ([0, 1000, 1200, -100000, 2000], [2000, 0, 2000, 0], [-5, 300, 3000, 2000], [700, 650, 1999, 100, 2 ** 31 - 1],
+                    [1900, 2000, 5, -2 ** 31], [2001, 2002]):
+        print("prompt attention", causal, heads, group, dim, offsets, flush=True)
+        big = torch.full((guard + tokens + guard, heads * group, dim), 7.0, dtype=F16, device="cuda")
+        fc.prompt_attention(q, k, v, ints(offsets), 1000, causal, out=big[guard:guard + tokens])
+        assert bool((big[:guard] == 7).all()) and bool((big[guard + tokens:] == 7).all())
+    lengths = [40, 333]
+    big = torch.full((tokens, heads * group, dim), 7.0, dtype=F16, device="cuda")
+    fc.prompt_attention(q, k, v, ints([900, 940, 1273]), 333, causal, out=big)
+    assert bool((big[:900] == 7).all()) and bool((big[1273:] == 7).all())
+    want, weight = prompt_reference(q[900:1273], k[900:1273], v[900:1273], lengths, causal, dim ** -0.5)
+    check(big[900:1273], want, weight, F16, False)
+
+
 # ---- calls ----
 
 def test_strided_operands_and_results(fc):
