@@ -308,7 +308,8 @@ FC_API int fc_allreduce_sim_rot(const void *x_f16, int n_src, int64_t tokens, in
  *
  * Sequences are packed: the call's new tokens of sequence b are offsets[b] <= t < offsets[b + 1] (int32 [sequences + 1], offsets[0] = 0,
  * ascending, offsets[sequences] = tokens; equal neighbours: nothing new).  All index arrays are device memory; the kernels
- * check what they read from them, and a token, page or position outside its tensor is neither read nor written.
+ * check what they read from them, and a token, page or position outside its tensor is neither read nor written.  (Where offsets do
+ * not ascend, which tokens are computed is unspecified.)
  */
 #define FC_TYPE_F16 0
 #define FC_TYPE_BF16 1

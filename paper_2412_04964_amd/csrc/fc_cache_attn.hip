@@ -169,6 +169,7 @@ __global__ void __launch_bounds__(64 * WAVES, FORM != kByContext || DIM == 256 |
     if constexpr (RANGES) {
         int off = 0, next = 0, held = 0;
         uint32_t sum = 0, work = 0;
+        bool astray = false;
         for (int c = 0; c < a.step.sequences; c += 64)
             if (c + lane < a.step.sequences) {
                 off = a.step.offsets[c + lane];
@@ -177,9 +178,11 @@ __global__ void __launch_bounds__(64 * WAVES, FORM != kByContext || DIM == 256 |
                 const Job j = job_of(a, off, next, held, page_shift, kRows);
                 work = j.units * j.blocks * a.heads;
                 sum += work;
+                astray |= off < 0 || next < off || next > a.step.tokens;
             }
         uint32_t upto = running_sum(sum, lane);
-        const uint32_t total = __builtin_amdgcn_readlane(upto, 63);
+        // the units of offsets that do not ascend may be more than 32 bits count: none of them is done
+        const uint32_t total = __any(astray) ? 0 : __builtin_amdgcn_readlane(upto, 63);
         const Ranges ranges(total, gridDim.x, kLeast);
         if (blockIdx.x == 0 && threadIdx.x == 0) a.plan[0] = total;
         if (blockIdx.x >= ranges.count) return;
@@ -570,6 +573,7 @@ __global__ void __launch_bounds__(256) k_cache_attention_join(CacheAttentionArgs
     int64_t place0, step, places;                       // of the first piece and of the others behind it
     int pieces;
     if constexpr (RANGES) {
+        if (total == 0) return;
         const Ranges ranges(total, a.workgroups, kLeast);
         const int64_t row = (token - off) * a.group + (h - head * a.group);
         const int block = (int)(row / block_rows), row_at = (int)(row - (int64_t)block * block_rows);

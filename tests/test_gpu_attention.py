@@ -359,6 +359,34 @@ def test_cache_attention_beyond_32_bit_offsets(fc):
     check(got, want, weight, F16, False)
 
 
+@pytest.mark.parametrize("form", ["whole", "pieces", "ranges"])
+def test_cache_attention_stays_in_its_tensors(fc, form):
+    # whatever offsets, lengths and page table are, only rows of q's tokens are written.  Ranges: sequences that overlap, with more
+    # pairs of query and context together than 32 bits count
+    heads, group, dim, page, tokens, guard = 1, 8, 64, 64, 4096, 100
+    width = (1 << 20) // page
+    cache = new_cache(3, heads, page, dim, fill=1)
+    for s in cache[2:]:
+        s.fill_(0.01)
+    q, _ = fused(tokens, (heads * group, 1), dim, F16, 3)
+    overlapping = [0, 4096] * 128 + [1000, 4096] * 128 + [1000]
+    few = [[0, 5, 9000, -1, 4096], [4096, 0, 7, 3, 2 ** 31 - 1], [-2 ** 31, 3, 4097, 2, 1]]
+    for offsets in [overlapping] if form == "ranges" else few:
+        sequences = len(offsets) - 1
+        held = [2 ** 31 - 1] * sequences if form == "ranges" else [500, 2 ** 31 - 1, -2 ** 31, 100]
+        queries, longest = (tokens, 1 << 20) if form == "ranges" else (8, 300 if form == "whole" else 6000)
+        table = torch.randint(-1, 4, (sequences, width if form == "ranges" else 10), generator=gen(1)).to(torch.int32)
+        need = fc.cache_attention_workspace_bytes(tokens, sequences, heads, group, dim, queries, longest)
+        assert (need == 0) == (form == "whole")
+        print("cache attention", form, sequences, offsets[:5], need, flush=True)
+        big = torch.full((guard + tokens + guard, heads * group, dim), 7.0, dtype=F16, device="cuda")
+        space = torch.full((guard * 16 + need + guard * 16,), 7, dtype=torch.uint8, device="cuda")
+        fc.cache_attention(q, cache, table.cuda(), ints(offsets), ints(held), queries, longest, out=big[guard:guard + tokens],
+                           workspace=space[guard * 16:guard * 16 + need])
+        assert bool((big[:guard] == 7).all()) and bool((big[guard + tokens:] == 7).all())
+        assert bool((space[:guard * 16] == 7).all()) and bool((space[guard * 16 + need:] == 7).all())
+
+
 # ---- prompts ----
 
 def prompt_reference(q, k, v, lengths, causal, scale):
