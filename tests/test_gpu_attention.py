@@ -340,6 +340,39 @@ def test_cache_attention_extremes(fc, quantizer):
     check(got, want, weight, BF16, False)
 
 
+def peaked_cache(heads, dim, page, quantizer, held, table, seed):
+    """the first token of each sequence has the largest key code everywhere and a value of 0 in every other element; all other keys are 0"""
+    cache = filled_cache(int(table.max()) + 2, heads, page, dim, quantizer, held, [1] * len(held), table, seed)
+    for t in cache[2:]:
+        t.fill_(2.0 ** -7)
+    for b, n in enumerate(held):
+        for index in range(-(-(n + 1) // page)):
+            cache[0][int(table[b, index])] = 0
+    first = table[:, 0].long()
+    cache[0][first, :, 0] = codes_of(torch.tensor([TOP[quantizer]]), quantizer).cuda()
+    cache[1][first, :, 0, ::2] = 0
+    return cache
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("quantizer", [SYM, FP8])
+@pytest.mark.parametrize("heads,group,dim,held", [(1, 1, 128, [1000]), (2, 4, 64, [3000, 40]), (1, 3, 256, [300]), (8, 2, 128, [30000, 17, 29000])])
+def test_cache_attention_of_one_token_far_above_the_rest(fc, dtype, quantizer, heads, group, dim, held):
+    # what the elements have in which the first token is 0 comes from weights far below its own
+    page = 64
+    width = max(held) // page + 1
+    table = page_table(len(held), width, len(held) * width + 1, 2)
+    cache = peaked_cache(heads, dim, page, quantizer, held, table, 3)
+    q = torch.ones((len(held), heads * group, dim), dtype=dtype, device="cuda")
+    offsets = list(range(len(held) + 1))
+    for above in (0.0, 9.4, 14.7, 17.6, 20.35, 21.3, 23.7, 25.6):                   # powers of two
+        scale = above * math.log(2) / (dim * TOP[quantizer] * 2.0 ** -7) if above else dim ** -0.5 * 1e-3
+        got = fc.cache_attention(q, cache, table.cuda(), ints(offsets), ints(held), 1, max(held) + 1, quantizer, scale=scale)
+        print("cache attention", dtype, quantizer, heads, group, dim, held, above, flush=True)
+        want, weight = cache_reference(q, cache, table, offsets, held, quantizer, scale)
+        check(got, want, weight, dtype, False)
+
+
 def test_cache_attention_beyond_32_bit_offsets(fc):
     heads, dim, page = 8, 128, 64
     pages = (1 << 32) // (heads * dim * page) + 40
