@@ -21,7 +21,8 @@ namespace {
 
 constexpr int64_t kMaxContext = 0x7FFF0000;
 constexpr float kSlack = 8.0f;          // in powers of two
-constexpr float kMost = 65504.0f, kAim = 4096.0f, kTiny = 1e-30f;
+constexpr float kMost = 65504.0f, kAim = 4096.0f;
+constexpr float kLow = 0x1p-40f, kHigh = 0x1p10f;     // what scales of values ordinarily lie between
 constexpr int kLeast = 8;               // units of a range
 constexpr int kPiece = 4;               // of a piece, at least (8: 16 contexts of 1536 tokens 12.4 us instead of 11.7)
 
@@ -293,9 +294,11 @@ __global__ void __launch_bounds__(64 * WAVES, FORM != kByContext || DIM == 256 |
         float ks = 0.0f, vs = 0.0f;
         const auto look_up = [&](int base) {
             page = 0;
-            ks = vs = 0.0f;
+            ks = 0.0f;
+            vs = kLow;                                  // (of tiles that are not there: an ordinary one, which raises nothing)
             if (base + lane < stop && (base + lane) * kTile < context) {
                 const int id = a.cache.table[(int64_t)b * a.cache.table_width + ((base + lane) * kTile >> page_shift)];
+                vs = 0.0f;
                 if (id >= 0 && id < a.cache.pages) {
                     page = id;
                     ks = a.cache.k_scales[(int64_t)id * a.heads + head];
@@ -358,8 +361,7 @@ __global__ void __launch_bounds__(64 * WAVES, FORM != kByContext || DIM == 256 |
 #pragma unroll
             for (int o = 0; o < kOut; ++o) acc[x][o] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
             top[x] = -FLT_MAX;
-            total[x] = 0.0f;
-            ref[x] = kTiny;
+            total[x] = ref[x] = 0.0f;
         }
         // the sums' unit: they are acc * was, and are acc * ref afterwards
         const auto rebase = [&](int x, float was, float least) {
@@ -378,6 +380,20 @@ __global__ void __launch_bounds__(64 * WAVES, FORM != kByContext || DIM == 256 |
             }
             // the scales are here before the loop, where waiting for them would wait for all that is on its way
             asm volatile("" : "+v"(ks), "+v"(vs));
+            // The sums' unit is no less than 2^-100 of these tiles' largest scale, so that a scale in it stays finite: 2^-100 itself for
+            // ordinary scales
+            float least = 0x1p-100f;
+            if (__any(!(vs >= kLow && vs <= kHigh))) {
+                const float v = vs <= FLT_MAX ? vs * 0x1p-100f : 0.0f;
+                least = FLT_MIN;
+#pragma unroll 1
+                for (int l = 0; l < 64; ++l) least = fmaxf(least, lane_f(v, l));       // (shuffles take registers that the loop has not got)
+            }
+#pragma unroll
+            for (int x = 0; x < ROW_TILES; ++x) {
+                if (base == begin) ref[x] = least;      // there are no sums yet
+                else if (__any(ref[x] < least)) rebase(x, ref[x], least);
+            }
             for (int i = 0; i < n; i += 2) {
                 const int first = (base + i) * kTile;
                 wait_vm<2 * kPieces>();                 // K is here, V may be on its way
@@ -421,7 +437,7 @@ __global__ void __launch_bounds__(64 * WAVES, FORM != kByContext || DIM == 256 |
                         const float now = fmaxf(top[x], max4(most)), shrink = __builtin_amdgcn_exp2f(top[x] - now);
                         top[x] = now;
                         total[x] *= shrink;
-                        rebase(x, ref[x] * shrink, kTiny);
+                        rebase(x, ref[x] * shrink, least);
                     }
                     float p[8], w[8];
 #pragma unroll
@@ -437,7 +453,7 @@ __global__ void __launch_bounds__(64 * WAVES, FORM != kByContext || DIM == 256 |
                     };
                     const float weight = weigh();
                     if (__any(weight > kMost)) {
-                        rebase(x, ref[x], max4(weight) * ref[x] * (1.0f / kAim));
+                        rebase(x, ref[x], max4(weight) * (1.0f / kAim) * ref[x]);
                         weigh();
                     }
 #pragma unroll

@@ -340,6 +340,26 @@ def test_cache_attention_extremes(fc, quantizer):
     check(got, want, weight, BF16, False)
 
 
+@pytest.mark.parametrize("quantizer", [SYM, FP8])
+@pytest.mark.parametrize("heads,group,dim,page,held,new", [(2, 4, 128, 16, [100, 450], [1, 1]), (1, 5, 64, 32, [3000], [3]),
+                                                           (8, 2, 256, 64, [30000, 5], [1, 2])])
+def test_cache_attention_over_the_range_of_bfloat16(fc, quantizer, heads, group, dim, page, held, new):
+    # page scales up to where sums of that many tokens still fit fp32, down to the least one, and pages of both in one context
+    width = max(-(-(h + n) // page) for h, n in zip(held, new))
+    pages = len(held) * width + 1
+    table = page_table(len(held), width, pages, 1)
+    q, _ = fused(sum(new), (heads * group, 1), dim, BF16, 9)
+    offsets = [0] + [int(i) for i in np.cumsum(new)]
+    for name, scales in (("1e9", [1e9]), ("1e12", [1e12]), ("1e30", [1e30]), ("1e-30", [1e-30]), ("least", [FLT_MIN]), ("least, 1e30", [FLT_MIN, 1e30]),
+                         ("1, 1e20", [1.0, 1.0, 1e20]), ("many", [10.0 ** i for i in range(-37, 31)])):
+        cache = filled_cache(pages, heads, page, dim, quantizer, held, new, table, 5)
+        cache[3].copy_(torch.tensor([scales[i % len(scales)] for i in range(pages)], device="cuda")[:, None].expand(-1, heads))
+        print("cache attention", quantizer, heads, group, dim, page, held, new, name, flush=True)
+        got = fc.cache_attention(q, cache, table.cuda(), ints(offsets), ints(held), max(new), max(h + n for h, n in zip(held, new)), quantizer)
+        want, weight = cache_reference(q, cache, table, offsets, held, quantizer, dim ** -0.5)
+        check(got, want, weight, BF16, False)
+
+
 def peaked_cache(heads, dim, page, quantizer, held, table, seed):
     """the first token of each sequence has the largest key code everywhere and a value of 0 in every other element; all other keys are 0"""
     cache = filled_cache(int(table.max()) + 2, heads, page, dim, quantizer, held, [1] * len(held), table, seed)
