@@ -362,7 +362,8 @@ FC_API int fc_cache_append(const void *k, int64_t k_token_stride, int64_t k_head
  * tokens t < held + i + 1,
  *     o = sum_t w_t v_t,  w = softmax over t of scale * q . k_t          (scale positive and finite)
  * q, out: [tokens, heads * group, dim]; query heads h * group ... use key/value head h.  A query that sees nothing gets zeros;
- * what the pages hold beyond the tokens of the sequence has no influence.  Scales are positive and finite, as the append makes
+ * what the pages hold beyond the tokens that it sees has no influence, NaN codes and scales that are not finite included (a NaN among
+ * the value codes of a step's tokens may make NaN of all elements of the queries that see it).  Scales are positive and finite, as the append makes
  * them; sums run over weights of up to 2^8 before they are divided, so 2^8 times the tokens' |v| together must stay within fp32.
  * queries, longest: the most new tokens, and the most tokens in all, of a sequence.  They size the launch and the workspace;
  * sequences beyond them are computed all the same, more slowly.  Entries of the page table that the context uses must be pages of

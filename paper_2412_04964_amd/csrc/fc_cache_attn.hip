@@ -380,11 +380,11 @@ __global__ void __launch_bounds__(64 * WAVES, FORM != kByContext || DIM == 256 |
             }
             // the scales are here before the loop, where waiting for them would wait for all that is on its way
             asm volatile("" : "+v"(ks), "+v"(vs));
-            // The sums' unit is no less than 2^-100 of these tiles' largest scale, so that a scale in it stays finite: 2^-100 itself for
-            // ordinary scales
+            // The sums' unit is no less than 2^-116 of these tiles' largest scale, so that a scale in it, and 2^8 times that, stay finite:
+            // 2^-100 for ordinary scales
             float least = 0x1p-100f;
             if (__any(!(vs >= kLow && vs <= kHigh))) {
-                const float v = vs <= FLT_MAX ? vs * 0x1p-100f : 0.0f;
+                const float v = vs <= FLT_MAX ? vs * 0x1p-116f : 0.0f;
                 least = FLT_MIN;
 #pragma unroll 1
                 for (int l = 0; l < 64; ++l) least = fmaxf(least, lane_f(v, l));       // (shuffles take registers that the loop has not got)
@@ -434,7 +434,8 @@ __global__ void __launch_bounds__(64 * WAVES, FORM != kByContext || DIM == 256 |
                         most = fmaxf(most, fmaxf(fmaxf(s[x][t][0], s[x][t][1]), fmaxf(s[x][t][2], s[x][t][3])) * scale[t]);
                     }
                     if (__any(most > top[x] + kSlack)) {
-                        const float now = fmaxf(top[x], max4(most)), shrink = __builtin_amdgcn_exp2f(top[x] - now);
+                        most = max4(most);              // only rows that passed their own: no row's bits depend on others
+                        const float now = most > top[x] + kSlack ? most : top[x], shrink = __builtin_amdgcn_exp2f(top[x] - now);
                         top[x] = now;
                         total[x] *= shrink;
                         rebase(x, ref[x] * shrink, least);
@@ -451,16 +452,51 @@ __global__ void __launch_bounds__(64 * WAVES, FORM != kByContext || DIM == 256 |
                         for (int r = 0; r < 8; ++r) w[r] = p[r] * unit[r / 4];
                         return fmaxf(fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3])), fmaxf(fmaxf(w[4], w[5]), fmaxf(w[6], w[7])));
                     };
-                    const float weight = weigh();
+                    float weight = weigh();
                     if (__any(weight > kMost)) {
-                        rebase(x, ref[x], max4(weight) * (1.0f / kAim) * ref[x]);
+                        weight = max4(weight);
+                        rebase(x, ref[x], weight > kMost ? weight * (1.0f / kAim) * ref[x] : 0.0f);
                         weigh();
                     }
+                    if (masked)                         // whatever the scale of what a row does not see
+#pragma unroll
+                        for (int r = 0; r < 8; ++r)
+                            if (p[r] == 0.0f) w[r] = 0.0f;
 #pragma unroll
                     for (int r = 0; r < 4; ++r) pf[x][r] = narrow2<false>(w[2 * r], w[2 * r + 1]);
                 }
                 if (more) wait_vm<2 * kPieces>();       // V is here, the next K may be on its way
                 else wait_vm<0>();
+                if constexpr (FP8) {
+                    // E4M3's NaN among values that some rows of the block do not see: taken out, it goes into the weights of those that do
+                    if (masked && job.queries > 1) {
+                        uint32_t bad = 0;               // one bit for each of the tokens
+#pragma unroll 1
+                        for (int i = 0; i < 2 * kPieces; ++i) {
+                            uintx4 *const place = (uintx4 *)(tile_v + i * 1024 + lane * 16);
+                            uintx4 w = *place;
+                            uint32_t any = 0;
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const uint32_t nan = (((w[j] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) >> 7;     // 1 in its byte
+                                w[j] &= ~(nan * 0xFFu);
+                                any |= nan;
+                            }
+                            if (any) *place = w;
+                            for (uint64_t lanes = __ballot(any); lanes; lanes &= lanes - 1) bad |= 1u << (i * kPieceRows + __builtin_ctzll(lanes) / (DIM / 16));
+                        }
+                        if (bad) {
+                            const uint32_t mine[2] = {bad >> (quad * 4), bad >> (kTile + quad * 4)};
+#pragma unroll
+                            for (int x = 0; x < ROW_TILES; ++x)
+#pragma unroll
+                                for (int r = 0; r < 8; ++r) {
+                                    const uint32_t half = 0xFFFFu << 16 * (r & 1);
+                                    if ((mine[r / 4] >> r % 4 & 1) && (pf[x][r / 2] & half)) pf[x][r / 2] |= half;
+                                }
+                        }
+                    }
+                }
                 uint32_t vf[2][4][kWords];
 #pragma unroll
                 for (int t = 0; t < 2; ++t)

@@ -393,6 +393,44 @@ def test_cache_attention_of_one_token_far_above_the_rest(fc, dtype, quantizer, h
         check(got, want, weight, dtype, False)
 
 
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("quantizer", [SYM, FP8])
+@pytest.mark.parametrize("heads,group,dim", [(2, 3, 64), (2, 8, 128), (2, 1, 256)])
+@pytest.mark.parametrize("longest", [205, 6000, 1 << 20])                           # one workgroup a context, pieces, ranges
+def test_cache_attention_sees_nothing_of_later_tokens(fc, dtype, quantizer, heads, group, dim, longest):
+    # of several new tokens: later queries, and infinities and NaN among later keys, values and scales, change no bit of earlier rows
+    page, held, new = 16, [62, 200], [5, 4]                                          # the third and no one's tokens begin a page
+    table = page_table(2, 13, 27, 1)
+    cache = filled_cache(27, heads, page, dim, quantizer, held, new, table, 4)
+    q, _ = fused(9, (heads * group, 1), dim, dtype, 3)
+
+    def attend(q, cache):
+        return fc.cache_attention(q, cache, table.cuda(), ints([0, 5, 9]), ints(held), 5, longest, quantizer)
+
+    clean = attend(q, cache)
+    print("cache attention", dtype, quantizer, heads, group, dim, longest, flush=True)
+    loud = q.clone()
+    loud[2:5] *= 40                                                                  # raises maxima of the rows beside
+    loud[7] = math.nan
+    got = attend(loud, cache)
+    assert same(got[:2], clean[:2]) and same(got[5:7], clean[5:7]) and same(got[8], clean[8]) and bool(torch.isnan(got[7]).all())
+    last = int(table[0, 4])                                                          # page of the first sequence's tokens from 64 on
+    for which, value in ((2, math.inf), (2, math.nan), (3, math.inf), (3, math.nan), (3, 1e30)):
+        broken = tuple(t.clone() for t in cache)
+        broken[which][last] = value
+        got = attend(q, broken)
+        assert same(got[:2], clean[:2]) and same(got[5:], clean[5:]), (which, value)
+        if value != 1e30 and (which, value) != (2, math.inf):                        # (scores of minus infinity weigh nothing)
+            assert not bool(torch.isfinite(got[2:5]).all(-1).any())
+    if quantizer == FP8:
+        broken = tuple(t.clone() for t in cache)
+        broken[0][last, 0, 1, 3] = 0x7F                                              # token 65: key of one head, value of the other
+        broken[1][last, 1, 1, dim - 2] = 0xFF
+        got = attend(q, broken)
+        assert same(got[:3], clean[:3]) and same(got[5:], clean[5:])
+        assert bool(torch.isnan(got[3:5, :group]).all()) and bool(torch.isnan(got[3:5, group:, dim - 2]).all())
+
+
 def test_cache_attention_beyond_32_bit_offsets(fc):
     heads, dim, page = 8, 128, 64
     pages = (1 << 32) // (heads * dim * page) + 40
