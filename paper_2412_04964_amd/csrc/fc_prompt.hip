@@ -6,7 +6,10 @@
 // running maximum and sum of its column: one pass over K and V, and nothing but K and V goes through LDS.
 //   K and V tiles go from memory straight to LDS, one tile ahead of the arithmetic; beyond the sequence's end they are zeros.
 //   Rows of a tile lie as in memory, their 16-byte units exchanged (unit ^ swizzle of the row) so that reads find every bank once.
-//   The running maximum is raised only when a score passes it by kSlack; the sums carry the same factor either way.
+//   Weights are rounded to the type of the values, their sum adds them before that.  Their unit is the running maximum: bfloat16 has the
+//   range for all that are lower, so it is raised only, and when a score passes it by kSlack.  Binary16 has not: the unit follows a tile's
+//   largest score up and down when that is kSlack away, and the largest is put at 2^kBias, so that a tile's weights have 11 bits
+//   down to 2^-9 of its largest however far that is below the row's (down to 2^-kReach, where they are lost).
 // Matrix instructions and the exponentials between them bound it, at a clock that falls under this load (1.4 to 1.7 GHz counted):
 // 16384 tokens, 16 heads, causal, bfloat16: 941 to 1021 us, 1.17 to 1.08 PFLOP/s, where a library's 16384^3 product reaches 1.31.
 // 11 ragged prompts, 8191 tokens, 40 heads, binary16: 126 us, where edges and what surrounds the loop weigh more.
@@ -17,7 +20,9 @@ namespace {
 
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 
-constexpr float kSlack = 8.0f;          // in powers of two
+// in powers of two: how far a tile's largest score may be from the unit; where it is put; how far below the row's largest the unit may go
+template <bool BF16> constexpr float kSlack = BF16 ? 8.0f : 10.0f;
+constexpr float kBias = 5.0f, kReach = 60.0f;
 
 // what the number of a 16-byte unit is exchanged by in row t of a tile: 16 rows of K, read one unit each, and four of V, read 64 bytes
 // each, take every bank once
@@ -149,7 +154,7 @@ __global__ void __launch_bounds__(SPLIT ? 512 : 256, SPLIT || TOKENS == 64 ? 2 :
     for (int o = 0; o < kOut; ++o)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[o][r] = 0.0f;
-    float top = -FLT_MAX, total = 0.0f;
+    float top = -FLT_MAX, peak = -FLT_MAX, total = 0.0f;
 
     const int end = a.causal && first + kRows < n ? first + kRows : n;      // of the workgroup
     // a wavefront without rows takes no tokens (11 ragged prompts, 8191 tokens, 40 heads: 128.9 -> 125.6 us)
@@ -192,10 +197,23 @@ __global__ void __launch_bounds__(SPLIT ? 512 : 256, SPLIT || TOKENS == 64 ? 2 :
         for (int h = 0; h < kHalves; ++h)
 #pragma unroll
             for (int r = 0; r < 16; ++r) most = fmaxf(most, s[h][r]);
-        most *= factor;
-        if (__any(most > top + kSlack)) {
+        bool away;
+        if constexpr (BF16) {
+            most *= factor;
+            away = most > top + kSlack<BF16>;
+        } else {
+            most = __builtin_fmaf(most, factor, -kBias);
+            if (t0 + kTokens > clear) most = fmaxf(most, __shfl_xor(most, 32));      // a lane may have nothing that its row sees
+            away = fabsf(most - top) > kSlack<BF16>;
+        }
+        if (__any(away)) {
             most = fmaxf(most, __shfl_xor(most, 32));
-            const float now = fmaxf(top, most), shrink = __builtin_amdgcn_exp2f(top - now);
+            float now = fmaxf(top, most);
+            if constexpr (!BF16) {
+                now = fabsf(most - top) > kSlack<BF16> ? fmaxf(most, peak - kReach) : top;
+                peak = fmaxf(peak, now);
+            }
+            const float shrink = __builtin_amdgcn_exp2f(top - now);
             top = now;
             total *= shrink;
 #pragma unroll

@@ -563,6 +563,48 @@ def test_prompt_attention_sees_nothing_of_later_tokens(fc, dtype, dim, lengths):
         at += n
 
 
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("heads,group,dim,n,first", [(1, 1, 128, 3000, 0), (2, 1, 64, 700, 0), (16, 4, 128, 1100, 0), (8, 8, 64, 1000, 0), (2, 4, 128, 20000, 0),
+                                                     (2, 2, 128, 5000, 3333), (8, 8, 128, 1200, 700)])
+def test_prompt_attention_of_one_token_far_above_the_rest(fc, dtype, causal, heads, group, dim, n, first):
+    # Token `first` has a score of `above` powers of two over all others, which are alike, and a value of 0 in every other element: what
+    # those elements have comes from weights far below its own.  The definition in 64 bits is then a quotient of running sums.
+    v = torch.randn((n, heads, dim), generator=gen(n + dim)).to(dtype)
+    v[first, :, ::2] = 0
+    k = torch.zeros((n, heads, dim), dtype=dtype)
+    k[first] = 1
+    q = torch.ones((n, heads * group, dim), dtype=dtype, device="cuda")
+    on_card = k.cuda(), v.cuda()
+    for above in (9.4, 14.7, 17.6, 20.35, 21.3, 23.7, 25.6, 31.3, 38.5, 59.0):
+        w = torch.ones(n, dtype=torch.float64)
+        w[first] = 2.0 ** above
+        sums = [((w[:, None, None] * x).cumsum(0) if causal else (w[:, None, None] * x).sum(0, keepdim=True).expand(n, -1, -1)) for x in (v.double(), v.double().abs())]
+        total = w.cumsum(0)[:, None, None] if causal else w.sum()
+        want, weight = ((x / total).repeat_interleave(group, 1) for x in sums)
+        print("prompt attention", dtype, causal, heads, group, dim, n, first, above, flush=True)
+        got = fc.prompt_attention(q, *on_card, ints([0, n]), n, causal, scale=above * math.log(2) / dim)
+        check(got, want, weight, dtype, dtype == BF16)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("heads,group,dim,lengths", [(1, 1, 128, [600, 37]), (1, 2, 64, [129, 900]), (16, 4, 64, [500, 470]), (16, 4, 128, [520, 480])])
+def test_prompt_attention_with_peaks(fc, dtype, causal, heads, group, dim, lengths):
+    # scores of tens: the running maximum rises by more than any slack, early and late, and falls far behind
+    q, k, v = (t.clone() for t in fused(sum(lengths), (heads * group, heads, heads), dim, dtype, 21))
+    q *= 8
+    for n, loud in enumerate((3.0, 0.05, 1.5)):
+        kk = k.clone()
+        kk[n * 61:n * 61 + 200] *= loud                                              # stretches of loud and quiet keys
+        kk[-150:] /= loud
+        scale = dim ** -0.5 / max(1.0, loud)                                         # |score| < 64
+        print("prompt attention", dtype, causal, heads, group, dim, lengths, loud, flush=True)
+        got = fc.prompt_attention(q, kk, v, offsets_of(lengths), max(lengths), causal, scale=scale)
+        want, weight = prompt_reference(q, kk, v, lengths, causal, scale)
+        check(got, want, weight, dtype, dtype == BF16)
+
+
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("heads,group,dim", [(1, 2, 64), (16, 4, 128)])         # tokens split over wavefronts, and not
 def test_prompt_attention_stays_in_its_tensors(fc, causal, heads, group, dim):
