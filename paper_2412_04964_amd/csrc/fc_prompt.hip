@@ -150,11 +150,16 @@ __global__ void __launch_bounds__(SPLIT ? 512 : 256, SPLIT || TOKENS == 64 ? 2 :
     const int at_v = v_row * kRow + ((((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) ^ swizzle<DIM, false>(v_row)) * 16 + (lane & 1) * 8;
 
     floatx16 acc[kOut];
+    float top, peak, total;
+    const auto clear_sums = [&] {
 #pragma unroll
-    for (int o = 0; o < kOut; ++o)
+        for (int o = 0; o < kOut; ++o)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) acc[o][r] = 0.0f;
-    float top = -FLT_MAX, peak = -FLT_MAX, total = 0.0f;
+            for (int r = 0; r < 16; ++r) acc[o][r] = 0.0f;
+        top = peak = -FLT_MAX;
+        total = 0.0f;
+    };
+    clear_sums();
 
     const int end = a.causal && first + kRows < n ? first + kRows : n;      // of the workgroup
     // a wavefront without rows takes no tokens (11 ragged prompts, 8191 tokens, 40 heads: 128.9 -> 125.6 us)
@@ -183,15 +188,15 @@ __global__ void __launch_bounds__(SPLIT ? 512 : 256, SPLIT || TOKENS == 64 ? 2 :
                 s[h] = mma32<BF16>(*(const uintx4 *)(lds_k + (at_k ^ (j << 5)) + h * 32 * kRow), qf[j], s[h]);
     };
     uintx4 pf[2 * kHalves];
+    const auto mask = [&](int t0) {
+        const int sees = (a.causal && row < n - 1 ? row + 1 : n) - t0 - 4 * side;
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (h * 32 + 8 * (r / 4) + r % 4 >= sees) s[h][r] = -__builtin_inff();
+    };
     const auto weights = [&](int t0) {
-        if (t0 + kTokens > clear) {
-            const int sees = (a.causal && row < n - 1 ? row + 1 : n) - t0 - 4 * side;
-#pragma unroll
-            for (int h = 0; h < kHalves; ++h)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (h * 32 + 8 * (r / 4) + r % 4 >= sees) s[h][r] = -__builtin_inff();
-        }
         float most = s[0][0];
 #pragma unroll
         for (int h = 0; h < kHalves; ++h)
@@ -208,7 +213,8 @@ __global__ void __launch_bounds__(SPLIT ? 512 : 256, SPLIT || TOKENS == 64 ? 2 :
         }
         if (__any(away)) {
             most = fmaxf(most, __shfl_xor(most, 32));
-            float now = fmaxf(top, most);
+            // only rows that are away themselves: no row's bits depend on others
+            float now = most > top + kSlack<BF16> ? most : top;
             if constexpr (!BF16) {
                 now = fabsf(most - top) > kSlack<BF16> ? fmaxf(most, peak - kReach) : top;
                 peak = fmaxf(peak, now);
@@ -239,6 +245,37 @@ __global__ void __launch_bounds__(SPLIT ? 512 : 256, SPLIT || TOKENS == 64 ? 2 :
                 acc[o] = mma32<BF16>(uintx4{lo[0], lo[1], hi[0], hi[1]}, pf[m], acc[o]);
             }
     };
+    // In a tile that not all rows see whole, an infinity or NaN among the values would be NaN times the weight of 0 of those that do not.
+    // Such values are left out of the products and added to the rows that see them.
+    const auto not_finite = [](uint32_t w) { return (w & 0x7FFF7FFFu) + (BF16 ? 0x00800080u : 0x04000400u); };      // in the sign bits of w's halves
+    const auto finite_only = [&](uint32_t w) { return w & ~(((not_finite(w) & 0x80008000u) >> 15) * 0xFFFFu); };
+    const auto any_not_finite = [&](const uint8_t *lds_v) {
+        uint32_t any = 0;
+#pragma unroll
+        for (int i = 0; i < kTile / 1024; ++i) {
+            const uintx4 w = *(const uintx4 *)(lds_v + i * 1024 + lane * 16);
+            any |= not_finite(w[0]) | not_finite(w[1]) | not_finite(w[2]) | not_finite(w[3]);
+        }
+        return __any(any & 0x80008000u) != 0;
+    };
+    const auto add_not_finite = [&](const uint8_t *lds_v, int t0) {
+#pragma unroll 1
+        for (int t = 0; t < kTokens; ++t) {
+            const uint8_t *p = lds_v + t * kRow + side * 8;
+            const bool seen = t0 + t <= row;
+#pragma unroll
+            for (int o = 0; o < kOut; ++o)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    const uintx2 w = *(const uintx2 *)(p + ((o * 4 + r / 4) ^ swizzle<DIM, false>(t)) * 16);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t bits = i & 1 ? w[i / 2] >> 16 : w[i / 2] & 0xFFFFu;
+                        if (seen && (not_finite(bits) & 0x8000u)) acc[o][r + i] += widen<BF16>(bits);
+                    }
+                }
+        }
+    };
     // the queries are here before the loop, where waiting for them would wait for the tiles that are loaded ahead
     const auto queries_here = [&] {
 #pragma unroll
@@ -263,9 +300,19 @@ __global__ void __launch_bounds__(SPLIT ? 512 : 256, SPLIT || TOKENS == 64 ? 2 :
             if (more)
 #pragma unroll
                 for (int g = 0; g < kGroups; ++g) load_k(t0 + kWaves * kTokens, g, tile_k);
+            if (t0 + kTokens > clear) mask(t0);
             weights(t0);
             if (more) wait_vm<kLoads>();                 // V is here, the next K may be on its way
             else wait_vm<0>();
+            if (a.causal && t0 + kTokens > clear && any_not_finite(tile_v)) {
+                add_not_finite(tile_v, t0);
+#pragma unroll 1
+                for (int i = 0; i < kTile / 1024; ++i) {
+                    uintx4 *const place = (uintx4 *)(tile_v + i * 1024 + lane * 16);
+                    const uintx4 w = *place;
+                    *place = uintx4{finite_only(w[0]), finite_only(w[1]), finite_only(w[2]), finite_only(w[3])};
+                }
+            }
             add_values(tile_v);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             if (more)
@@ -273,6 +320,7 @@ __global__ void __launch_bounds__(SPLIT ? 512 : 256, SPLIT || TOKENS == 64 ? 2 :
                 for (int g = 0; g < kGroups; ++g) load_v(t0 + kWaves * kTokens, g, tile_v);
         }
     } else {
+        __shared__ int again;
         const auto load = [&](int t0, int to) {
             if constexpr (kGroups == kWaves) {
                 load_k(t0, wave, tiles[to]);
@@ -285,11 +333,16 @@ __global__ void __launch_bounds__(SPLIT ? 512 : 256, SPLIT || TOKENS == 64 ? 2 :
         const auto compute = [&](int t0, int from) {
             if (t0 >= my_end) return;
             scores(tiles[from]);
+            if (t0 + kTokens > clear) {
+                mask(t0);
+                if (a.causal && any_not_finite(tiles[from + 1])) again = 1;
+            }
             weights(t0);
             add_values(tiles[from + 1]);
         };
         const auto arrived = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
         load(0, 0);
+        if (threadIdx.x == 0) again = 0;
         queries_here();
         arrived();
         for (int t0 = 0; t0 < end; t0 += 2 * kTokens) {
@@ -300,6 +353,34 @@ __global__ void __launch_bounds__(SPLIT ? 512 : 256, SPLIT || TOKENS == 64 ? 2 :
             if (t0 + 2 * kTokens < end) load(t0 + 2 * kTokens, 0);
             compute(t0 + kTokens, 2);
             arrived();
+        }
+        // The workgroup's rows once more, in the same steps, where there were such values (that care in the loop above would cost all calls
+        // 4 to 6 %; a tile is other wavefronts' too, so they cannot be taken out of it)
+        if (__builtin_amdgcn_readfirstlane(again)) {
+            clear_sums();
+            for (int t0 = 0; t0 < end; t0 += kTokens) {
+                load(t0, 0);
+                arrived();
+                if (t0 < my_end) {
+                    const bool masked = t0 + kTokens > clear;
+                    scores(tiles[0]);
+                    if (masked) mask(t0);
+                    weights(t0);
+                    if (masked) add_not_finite(tiles[1], t0);
+                    const uint32_t keep = masked ? 0u : 0xFFFFFFFFu;        // of what is not finite
+#pragma unroll
+                    for (int m = 0; m < 2 * kHalves; ++m)
+#pragma unroll
+                        for (int o = 0; o < kOut; ++o) {
+                            const uint8_t *p = tiles[1] + (at_v ^ (o << 6)) + m * 16 * kRow;
+                            const uintx2 lo = transposed(p), hi = transposed(p + 8 * kRow);
+                            const uintx4 w = {lo[0], lo[1], hi[0], hi[1]};
+                            acc[o] = mma32<BF16>(uintx4{finite_only(w[0]) | (w[0] & keep), finite_only(w[1]) | (w[1] & keep), finite_only(w[2]) | (w[2] & keep),
+                                                        finite_only(w[3]) | (w[3] & keep)}, pf[m], acc[o]);
+                        }
+                }
+                arrived();
+            }
         }
     }
 
@@ -344,46 +425,6 @@ __global__ void __launch_bounds__(SPLIT ? 512 : 256, SPLIT || TOKENS == 64 ? 2 :
             __syncthreads();
         }
         if (wave) return;
-    }
-    // An infinity or NaN among the values of a token that a row does not see, but another row of its tile does, is NaN times its weight of
-    // zero.  Rows with such results are computed again, one token after the other, by what each row sees.
-    float finite = 0.0f;
-#pragma unroll
-    for (int o = 0; o < kOut; ++o)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) finite = __builtin_fmaf(acc[o][r], 0.0f, finite);
-    if (a.causal && __any(finite != 0.0f)) {
-        top = -FLT_MAX;
-        total = 0.0f;
-#pragma unroll
-        for (int o = 0; o < kOut; ++o)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[o][r] = 0.0f;
-        const uint16_t *again = (const uint16_t *)a.q.ptr + (off + (row < n ? row : n - 1)) * a.q.token + head * a.q.head + side * 8;
-        for (int t = 0; t < my_end; ++t) {
-            float dot = 0.0f;
-#pragma unroll
-            for (int j = 0; j < kSteps; ++j) {
-                float x[8], y[8];
-                widen8<BF16>(*(const uintx4 *)(again + 16 * j), x);
-                widen8<BF16>(*(const uintx4 *)(k + (int64_t)t * stride_k + 16 * j + side * 8), y);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) dot = __builtin_fmaf(x[i], y[i], dot);
-            }
-            dot = (dot + __shfl_xor(dot, 32)) * factor;
-            if (t > row) continue;
-            const float now = fmaxf(top, dot), shrink = __builtin_amdgcn_exp2f(top - now), p = __builtin_amdgcn_exp2f(dot - now);
-            top = now;
-            total = total * shrink + p;
-#pragma unroll
-            for (int o = 0; o < kOut; ++o)
-#pragma unroll
-                for (int r = 0; r < 16; r += 4) {
-                    const uintx2 w = *(const uintx2 *)(v + (int64_t)t * stride_v + o * 32 + 2 * r + 4 * side);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[o][r + i] = __builtin_fmaf(p, widen<BF16>(i & 1 ? w[i / 2] >> 16 : w[i / 2] & 0xFFFFu), acc[o][r + i] * shrink);
-                }
-        }
     }
     // through LDS, where the tiles are done with, so that a wavefront stores whole rows (a lane has 4 elements of a row at a time)
     const float inv = total == 0.0f ? 0.0f : 1.0f / total;

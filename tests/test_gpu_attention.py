@@ -605,6 +605,33 @@ def test_prompt_attention_with_peaks(fc, dtype, causal, heads, group, dim, lengt
         check(got, want, weight, dtype, dtype == BF16)
 
 
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("heads,group,dim,lengths", [(1, 2, 64, [70, 300]), (2, 1, 128, [65, 410]), (8, 8, 64, [130, 900]), (4, 8, 128, [64, 1700]), (16, 4, 128, [90, 3100])])
+def test_no_bit_of_a_causal_row_depends_on_later_tokens(fc, dtype, heads, group, dim, lengths):
+    # by 8 and 4 wavefronts, tiles of 32 and 64 tokens: louder queries, keys and values, infinities and NaN from token p of the last sequence on
+    q, k, v = (t.clone() for t in fused(sum(lengths), (heads * group, heads, heads), dim, dtype, 30))
+    offsets, at = offsets_of(lengths), lengths[0]
+    clean = fc.prompt_attention(q, k, v, offsets, max(lengths))
+    for p in (1, 17, 32, 47, 63, lengths[1] - 3):
+        for what in ("loud", "inf", "nan", "mixed"):
+            qq, kk, vv = q.clone(), k.clone(), v.clone()
+            if what == "loud":
+                for t in (qq, kk, vv):
+                    t[at + p:at + p + 20] *= 30
+            elif what == "mixed":
+                qq[at + p], kk[at + p + 1, :, 3], vv[at + p, :, 1], vv[at + p, :, 2] = math.nan, -math.inf, math.inf, math.nan
+                vv[at + p + 2, :, 1] = -math.inf
+            else:
+                vv[at + p, :, dim - 1] = math.inf if what == "inf" else math.nan
+            got = fc.prompt_attention(qq, kk, vv, offsets, max(lengths))
+            print("prompt attention", dtype, heads, group, dim, lengths, p, what, flush=True)
+            assert same(got[:at + p], clean[:at + p]), (p, what)
+            if what in ("inf", "nan"):
+                assert same(got[..., :dim - 1], clean[..., :dim - 1])
+                rest = got[at + p:, :, dim - 1]
+                assert bool((rest == math.inf if what == "inf" else torch.isnan(rest)).all()), (p, what)
+
+
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("heads,group,dim", [(1, 2, 64), (16, 4, 128)])         # tokens split over wavefronts, and not
 def test_prompt_attention_stays_in_its_tensors(fc, causal, heads, group, dim):
