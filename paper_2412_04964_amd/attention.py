@@ -9,7 +9,7 @@ held before.  A cache is a tuple (k_cache, v_cache, k_scales, v_scales): codes u
 
 Every call is asynchronous on ``torch.cuda.current_stream()``, reads no device value on the host and can be captured into a HIP graph;
 with `out` (and `workspace`) given it allocates nothing.  Serving only: no call records a gradient (``rotary(..., inverse=True)`` is
-the rotation's).
+the rotation's), so activations that require one are refused unless gradients are off (``torch.no_grad()``).
 """
 from __future__ import annotations
 
@@ -53,6 +53,8 @@ def _rows(t, what, dtype=None, shape=None):
     if t.device.index != torch.cuda.current_device():
         raise ValueError("%s lives on %s but the current device is cuda:%d; the C ABI works on the current device"
                          % (what, t.device, torch.cuda.current_device()))
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError("%s requires a gradient, which no attention call records: call it under torch.no_grad(), or on %s.detach()" % (what, what))
     if t.numel() and (t.stride(2) != 1 or any(s % 8 for s in _strides(t)) or t.data_ptr() % 16):
         raise ValueError("%s must have a dense last axis, other strides that are multiples of 8 elements and a 16-byte aligned "
                          "start, got strides %s" % (what, tuple(t.stride())))

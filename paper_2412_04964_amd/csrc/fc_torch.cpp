@@ -20,6 +20,7 @@
 #include <ATen/ATen.h>
 #include <ATen/hip/EmptyTensor.h>
 #include <ATen/PythonTorchFunctionTLS.h>
+#include <c10/core/GradMode.h>
 #include <c10/core/impl/LocalDispatchKeySet.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
@@ -493,6 +494,7 @@ bool activation(PyObject *o, at::ScalarType dtype, int device, Activation &a)
     if (!THPVariable_CheckExact(o)) return false;
     const at::Tensor &t = THPVariable_Unpack(o);
     if (!t.defined() || !ordinary_keys(t) || !t.is_cuda() || t.device().index() != device) return false;
+    if (t.requires_grad() && c10::GradMode::is_enabled()) return false;        // attention.py refuses it
     if (dtype == at::ScalarType::Undefined ? t.scalar_type() != at::kHalf && t.scalar_type() != at::kBFloat16 : t.scalar_type() != dtype)
         return false;
     return describe(t, a);

@@ -799,6 +799,30 @@ def test_refusals(fc):
     torch.cuda.synchronize()
 
 
+def test_calls_that_a_gradient_would_have_to_pass_are_refused(fc):
+    q, k, v = (t.clone() for t in fused(8, (4, 2, 2), 64, BF16, 0))
+    o, held, pages, p = ints([0, 8]), ints([0]), torch.zeros((1, 1), dtype=torch.int32, device="cuda"), torch.arange(8, dtype=torch.int32, device="cuda")
+    cache, table = new_cache(1, 2, 16, 64), fc.rotary_table(16, fc.rotary_frequencies(64))
+    calls = {"rotary": lambda q, k, v: fc.rotary(q, table, p), "append": lambda q, k, v: fc.cache_append(k, v, cache, pages, o, held, 8)[0],
+             "cache": lambda q, k, v: fc.cache_attention(q, cache, pages, o, held, 8, 8), "prompt": lambda q, k, v: fc.prompt_attention(q, k, v, o, 8)}
+    uses = {"rotary": (0,), "append": (1, 2), "cache": (0,), "prompt": (0, 1, 2)}
+    for name, call in calls.items():
+        want = call(q, k, v).clone()
+        for i in uses[name]:
+            args = [q, k, v]
+            args[i] = args[i].clone().requires_grad_()
+            with pytest.raises(ValueError, match="gradient"):
+                call(*args)
+            args[i] = args[i] * 1                                                # not a leaf
+            with pytest.raises(ValueError, match="gradient"):
+                call(*args)
+            with torch.no_grad():
+                assert torch.equal(call(*args), want)
+            assert torch.equal(call(*(t.detach() for t in args)), want)
+    with pytest.raises(ValueError, match="gradient"):
+        fc.rotary(q, table, p, out=torch.empty_like(q).requires_grad_())
+
+
 def test_ordinary_calls_are_native(fc):
     # what the module does not take it returns as None, and the checked path makes the same call
     native = fc.binding._calls()
