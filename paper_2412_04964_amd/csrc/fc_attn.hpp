@@ -34,7 +34,7 @@ struct Cache {
 };
 
 // An input that does not fit the 256 MB memory-side cache beside what is made of it; smaller ones have just been written there.
-inline bool beyond_cache(int64_t bytes) { return bytes > ((int64_t)128 << 20); }
+inline bool beyond_cache(double bytes) { return bytes > 128 << 20; }
 
 struct RotaryArgs {
     Rows x, y;

@@ -736,13 +736,15 @@ hipError_t attend_types(const CacheAttentionArgs &a, hipStream_t stream)
 
 void cache_attention_plan(int sequences, int heads, int group, int dim, int64_t queries, int64_t longest, CacheAttentionArgs *a)
 {
-    const int64_t tiles = (queries * group + 15) / 16, pairs = (longest + 2 * kTile - 1) / (2 * kTile), contexts = (int64_t)sequences * heads;
+    // what may be announced is as much as its type holds, and the products of that more than 64 bits
+    const int64_t tiles = (queries * group + 15) / 16, pairs = (longest + 2 * kTile - 1) / (2 * kTile);
+    const double contexts = (double)sequences * heads;
     // Three tiles of rows at a time read the context once for 48 rows, but leave fewer workgroups; us for 40 rows of 8 heads by context with
     // two and three: 4000 tokens 21.6 / 28.0, 16000 28.7 / 34.0, 131071 73.8 / 62.2
     a->row_tiles = dim == 256 || tiles == 1 ? 1 : tiles == 2 || contexts * pairs < 16384 ? 2 : 3;
     const int64_t blocks = (tiles + a->row_tiles - 1) / a->row_tiles;
     a->row_blocks = blocks > 4096 ? 4096 : (int)blocks;
-    const int64_t groups = contexts * blocks, units = groups * pairs;
+    const double groups = contexts * blocks, units = groups * pairs;
     a->splits = 1;
     a->workgroups = 0;
     if (pairs <= waves_of(dim, a->row_tiles) * (groups >= 192 ? 12 : 3)) {
@@ -752,13 +754,12 @@ void cache_attention_plan(int sequences, int heads, int group, int dim, int64_t 
         // Pieces, a workgroup each: as many as one or two for every compute unit, and few enough to be joined quickly.  us in pieces / in equal
         // ranges, which have to be found first: 16 contexts of 3000 tokens 12.3 / 17.1, 64 of 4000 18.0 / 22.6, 8 of 40000 23.1 / 26.4;
         // 256 / 512 pieces: 16 of 3000 12.3 / 13.5, 64 of 4000 20.0 / 18.0; 2 of 32000 with 125 and 250 each 17.1 / 23.2
-        const int64_t fit = (units > 4096 ? 512 : 256) / groups, most = pairs / kPiece, splits = fit < most ? fit : most;
+        const int64_t fit = (units > 4096 ? 512 : 256) / (int64_t)groups, most = pairs / kPiece, splits = fit < most ? fit : most;
         a->splits = (int)(splits < 1 ? 1 : splits < 128 ? splits : 128);
     } else {
         // Two workgroups of four wavefronts a compute unit hold enough loads in flight; 512 / 1024 / 2048 of them for 64 x 8 contexts of up to
         // 8192: 142 / 143 / 147 us.  160 contexts of up to 8192 in ranges / in pieces 52.5 / 58.2
-        const int64_t want = (units + kLeast - 1) / kLeast;
-        a->workgroups = want < 512 ? (int)want : 512;
+        a->workgroups = units < 512 * kLeast ? ((int)units + kLeast - 1) / kLeast : 512;
     }
     // what one workgroup reads and the memory-side cache does not hold is marked as read once (157 -> 143 us there)
     a->stream = blocks == 1 && beyond_cache(contexts * longest * 2 * dim);

@@ -67,6 +67,15 @@ def test_cache_attention_argument_checks(L):
         assert L.fc_cache_attention_workspace_bytes(*bad) == 0
 
 
+def test_more_announced_work_never_plans_for_less(L):
+    # announced queries and tokens are bounds, up to the largest that their types hold
+    most = (1 << 31) - 1
+    for sequences, heads in ((256, 8), (65536, 64), (most, 8), (1, 1)):
+        for longest in (1 << 20, 1 << 26, most):
+            need = [L.fc_cache_attention_workspace_bytes(64, sequences, heads, 8, 128, queries, longest) for queries in (4096, 1 << 20, 1 << 28, most)]
+            assert need[0] > 0 and need == [need[0]] * 4, (sequences, heads, longest, need)
+
+
 def prompt(L, q=P, k=P, v=P, tokens=4, heads=2, group=2, dim=64, type=0, offsets=P, sequences=1, longest=4, out=P, vt=128):
     return L.fc_prompt_attention(q, 256, 64, k, 128, 64, v, vt, 64, tokens, heads, group, dim, type, offsets, sequences, longest, 1, 0.1, out,
                                  256, 64, None)
