@@ -36,6 +36,15 @@ struct Cache {
 // An input that does not fit the 256 MB memory-side cache beside what is made of it; smaller ones have just been written there.
 inline bool beyond_cache(double bytes) { return bytes > 128 << 20; }
 
+// Launches of `workgroups` workgroups of `lanes`, unless they are more than the runtime takes (2^32 - 1 lanes)
+constexpr hipError_t kTooLarge = hipErrorInvalidConfiguration;
+inline bool launchable(int64_t workgroups, int lanes) { return workgroups <= ((int64_t)1 << 32) / lanes - 1; }
+template <typename K, typename... A>
+inline hipError_t launch_many(K *kernel, int64_t workgroups, int lanes, hipStream_t stream, A... a)
+{
+    return launchable(workgroups, lanes) ? launch_kernel(kernel, dim3((uint32_t)workgroups), dim3(lanes), stream, a...) : kTooLarge;
+}
+
 struct RotaryArgs {
     Rows x, y;
     const float *table;

@@ -44,8 +44,7 @@ int check_cache(const void *k, const void *v, const float *k_scales, const float
     return aligned16(k) && aligned16(v) ? FC_OK : FC_ERR_ALIGN;
 }
 
-// a launch of this many workgroups of `lanes` is one that the runtime takes
-bool launchable(int64_t workgroups, int lanes) { return workgroups <= ((int64_t)1 << 32) / lanes - 1; }
+int result(hipError_t e) { return e == fc::kTooLarge ? FC_ERR_SHAPE : fc::hip_result(e); }
 
 // a softmax of a finite, positive multiple of the scores: the largest one stays the largest
 int check_scale(float scale) { return scale > 0.0f && scale <= FLT_MAX ? FC_OK : FC_ERR_SHAPE; }
@@ -67,8 +66,7 @@ int fc_rotary_table(const double *frequencies, int64_t rows_, int rotary, double
     if (rotary < 2 || rotary % 2 || rotary > 4096 || rows_ < 0 || rows_ > kMaxTokens) return FC_ERR_SHAPE;
     if (rows_ == 0) return FC_OK;
     if (!frequencies || !table) return FC_ERR_NULL;
-    if (!launchable((rows_ * (rotary / 2) + 255) / 256, 256)) return FC_ERR_SHAPE;
-    return fc::hip_result(fc::launch_rotary_table(frequencies, rows_, rotary, magnitude, table, static_cast<hipStream_t>(hip_stream)));
+    return result(fc::launch_rotary_table(frequencies, rows_, rotary, magnitude, table, static_cast<hipStream_t>(hip_stream)));
 }
 
 int fc_rotary(const void *x, int64_t x_token_stride, int64_t x_head_stride, const float *table, int64_t table_rows,
@@ -83,7 +81,6 @@ int fc_rotary(const void *x, int64_t x_token_stride, int64_t x_head_stride, cons
     if (!table || !positions) return FC_ERR_NULL;
     if ((rc = check_rows(x, x_token_stride, x_head_stride)) != FC_OK) return rc;
     if ((rc = check_rows(y, y_token_stride, y_head_stride)) != FC_OK) return rc;
-    if (!launchable((tokens * heads * dim + 255) / 256, 256)) return FC_ERR_SHAPE;
     fc::RotaryArgs a;
     a.x = rows(x, x_token_stride, x_head_stride);
     a.y = rows(y, y_token_stride, y_head_stride);
@@ -97,7 +94,7 @@ int fc_rotary(const void *x, int64_t x_token_stride, int64_t x_head_stride, cons
     a.interleaved = interleaved != 0;
     a.inverse = inverse != 0;
     a.bf16 = type == FC_TYPE_BF16;
-    return fc::hip_result(fc::launch_rotary(a, static_cast<hipStream_t>(hip_stream)));
+    return result(fc::launch_rotary(a, static_cast<hipStream_t>(hip_stream)));
 }
 
 int fc_cache_append(const void *k, int64_t k_token_stride, int64_t k_head_stride, const void *v, int64_t v_token_stride, int64_t v_head_stride,
@@ -116,7 +113,6 @@ int fc_cache_append(const void *k, int64_t k_token_stride, int64_t k_head_stride
     if (!offsets || !held || (rotary && !table)) return FC_ERR_NULL;
     if ((rc = check_rows(k, k_token_stride, k_head_stride)) != FC_OK) return rc;
     if ((rc = check_rows(v, v_token_stride, v_head_stride)) != FC_OK) return rc;
-    if (!launchable((tokens / page + 2 * (int64_t)sequences + 8) * 2 * heads, 512)) return FC_ERR_SHAPE;
     fc::AppendArgs a;
     a.k = rows(k, k_token_stride, k_head_stride);
     a.v = rows(v, v_token_stride, v_head_stride);
@@ -131,7 +127,7 @@ int fc_cache_append(const void *k, int64_t k_token_stride, int64_t k_head_stride
     a.interleaved = interleaved != 0;
     a.fp8 = quantizer == FC_QUANTIZER_FP8;
     a.bf16 = type == FC_TYPE_BF16;
-    return fc::hip_result(fc::launch_cache_append(a, static_cast<hipStream_t>(hip_stream)));
+    return result(fc::launch_cache_append(a, static_cast<hipStream_t>(hip_stream)));
 }
 
 size_t fc_cache_attention_workspace_bytes(int64_t tokens, int sequences, int heads, int group, int dim, int64_t queries, int64_t longest)
@@ -160,14 +156,20 @@ int fc_cache_attention(const void *q, int64_t q_token_stride, int64_t q_head_str
     fc::cache_attention_plan(sequences, heads, group, dim, queries, longest, &a);
     // ranges are counted in 32 bits: up to this many units, whatever the arrays say
     const double units = ((double)table_width * page / 32 + 1) * heads * ((double)tokens * group / 16 + sequences);
-    if (units >= 2147483648.0) {
+    const int64_t rows_ = tokens * heads * group;
+    if (rows_ / 16 > kMaxTokens) return FC_ERR_SHAPE;
+    if (units >= 2147483648.0 || !fc::launchable((rows_ + 3) / 4, 256)) {              // or more rows than are joined
         a.workgroups = 0;
         a.splits = 1;
+    }
+    if (!a.workgroups) {                 // a workgroup takes every row_blocks-th block of a sequence: no more of them than are launched
+        const int64_t blocks = (((int64_t)1 << 32) / 512 - 1) / ((int64_t)sequences * heads * a.splits);
+        if (blocks < 1) return FC_ERR_SHAPE;
+        if (a.row_blocks > blocks) a.row_blocks = (int)blocks;
     }
     const size_t need = fc::cache_attention_workspace(a, tokens, sequences, heads * group, dim);
     if (need && (!workspace || workspace_bytes < need)) return FC_ERR_WORKSPACE;
     if (need && !aligned16(workspace)) return FC_ERR_ALIGN;
-    if (!launchable((int64_t)sequences * a.row_blocks * heads * a.splits, 512) || !launchable(tokens * heads * group, 256)) return FC_ERR_SHAPE;
     a.q = rows(q, q_token_stride, q_head_stride);
     a.out = rows(out, out_token_stride, out_head_stride);
     a.step = {offsets, held, sequences, tokens};
@@ -181,7 +183,7 @@ int fc_cache_attention(const void *q, int64_t q_token_stride, int64_t q_head_str
     a.dim = dim;
     a.fp8 = quantizer == FC_QUANTIZER_FP8;
     a.bf16 = type == FC_TYPE_BF16;
-    return fc::hip_result(fc::launch_cache_attention(a, static_cast<hipStream_t>(hip_stream)));
+    return result(fc::launch_cache_attention(a, static_cast<hipStream_t>(hip_stream)));
 }
 
 int fc_prompt_attention(const void *q, int64_t q_token_stride, int64_t q_head_stride, const void *k, int64_t k_token_stride,
@@ -200,9 +202,9 @@ int fc_prompt_attention(const void *q, int64_t q_token_stride, int64_t q_head_st
     if ((rc = check_rows(k, k_token_stride, k_head_stride)) != FC_OK) return rc;
     if ((rc = check_rows(v, v_token_stride, v_head_stride)) != FC_OK) return rc;
     if ((rc = check_rows(out, out_token_stride, out_head_stride)) != FC_OK) return rc;
-    // 32-bit offsets in a tile; a grid of 32-row workgroups at most
+    // 32-bit offsets in a tile, and tokens of a sequence
+    if (tokens > kMaxTokens - 1024) return FC_ERR_SHAPE;
     if (k_token_stride >= 1 << 25 || v_token_stride >= 1 << 25 || k_token_stride < 0 || v_token_stride < 0) return FC_ERR_SHAPE;
-    if (!launchable((tokens / 32 + sequences) * heads * group, 512)) return FC_ERR_SHAPE;
     fc::PromptArgs a;
     a.q = rows(q, q_token_stride, q_head_stride);
     a.k = rows(k, k_token_stride, k_head_stride);
@@ -218,7 +220,7 @@ int fc_prompt_attention(const void *q, int64_t q_token_stride, int64_t q_head_st
     a.dim = dim;
     a.causal = causal != 0;
     a.bf16 = type == FC_TYPE_BF16;
-    return fc::hip_result(fc::launch_prompt_attention(a, static_cast<hipStream_t>(hip_stream)));
+    return result(fc::launch_prompt_attention(a, static_cast<hipStream_t>(hip_stream)));
 }
 
 }  // extern "C"

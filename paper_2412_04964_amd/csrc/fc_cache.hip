@@ -280,15 +280,15 @@ hipError_t append(const AppendArgs &a, hipStream_t stream)
     const int shift = log2_int(a.cache.page);
     if (a.longest == 1) {
         const int64_t lanes = (int64_t)a.step.sequences * 2 * a.heads * (DIM / 8);
-        return launch_kernel(k_cache_append_one<DIM, FP8, BF16>, dim3((uint32_t)((lanes + 255) / 256)), dim3(256), stream, a, shift);
+        return launch_many(k_cache_append_one<DIM, FP8, BF16>, (lanes + 255) / 256, 256, stream, a, shift);
     }
     const int64_t units = (a.step.tokens >> shift) + 2 * (int64_t)a.step.sequences;
     const int lanes = a.cache.page * DIM / 32 < 64 ? 64 : a.cache.page * DIM / 32;
-    const dim3 grid((uint32_t)((units + 7) / 8 * 8 * 2 * a.heads));
-    if (a.rotary % 16) return launch_kernel(k_cache_append<DIM, FP8, BF16, false, false>, grid, dim3(lanes), stream, a, shift);
+    const int64_t grid = (units + 7) / 8 * 8 * 2 * a.heads;
+    if (a.rotary % 16) return launch_many(k_cache_append<DIM, FP8, BF16, false, false>, grid, lanes, stream, a, shift);
     // us for 32771 tokens of 8 heads of 128 (134 MB) ordinary / as a stream: 45.1 / 42.3; for 4096 tokens 8.9 / 9.8
-    return beyond_cache(a.step.tokens * a.heads * DIM * 4) ? launch_kernel(k_cache_append<DIM, FP8, BF16, true, true>, grid, dim3(lanes), stream, a, shift)
-                                                           : launch_kernel(k_cache_append<DIM, FP8, BF16, true, false>, grid, dim3(lanes), stream, a, shift);
+    return beyond_cache(a.step.tokens * a.heads * DIM * 4) ? launch_many(k_cache_append<DIM, FP8, BF16, true, true>, grid, lanes, stream, a, shift)
+                                                           : launch_many(k_cache_append<DIM, FP8, BF16, true, false>, grid, lanes, stream, a, shift);
 }
 
 template <int DIM>

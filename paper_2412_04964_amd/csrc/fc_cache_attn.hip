@@ -697,7 +697,7 @@ hipError_t attend_rows(const CacheAttentionArgs &a, hipStream_t stream)
     const int shift = log2_int(a.cache.page);
     constexpr int kWaves = waves_of(DIM, ROW_TILES);
     const int64_t groups = (int64_t)a.step.sequences * a.row_blocks * a.heads;
-    const auto go = [&](auto *kernel, int64_t grid, int waves) { return launch_kernel(kernel, dim3((uint32_t)grid), dim3(64 * waves), stream, a, shift); };
+    const auto go = [&](auto *kernel, int64_t grid, int waves) { return launch_many(kernel, grid, 64 * waves, stream, a, shift); };
     if (!a.workgroups && a.splits == 1)
         return a.stream ? go(k_cache_attention<DIM, FP8, BF16, ROW_TILES, kWaves, kByContext, true>, groups, kWaves)
                         : go(k_cache_attention<DIM, FP8, BF16, ROW_TILES, kWaves, kByContext, false>, groups, kWaves);

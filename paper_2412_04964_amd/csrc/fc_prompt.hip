@@ -463,15 +463,15 @@ hipError_t prompt(const PromptArgs &a, hipStream_t stream)
     const int query_heads = a.heads * a.group;
     const int64_t wide = (a.tokens >> 7) + a.sequences, narrow = (a.tokens >> 5) + a.sequences;
     if (split_is_faster(a, wide, narrow))
-        return launch_kernel(k_prompt_attention<DIM, BF16, true, 32>, dim3((uint32_t)(narrow * query_heads)), dim3(512), stream, a, (int)narrow);
-    const dim3 grid((uint32_t)(wide * query_heads));
+        return launch_many(k_prompt_attention<DIM, BF16, true, 32>, narrow * query_heads, 512, stream, a, (int)narrow);
+    const int64_t grid = wide * query_heads;
     // Three workgroups on a compute unit, where there are two rounds of them and more; us for tiles of 64 / 32 tokens: 16384 tokens of 16 heads
     // of 128 (2064 workgroups) 966 / 951, 8191 packed ones of 40 heads (3000) 136 / 126, but 8 x 512 tokens of 32 heads (1280) 41.4 / 42.7, 8192 of
     // 8 heads (520) 164 / 197, 4096 (264) 72 / 94.  Heads of 64 have four workgroups with 64 tokens: 548 / 559.
     if constexpr (DIM == 128) {
-        if (wide * query_heads > 1536) return launch_kernel(k_prompt_attention<DIM, BF16, false, 32>, grid, dim3(256), stream, a, (int)wide);
+        if (wide * query_heads > 1536) return launch_many(k_prompt_attention<DIM, BF16, false, 32>, grid, 256, stream, a, (int)wide);
     }
-    return launch_kernel(k_prompt_attention<DIM, BF16, false, 64>, grid, dim3(256), stream, a, (int)wide);
+    return launch_many(k_prompt_attention<DIM, BF16, false, 64>, grid, 256, stream, a, (int)wide);
 }
 
 }  // namespace

@@ -123,10 +123,10 @@ template <bool BF16, bool INTERLEAVED>
 hipError_t rotary_pieces(const RotaryArgs &a, hipStream_t stream)
 {
     const int64_t lanes = a.tokens * a.heads * (a.dim / 16);
-    const dim3 grid((uint32_t)((lanes + 255) / 256));
+    const int64_t grid = (lanes + 255) / 256;
     const bool stream_x = beyond_cache(lanes * 32) && (INTERLEAVED || a.rotary == a.dim);
-    return stream_x ? launch_kernel(k_rotary<BF16, INTERLEAVED, true>, grid, dim3(256), stream, a, a.dim / 16)
-                    : launch_kernel(k_rotary<BF16, INTERLEAVED, false>, grid, dim3(256), stream, a, a.dim / 16);
+    return stream_x ? launch_many(k_rotary<BF16, INTERLEAVED, true>, grid, 256, stream, a, a.dim / 16)
+                    : launch_many(k_rotary<BF16, INTERLEAVED, false>, grid, 256, stream, a, a.dim / 16);
 }
 
 }  // namespace
@@ -134,7 +134,7 @@ hipError_t rotary_pieces(const RotaryArgs &a, hipStream_t stream)
 hipError_t launch_rotary_table(const double *frequencies, int64_t rows, int rotary, double magnitude, float *table, hipStream_t stream)
 {
     const int64_t lanes = rows * (rotary / 2);
-    return launch_kernel(k_rotary_table, dim3((uint32_t)((lanes + 255) / 256)), dim3(256), stream, frequencies, rows, rotary / 2, magnitude, table);
+    return launch_many(k_rotary_table, (lanes + 255) / 256, 256, stream, frequencies, rows, rotary / 2, magnitude, table);
 }
 
 hipError_t launch_rotary(const RotaryArgs &a, hipStream_t stream)
@@ -144,8 +144,8 @@ hipError_t launch_rotary(const RotaryArgs &a, hipStream_t stream)
         return a.interleaved ? rotary_pieces<false, true>(a, stream) : rotary_pieces<false, false>(a, stream);
     }
     const int64_t lanes = a.tokens * a.heads * (a.dim - a.rotary / 2);
-    const dim3 grid((uint32_t)((lanes + 255) / 256));
-    return a.bf16 ? launch_kernel(k_rotary_any<true>, grid, dim3(256), stream, a) : launch_kernel(k_rotary_any<false>, grid, dim3(256), stream, a);
+    const int64_t grid = (lanes + 255) / 256;
+    return a.bf16 ? launch_many(k_rotary_any<true>, grid, 256, stream, a) : launch_many(k_rotary_any<false>, grid, 256, stream, a);
 }
 
 }  // namespace fc

@@ -1,9 +1,13 @@
 """Attention operators without a GPU: argument checks of the C entry points, and the frequencies of scaled rotations."""
+import json
 import math
+import subprocess
+import sys
 
 import pytest
 
 import paper_2412_04964_amd as fc
+import launches
 
 P = 0x10000      # a fake, 16-byte aligned, non-NULL device address; never dereferenced
 
@@ -121,3 +125,63 @@ def test_scaled_frequencies():
         fc.rotary_frequencies(8, method="other")
     with pytest.raises(ValueError):
         fc.rotary_frequencies(8, method="bands", factor=2.0)
+
+
+_CHILD = """
+import ctypes, json, sys
+ctypes.CDLL(sys.argv[1], ctypes.RTLD_GLOBAL)
+L = ctypes.CDLL(sys.argv[2])
+L.fc_cache_attention_workspace_bytes.restype = ctypes.c_size_t
+for name, args in json.load(sys.stdin):
+    if name == "fc_cache_attention":
+        args[-2] = L.fc_cache_attention_workspace_bytes(*[ctypes.c_int64(args[i]) for i in (3, 19, 4, 5, 6, 20, 21)])
+    print("R", getattr(L, name)(*[ctypes.c_float(a) if isinstance(a, float) else ctypes.c_int64(a) for a in args]), flush=True)
+"""
+
+
+def launched(*calls):
+    """(return code, launches) of each call, where nothing runs and no address is followed (launches.py)"""
+    r = subprocess.run([sys.executable, "-c", _CHILD, launches._stand_in(), launches.LIB], input=json.dumps(calls), capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    out, seen = [], []
+    for line in r.stdout.splitlines():
+        if line.startswith("L "):
+            _, name, grid, block, _ = line.split()
+            seen.append((launches._readable(name), int(grid), int(block)))
+        else:
+            out.append((int(line[2:]), seen))
+            seen = []
+    return out
+
+
+def rotary_call(tokens, heads, dim, turned):
+    return "fc_rotary", [P, heads * dim, dim, P, 8, P, tokens, heads, dim, turned, 0, 0, 0, P, heads * dim, dim, 0]
+
+
+def append_call(tokens, heads, dim, page, sequences, longest):
+    return "fc_cache_append", [P, heads * dim, dim, P, heads * dim, dim, tokens, heads, dim, 0, 0, 0, 0, 0, 1, P, P, P, P, 1000, page, P, 1000, P, P, sequences, longest, 0]
+
+
+def cache_call(tokens, heads, group, dim, sequences, queries, longest, width=1000):
+    n = heads * group * dim
+    return "fc_cache_attention", [P, n, dim, tokens, heads, group, dim, 0, 1, P, P, P, P, 1000, 64, P, width, P, P, sequences, queries, longest, 0.1, P, n, dim, P, 0, 0]
+
+
+def prompt_call(tokens, heads, group, dim, sequences, longest):
+    n = heads * group * dim
+    return "fc_prompt_attention", [P, n, dim, P, heads * dim, dim, P, heads * dim, dim, tokens, heads, group, dim, 0, P, sequences, longest, 1, 0.1, P, n, dim, 0]
+
+
+def test_calls_are_launched_up_to_what_the_runtime_takes():
+    fine = [rotary_call(1 << 20, 64, 128, 128), rotary_call((1 << 29) - 64, 1, 128, 128), rotary_call(1 << 20, 60, 80, 24),
+            append_call(1 << 22, 64, 64, 16, 1, 1 << 22), append_call(1 << 16, 128, 256, 64, 1 << 16, 1),
+            cache_call(1 << 18, 8, 16, 128, 1, 1 << 18, 1 << 18), cache_call(1 << 20, 8, 16, 128, 4, 1 << 18, 1 << 18),
+            cache_call(1 << 19, 8, 16, 128, 1 << 19, 1, 300), cache_call(4096, 8, 8, 64, 4096, (1 << 31) - 1, 300), cache_call(1 << 20, 16, 1, 64, 1 << 20, 1, 1 << 15, 1),
+            prompt_call(1 << 22, 8, 8, 128, 1, 1 << 22), prompt_call(1 << 24, 8, 8, 64, 1 << 14, 1024)]
+    for call, (rc, seen) in zip(fine, launched(*fine)):
+        assert rc == 0 and seen, (call, rc, seen)
+    # one step more than is launched is refused before anything is
+    for call, (rc, seen) in zip(fine, launched(rotary_call(1 << 29, 1, 128, 128), rotary_call(1 << 26, 1, 80, 24), append_call(1 << 30, 64, 256, 16, 1, 1 << 30),
+                                               append_call(1 << 30, 16, 256, 64, 1 << 30, 1), cache_call(1 << 28, 64, 16, 64, 1 << 28, 1, 300),
+                                               prompt_call((1 << 31) - 1, 1, 1, 64, 1, 1 << 30), prompt_call(1 << 30, 64, 1, 64, 1, 1 << 30))):
+        assert rc == -4 and not seen, (rc, seen)

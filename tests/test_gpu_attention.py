@@ -873,6 +873,21 @@ def test_large_calls_equal_their_parts(fc):
         assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
 
 
+def test_rotary_of_more_than_32_bits_of_elements(fc):
+    # 2^32 elements and more: the last tokens of a call equal a call of them alone
+    tokens, heads, dim = (1 << 20) + 5, 64, 64
+    x = torch.empty((tokens, heads, dim), dtype=F16, device="cuda")
+    x[-64:] = torch.randn((64, heads, dim), generator=gen(1)).to(F16).cuda()
+    x[:64] = x[-64:]
+    for turned_part, interleaved in ((64, False), (12, True)):
+        table = fc.rotary_table(100, fc.rotary_frequencies(turned_part))
+        positions = (torch.arange(tokens, device="cuda") % 100).to(torch.int32)
+        y = fc.rotary(x, table, positions, interleaved)
+        for part in (slice(0, 64), slice(tokens - 64, tokens)):
+            assert same(y[part], fc.rotary(x[part], table, positions[part], interleaved))
+        del y
+
+
 # ---- the layer ----
 
 @pytest.mark.parametrize("quantizer,bound", [(SYM, 0.06), (FP8, 0.09)])
