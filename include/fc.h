@@ -304,7 +304,11 @@ FC_API int fc_allreduce_sim_rot(const void *x_f16, int n_src, int64_t tokens, in
  *
  * Activations are 16-bit (`type`: FC_TYPE_F16 or FC_TYPE_BF16) tensors [tokens, heads, dim] whose last axis is dense; token and head
  * strides are in elements, any multiple of 8 (views of a joint projection pass as they are), base pointers are 16-byte
- * aligned.  Arithmetic and sums are in fp32.
+ * aligned.  Arithmetic and sums are in fp32, except that the two attention calls round what goes into their matrix products to 16 bits:
+ *     over the cache    softmax weights times their pages' scales to binary16: 11 bits for what is less than 2^26 below a row's largest,
+ *                       what is 2^37 below may be lost; bfloat16 queries to binary16 after a power of two per row
+ *     over prompts      softmax weights to `type`; binary16: 11 bits for what is less than 2^9 below the largest of 32 or 64 tokens
+ * The weights' sum is of the unrounded ones.
  *
  * Sequences are packed: the call's new tokens of sequence b are offsets[b] <= t < offsets[b + 1] (int32 [sequences + 1], offsets[0] = 0,
  * ascending, offsets[sequences] = tokens; equal neighbours: nothing new).  All index arrays are device memory; the kernels

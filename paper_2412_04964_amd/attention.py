@@ -116,12 +116,14 @@ def rotary_frequencies(rotary: int, base: float = 10000.0, method: str = "none",
                        low: float = 1.0, high: float = 4.0):
     """float64 [rotary / 2] on the host: the angles by which a pair turns per position, base^(-2 i / rotary), for contexts `factor`
     times as long as trained:
-      "linear"  every frequency divided by factor
-      "base"    base times factor^(rotary / (rotary - 2)): the slowest pair gets factor, the fastest none
+      "linear"  every frequency divided by factor (position interpolation: Chen et al. 2023, arXiv 2306.15595)
+      "base"    base times factor^(rotary / (rotary - 2)): the slowest pair gets factor, the fastest none (NTK-aware scaling, as
+                described by Peng et al. 2023, arXiv 2309.00071)
       "bands"   pairs with at most `low` turns in the `original` context divided by factor, those with `high` and more unchanged,
-                in between by a mix that is linear in the number of turns
+                in between by a mix that is linear in the number of turns (NTK-by-parts, the same paper)
       "ramp"    the same with a mix that is linear in the pair's index, between the indices where a pair has `high` and `low` turns
-                (rounded outwards); goes with a magnitude of 0.1 ln(factor) + 1"""
+                (rounded outwards, as published models compute it); goes with a magnitude of 0.1 ln(factor) + 1 (YaRN, the same paper)
+    Checked against these formulas, not against another implementation's output."""
     torch = _torch()
     if rotary < 2 or rotary % 2 or factor <= 0 or base <= 1:
         raise ValueError("rotary must be even and positive, factor positive and base above 1")

@@ -69,7 +69,9 @@ struct CacheAttentionArgs {
     Rows q, out;
     Step step;
     Cache cache;
-    float *partial;            // [workgroups, 2, rows, dim] sums, then [workgroups, 2, rows, 2] maxima and weights
+    // [places, dim] sums, then [places, 2] maxima and weights.  Places: [workgroups, 2, rows of a workgroup] of equal ranges (see the join);
+    // [tokens, query heads, splits] of pieces
+    float *partial;
     float scale;
     int heads, group, dim, fp8, bf16;
     // cache_attention_plan's: 16-row tiles that a workgroup takes; workgroups that share all sequences' contexts evenly, or 0: one for each
@@ -166,7 +168,7 @@ __device__ __forceinline__ floatx4 mma16(uintx4 a, uintx4 b, floatx4 c)
 
 // 16 bytes per lane from memory to lds + 16 lane.  Not the builtin: the compiler would make LDS reads of what has arrived wait for what is
 // on its way.  Who reads it waits for vmcnt himself, and has read what was there before.  (A wait state between the write of m0, which
-// nothing else in these kernels has a value in, and its use.)  STREAM: marked as read once.
+// the compiler keeps nothing in, and its use.)  m0 holds the address: the kernels go up to 128 KB (prompts, split tokens).  STREAM: marked as read once.
 template <bool STREAM>
 __device__ __forceinline__ void load_to_lds(uintx4 rsrc, int offset, uint32_t lds)
 {

@@ -153,7 +153,7 @@ template <int DIM> constexpr int kTileBytes = kTile * DIM;
 template <int DIM> __device__ __forceinline__ constexpr int swizzle(int row) { return row / (256 / DIM) & (DIM / 16 - 1); }
 
 // The rows of a sequence's queries and the heads that share K and V, 16 ROW_TILES of them at a time.  RANGES: a workgroup has a range of
-// all units, as described at ranges_of; else a block of rows of one sequence and head, from its first token to its last.
+// all units (Ranges); else a block of rows of one sequence and head, from its first token to its last.
 template <int DIM, bool FP8, bool BF16, int ROW_TILES, int WAVES, int FORM, bool STREAM>
 __global__ void __launch_bounds__(64 * WAVES, FORM != kByContext || DIM == 256 || ROW_TILES > 1 ? 2 : 4) k_cache_attention(CacheAttentionArgs a, int page_shift)
 {
@@ -231,7 +231,6 @@ __global__ void __launch_bounds__(64 * WAVES, FORM != kByContext || DIM == 256 |
     __shared__ float join_max[WAVES][16], join_sum[WAVES][16];
     float(*join)[16][DIM + 4] = reinterpret_cast<float(*)[16][DIM + 4]>(stages);       // [WAVES / 2], when the stages are done with
     static_assert(sizeof(stages) >= sizeof(float) * WAVES / 2 * 16 * (DIM + 4), "the wavefronts' sums fit the stages");
-    static_assert(sizeof(stages) <= 65536, "m0 has 16 bits of an LDS address");
     // this lane's places: of the pieces that it brings to a tile, and of its operands in one
     constexpr int kPieces = kTileBytes<DIM> / 1024, kPieceRows = 1024 / DIM;
     int bring_at[kPieces];

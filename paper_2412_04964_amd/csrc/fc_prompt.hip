@@ -116,8 +116,8 @@ __global__ void __launch_bounds__(SPLIT ? 512 : 256, SPLIT || TOKENS == 64 ? 2 :
         head = blockIdx.x % query_heads;
         unit = units - 1 - blockIdx.x / query_heads;
     }
-    // late rows, which see most, come first; where all workgroups are on the chip at once, the second ones on a compute unit go from early rows
-    // to late ones, so that the longest run beside the shortest (8192 tokens of 8 heads 165 -> 157 us)
+    // late rows, which see most, come first; where (nearly) all workgroups are on the chip at once, two on a compute unit, the second ones
+    // go from early rows to late ones, so that the longest run beside the shortest (8192 tokens of 8 heads, 520 workgroups, 165 -> 157 us)
     if (!SPLIT && units * query_heads > 256 && units * query_heads <= 640) {
         const int u = units - 1 - unit, once = 256 / query_heads;
         if (u >= once) unit = u - once;
