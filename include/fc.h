@@ -385,8 +385,8 @@ FC_API int fc_cache_attention(const void *q, int64_t q_token_stride, int64_t q_h
 /*
  * Attention of whole prompts to themselves: query i of a sequence sees all its tokens, or causal != 0: those up to i.
  * q, out: [tokens, heads * group, dim]; k, v: [tokens, heads, dim]; dim in {64, 128}; token strides of k and v below 2^25.
- * longest: the most tokens of a sequence; it only chooses the form of the launch.  Causal rows depend on nothing of later tokens,
- * infinities and NaN among them included.
+ * longest: the most tokens of a sequence; it only chooses the form of the launch.  No bit of a causal row depends on later tokens,
+ * infinities and NaN among them included.  bfloat16: 2^8 times the tokens' |v| together must stay within fp32.
  */
 FC_API int fc_prompt_attention(const void *q, int64_t q_token_stride, int64_t q_head_stride, const void *k, int64_t k_token_stride,
                                int64_t k_head_stride, const void *v, int64_t v_token_stride, int64_t v_head_stride, int64_t tokens,

@@ -13,7 +13,7 @@
 // workgroups by a second kernel through the workspace (cache_attention_plan says which contexts are, and how).
 // Memory bounds large batches: 2 bytes per token, head and element against 2 multiply-adds for each query head.  64 x 8 contexts of up to
 // 8192 tokens, 807 MB: 138 us, 5.9 TB/s, where a bare stream of such pieces reaches 6.8.  Few requests are bound by latency: 8 of 1536 tokens
-// 11.7 us, two launches and in each a chain of three reads; a lone step of a wavefront takes 1.2 us for its 250 to 340 vector instructions.
+// 11.7 us, two launches and in each a chain of three reads; a lone step of a wavefront takes 1.2 us for its 250 to 350 vector instructions.
 #include "fc_attn.hpp"
 
 namespace fc {

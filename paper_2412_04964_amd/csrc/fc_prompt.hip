@@ -10,9 +10,9 @@
 //   range for all that are lower, so it is raised only, and when a score passes it by kSlack.  Binary16 has not: the unit follows a tile's
 //   largest score up and down when that is kSlack away, and the largest is put at 2^kBias, so that a tile's weights have 11 bits
 //   down to 2^-9 of its largest however far that is below the row's (down to 2^-kReach, where they are lost).
-// Matrix instructions and the exponentials between them bound it, at a clock that falls under this load (1.4 to 1.7 GHz counted):
-// 16384 tokens, 16 heads, causal, bfloat16: 941 to 1021 us, 1.17 to 1.08 PFLOP/s, where a library's 16384^3 product reaches 1.31.
-// 11 ragged prompts, 8191 tokens, 40 heads, binary16: 126 us, where edges and what surrounds the loop weigh more.
+// Matrix instructions and the exponentials between them bound it, at a clock that falls under this load (1.5 to 1.7 GHz counted):
+// 16384 tokens, 16 heads, causal, bfloat16: 965 to 1036 us by card, 1.14 to 1.06 PFLOP/s, where a library's 16384^3 product reaches 1.31.
+// 11 ragged prompts, 8191 tokens, 40 heads, binary16: 129 to 136 us, where edges and what surrounds the loop weigh more.
 #include "fc_attn.hpp"
 
 namespace fc {
@@ -446,8 +446,8 @@ __global__ void __launch_bounds__(SPLIT ? 512 : 256, SPLIT || TOKENS == 64 ? 2 :
 // Whether workgroups of 32 rows whose wavefronts split the tokens are faster than those of 128 rows, by what both were measured to take
 // in tenths of a microsecond.  128 rows: as long as the longest sequence's last rows, 1.1 us (0.8 with heads of 64) for 64 tokens, while
 // no more than two workgroups share a compute unit.  32 rows: rounds of one workgroup (two) a compute unit, 3.2 us and 1.5 us for 256
-// tokens each.  us, 8 heads of 128, causal, 128 / 32 rows: 1024 tokens 24.2 / 12.8, 2048 41.9 / 25.5, 4096 77.2 / 68.7, 8192 172 / 219;
-// 16 heads, 2048 tokens 42.9 / 48.6; 8 sequences of 1024 tokens 47.0 / 87.3.
+// tokens each.  us, 8 heads of 128, causal, 128 / 32 rows: 1024 tokens 22.6 / 13.0, 2048 39.4 / 25.8, 4096 72.7 / 69.4, 8192 163 / 221;
+// 16 heads, 2048 tokens 40.3 / 49.5; 8 sequences of 1024 tokens 44.0 / 88.3.
 bool split_is_faster(const PromptArgs &a, int64_t wide, int64_t narrow)
 {
     const int64_t heads = a.heads * a.group, longest = a.longest < a.tokens ? a.longest : a.tokens;
@@ -466,8 +466,8 @@ hipError_t prompt(const PromptArgs &a, hipStream_t stream)
         return launch_many(k_prompt_attention<DIM, BF16, true, 32>, narrow * query_heads, 512, stream, a, (int)narrow);
     const int64_t grid = wide * query_heads;
     // Three workgroups on a compute unit, where there are two rounds of them and more; us for tiles of 64 / 32 tokens: 16384 tokens of 16 heads
-    // of 128 (2064 workgroups) 966 / 951, 8191 packed ones of 40 heads (3000) 136 / 126, but 8 x 512 tokens of 32 heads (1280) 41.4 / 42.7, 8192 of
-    // 8 heads (520) 164 / 197, 4096 (264) 72 / 94.  Heads of 64 have four workgroups with 64 tokens: 548 / 559.
+    // of 128 (2064 workgroups) 1003 / 999, 8191 packed ones of 40 heads (2960) 138 / 130, but 8192 of 8 heads (520) 162 / 190, 4096 (264) 73 / 94;
+    // 8 x 512 tokens of 32 heads (1280) 42 / 40.  Heads of 64 have four workgroups with 64 tokens.
     if constexpr (DIM == 128) {
         if (wide * query_heads > 1536) return launch_many(k_prompt_attention<DIM, BF16, false, 32>, grid, 256, stream, a, (int)wide);
     }
