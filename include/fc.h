@@ -317,6 +317,7 @@ FC_API int fc_allreduce_sim_rot(const void *x_f16, int n_src, int64_t tokens, in
  */
 #define FC_TYPE_F16 0
 #define FC_TYPE_BF16 1
+#define FC_TYPE_F32 2         /* the weight of a norm only */
 
 /*
  * The table of a rotation: for row r and pair i < rotary / 2, with angle = r * frequencies[i] in 64 bits,
@@ -392,6 +393,76 @@ FC_API int fc_prompt_attention(const void *q, int64_t q_token_stride, int64_t q_
                                int64_t k_head_stride, const void *v, int64_t v_token_stride, int64_t v_head_stride, int64_t tokens,
                                int heads, int group, int dim, int type, const int32_t *offsets, int sequences, int64_t longest, int causal,
                                float scale, void *out, int64_t out_token_stride, int64_t out_head_stride, void *hip_stream);
+
+/*
+ * ---- The cache's pages when sequences fork, grow, end, and move together ----
+ *
+ * page_table, held: as above.  uses: int32 [pages], in how many rows of the table a page is named; 0 is a free page.  An entry outside
+ * [0, pages) is no page.  A page that is not full of a sequence's tokens, and those reserved beyond them, are not shared but as
+ * fc_pages_fork leaves them.  Everything is decided on the device, in whole numbers that do not depend on the order of execution.  Where a
+ * model has a cache for each layer, tables and counts are common to them and fc_cache_copy is called for each.
+ *
+ * fc_pages_fork makes the table of the next step: its row b is what row parents[b] of the old one holds, the first ceil(held / page)
+ * entries, and -1 behind them; a parent outside [0, sequences) gives an empty row (held 0).  So rows are kept, copied (they share their
+ * pages, the partly filled one included), reordered and dropped at once, and their number may change.  uses gains what the new table
+ * names and loses what the old one named.  page_table_out [rows, table_width], held_out [rows]: not the old ones.
+ */
+FC_API int fc_pages_fork(const int32_t *page_table, const int32_t *held, int sequences, int table_width, int page, int32_t *uses, int64_t pages,
+                         const int32_t *parents, int rows, int32_t *page_table_out, int32_t *held_out, void *hip_stream);
+
+/*
+ * Pages for the step's tokens (offsets, held as for fc_cache_append, before it): every slot that they go to and that has no page gets one;
+ * a partly filled page that is named elsewhere too gives way to a fresh one, into which fc_cache_copy copies it: source[b] -> target[b]
+ * (int32 [sequences], -1 and -1 where there is nothing to copy).  If all rows that name such a page write to it, the last one keeps it.
+ * Fresh pages are the lowest-numbered free ones, handed out by row, then slot; uses follows.  Slots beyond table_width are left out.
+ * lacking: int32 [1], how many free pages are missing; if that is not 0, table and uses are as they were and nothing is to be copied.
+ * workspace: fc_pages_reserve_workspace_bytes(pages) bytes, 16-byte aligned, contents unspecified.
+ */
+FC_API size_t fc_pages_reserve_workspace_bytes(int64_t pages);
+FC_API int fc_pages_reserve(int32_t *page_table, const int32_t *held, const int32_t *offsets, int sequences, int table_width, int page,
+                            int32_t *uses, int64_t pages, int32_t *source, int32_t *target, int32_t *lacking, void *workspace,
+                            size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Moves the U pages in use (uses > 0) to numbers below U: the k-th free page below U, ascending, takes the k-th used page from U on,
+ * source[k] -> target[k] (int32 [pages / 2], -1 behind the last), for fc_cache_copy.  page_table_out, uses_out: table and counts
+ * afterwards; the table may be written in place, the counts not.  used: int32 [1], U.  Entries that name no page in use stay.
+ * workspace: fc_pages_compact_workspace_bytes(pages) bytes, 16-byte aligned, contents unspecified.
+ */
+FC_API size_t fc_pages_compact_workspace_bytes(int64_t pages);
+FC_API int fc_pages_compact(const int32_t *page_table, int64_t sequences, int table_width, const int32_t *uses, int64_t pages,
+                            int32_t *page_table_out, int32_t *uses_out, int32_t *source, int32_t *target, int32_t *used, void *workspace,
+                            size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Copies pages of a cache: page target[i] becomes page source[i], codes and scales of keys and values.  Pairs with a page outside
+ * [0, pages) are left out.  No page is a target twice, or both a target and a source (what such a page holds is unspecified).
+ */
+FC_API int fc_cache_copy(void *k_cache, void *v_cache, float *k_scales, float *v_scales, int64_t pages, int heads, int page, int dim,
+                         const int32_t *source, const int32_t *target, int64_t count, void *hip_stream);
+
+/*
+ * ---- The norm behind an all-reduce, with the residual's addition ----
+ *
+ * x, residual, sum, y: 16-bit rows [tokens, hidden], dense but for the row stride (elements, a multiple of 8), 16-byte aligned; hidden a multiple
+ * of 8 up to 32768.  residual may be NULL (nothing is added), sum too (x + residual is not kept).  weight [hidden]: of weight_type, which is
+ * type or FC_TYPE_F32.  eps positive and finite.  sum and y may be x or residual where their strides are equal; otherwise nothing overlaps.
+ * Results are bit-identical, except where two correctly rounded 64-bit sums of the squares differ, to
+ *     h   = x + residual                          fp32;  sum = h rounded to the type
+ *     d   = fp32(1 / sqrt(sum of h * h / hidden + eps))          squares, sum, divides and root in 64 bits
+ *     y   = (h * d) * weight                      fp32, then rounded to the type
+ * or, as fc_quantize_sym (8 bit) and fc_quantize_fp8 have them, codes [tokens, hidden] and scales [tokens, hidden / group] of y in fp32:
+ *     s   = max|y| / top    over the group; if !(s >= FLT_MIN): s = 1;  top 127 or 448
+ *     q   = round(y * (1 / s))                    IEEE divides, ties to even
+ * group: a power of two in [32, 16384] that divides hidden, or hidden itself (one scale a token, any hidden).  quantizer: FC_QUANTIZER_SYM, _FP8.
+ * Inputs that are not finite give unspecified codes.
+ */
+FC_API int fc_rms_norm(const void *x, int64_t x_stride, const void *residual, int64_t residual_stride, const void *weight, int weight_type,
+                       int64_t tokens, int hidden, double eps, int type, void *sum, int64_t sum_stride, void *y, int64_t y_stride,
+                       void *hip_stream);
+FC_API int fc_rms_norm_quantize(const void *x, int64_t x_stride, const void *residual, int64_t residual_stride, const void *weight,
+                                int weight_type, int64_t tokens, int hidden, double eps, int type, int group, int quantizer, void *sum,
+                                int64_t sum_stride, void *codes, float *scales, void *hip_stream);
 
 /* Static, NUL-terminated description of an FC_* code.  Host pointer, never NULL. */
 FC_API const char *fc_strerror(int code);

@@ -52,6 +52,8 @@ from .attention import (  # noqa: F401
     rotary_frequencies,
     rotary_table,
 )
+from .norm import rms_norm, rms_norm_quantize  # noqa: F401
+from .pages import cache_copy, pages_compact, pages_fork, pages_reserve  # noqa: F401
 
 __all__ = [
     "QUANTIZER_ASYM", "QUANTIZER_FP8", "QUANTIZER_SYM", "allreduce_sim_rot", "dequantize_rot", "quantize_rot",
@@ -62,5 +64,6 @@ __all__ = [
     "quantize_sym", "strerror", "version",
     "cache_append", "cache_attention", "cache_attention_workspace_bytes", "prompt_attention", "rotary",
     "rotary_frequencies", "rotary_table",
+    "cache_copy", "pages_compact", "pages_fork", "pages_reserve", "rms_norm", "rms_norm_quantize",
     "allreduce_sim_cmeta", "dequant_reduce_requant_cmeta", "dequantize_cmeta", "quantize_cmeta",
 ]

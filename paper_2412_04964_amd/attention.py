@@ -93,8 +93,8 @@ def _step(offsets, held=None):
     return n
 
 
-def _cache(cache, pages, sequences):
-    """(heads, page, dim, number of pages, width of the page table) of a checked cache"""
+def _cache(cache, pages=None, sequences=0):
+    """(heads, page, dim, number of pages) of a checked cache, and the width of its page table if there is one"""
     torch = _torch()
     if len(cache) != 4:
         raise ValueError("cache must hold k_cache, v_cache, k_scales and v_scales")
@@ -105,6 +105,8 @@ def _cache(cache, pages, sequences):
     _shape(_dev(v, torch.uint8, "v_cache"), k.shape, "v_cache")
     _shape(_dev(ks, torch.float32, "k_scales"), k.shape[:2], "k_scales")
     _shape(_dev(vs, torch.float32, "v_scales"), k.shape[:2], "v_scales")
+    if pages is None:
+        return k.shape[1], k.shape[2], k.shape[3], k.shape[0]
     _dev(pages, torch.int32, "pages")
     if pages.dim() != 2:
         raise ValueError("pages must be int32 [sequences, width], got shape %s" % (tuple(pages.shape),))

@@ -118,6 +118,23 @@ def lib() -> ctypes.CDLL:
         L.fc_cache_attention.restype = i32
         L.fc_prompt_attention.argtypes = [*rows, *rows, *rows, i64, i32, i32, i32, i32, vp, i32, i64, i32, f32, *rows, vp]
         L.fc_prompt_attention.restype = i32
+        L.fc_pages_fork.argtypes = [vp, vp, i32, i32, i32, vp, i64, vp, i32, vp, vp, vp]
+        L.fc_pages_fork.restype = i32
+        L.fc_pages_reserve_workspace_bytes.argtypes = [i64]
+        L.fc_pages_reserve_workspace_bytes.restype = sz
+        L.fc_pages_reserve.argtypes = [vp, vp, vp, i32, i32, i32, vp, i64, vp, vp, vp, vp, sz, vp]
+        L.fc_pages_reserve.restype = i32
+        L.fc_pages_compact_workspace_bytes.argtypes = [i64]
+        L.fc_pages_compact_workspace_bytes.restype = sz
+        L.fc_pages_compact.argtypes = [vp, i64, i32, vp, i64, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.fc_pages_compact.restype = i32
+        L.fc_cache_copy.argtypes = [vp, vp, vp, vp, i64, i32, i32, i32, vp, vp, i64, vp]
+        L.fc_cache_copy.restype = i32
+        row = [vp, i64]                                  # a tensor [tokens, hidden]: address, row stride
+        L.fc_rms_norm.argtypes = [*row, *row, vp, i32, i64, i32, f64, i32, *row, *row, vp]
+        L.fc_rms_norm.restype = i32
+        L.fc_rms_norm_quantize.argtypes = [*row, *row, vp, i32, i64, i32, f64, i32, i32, i32, *row, vp, vp, vp]
+        L.fc_rms_norm_quantize.restype = i32
         L.fc_strerror.argtypes = [i32]
         L.fc_strerror.restype = ctypes.c_char_p
         L.fc_last_hip_error.argtypes = []

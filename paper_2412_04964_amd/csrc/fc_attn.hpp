@@ -92,6 +92,52 @@ struct PromptArgs {
 };
 hipError_t launch_prompt_attention(const PromptArgs &a, hipStream_t stream);
 
+// The norm of rows [tokens, hidden]; strides in elements
+struct NormArgs {
+    const void *x, *residual, *weight;                  // residual may be null
+    void *sum, *y;                                      // sum may be null; y: 16-bit rows, or codes
+    float *scales;
+    int64_t x_row, residual_row, sum_row, y_row, tokens;
+    double eps;
+    int hidden, group, codes, bf16, weight_f32;         // codes: 0 for 16 bits, or kSigned, kE4M3
+};
+enum { kWide16 = 0, kSigned = 1, kE4M3 = 2 };
+hipError_t launch_rms_norm(const NormArgs &a, hipStream_t stream);
+
+// Page tables [sequences, width], pages in use by count, and the pairs of pages that a call has copied
+struct ForkArgs {
+    const int32_t *table, *held, *parents;
+    int32_t *uses, *table_out, *held_out;
+    int64_t pages;
+    int sequences, rows, width, page;                   // rows: of the new table
+};
+hipError_t launch_pages_fork(const ForkArgs &a, hipStream_t stream);
+
+struct ReserveArgs {
+    int32_t *table, *uses, *source, *target, *lacking, *fresh;        // fresh: [pages], scratch
+    const int32_t *held, *offsets;
+    int64_t pages;
+    int sequences, width, page;
+};
+hipError_t launch_pages_reserve(const ReserveArgs &a, hipStream_t stream);
+
+struct CompactArgs {
+    const int32_t *table, *uses;
+    int32_t *table_out, *uses_out, *source, *target, *used, *counts, *rank;        // counts, rank: scratch
+    int64_t pages, entries;                             // entries: of the table
+};
+constexpr int kSegment = 4096;                          // pages that a workgroup counts
+hipError_t launch_pages_compact(const CompactArgs &a, hipStream_t stream);
+
+struct CopyArgs {
+    uint8_t *k, *v;
+    float *k_scales, *v_scales;
+    const int32_t *source, *target;
+    int64_t pages, count, bytes;                        // bytes: of a page in one of the caches
+    int heads;
+};
+hipError_t launch_cache_copy(const CopyArgs &a, hipStream_t stream);
+
 #if defined(__HIPCC__)
 
 typedef _Float16 half2 __attribute__((ext_vector_type(2)));
@@ -147,6 +193,27 @@ template <bool BF16>
 __device__ __forceinline__ uintx4 narrow8(const float (&f)[8])
 {
     return uintx4{narrow2<BF16>(f[0], f[1]), narrow2<BF16>(f[2], f[3]), narrow2<BF16>(f[4], f[5]), narrow2<BF16>(f[6], f[7])};
+}
+
+// what the largest magnitude of a scale's values becomes
+template <bool FP8> constexpr float kTop = FP8 ? 448.0f : 127.0f;
+
+// 4 values -> codes.  Signed codes: 1.5 * 2^23 added to a value in (-2^22, 2^22) leaves it, rounded to nearest even, in the low bits.
+// CLAMP: a value may be beyond the codes; those of x * (1 / s') with |x| <= top * s' round to at most top.
+template <bool FP8, bool CLAMP = false>
+__device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d)
+{
+    if constexpr (FP8) {
+        const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+        return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true);
+    } else {
+        const auto one = [](float v) {
+            if constexpr (CLAMP) v = fminf(fmaxf(v, -127.0f), 127.0f);
+            return __builtin_bit_cast(uint32_t, v + 12582912.0f);
+        };
+        const uint32_t ab = __builtin_amdgcn_perm(one(b), one(a), 0x0C0C0400u), cd = __builtin_amdgcn_perm(one(d), one(c), 0x04000C0Cu);
+        return ab | cd;
+    }
 }
 
 // D[32][32] += A[32][16] B[16][32].  Lane l holds row (A) or column (B) l % 32, contraction indices 8 (l / 32) + 0..7; of the result

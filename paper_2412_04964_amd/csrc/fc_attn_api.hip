@@ -57,6 +57,40 @@ int check_attention(int64_t tokens, int sequences, int heads, int group, int dim
     return queries < 1 || queries > kMaxTokens || longest < 1 || longest > kMaxTokens ? FC_ERR_SHAPE : FC_OK;
 }
 
+int check_pages(int64_t pages, int page, int table_width)
+{
+    return (page != 16 && page != 32 && page != 64) || pages < 1 || pages > kMaxTokens || table_width < 1 ? FC_ERR_SHAPE : FC_OK;
+}
+
+// what both forms of the norm take; with tokens == 0 no pointer is looked at
+int check_norm(const void *x, int64_t x_stride, const void *residual, int64_t residual_stride, const void *weight, int weight_type, int64_t tokens,
+               int hidden, double eps, int type, void *sum, int64_t sum_stride, fc::NormArgs *a)
+{
+    if (check_type(type) != FC_OK || (weight_type != type && weight_type != FC_TYPE_F32)) return FC_ERR_TYPE;
+    if (tokens < 0 || tokens > kMaxTokens || hidden < 8 || hidden % 8 || hidden > 32768 || !(eps > 0.0 && eps <= DBL_MAX)) return FC_ERR_SHAPE;
+    *a = {};
+    if (tokens == 0) return FC_OK;
+    if (!weight) return FC_ERR_NULL;
+    int rc = check_rows(x, x_stride, 0);
+    if (rc != FC_OK || (residual && (rc = check_rows(residual, residual_stride, 0)) != FC_OK)) return rc;
+    if (sum && (rc = check_rows(sum, sum_stride, 0)) != FC_OK) return rc;
+    if (!aligned16(weight)) return FC_ERR_ALIGN;
+    a->x = x;
+    a->residual = residual;
+    a->weight = weight;
+    a->sum = sum;
+    a->x_row = x_stride;
+    a->residual_row = residual_stride;
+    a->sum_row = sum_stride;
+    a->tokens = tokens;
+    a->eps = eps;
+    a->hidden = hidden;
+    a->group = hidden;
+    a->bf16 = type == FC_TYPE_BF16;
+    a->weight_f32 = weight_type == FC_TYPE_F32;
+    return FC_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -221,6 +255,142 @@ int fc_prompt_attention(const void *q, int64_t q_token_stride, int64_t q_head_st
     a.causal = causal != 0;
     a.bf16 = type == FC_TYPE_BF16;
     return result(fc::launch_prompt_attention(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+// ---- the cache's pages ----
+
+int fc_pages_fork(const int32_t *page_table, const int32_t *held, int sequences, int table_width, int page, int32_t *uses, int64_t pages,
+                  const int32_t *parents, int rows_, int32_t *page_table_out, int32_t *held_out, void *hip_stream)
+{
+    const int rc = check_pages(pages, page, table_width);
+    if (rc != FC_OK) return rc;
+    if (sequences < 0 || rows_ < 0) return FC_ERR_SHAPE;
+    if (sequences == 0 && rows_ == 0) return FC_OK;
+    if (!uses || (sequences && (!page_table || !held)) || (rows_ && (!parents || !page_table_out || !held_out))) return FC_ERR_NULL;
+    fc::ForkArgs a;
+    a.table = page_table;
+    a.held = held;
+    a.parents = parents;
+    a.uses = uses;
+    a.table_out = page_table_out;
+    a.held_out = held_out;
+    a.pages = pages;
+    a.sequences = sequences;
+    a.rows = rows_;
+    a.width = table_width;
+    a.page = page;
+    return result(fc::launch_pages_fork(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+size_t fc_pages_reserve_workspace_bytes(int64_t pages) { return pages < 1 || pages > kMaxTokens ? 0 : (size_t)pages * sizeof(int32_t); }
+
+int fc_pages_reserve(int32_t *page_table, const int32_t *held, const int32_t *offsets, int sequences, int table_width, int page, int32_t *uses,
+                     int64_t pages, int32_t *source, int32_t *target, int32_t *lacking, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    const int rc = check_pages(pages, page, table_width);
+    if (rc != FC_OK) return rc;
+    if (sequences < 0) return FC_ERR_SHAPE;
+    if (!uses || !offsets || !lacking || (sequences && (!page_table || !held || !source || !target))) return FC_ERR_NULL;
+    if (!workspace || workspace_bytes < fc_pages_reserve_workspace_bytes(pages)) return FC_ERR_WORKSPACE;
+    if (!aligned16(workspace)) return FC_ERR_ALIGN;
+    fc::ReserveArgs a;
+    a.table = page_table;
+    a.uses = uses;
+    a.source = source;
+    a.target = target;
+    a.lacking = lacking;
+    a.fresh = static_cast<int32_t *>(workspace);
+    a.held = held;
+    a.offsets = offsets;
+    a.pages = pages;
+    a.sequences = sequences;
+    a.width = table_width;
+    a.page = page;
+    return result(fc::launch_pages_reserve(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+size_t fc_pages_compact_workspace_bytes(int64_t pages)
+{
+    return pages < 1 || pages > kMaxTokens ? 0 : (size_t)(pages + (pages + fc::kSegment - 1) / fc::kSegment) * sizeof(int32_t);
+}
+
+int fc_pages_compact(const int32_t *page_table, int64_t sequences, int table_width, const int32_t *uses, int64_t pages, int32_t *page_table_out,
+                     int32_t *uses_out, int32_t *source, int32_t *target, int32_t *used, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    if (pages < 1 || pages > kMaxTokens || table_width < 1 || sequences < 0 || sequences > kMaxTokens) return FC_ERR_SHAPE;
+    if (!uses || !uses_out || !used || (pages > 1 && (!source || !target)) || (sequences && (!page_table || !page_table_out))) return FC_ERR_NULL;
+    if (!workspace || workspace_bytes < fc_pages_compact_workspace_bytes(pages)) return FC_ERR_WORKSPACE;
+    if (!aligned16(workspace)) return FC_ERR_ALIGN;
+    fc::CompactArgs a;
+    a.table = page_table;
+    a.uses = uses;
+    a.table_out = page_table_out;
+    a.uses_out = uses_out;
+    a.source = source;
+    a.target = target;
+    a.used = used;
+    a.rank = static_cast<int32_t *>(workspace);
+    a.counts = a.rank + pages;
+    a.pages = pages;
+    a.entries = sequences * table_width;
+    return result(fc::launch_pages_compact(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+int fc_cache_copy(void *k_cache, void *v_cache, float *k_scales, float *v_scales, int64_t pages, int heads, int page, int dim,
+                  const int32_t *source, const int32_t *target, int64_t count, void *hip_stream)
+{
+    const int rc = check_pages(pages, page, 1);
+    if (rc != FC_OK) return rc;
+    if (heads < 1 || heads > kMaxHeads || (dim != 64 && dim != 128 && dim != 256) || count < 0 || count > kMaxTokens) return FC_ERR_SHAPE;
+    if (count == 0) return FC_OK;
+    if (!k_cache || !v_cache || !k_scales || !v_scales || !source || !target) return FC_ERR_NULL;
+    if (!aligned16(k_cache) || !aligned16(v_cache)) return FC_ERR_ALIGN;
+    fc::CopyArgs a;
+    a.k = static_cast<uint8_t *>(k_cache);
+    a.v = static_cast<uint8_t *>(v_cache);
+    a.k_scales = k_scales;
+    a.v_scales = v_scales;
+    a.source = source;
+    a.target = target;
+    a.pages = pages;
+    a.count = count;
+    a.bytes = (int64_t)heads * page * dim;
+    a.heads = heads;
+    return result(fc::launch_cache_copy(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+// ---- the norm behind an all-reduce ----
+
+int fc_rms_norm(const void *x, int64_t x_stride, const void *residual, int64_t residual_stride, const void *weight, int weight_type, int64_t tokens,
+                int hidden, double eps, int type, void *sum, int64_t sum_stride, void *y, int64_t y_stride, void *hip_stream)
+{
+    fc::NormArgs a;
+    int rc = check_norm(x, x_stride, residual, residual_stride, weight, weight_type, tokens, hidden, eps, type, sum, sum_stride, &a);
+    if (rc != FC_OK || tokens == 0) return rc;
+    if ((rc = check_rows(y, y_stride, 0)) != FC_OK) return rc;
+    a.y = y;
+    a.y_row = y_stride;
+    a.codes = fc::kWide16;
+    return result(fc::launch_rms_norm(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+int fc_rms_norm_quantize(const void *x, int64_t x_stride, const void *residual, int64_t residual_stride, const void *weight, int weight_type,
+                         int64_t tokens, int hidden, double eps, int type, int group, int quantizer, void *sum, int64_t sum_stride, void *codes,
+                         float *scales, void *hip_stream)
+{
+    fc::NormArgs a;
+    int rc = check_code(quantizer);
+    if (rc != FC_OK) return rc;
+    if ((rc = check_norm(x, x_stride, residual, residual_stride, weight, weight_type, tokens, hidden, eps, type, sum, sum_stride, &a)) != FC_OK) return rc;
+    if (group != hidden && (group < 32 || group > 16384 || (group & (group - 1)) || hidden % group)) return FC_ERR_GROUP;
+    if (tokens == 0) return FC_OK;
+    if (!codes || !scales) return FC_ERR_NULL;
+    if (!aligned16(codes)) return FC_ERR_ALIGN;
+    a.y = codes;
+    a.scales = scales;
+    a.group = group;
+    a.codes = quantizer == FC_QUANTIZER_FP8 ? fc::kE4M3 : fc::kSigned;
+    return result(fc::launch_rms_norm(a, static_cast<hipStream_t>(hip_stream)));
 }
 
 }  // extern "C"

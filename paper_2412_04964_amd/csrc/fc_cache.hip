@@ -13,26 +13,6 @@
 namespace fc {
 namespace {
 
-template <bool FP8> constexpr float kTop = FP8 ? 448.0f : 127.0f;
-
-// 4 values -> codes.  Signed codes: 1.5 * 2^23 added to a value in (-2^22, 2^22) leaves it, rounded to nearest even, in the low bits.
-// CLAMP: a value may be beyond the codes; those of x * (1 / s') with |x| <= top * s' round to at most top.
-template <bool FP8, bool CLAMP = false>
-__device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d)
-{
-    if constexpr (FP8) {
-        const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-        return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true);
-    } else {
-        const auto one = [](float v) {
-            if constexpr (CLAMP) v = fminf(fmaxf(v, -127.0f), 127.0f);
-            return __builtin_bit_cast(uint32_t, v + 12582912.0f);
-        };
-        const uint32_t ab = __builtin_amdgcn_perm(one(b), one(a), 0x0C0C0400u), cd = __builtin_amdgcn_perm(one(d), one(c), 0x04000C0Cu);
-        return ab | cd;
-    }
-}
-
 // the four codes of a word times r, as codes again
 template <bool FP8>
 __device__ __forceinline__ uint32_t rescale4(uint32_t w, float r)

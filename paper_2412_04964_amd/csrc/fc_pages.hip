@@ -1,0 +1,329 @@
+// fc_pages.hip -- the pages of the cache when sequences fork, grow, end, and move together; copies of pages.
+//
+// A page table row names the pages of a sequence, uses[p] how many rows name page p (0: free).  All results are whole numbers that do not
+// depend on the order in which workgroups run: counts are added atomically, fresh pages are the lowest free ones in the order of
+// (sequence, slot), and pages move in ascending order.
+#include "fc_attn.hpp"
+
+namespace fc {
+namespace {
+
+// entries of a row that hold tokens
+__device__ __forceinline__ int64_t filled_slots(int64_t held, int page_shift) { return held > 0 ? (held + (1 << page_shift) - 1) >> page_shift : 0; }
+
+// Workgroups [0, rows) write the new table's rows; the others release or share the pages of an old row, by how many new rows have it as parent.
+__global__ void __launch_bounds__(256) k_pages_fork(ForkArgs a, int page_shift)
+{
+    if (blockIdx.x < (uint32_t)a.rows) {
+        const int b = blockIdx.x, parent = a.parents[b];
+        const bool there = parent >= 0 && parent < a.sequences;
+        const int64_t held = there ? a.held[parent] : 0, filled = filled_slots(held, page_shift);
+        const int32_t *from = a.table + (int64_t)(there ? parent : 0) * a.width;
+        for (int i = threadIdx.x; i < a.width; i += 256) {
+            int id = -1;
+            if (i < filled) {
+                id = from[i];
+                if (id < 0 || id >= a.pages) id = -1;
+            }
+            a.table_out[(int64_t)b * a.width + i] = id;
+        }
+        if (threadIdx.x == 0) a.held_out[b] = (int32_t)held;
+        return;
+    }
+    const int b = blockIdx.x - a.rows;
+    __shared__ int children;
+    if (threadIdx.x == 0) children = 0;
+    __syncthreads();
+    int mine = 0;
+    for (int i = threadIdx.x; i < a.rows; i += 256) mine += a.parents[i] == b;
+    if (mine) atomicAdd(&children, mine);
+    __syncthreads();
+    const int64_t filled = filled_slots(a.held[b], page_shift);
+    const int change = children - 1;
+    for (int i = threadIdx.x; i < a.width; i += 256) {
+        const int by = i < filled ? change : -1;         // what is reserved beyond the tokens held is given back
+        const int id = a.table[(int64_t)b * a.width + i];
+        if (by && id >= 0 && id < a.pages) atomicAdd(&a.uses[id], by);
+    }
+}
+
+// sums of the lanes up to this one
+__device__ __forceinline__ int upto(int v, int lane)
+{
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        const int u = __shfl_up(v, m);
+        if (lane >= m) v += u;
+    }
+    return v;
+}
+
+// Sum of `v` over the lanes of a workgroup of 16 wavefronts before this one, and over all.  Two barriers.
+__device__ __forceinline__ int before(int v, int (&sums)[16], int *all)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, run = upto(v, lane);
+    __syncthreads();
+    if (lane == 63) sums[wave] = run;
+    __syncthreads();
+    int base = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+        if (w < wave) base += sums[w];
+        total += sums[w];
+    }
+    *all = total;
+    return base + run - v;
+}
+
+// The slots of a sequence's table row that its new tokens go to
+struct Slots {
+    int first, count;
+    bool partial;                                        // the first one holds tokens already
+};
+__device__ __forceinline__ Slots slots_of(const ReserveArgs &a, int b, int page_shift)
+{
+    const int64_t held = a.held[b], end = held + ((int64_t)a.offsets[b + 1] - a.offsets[b]), begin = held > 0 ? held : 0;
+    const int64_t first = begin >> page_shift;
+    int64_t last = (end - 1) >> page_shift;
+    if (last >= a.width) last = a.width - 1;
+    if (end <= begin || first > last) return {0, 0, false};
+    return {(int)first, (int)(last - first) + 1, (begin & ((1 << page_shift) - 1)) != 0};
+}
+
+// One workgroup for the step.  While it runs, source[b] is the partly filled page that sequence b writes to, or -1, and target[b] where its
+// fresh pages begin among all.
+__global__ void __launch_bounds__(1024) k_pages_reserve(ReserveArgs a, int page_shift)
+{
+    __shared__ int sums[16];
+    __shared__ int staged[1024];
+    const auto none = [&](int id) { return id < 0 || id >= a.pages; };
+    for (int b = threadIdx.x; b < a.sequences; b += 1024) {
+        const Slots s = slots_of(a, b, page_shift);
+        int mine = -1;
+        if (s.count && s.partial) {
+            mine = a.table[(int64_t)b * a.width + s.first];
+            if (none(mine)) mine = -1;
+        }
+        a.source[b] = mine;
+    }
+    __syncthreads();
+    // who copies, and how many fresh pages each sequence takes
+    int needed = 0;
+    for (int c = 0; c < a.sequences; c += 1024) {
+        const int b = c + threadIdx.x;
+        const bool here = b < a.sequences;
+        const int mine = here ? a.source[b] : -1, users = mine >= 0 ? a.uses[mine] : 0;
+        int writers = 0, later = 0;
+        for (int d = 0; d < a.sequences; d += 1024) {
+            __syncthreads();
+            staged[threadIdx.x] = d + threadIdx.x < a.sequences ? a.source[d + threadIdx.x] : -1;
+            __syncthreads();
+            if (users > 1) {
+                const int n = a.sequences - d < 1024 ? a.sequences - d : 1024;
+                for (int i = 0; i < n; ++i) {
+                    const bool same = staged[i] == mine;
+                    writers += same;
+                    later += same && d + i > b;
+                }
+            }
+        }
+        const bool copies = users > 1 && (later || writers < users);
+        int want = copies;
+        if (here) {
+            const Slots s = slots_of(a, b, page_shift);
+            for (int i = 0; i < s.count; ++i) want += none(a.table[(int64_t)b * a.width + s.first + i]);
+        }
+        int all;
+        const int start = needed + before(want, sums, &all);
+        if (here) a.target[b] = copies ? ~start : start;  // (who does not copy has a start of 0 or more)
+        needed += all;
+    }
+    // the lowest free pages
+    int found = 0;
+    for (int64_t p0 = 0; p0 < a.pages && found < needed; p0 += 4096) {
+        const int64_t p = p0 + 4 * threadIdx.x;
+        bool free[4];
+        int mine = 0, all;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            free[i] = p + i < a.pages && a.uses[p + i] == 0;
+            mine += free[i];
+        }
+        int at = found + before(mine, sums, &all);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (free[i]) {
+                if (at < needed) a.fresh[at] = (int)(p + i);
+                ++at;
+            }
+        found += all;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) *a.lacking = found < needed ? needed - found : 0;
+    for (int b = threadIdx.x; b < a.sequences; b += 1024) {
+        const int mark = a.target[b];
+        const bool copies = mark < 0 && found >= needed;
+        int at = mark < 0 ? ~mark : mark;
+        int target = -1;
+        if (found >= needed) {
+            const Slots s = slots_of(a, b, page_shift);
+            int32_t *row = a.table + (int64_t)b * a.width + s.first;
+            for (int i = 0; i < s.count; ++i) {
+                const bool copy = copies && i == 0;
+                if (!copy && !none(row[i])) continue;
+                const int id = a.fresh[at++];
+                row[i] = id;
+                a.uses[id] = 1;
+                if (copy) target = id;
+            }
+            if (copies) atomicAdd(&a.uses[a.source[b]], -1);
+        }
+        a.target[b] = target;
+        if (!copies) a.source[b] = -1;
+    }
+}
+
+// used pages of each segment
+__global__ void __launch_bounds__(256) k_pages_count(CompactArgs a)
+{
+    __shared__ int total;
+    if (threadIdx.x == 0) total = 0;
+    __syncthreads();
+    int n = 0;
+    for (int i = threadIdx.x; i < kSegment; i += 256) {
+        const int64_t p = (int64_t)blockIdx.x * kSegment + i;
+        n += p < a.pages && a.uses[p] > 0;
+    }
+    if (n) atomicAdd(&total, n);
+    __syncthreads();
+    if (threadIdx.x == 0) a.counts[blockIdx.x] = total;
+}
+
+// Each segment's free pages below U (the pages in use) and used ones from U on, as the k-th of all
+__global__ void __launch_bounds__(1024) k_pages_pair(CompactArgs a, int segments)
+{
+    __shared__ int sums[16];
+    const int64_t p0 = (int64_t)blockIdx.x * kSegment;
+    int earlier = 0, all = 0;                            // used pages before this segment; all of them
+    {
+        int mine = 0, rest = 0, n;
+        for (int i = threadIdx.x; i < segments; i += 1024) {
+            const int c = a.counts[i];
+            mine += i < (int)blockIdx.x ? c : 0;
+            rest += c;
+        }
+        before(mine, sums, &n);
+        earlier = n;
+        before(rest, sums, &n);
+        all = n;
+    }
+    // used pages before page U
+    int below = 0;
+    {
+        const int segment = all / kSegment;
+        int mine = 0, n;
+        for (int i = threadIdx.x; i < segment; i += 1024) mine += a.counts[i];
+        for (int i = threadIdx.x; i < all % kSegment; i += 1024) mine += a.uses[(int64_t)segment * kSegment + i] > 0;
+        before(mine, sums, &n);
+        below = n;
+    }
+    const int moves = all - below;
+    const int64_t p = p0 + 4 * threadIdx.x;
+    int use[4], mine = 0, n;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        use[i] = p + i < a.pages ? a.uses[p + i] : 0;
+        mine += use[i] > 0;
+    }
+    int at = earlier + before(mine, sums, &n);           // used pages before this lane's
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (p + i >= a.pages) break;
+        const bool used = use[i] > 0;
+        if (p + i < all) {
+            if (used) a.uses_out[p + i] = use[i];
+            else a.target[(int)(p + i) - at] = (int)(p + i);
+        } else {
+            a.uses_out[p + i] = 0;
+            if (used) {
+                a.source[at - below] = (int)(p + i);
+                a.rank[p + i] = at - below;
+            }
+        }
+        at += used;
+    }
+    // the places of pairs that there are none of
+    for (int64_t k = p0 / 2 + threadIdx.x; k < (p0 + kSegment) / 2 && k < a.pages / 2; k += 1024)
+        if (k >= moves) a.source[k] = a.target[k] = -1;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.used = all;
+}
+
+// The table's entries and the counts of pages that moved
+__global__ void __launch_bounds__(256) k_pages_move(CompactArgs a)
+{
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int all = *a.used;
+    if (i < a.entries) {
+        int id = a.table[i];
+        if (id >= all && id < a.pages && a.uses[id] > 0) id = a.target[a.rank[id]];
+        a.table_out[i] = id;
+    }
+    if (i < a.pages / 2) {
+        const int to = a.target[i];
+        if (to >= 0) a.uses_out[to] = a.uses[a.source[i]];
+    }
+}
+
+constexpr int64_t kCopy = 16384;                         // bytes of each cache that a workgroup copies
+
+__global__ void __launch_bounds__(256) k_cache_copy(CopyArgs a, int parts)
+{
+    const int64_t pair = blockIdx.x / parts;
+    const int part = blockIdx.x - (int)pair * parts;
+    const int64_t from = a.source[pair], to = a.target[pair];
+    if (from < 0 || to < 0 || from >= a.pages || to >= a.pages || from == to) return;
+    const int64_t left = a.bytes - part * kCopy;
+    for (int64_t i = threadIdx.x * 16; i < kCopy && i < left; i += 256 * 16) {
+        const int64_t at = part * kCopy + i;
+        const uintx4 k = *(const uintx4 *)(a.k + from * a.bytes + at), v = *(const uintx4 *)(a.v + from * a.bytes + at);
+        *(uintx4 *)(a.k + to * a.bytes + at) = k;
+        *(uintx4 *)(a.v + to * a.bytes + at) = v;
+    }
+    if (part == 0)
+        for (int h = threadIdx.x; h < a.heads; h += 256) {
+            a.k_scales[to * a.heads + h] = a.k_scales[from * a.heads + h];
+            a.v_scales[to * a.heads + h] = a.v_scales[from * a.heads + h];
+        }
+}
+
+int log2_of(int page) { return page == 16 ? 4 : page == 32 ? 5 : 6; }
+
+}  // namespace
+
+hipError_t launch_pages_fork(const ForkArgs &a, hipStream_t stream)
+{
+    return launch_many(k_pages_fork, (int64_t)a.rows + a.sequences, 256, stream, a, log2_of(a.page));
+}
+
+hipError_t launch_pages_reserve(const ReserveArgs &a, hipStream_t stream)
+{
+    return launch_many(k_pages_reserve, 1, 1024, stream, a, log2_of(a.page));
+}
+
+hipError_t launch_pages_compact(const CompactArgs &a, hipStream_t stream)
+{
+    const int64_t segments = (a.pages + kSegment - 1) / kSegment, most = a.entries > a.pages / 2 ? a.entries : a.pages / 2;
+    if (!launchable((most + 255) / 256, 256)) return kTooLarge;        // before anything is
+    hipError_t e = launch_many(k_pages_count, segments, 256, stream, a);
+    if (e == hipSuccess) e = launch_many(k_pages_pair, segments, 1024, stream, a, (int)segments);
+    if (e == hipSuccess && most) e = launch_many(k_pages_move, (most + 255) / 256, 256, stream, a);
+    return e;
+}
+
+hipError_t launch_cache_copy(const CopyArgs &a, hipStream_t stream)
+{
+    const int64_t parts = (a.bytes + kCopy - 1) / kCopy;
+    return a.count > (int64_t)1 << 32 ? kTooLarge : launch_many(k_cache_copy, a.count * parts, 256, stream, a, (int)parts);
+}
+
+}  // namespace fc

@@ -42,7 +42,9 @@ namespace {
     X(fc_dequantize) X(fc_dequantize_sym) X(fc_dequantize_fp8) X(fc_dequantize_cmeta) X(fc_dequantize_rot)           \
     X(fc_allreduce_sim) X(fc_allreduce_sim_sym) X(fc_allreduce_sim_fp8) X(fc_allreduce_sim_cmeta)                    \
     X(fc_allreduce_sim_rot) X(fc_allreduce_sim_workspace_bytes)                                                      \
-    X(fc_rotary) X(fc_cache_append) X(fc_cache_attention_workspace_bytes) X(fc_cache_attention) X(fc_prompt_attention)
+    X(fc_rotary) X(fc_cache_append) X(fc_cache_attention_workspace_bytes) X(fc_cache_attention) X(fc_prompt_attention) \
+    X(fc_pages_fork) X(fc_pages_reserve_workspace_bytes) X(fc_pages_reserve) X(fc_pages_compact_workspace_bytes) X(fc_pages_compact)     \
+    X(fc_cache_copy) X(fc_rms_norm) X(fc_rms_norm_quantize)
 
 struct Library {
 #define FC_MEMBER(f) decltype(&::f) f = nullptr;
@@ -710,6 +712,319 @@ PyObject *prompt_attention(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     END_HANDLE_TH_ERRORS
 }
 
+// ---- norm.py's calls ----
+
+// A [tokens, hidden] activation as the C ABI takes it
+struct Row {
+    const at::Tensor *t = nullptr;
+    void *ptr = nullptr;
+    int64_t stride = 0;
+};
+
+bool describe(const at::Tensor &t, Row &r)
+{
+    if (t.dim() != 2 || t.numel() == 0 || t.stride(1) != 1) return false;
+    r.t = &t;
+    r.ptr = t.data_ptr();
+    r.stride = t.size(0) > 1 ? t.stride(0) : 0;
+    return r.stride % 8 == 0 && (reinterpret_cast<uintptr_t>(r.ptr) & 15) == 0;
+}
+
+// `o` on GPU `device`, of the type and shape of `like` if that is given, else of either 16-bit type
+bool row(PyObject *o, const at::Tensor *like, int device, Row &r)
+{
+    if (!THPVariable_CheckExact(o)) return false;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (!t.defined() || !ordinary_keys(t) || !t.is_cuda() || t.device().index() != device) return false;
+    if (t.requires_grad() && c10::GradMode::is_enabled()) return false;        // norm.py refuses it
+    if (like ? t.scalar_type() != like->scalar_type() || t.sizes() != like->sizes() : t.scalar_type() != at::kHalf && t.scalar_type() != at::kBFloat16)
+        return false;
+    return describe(t, r);
+}
+
+bool row_result(PyObject *out, const Row &like, int device, at::Tensor &own, Row &r)
+{
+    if (out == Py_None) {
+        own = empty({like.t->size(0), like.t->size(1)}, like.t->scalar_type(), *like.t);
+        return describe(own, r);
+    }
+    return row(out, like.t, device, r) && (r.t->size(0) == 1 || r.stride >= r.t->size(1));
+}
+
+struct Norm {
+    Row x, r;
+    const at::Tensor *weight = nullptr;
+    double eps = 0;
+    int64_t tokens = 0;
+    int hidden = 0, type = 0, weight_type = 0;
+
+    bool take(PyObject *px, PyObject *pw, PyObject *pe, PyObject *pr, PyObject *sum_out, int device)
+    {
+        if (device < 0 || !row(px, nullptr, device, x) || !PyFloat_CheckExact(pe)) return false;
+        eps = PyFloat_AS_DOUBLE(pe);
+        type = x.t->scalar_type() == at::kBFloat16 ? FC_TYPE_BF16 : FC_TYPE_F16;
+        weight = plain(pw, x.t->scalar_type(), device);
+        weight_type = type;
+        if (!weight) {
+            weight = plain(pw, at::kFloat, device);
+            weight_type = FC_TYPE_F32;
+        }
+        if (!weight || weight->dim() != 1 || weight->size(0) != x.t->size(1) || x.t->size(1) > 32768 || x.t->size(0) > 0x7FFFFFFF) return false;
+        if ((weight->requires_grad() && c10::GradMode::is_enabled()) || (reinterpret_cast<uintptr_t>(weight->data_ptr()) & 15) != 0) return false;
+        tokens = x.t->size(0);
+        hidden = (int)x.t->size(1);
+        return pr == Py_None ? sum_out == Py_None : row(pr, x.t, device, r);
+    }
+};
+
+// (x, weight, eps, residual, out, sum_out)
+PyObject *rms_norm(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    HANDLE_TH_ERRORS
+    if (n_args != 6 || !plain_context()) return fallback();
+    const int device = device_of(a[0]);
+    Norm n;
+    Row y, sum;
+    if (!n.take(a[0], a[1], a[2], a[3], a[5], device)) return fallback();
+    at::Tensor own, own_sum;
+    if (!row_result(a[4], n.x, device, own, y) || (n.r.t && !row_result(a[5], n.x, device, own_sum, sum)) || sum.ptr == y.ptr) return fallback();
+    void *stream = stream_of(device);
+    const void *weight = n.weight->data_ptr();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = lib.fc_rms_norm(n.x.ptr, n.x.stride, n.r.ptr, n.r.stride, weight, n.weight_type, n.tokens, n.hidden, n.eps, n.type, sum.ptr, sum.stride,
+                         y.ptr, y.stride, stream);
+    Py_END_ALLOW_THREADS
+    if (!done(rc, "fc_rms_norm")) return nullptr;
+    if (!n.r.t) return wrapped(a[4], own);
+    return Py_BuildValue("(NN)", wrapped(a[4], own), wrapped(a[5], own_sum));
+    END_HANDLE_TH_ERRORS
+}
+
+// (x, weight, eps, group, quantizer, residual, out, sum_out)
+PyObject *rms_norm_quantize(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    HANDLE_TH_ERRORS
+    if (n_args != 8 || !plain_context()) return fallback();
+    const int device = device_of(a[0]);
+    Norm n;
+    Row sum;
+    int64_t group, quantizer;
+    if (!n.take(a[0], a[1], a[2], a[5], a[7], device) || !integer(a[3], group) || !integer(a[4], quantizer)) return fallback();
+    if (group != n.hidden && !geometry(n.hidden, group)) return fallback();
+    Coded c;
+    if (a[6] != Py_None && !c.take(a[6], 2, n.tokens, n.hidden, group, 8, at::kFloat, device, false)) return fallback();
+    at::Tensor own_sum;
+    if (n.r.t && !row_result(a[7], n.x, device, own_sum, sum)) return fallback();
+    if (a[6] == Py_None) c.allocate(2, n.tokens, n.hidden, group, 8, at::kFloat, *n.x.t);
+    if (sum.ptr == c.ptr(0)) return fallback();
+    void *stream = stream_of(device), *codes = c.ptr(0);
+    float *scales = (float *)c.ptr(1);
+    const void *weight = n.weight->data_ptr();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = lib.fc_rms_norm_quantize(n.x.ptr, n.x.stride, n.r.ptr, n.r.stride, weight, n.weight_type, n.tokens, n.hidden, n.eps, n.type, (int)group,
+                                  (int)quantizer, sum.ptr, sum.stride, codes, scales, stream);
+    Py_END_ALLOW_THREADS
+    if (!done(rc, "fc_rms_norm_quantize")) return nullptr;
+    PyObject *pair = c.result(2, 0);
+    if (!n.r.t || !pair) return pair;
+    PyObject *r = Py_BuildValue("(OON)", PyTuple_GET_ITEM(pair, 0), PyTuple_GET_ITEM(pair, 1), wrapped(a[7], own_sum));
+    Py_DECREF(pair);
+    return r;
+    END_HANDLE_TH_ERRORS
+}
+
+// ---- pages.py's calls ----
+
+// `out` None: new int32 tensors of these shapes, else the caller's from a tuple
+template <size_t N>
+struct Ints {
+    std::array<const at::Tensor *, N> t{};
+    std::array<at::Tensor, N> own;
+    PyObject *given = nullptr;
+
+    bool take(PyObject *out, const std::array<std::array<int64_t, 2>, N> &shapes, const at::Tensor &like, int device)      // (second size -1: a vector)
+    {
+        if (out == Py_None) {
+            for (size_t i = 0; i < N; ++i) {
+                own[i] = shapes[i][1] < 0 ? empty({shapes[i][0]}, at::kInt, like) : empty({shapes[i][0], shapes[i][1]}, at::kInt, like);
+                t[i] = &own[i];
+            }
+            return true;
+        }
+        if (!PyTuple_CheckExact(out) || PyTuple_GET_SIZE(out) != (Py_ssize_t)N) return false;
+        given = out;
+        for (size_t i = 0; i < N; ++i) {
+            PyObject *o = PyTuple_GET_ITEM(out, i);
+            t[i] = plain(o, at::kInt, device);
+            if (!t[i] || (shapes[i][1] < 0 ? t[i]->dim() != 1 || t[i]->size(0) != shapes[i][0] : !shape2(*t[i], shapes[i][0], shapes[i][1]))) return false;
+        }
+        return true;
+    }
+    int32_t *ptr(size_t i) const { return (int32_t *)t[i]->data_ptr(); }
+    PyObject *result() const
+    {
+        if (given) {
+            Py_INCREF(given);
+            return given;
+        }
+        PyObject *r = PyTuple_New(N);
+        for (size_t i = 0; r && i < N; ++i) {
+            PyObject *o = THPVariable_Wrap(own[i]);
+            if (!o) {
+                Py_DECREF(r);
+                return nullptr;
+            }
+            PyTuple_SET_ITEM(r, i, o);
+        }
+        return r;
+    }
+};
+
+bool apart(const at::Tensor &a, const at::Tensor &b)
+{
+    const char *pa = (const char *)a.data_ptr(), *pb = (const char *)b.data_ptr();
+    return a.numel() == 0 || b.numel() == 0 || pa + a.nbytes() <= pb || pb + b.nbytes() <= pa;
+}
+
+// (pages, held, uses, parents, page, out)
+PyObject *pages_fork(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    HANDLE_TH_ERRORS
+    if (n_args != 6 || !plain_context()) return fallback();
+    const int device = device_of(a[0]);
+    if (device < 0) return fallback();
+    const at::Tensor *table = plain(a[0], at::kInt, device), *uses = plain(a[2], at::kInt, device), *parents = plain(a[3], at::kInt, device);
+    int64_t page;
+    if (!table || table->dim() != 2 || table->numel() == 0 || !uses || uses->dim() != 1 || uses->numel() == 0 || !parents || parents->dim() != 1 || parents->numel() == 0 ||
+        !integer(a[4], page) || table->size(0) > 0x7FFFFFFF || table->size(1) > 0x7FFFFFFF || parents->size(0) > 0x7FFFFFFF)
+        return fallback();
+    const at::Tensor *held = vector(a[1], table->size(0), device);
+    const int64_t rows = parents->size(0), width = table->size(1), count = uses->size(0);
+    Ints<2> out;
+    if (!held || !out.take(a[5], {{{rows, width}, {rows, -1}}}, *table, device)) return fallback();
+    if (out.given) {
+        for (const at::Tensor *old : {table, held, uses, parents})
+            if (!apart(*out.t[0], *old) || !apart(*out.t[1], *old)) return fallback();
+        if (!apart(*out.t[0], *out.t[1])) return fallback();
+    }
+    const int sequences = (int)table->size(0);
+    const int32_t *pt = (const int32_t *)table->data_ptr(), *ph = (const int32_t *)held->data_ptr(), *pp = (const int32_t *)parents->data_ptr();
+    int32_t *pu = (int32_t *)uses->data_ptr(), *nt = out.ptr(0), *nh = out.ptr(1);
+    void *stream = stream_of(device);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = lib.fc_pages_fork(pt, ph, sequences, (int)width, (int)page, pu, count, pp, (int)rows, nt, nh, stream);
+    Py_END_ALLOW_THREADS
+    if (!done(rc, "fc_pages_fork")) return nullptr;
+    return out.result();
+    END_HANDLE_TH_ERRORS
+}
+
+// the caller's workspace, or a new one
+const at::Tensor *space(PyObject *o, size_t need, const at::Tensor &like, int device, at::Tensor &own)
+{
+    if (o == Py_None) {
+        own = empty({(int64_t)need}, at::kByte, like);
+        return &own;
+    }
+    const at::Tensor *t = plain(o, at::kByte, device);
+    return t && (size_t)t->numel() >= need ? t : nullptr;
+}
+
+// (pages, held, uses, offsets, page, out, workspace)
+PyObject *pages_reserve(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    HANDLE_TH_ERRORS
+    if (n_args != 7 || !plain_context()) return fallback();
+    const int device = device_of(a[0]);
+    if (device < 0) return fallback();
+    const at::Tensor *table = plain(a[0], at::kInt, device), *uses = plain(a[2], at::kInt, device);
+    int64_t page;
+    if (!table || table->dim() != 2 || table->numel() == 0 || !uses || uses->dim() != 1 || uses->numel() == 0 || !integer(a[4], page) ||
+        table->size(0) > 0x7FFFFFFF || table->size(1) > 0x7FFFFFFF)
+        return fallback();
+    const int64_t sequences = table->size(0), width = table->size(1), count = uses->size(0);
+    const at::Tensor *held = vector(a[1], sequences, device), *offsets = vector(a[3], sequences + 1, device);
+    if (!held || !offsets) return fallback();
+    at::Tensor own;
+    const at::Tensor *ws = space(a[6], lib.fc_pages_reserve_workspace_bytes(count), *table, device, own);
+    Ints<3> out;
+    if (!ws || !out.take(a[5], {{{sequences, -1}, {sequences, -1}, {1, -1}}}, *table, device)) return fallback();
+    int32_t *pt = (int32_t *)table->data_ptr(), *pu = (int32_t *)uses->data_ptr(), *source = out.ptr(0), *target = out.ptr(1), *lacking = out.ptr(2);
+    const int32_t *ph = (const int32_t *)held->data_ptr(), *po = (const int32_t *)offsets->data_ptr();
+    void *stream = stream_of(device), *pw = ws->data_ptr();
+    const size_t bytes = ws->numel();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = lib.fc_pages_reserve(pt, ph, po, (int)sequences, (int)width, (int)page, pu, count, source, target, lacking, pw, bytes, stream);
+    Py_END_ALLOW_THREADS
+    if (!done(rc, "fc_pages_reserve")) return nullptr;
+    return out.result();
+    END_HANDLE_TH_ERRORS
+}
+
+// (pages, uses, out, workspace)
+PyObject *pages_compact(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    HANDLE_TH_ERRORS
+    if (n_args != 4 || !plain_context()) return fallback();
+    const int device = device_of(a[0]);
+    if (device < 0) return fallback();
+    const at::Tensor *table = plain(a[0], at::kInt, device), *uses = plain(a[1], at::kInt, device);
+    if (!table || table->dim() != 2 || table->numel() == 0 || !uses || uses->dim() != 1 || uses->numel() == 0 || table->size(0) > 0x7FFFFFFF ||
+        table->size(1) > 0x7FFFFFFF)
+        return fallback();
+    const int64_t sequences = table->size(0), width = table->size(1), count = uses->size(0);
+    at::Tensor own;
+    const at::Tensor *ws = space(a[3], lib.fc_pages_compact_workspace_bytes(count), *table, device, own);
+    Ints<5> out;
+    if (!ws || !out.take(a[2], {{{sequences, width}, {count, -1}, {count / 2, -1}, {count / 2, -1}, {1, -1}}}, *table, device)) return fallback();
+    if (out.given && ((out.ptr(0) != table->data_ptr() && !apart(*out.t[0], *table)) || !apart(*out.t[1], *uses))) return fallback();
+    const int32_t *pt = (const int32_t *)table->data_ptr(), *pu = (const int32_t *)uses->data_ptr();
+    int32_t *nt = out.ptr(0), *nu = out.ptr(1), *source = out.ptr(2), *target = out.ptr(3), *used = out.ptr(4);
+    void *stream = stream_of(device), *pw = ws->data_ptr();
+    const size_t bytes = ws->numel();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = lib.fc_pages_compact(pt, sequences, (int)width, pu, count, nt, nu, source, target, used, pw, bytes, stream);
+    Py_END_ALLOW_THREADS
+    if (!done(rc, "fc_pages_compact")) return nullptr;
+    return out.result();
+    END_HANDLE_TH_ERRORS
+}
+
+// (cache, source, target)
+PyObject *cache_copy(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    HANDLE_TH_ERRORS
+    if (n_args != 3 || !plain_context() || !PyTuple_CheckExact(a[0]) || PyTuple_GET_SIZE(a[0]) != 4) return fallback();
+    const int device = device_of(a[1]);
+    if (device < 0) return fallback();
+    const at::Tensor *source = plain(a[1], at::kInt, device);
+    const at::Tensor *k = plain(PyTuple_GET_ITEM(a[0], 0), at::kByte, device), *v = plain(PyTuple_GET_ITEM(a[0], 1), at::kByte, device),
+                     *ks = plain(PyTuple_GET_ITEM(a[0], 2), at::kFloat, device), *vs = plain(PyTuple_GET_ITEM(a[0], 3), at::kFloat, device);
+    if (!source || source->dim() != 1 || !k || !v || !ks || !vs || k->dim() != 4 || v->sizes() != k->sizes() || !shape2(*ks, k->size(0), k->size(1)) ||
+        !shape2(*vs, k->size(0), k->size(1)) || k->numel() == 0 || k->size(1) > 65536 || k->size(2) > 64 || k->size(3) > 256)
+        return fallback();
+    const at::Tensor *target = vector(a[2], source->size(0), device);
+    if (!target) return fallback();
+    void *pk = k->data_ptr(), *pv = v->data_ptr(), *stream = stream_of(device);
+    float *sk = (float *)ks->data_ptr(), *sv = (float *)vs->data_ptr();
+    const int32_t *from = (const int32_t *)source->data_ptr(), *to = (const int32_t *)target->data_ptr();
+    const int64_t pages = k->size(0), pairs = source->size(0);
+    const int heads = (int)k->size(1), page = (int)k->size(2), dim = (int)k->size(3);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = lib.fc_cache_copy(pk, pv, sk, sv, pages, heads, page, dim, from, to, pairs, stream);
+    Py_END_ALLOW_THREADS
+    if (!done(rc, "fc_cache_copy")) return nullptr;
+    Py_INCREF(a[0]);
+    return a[0];
+    END_HANDLE_TH_ERRORS
+}
+
 // load(path, on_error): the functions of the library that the process already holds under `path`
 PyObject *load(PyObject *, PyObject *args)
 {
@@ -752,6 +1067,9 @@ PyMethodDef methods[] = {
     FC_METHOD("allreduce_sim_rot", allreduce<kRot>),
     FC_METHOD("rotary", rotary), FC_METHOD("cache_append", cache_append), FC_METHOD("cache_attention", cache_attention),
     FC_METHOD("prompt_attention", prompt_attention),
+    FC_METHOD("rms_norm", rms_norm), FC_METHOD("rms_norm_quantize", rms_norm_quantize),
+    FC_METHOD("pages_fork", pages_fork), FC_METHOD("pages_reserve", pages_reserve), FC_METHOD("pages_compact", pages_compact),
+    FC_METHOD("cache_copy", cache_copy),
     {nullptr, nullptr, 0, nullptr},
 };
 

@@ -1,0 +1,129 @@
+"""Norm and page operators without a GPU: argument checks of the C entry points, and the launches that they make."""
+import json
+import subprocess
+import sys
+
+import pytest
+
+import paper_2412_04964_amd as fc
+import launches
+
+P = 0x10000      # a fake, 16-byte aligned, non-NULL device address; never dereferenced
+
+
+@pytest.fixture(scope="module")
+def L():
+    return fc.lib()
+
+
+def norm(L, x=P, xs=512, r=None, rs=0, w=P, wt=0, tokens=4, hidden=512, eps=1e-5, type=0, sum=None, ss=0, y=P, ys=512):
+    return L.fc_rms_norm(x, xs, r, rs, w, wt, tokens, hidden, eps, type, sum, ss, y, ys, None)
+
+
+def coded(L, x=P, xs=512, r=None, rs=0, w=P, wt=2, tokens=4, hidden=512, eps=1e-5, type=1, group=64, quantizer=1, sum=None, codes=P, scales=P):
+    return L.fc_rms_norm_quantize(x, xs, r, rs, w, wt, tokens, hidden, eps, type, group, quantizer, sum, 512, codes, scales, None)
+
+
+def test_norm_argument_checks(L):
+    for call in (norm, coded):
+        assert call(L, type=2) == call(L, type=-1) == call(L, wt=3) == call(L, type=0, wt=1) == -8
+        assert call(L, tokens=-1) == call(L, hidden=0) == call(L, hidden=516) == call(L, hidden=32776) == -4
+        assert call(L, eps=0.0) == call(L, eps=-1.0) == call(L, eps=float("nan")) == call(L, eps=float("inf")) == -4
+        assert call(L, x=None) == call(L, w=None) == -1
+        assert call(L, x=P + 2) == call(L, xs=4) == call(L, r=P + 8) == call(L, r=P, rs=12) == call(L, sum=P + 8) == call(L, w=P + 4) == -5
+        assert call(L, tokens=0, x=None, w=None) == 0
+    assert norm(L, y=None) == -1 and norm(L, y=P + 2) == norm(L, ys=3) == norm(L, sum=P, ss=4) == -5
+    assert coded(L, quantizer=0) == coded(L, quantizer=3) == -8
+    assert coded(L, group=0) == coded(L, group=16) == coded(L, group=48) == coded(L, group=1024) == coded(L, hidden=520, group=512) == -3
+    assert coded(L, codes=None) == coded(L, scales=None) == -1 and coded(L, codes=P + 8) == -5
+    assert coded(L, tokens=0, codes=None, scales=None) == 0
+
+
+def fork(L, table=P, held=P, sequences=2, width=3, page=16, uses=P, pages=8, parents=P, rows=2, out=P, held_out=P):
+    return L.fc_pages_fork(table, held, sequences, width, page, uses, pages, parents, rows, out, held_out, None)
+
+
+def reserve(L, table=P, held=P, offsets=P, sequences=2, width=3, page=16, uses=P, pages=8, source=P, target=P, lacking=P, ws=P, bytes=32):
+    return L.fc_pages_reserve(table, held, offsets, sequences, width, page, uses, pages, source, target, lacking, ws, bytes, None)
+
+
+def compact(L, table=P, sequences=2, width=3, uses=P, pages=8, out=P, uses_out=P, source=P, target=P, used=P, ws=P, bytes=36):
+    return L.fc_pages_compact(table, sequences, width, uses, pages, out, uses_out, source, target, used, ws, bytes, None)
+
+
+def copy(L, k=P, v=P, ks=P, vs=P, pages=8, heads=2, page=16, dim=64, source=P, target=P, count=3):
+    return L.fc_cache_copy(k, v, ks, vs, pages, heads, page, dim, source, target, count, None)
+
+
+def test_page_argument_checks(L):
+    for call in (fork, reserve, compact):
+        assert call(L, width=0) == call(L, pages=0) == call(L, pages=1 << 31) == call(L, sequences=-1) == -4
+    for call in (fork, reserve, copy):
+        assert call(L, page=8) == call(L, page=48) == call(L, page=128) == -4
+    assert fork(L, rows=-1) == -4
+    for name in ("table", "held", "uses", "parents", "out", "held_out"):
+        assert fork(L, **{name: None}) == -1, name
+    assert fork(L, sequences=0, rows=0, uses=None) == 0
+    for name in ("table", "held", "offsets", "uses", "source", "target", "lacking"):
+        assert reserve(L, **{name: None}) == -1, name
+    assert L.fc_pages_reserve_workspace_bytes(8) == 32 and L.fc_pages_reserve_workspace_bytes(0) == 0
+    assert reserve(L, ws=None) == reserve(L, bytes=31) == -6 and reserve(L, ws=P + 4) == -5
+    for name in ("table", "uses", "out", "uses_out", "source", "target", "used"):
+        assert compact(L, **{name: None}) == -1, name
+    assert L.fc_pages_compact_workspace_bytes(8) == 36 and L.fc_pages_compact_workspace_bytes(-1) == 0
+    assert compact(L, ws=None) == compact(L, bytes=35) == -6 and compact(L, ws=P + 4) == -5
+    assert copy(L, pages=0) == copy(L, heads=0) == copy(L, dim=32) == copy(L, count=-1) == -4
+    for name in ("k", "v", "ks", "vs", "source", "target"):
+        assert copy(L, **{name: None}) == -1, name
+    assert copy(L, k=P + 8) == copy(L, v=P + 1) == -5
+    assert copy(L, count=0, k=None, source=None) == 0
+
+
+def test_cpu_tensors_are_refused():
+    torch = pytest.importorskip("torch")
+    i = torch.zeros(2, dtype=torch.int32)
+    for call in (lambda: fc.rms_norm(torch.zeros((2, 64), dtype=torch.float16), torch.zeros(64)), lambda: fc.pages_fork(i[:, None], i, i, i, 16),
+                 lambda: fc.pages_compact(i[:, None], i), lambda: fc.cache_copy((i, i, i, i), i, i)):
+        with pytest.raises(TypeError):
+            call()
+
+
+_CHILD = """
+import ctypes, json, sys
+ctypes.CDLL(sys.argv[1], ctypes.RTLD_GLOBAL)
+L = ctypes.CDLL(sys.argv[2])
+for name, args in json.load(sys.stdin):
+    print("R", getattr(L, name)(*[ctypes.c_double(a) if isinstance(a, float) else ctypes.c_int64(a) for a in args]), flush=True)
+"""
+
+
+def launched(*calls):
+    """(return code, [(kernel, workgroups, lanes), ...]) of each call, where nothing runs and no address is followed (launches.py)"""
+    r = subprocess.run([sys.executable, "-c", _CHILD, launches._stand_in(), launches.LIB], input=json.dumps(calls), capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    out, seen = [], []
+    for line in r.stdout.splitlines():
+        if line.startswith("L "):
+            _, name, grid, block, _ = line.split()
+            seen.append((launches._readable(name), int(grid), int(block)))
+        else:
+            out.append((int(line[2:]), seen))
+            seen = []
+    return out
+
+
+def norm_call(tokens, hidden):
+    return "fc_rms_norm", [P, hidden, P, hidden, P, 0, tokens, hidden, 1e-5, 0, P, hidden, P, hidden, 0]
+
+
+def test_calls_are_launched_up_to_what_the_runtime_takes():
+    most = (1 << 31) - 1
+    fine = [norm_call(1, 8), norm_call(most, 8), norm_call(most, 32768),
+            ("fc_pages_fork", [P, P, 1 << 22, 4, 16, P, most, P, 1 << 22, P, P, 0]), ("fc_pages_reserve", [P, P, P, 1 << 22, 4, 16, P, most, P, P, P, P, 1 << 34, 0]),
+            ("fc_pages_compact", [P, 1 << 10, 1 << 20, P, 1 << 30, P, P, P, P, P, P, 1 << 34, 0]), ("fc_cache_copy", [P, P, P, P, most, 8, 16, 128, P, P, 1 << 22, 0])]
+    for call, (rc, seen) in zip(fine, launched(*fine)):
+        assert rc == 0 and seen, (call, rc, seen)
+    over = [("fc_pages_fork", [P, P, 1 << 23, 4, 16, P, most, P, 1 << 23, P, P, 0]), ("fc_cache_copy", [P, P, P, P, most, 8, 16, 128, P, P, 1 << 24, 0]),
+            ("fc_pages_compact", [P, 1 << 12, 1 << 20, P, 8, P, P, P, P, P, P, 1 << 34, 0])]
+    for call, (rc, seen) in zip(over, launched(*over)):
+        assert rc == -4 and not seen, (call, rc, seen)
