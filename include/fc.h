@@ -395,6 +395,28 @@ FC_API int fc_prompt_attention(const void *q, int64_t q_token_stride, int64_t q_
                                float scale, void *out, int64_t out_token_stride, int64_t out_head_stride, void *hip_stream);
 
 /*
+ * Attention of a prompt that is taken in pieces: the step's new tokens, whose keys and values are at hand in 16 bits, over what their
+ * sequences hold in the cache and over themselves.  Query i of a sequence sees the held tokens of the cache and the new tokens j <= i; with
+ * held negative none of the cache, and the first -held new tokens have no place: nothing sees them, and they see nothing.
+ * q, out: [tokens, heads * group, dim]; k, v: [tokens, heads, dim], keys turned; dim in {64, 128}; token strides of k and v below 2^25.  The
+ * new tokens need not be in the cache, which is only read: fc_cache_append may come before or after.  Otherwise as fc_cache_attention.
+ * Products are of `type`, sums in fp32.  Weights, times the scales of their pages where the values are codes, are rounded to `type`: bfloat16
+ * 8 bits; binary16 11 bits for what is less than 2^8 below the largest of 64 tokens, absolutely 2^-15 of that one at least.  Pages whose value scale
+ * is 2^-36 of the largest among 1024 neighbouring tokens and less are taken as if it were that.  Sums must fit fp32 as there.
+ * What the pages hold beyond the held tokens has no influence, and no bit of a row depends on later tokens, infinities and NaN included.
+ * longest: the most tokens, held and new, of a sequence; it only sizes the launch.
+ * workspace: fc_chunk_attention_workspace_bytes(...) bytes, 16-byte aligned, contents unspecified.
+ */
+FC_API size_t fc_chunk_attention_workspace_bytes(int64_t tokens, int sequences, int heads, int group, int dim, int64_t longest);
+FC_API int fc_chunk_attention(const void *q, int64_t q_token_stride, int64_t q_head_stride, const void *k, int64_t k_token_stride,
+                              int64_t k_head_stride, const void *v, int64_t v_token_stride, int64_t v_head_stride, int64_t tokens,
+                              int heads, int group, int dim, int type, int quantizer, const void *k_cache, const void *v_cache,
+                              const float *k_scales, const float *v_scales, int64_t pages, int page, const int32_t *page_table,
+                              int table_width, const int32_t *offsets, const int32_t *held, int sequences, int64_t longest, float scale,
+                              void *out, int64_t out_token_stride, int64_t out_head_stride, void *workspace, size_t workspace_bytes,
+                              void *hip_stream);
+
+/*
  * ---- The cache's pages when sequences fork, grow, end, and move together ----
  *
  * page_table, held: as above.  uses: int32 [pages], in how many rows of the table a page is named; 0 is a free page.  An entry outside

@@ -47,6 +47,8 @@ from .attention import (  # noqa: F401
     cache_append,
     cache_attention,
     cache_attention_workspace_bytes,
+    chunk_attention,
+    chunk_attention_workspace_bytes,
     prompt_attention,
     rotary,
     rotary_frequencies,
@@ -64,6 +66,7 @@ __all__ = [
     "quantize_sym", "strerror", "version",
     "cache_append", "cache_attention", "cache_attention_workspace_bytes", "prompt_attention", "rotary",
     "rotary_frequencies", "rotary_table",
+    "chunk_attention", "chunk_attention_workspace_bytes",
     "cache_copy", "pages_compact", "pages_fork", "pages_reserve", "rms_norm", "rms_norm_quantize",
     "allreduce_sim_cmeta", "dequant_reduce_requant_cmeta", "dequantize_cmeta", "quantize_cmeta",
 ]

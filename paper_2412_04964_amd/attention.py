@@ -273,3 +273,39 @@ def prompt_attention(q, k, v, offsets, longest: int, causal: bool = True, scale=
         offsets.data_ptr(), sequences, longest, int(causal), dim ** -0.5 if scale is None else scale, y.data_ptr(), *_strides(y),
         _stream()), "fc_prompt_attention")
     return y
+
+
+def chunk_attention_workspace_bytes(tokens: int, sequences: int, heads: int, group: int, dim: int, longest: int) -> int:
+    return int(binding.lib().fc_chunk_attention_workspace_bytes(tokens, sequences, heads, group, dim, longest))
+
+
+def chunk_attention(q, k, v, cache, pages, offsets, held, longest: int, quantizer: int = QUANTIZER_SYM, scale=None, out=None, workspace=None):
+    """fc_chunk_attention: a prompt that is taken in pieces.  q [tokens, query heads, dim] over the held tokens of every sequence in the cache and
+    over the new ones up to itself, whose k, v [tokens, heads, dim] (keys turned) need not be in the cache.  longest: the most tokens,
+    held and new, that a sequence has.  scale: dim^-0.5 unless given."""
+    done = (binding._native or binding._calls()).chunk_attention(q, k, v, cache, pages, offsets, held, longest, quantizer, scale, out, workspace)
+    if done is not None:
+        return done
+    torch = _torch()
+    _rows(q, "q")
+    _rows(k, "k", q.dtype)
+    _rows(v, "v", q.dtype, tuple(k.shape))
+    sequences = _step(offsets, held)
+    heads, page, dim, count, width = _cache(cache, pages, sequences)
+    tokens = q.shape[0]
+    _shape(q, (tokens, q.shape[1], dim), "q")
+    _shape(k, (tokens, heads, dim), "k")
+    group = _group(q, heads, "cache")
+    y = _out_rows(out, q, tuple(q.shape))
+    need = chunk_attention_workspace_bytes(tokens, sequences, heads, group, dim, longest)
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    _dev(workspace, torch.uint8, "workspace")
+    if workspace.numel() < need:
+        raise FcError(-6, "fc_chunk_attention")
+    _check(binding.lib().fc_chunk_attention(
+        q.data_ptr(), *_strides(q), k.data_ptr(), *_strides(k), v.data_ptr(), *_strides(v), tokens, heads, group, dim, _type(q, "q"), quantizer,
+        cache[0].data_ptr(), cache[1].data_ptr(), cache[2].data_ptr(), cache[3].data_ptr(), count, page, pages.data_ptr(), width,
+        offsets.data_ptr(), held.data_ptr(), sequences, longest, dim ** -0.5 if scale is None else scale, y.data_ptr(), *_strides(y),
+        workspace.data_ptr(), workspace.numel(), _stream()), "fc_chunk_attention")
+    return y

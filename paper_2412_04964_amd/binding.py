@@ -118,6 +118,11 @@ def lib() -> ctypes.CDLL:
         L.fc_cache_attention.restype = i32
         L.fc_prompt_attention.argtypes = [*rows, *rows, *rows, i64, i32, i32, i32, i32, vp, i32, i64, i32, f32, *rows, vp]
         L.fc_prompt_attention.restype = i32
+        L.fc_chunk_attention_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i64]
+        L.fc_chunk_attention_workspace_bytes.restype = sz
+        L.fc_chunk_attention.argtypes = [*rows, *rows, *rows, i64, i32, i32, i32, i32, i32, vp, vp, vp, vp, i64, i32, vp, i32, vp, vp, i32, i64,
+                                         f32, *rows, vp, sz, vp]
+        L.fc_chunk_attention.restype = i32
         L.fc_pages_fork.argtypes = [vp, vp, i32, i32, i32, vp, i64, vp, i32, vp, vp, vp]
         L.fc_pages_fork.restype = i32
         L.fc_pages_reserve_workspace_bytes.argtypes = [i64]

@@ -49,7 +49,7 @@ UNITS = [("fc_api.hip", "api", []), ("fc_codec.hip", "codec", []), ("fc_wide.hip
          ("fc_rot.hip", "rot", []), ("fc_rot_rows.hip", "rot_rows", []), ("fc_rot_fine.hip", "rot_fine", []), ("fc_rot_sim.hip", "rot_sim", []),
          ("fc_small.hip", "small", []), ("fc_attn_api.hip", "attn_api", []), ("fc_rotary.hip", "rotary", []),
          ("fc_cache.hip", "cache", []), ("fc_cache_attn.hip", "cache_attn", []), ("fc_prompt.hip", "prompt", []),
-         ("fc_norm.hip", "norm", []), ("fc_pages.hip", "pages", [])]
+         ("fc_norm.hip", "norm", []), ("fc_pages.hip", "pages", []), ("fc_chunk.hip", "chunk", [])]
 for _c in range(4):      # one unit per quantizer: asymmetric, symmetric, FP8, asymmetric with binary16 metadata
     UNITS.append(("fc_sim.hip", "sim_%d" % _c, ["-DFC_SIM_CODEC=%d" % _c]))
     UNITS.append(("fc_sim_wide.hip", "sim_wide_%d" % _c, ["-DFC_SIM_CODEC=%d" % _c]))

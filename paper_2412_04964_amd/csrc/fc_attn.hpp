@@ -92,6 +92,21 @@ struct PromptArgs {
 };
 hipError_t launch_prompt_attention(const PromptArgs &a, hipStream_t stream);
 
+// Attention of the step's new tokens, which are at hand in 16 bits, over what their sequences hold in the cache and over themselves
+struct ChunkArgs {
+    Rows q, k, v, out;
+    Step step;
+    Cache cache;
+    // of the items that more than one workgroup has a part of: [workgroups, 2, 128 rows] of normalised results, then maxima and weights
+    float *partial;
+    uint64_t *plan;                                     // how many units there are, and where each sequence's begin
+    float scale;
+    int heads, group, dim, fp8, bf16, workgroups;
+};
+int chunk_workgroups(int64_t tokens, int sequences, int heads, int group, int dim, int64_t longest);
+size_t chunk_workspace(int workgroups, int sequences, int dim);
+hipError_t launch_chunk_attention(const ChunkArgs &a, hipStream_t stream);
+
 // The norm of rows [tokens, hidden]; strides in elements
 struct NormArgs {
     const void *x, *residual, *weight;                  // residual may be null
@@ -250,6 +265,30 @@ __device__ __forceinline__ uintx4 resource(const void *base, uint32_t bytes)
 {
     const uint64_t at = (uint64_t)base;
     return uintx4{(uint32_t)at, (uint32_t)(at >> 32) & 0xFFFFu, bytes, 0x00020000u};
+}
+
+// 4 codes of a word -> binary16
+template <bool FP8>
+__device__ __forceinline__ uintx2 halves(uint32_t w)
+{
+    if constexpr (FP8) {
+        return uintx2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true))};
+    } else {
+        // code + 128 under the exponent of 1024 is 1152 + code
+        const uint32_t u = w ^ 0x80808080u;
+        const half2 off = {(_Float16)-1152.0f, (_Float16)-1152.0f};
+        const half2 lo = __builtin_bit_cast(half2, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) + off;
+        const half2 hi = __builtin_bit_cast(half2, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) + off;
+        return uintx2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+    }
+}
+
+// until no more than N of this wavefront's loads are on their way
+template <int N>
+__device__ __forceinline__ void wait_vm()
+{
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
 // Which sequence has work unit u, where sequence b has at most (tokens of b) / 2^shift + extra units and therefore owns the numbers

@@ -257,6 +257,59 @@ int fc_prompt_attention(const void *q, int64_t q_token_stride, int64_t q_head_st
     return result(fc::launch_prompt_attention(a, static_cast<hipStream_t>(hip_stream)));
 }
 
+size_t fc_chunk_attention_workspace_bytes(int64_t tokens, int sequences, int heads, int group, int dim, int64_t longest)
+{
+    if (check_attention(tokens, sequences, heads, group, dim, 1, longest) != FC_OK || dim == 256) return 0;
+    return fc::chunk_workspace(fc::chunk_workgroups(tokens, sequences, heads, group, dim, longest), sequences, dim);
+}
+
+int fc_chunk_attention(const void *q, int64_t q_token_stride, int64_t q_head_stride, const void *k, int64_t k_token_stride, int64_t k_head_stride,
+                       const void *v, int64_t v_token_stride, int64_t v_head_stride, int64_t tokens, int heads, int group, int dim, int type,
+                       int quantizer, const void *k_cache, const void *v_cache, const float *k_scales, const float *v_scales, int64_t pages,
+                       int page, const int32_t *page_table, int table_width, const int32_t *offsets, const int32_t *held, int sequences,
+                       int64_t longest, float scale, void *out, int64_t out_token_stride, int64_t out_head_stride, void *workspace,
+                       size_t workspace_bytes, void *hip_stream)
+{
+    int rc = check_type(type);
+    if (rc != FC_OK || (rc = check_code(quantizer)) != FC_OK) return rc;
+    if ((rc = check_attention(tokens, sequences, heads, group, dim, 1, longest)) != FC_OK || (rc = check_scale(scale)) != FC_OK) return rc;
+    if (dim == 256) return FC_ERR_SHAPE;
+    if (tokens == 0) return FC_OK;
+    if ((rc = check_cache(k_cache, v_cache, k_scales, v_scales, pages, page, page_table, table_width)) != FC_OK) return rc;
+    if (!offsets || !held) return FC_ERR_NULL;
+    if ((rc = check_rows(q, q_token_stride, q_head_stride)) != FC_OK) return rc;
+    if ((rc = check_rows(k, k_token_stride, k_head_stride)) != FC_OK) return rc;
+    if ((rc = check_rows(v, v_token_stride, v_head_stride)) != FC_OK) return rc;
+    if ((rc = check_rows(out, out_token_stride, out_head_stride)) != FC_OK) return rc;
+    // 32-bit offsets in a tile, and tokens of a sequence
+    if (tokens > kMaxTokens - 1024) return FC_ERR_SHAPE;
+    if (k_token_stride >= 1 << 25 || v_token_stride >= 1 << 25 || k_token_stride < 0 || v_token_stride < 0) return FC_ERR_SHAPE;
+    // units of work are counted in 64 bits, whatever the arrays say
+    const double tiles = (double)table_width * page / 64 + (double)tokens / 64 + 2, blocks = (double)tokens * group / 128 + sequences;
+    if (tiles * blocks * heads >= 0x1p62) return FC_ERR_SHAPE;
+    fc::ChunkArgs a;
+    a.workgroups = fc::chunk_workgroups(tokens, sequences, heads, group, dim, longest);
+    const size_t need = fc::chunk_workspace(a.workgroups, sequences, dim);
+    if (!workspace || workspace_bytes < need) return FC_ERR_WORKSPACE;
+    if (!aligned16(workspace)) return FC_ERR_ALIGN;
+    a.q = rows(q, q_token_stride, q_head_stride);
+    a.k = rows(k, k_token_stride, k_head_stride);
+    a.v = rows(v, v_token_stride, v_head_stride);
+    a.out = rows(out, out_token_stride, out_head_stride);
+    a.step = {offsets, held, sequences, tokens};
+    a.cache = {static_cast<uint8_t *>(const_cast<void *>(k_cache)), static_cast<uint8_t *>(const_cast<void *>(v_cache)),
+               const_cast<float *>(k_scales), const_cast<float *>(v_scales), page_table, pages, page, table_width};
+    a.plan = static_cast<uint64_t *>(workspace);        // the partials behind it, on a 16-byte boundary
+    a.partial = reinterpret_cast<float *>(static_cast<char *>(workspace) + ((size_t)sequences + 2) / 2 * 16);
+    a.scale = scale;
+    a.heads = heads;
+    a.group = group;
+    a.dim = dim;
+    a.fp8 = quantizer == FC_QUANTIZER_FP8;
+    a.bf16 = type == FC_TYPE_BF16;
+    return result(fc::launch_chunk_attention(a, static_cast<hipStream_t>(hip_stream)));
+}
+
 // ---- the cache's pages ----
 
 int fc_pages_fork(const int32_t *page_table, const int32_t *held, int sequences, int table_width, int page, int32_t *uses, int64_t pages,

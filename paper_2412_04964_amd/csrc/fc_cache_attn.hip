@@ -29,23 +29,6 @@ constexpr int kPiece = 4;               // of a piece, at least (8: 16 contexts 
 constexpr int waves_of(int dim, int row_tiles) { return dim < 256 && row_tiles == 1 ? 8 : 4; }      // of a workgroup for a whole context
 constexpr int kTile = 16;               // tokens of a matrix instruction; a page holds whole tiles
 
-// 4 codes of a word -> binary16
-template <bool FP8>
-__device__ __forceinline__ uintx2 halves(uint32_t w)
-{
-    if constexpr (FP8) {
-        return uintx2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false)),
-                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true))};
-    } else {
-        // code + 128 under the exponent of 1024 is 1152 + code
-        const uint32_t u = w ^ 0x80808080u;
-        const half2 off = {(_Float16)-1152.0f, (_Float16)-1152.0f};
-        const half2 lo = __builtin_bit_cast(half2, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) + off;
-        const half2 hi = __builtin_bit_cast(half2, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) + off;
-        return uintx2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
-    }
-}
-
 // byte i of four words -> word i
 __device__ __forceinline__ void transpose4(uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t (&out)[4])
 {
@@ -71,13 +54,6 @@ __device__ __forceinline__ void load_words(const uint8_t *p, uint32_t (&w)[4])
     const uintx4 x = *(const uintx4 *)p;
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = x[i];
-}
-
-// until no more than N of this wavefront's loads are on their way
-template <int N>
-__device__ __forceinline__ void wait_vm()
-{
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
 // over the four lanes that share l % 16

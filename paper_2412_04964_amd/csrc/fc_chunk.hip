@@ -1,0 +1,624 @@
+// fc_chunk.hip -- attention of a chunk of new tokens, at hand in 16 bits, over what their sequences hold in the paged cache of 8-bit codes and
+// over themselves.
+//
+// Query i of a sequence that held L tokens before the step sees the L cached ones, k = sk ck and v = sv cv with the scales of their page
+// and head, and the new tokens j <= i:  o = sum_t softmax_t(scale q . k_t) v_t.
+// The rows of a key/value head are the queries times the query heads that share it.  A workgroup has 128 of them, 32 a wavefront, and takes 64
+// tokens at a time, first the cached ones, then the new.  As over prompts a wavefront forms S^T = K Q^T with 32 x 32 x 16 matrix instructions,
+// which leaves a lane with weights of the very tokens that it needs as operand of O^T = V^T P^T: scores and weights stay in registers.
+//   Both kinds of codes are exact in binary16 and in bfloat16: a tile's codes are converted once, on their way to LDS, for the workgroup's rows.
+//   sk multiplies scores.  sv would multiply weights; it goes into their exponents instead, w = 2^(s - top + log2(sv / unit)), and what sums
+//   of weights then have too much is divided out once for 16 tokens.  The unit of the sums is a power of two, common to the workgroup.
+//   The unit of a row's weights is its running maximum.  Binary16 has not the range for all that are lower: there it follows a tile's
+//   largest score up and down when that is kSlack away, and the largest is put at 2^kBias (kReach below the row's largest at most).
+// All work of the call, in units of a tile of 64 tokens for 128 rows, is cut into equal ranges, one a workgroup: contexts of any lengths
+// end together.  Rows that were cut are joined by a second kernel, from results that are normalised.
+#include "fc_attn_tiles.hpp"
+
+namespace fc {
+namespace {
+
+constexpr int kTokens = 64, kRows = 128, kWaves = 4;
+constexpr int kLeast = 2;               // units of a range
+template <bool BF16> constexpr float kSlack = BF16 ? 8.0f : 10.0f;
+constexpr float kBias = 4.0f, kReach = 36.0f;
+// how far below the largest unit so far the unit may go, and what a scale may be of it
+constexpr float kDeep = 0x1p-30f, kFaint = 0x1p-36f;
+
+// What there is to do for one sequence, for each key/value head: `blocks` of 128 rows, each over `cached` tiles and those new ones that it sees
+struct Job {
+    int64_t off, blocks, total;                          // total: units of all blocks
+    int n, held, skip, cached, fresh;                    // new tokens; tokens in the cache; new ones without a place; tiles of either kind
+};
+
+// units of new tokens of the first j blocks: block i - 1 sees the tokens before ceil(128 i / group), ceil(2 i / group) tiles of them
+__device__ __forceinline__ int64_t fresh_units(int64_t j, int group)
+{
+    const int64_t q = j / group;
+    const int r = (int)(j - q * group), over = r - group / 2;
+    return group * q * (q - 1) + q * (group + (group + 1) / 2) + 2 * q * r + r + (over > 0 ? over : 0);
+}
+
+__device__ __forceinline__ Job job_of(const ChunkArgs &a, int off, int next, int held, int page_shift)
+{
+    Job j;
+    j.off = off;
+    j.n = off < 0 || next < off || next > a.step.tokens ? 0 : next - off;
+    const int64_t room = (int64_t)a.cache.table_width << page_shift;
+    j.held = held < 0 ? 0 : held < room ? held : (int)room;
+    j.skip = held < 0 ? -(held + 1) < j.n ? -held : j.n : 0;
+    j.cached = (int)(((int64_t)j.held + kTokens - 1) / kTokens);
+    j.fresh = (int)(((int64_t)j.n + kTokens - 1) / kTokens);
+    j.blocks = ((int64_t)j.n * a.group + kRows - 1) / kRows;
+    j.total = j.blocks ? (j.blocks - 1) * j.cached + fresh_units(j.blocks - 1, a.group) + j.cached + j.fresh : 0;
+    return j;
+}
+
+__device__ __forceinline__ int64_t units_before(const Job &j, int64_t block, int group) { return block >= j.blocks ? j.total : block * j.cached + fresh_units(block, group); }
+
+// The units of all sequences, one behind the other, cut into ranges that differ by one unit at most; fewer of them where they would have
+// less than kLeast units
+struct Ranges {
+    uint64_t each;
+    uint32_t count, longer;                              // the first `longer` of them have one more than `each`
+    __device__ __forceinline__ Ranges(uint64_t total, uint32_t workgroups)
+    {
+        const uint64_t most = (total + kLeast - 1) / kLeast;
+        count = most < workgroups ? (uint32_t)most : workgroups;
+        each = count ? total / count : 0;
+        longer = (uint32_t)(total - count * each);
+    }
+    __device__ __forceinline__ uint64_t begin(uint32_t r) const { return r * each + (r < longer ? r : longer); }
+    __device__ __forceinline__ uint32_t of(uint64_t unit) const
+    {
+        const uint64_t split = longer * (each + 1);
+        return (uint32_t)(unit < split ? unit / (each + 1) : longer + (unit - split) / each);
+    }
+};
+
+__device__ __forceinline__ uint64_t running_sum(uint64_t v, int lane)
+{
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        const uint64_t u = __shfl_up(v, m);
+        if (lane >= m) v += u;
+    }
+    return v;
+}
+
+__device__ __forceinline__ uint64_t lane_u64(uint64_t v, int lane)
+{
+    const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)v, lane), hi = __builtin_amdgcn_readlane((uint32_t)(v >> 32), lane);
+    return (uint64_t)hi << 32 | lo;
+}
+__device__ __forceinline__ float lane_f(float v, int lane) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane)); }
+
+// 4 codes of a word -> two words of 16-bit values, which hold either kind exactly
+template <bool FP8, bool BF16>
+__device__ __forceinline__ uintx2 sixteen(uint32_t w)
+{
+    if constexpr (!BF16) return halves<FP8>(w);
+    else if constexpr (FP8)
+        return uintx2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true))};
+    else return uintx2{narrow2<true>((float)(int8_t)w, (float)(int8_t)(w >> 8)), narrow2<true>((float)(int8_t)(w >> 16), (float)(int8_t)(w >> 24))};
+}
+
+template <int DIM, bool FP8, bool BF16>
+__global__ void __launch_bounds__(64 * kWaves, 2) k_chunk_attention(ChunkArgs a, int page_shift)
+{
+    constexpr int kSteps = DIM / 16, kOut = DIM / 32, kRow = 2 * DIM, kTile = kTokens * kRow;
+    constexpr int kOutRow = kRow + 16;
+    constexpr int kFetch = DIM / 64, kPieces = DIM / 16;                 // loads of a tile's K or V codes; lanes of a token
+    __shared__ __attribute__((aligned(1024))) uint8_t tiles[4][kTile];
+    static_assert(sizeof(tiles) >= kWaves * 32 * kOutRow, "the results fit the tiles");
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, side = lane >> 5;
+    const int sequences = a.step.sequences, group = a.group;
+
+    // ---- this workgroup's range ----
+    uint64_t sum = 0;
+    bool astray = false;
+    int off = 0, next = 0, held = 0;
+    for (int c = 0; c < sequences; c += 64)
+        if (c + lane < sequences) {
+            off = a.step.offsets[c + lane];
+            next = a.step.offsets[c + lane + 1];
+            held = a.step.held[c + lane];
+            sum += (uint64_t)job_of(a, off, next, held, page_shift).total * a.heads;
+            astray |= off < 0 || next < off || next > a.step.tokens;
+        }
+    // (units of offsets that do not ascend may be more than 64 bits count: none of them is done)
+    const uint64_t total_units = __any(astray) ? 0 : lane_u64(running_sum(sum, lane), 63);
+    const Ranges ranges(total_units, gridDim.x);
+    if (blockIdx.x == 0 && threadIdx.x == 0) a.plan[0] = total_units;
+    if (blockIdx.x >= ranges.count) return;
+    // workgroups go to the 8 XCDs in turn: an XCD gets neighbouring ranges, whose K and V its L2 then holds
+    const uint32_t range = ranges.count % 8 == 0 ? (blockIdx.x & 7) * (ranges.count / 8) + (blockIdx.x >> 3) : blockIdx.x;
+    uint64_t at = ranges.begin(range);
+    const uint64_t end = ranges.begin(range + 1);
+    int b = -1;
+    uint64_t begins = 0, run = 0;
+    for (int c = 0; c < sequences; c += 64) {
+        uint64_t work = 0;
+        if (c + lane < sequences) {
+            off = a.step.offsets[c + lane];
+            next = a.step.offsets[c + lane + 1];
+            held = a.step.held[c + lane];
+            work = (uint64_t)job_of(a, off, next, held, page_shift).total * a.heads;
+        }
+        const uint64_t upto = run + running_sum(work, lane);
+        if (blockIdx.x == 0 && wave == 0 && c + lane < sequences) a.plan[1 + c + lane] = upto - work;
+        const uint64_t past = __ballot(upto > at);
+        if (b < 0 && past) {
+            const int l = __builtin_ctzll(past);
+            b = c + l;
+            begins = lane_u64(upto - work, l);
+            if (blockIdx.x) break;                       // the first one writes where every sequence begins
+        }
+        run = lane_u64(upto, 63);
+    }
+
+    // ---- places that do not change ----
+    const int stride_k = (int)a.k.token, stride_v = (int)a.v.token;
+    // (Addresses that are a few operations away from the lane's number are made where they are used: the loop has no registers for them.)
+    const auto afresh = [](int v) {
+        asm volatile("" : "+v"(v));
+        return v;
+    };
+    const int at_k = col * kRow + (side ^ swizzle<DIM, true>(col)) * 16;
+    const int v_row = 4 * side + (lane & 15) / 4;
+    const int at_v = v_row * kRow + ((((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) ^ swizzle<DIM, false>(v_row)) * 16 + (lane & 1) * 8;
+    const float factor = a.scale * 1.4426950408889634f;      // scores in powers of two
+    const auto arrived = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+
+    while (at < end) {
+        const Job job = job_of(a, a.step.offsets[b], a.step.offsets[b + 1], a.step.held[b], page_shift);
+        const uint64_t work = (uint64_t)job.total * a.heads;
+        if (at >= begins + work) {
+            begins += work;
+            ++b;
+            continue;
+        }
+        // ---- the item: a head, a block of rows, and its tiles [tile0, tile1) ----
+        const int head = (int)((at - begins) / job.total);
+        const int64_t within = (int64_t)(at - begins) - head * job.total;
+        int64_t lo = 0, hi = job.blocks - 1;
+        while (lo < hi) {
+            const int64_t mid = (lo + hi + 1) >> 1;
+            if (units_before(job, mid, group) <= within) lo = mid;
+            else hi = mid - 1;
+        }
+        const int64_t block = lo, before = units_before(job, block, group);
+        const int units = (int)(units_before(job, block + 1, group) - before);
+        const int tile0 = (int)(within - before);
+        const int tile1 = end - at < (uint64_t)(units - tile0) ? tile0 + (int)(end - at) : units;
+        at += tile1 - tile0;
+        const bool whole = tile0 == 0 && tile1 == units;
+        const int64_t rows = (int64_t)job.n * group, row0 = block * kRows + wave * 32, row = row0 + col;
+        const int n = job.n, cached = job.cached, skip = job.skip;
+        const bool idle = row0 >= rows;                  // this wavefront has no rows
+        const int query = (int)((row < rows ? row : rows - 1) / group), query_head = head * group + (int)((row < rows ? row : rows - 1) - (int64_t)query * group);
+        const int first_query = (int)(block * kRows / group);                    // of the workgroup
+        const int wave_first = (int)((row0 < rows ? row0 : rows - 1) / group), wave_last = (int)((row0 + 31 < rows ? row0 + 31 : rows - 1) / group);
+
+        uintx4 qf[kSteps];
+        {
+            const uint16_t *q = (const uint16_t *)a.q.ptr + (job.off + query) * a.q.token + query_head * a.q.head + side * 8;
+#pragma unroll
+            for (int j = 0; j < kSteps; ++j) qf[j] = *(const uintx4 *)(q + 16 * j);
+        }
+        const uint16_t *k = (const uint16_t *)a.k.ptr + job.off * a.k.token + head * a.k.head;
+        const uint16_t *v = (const uint16_t *)a.v.ptr + job.off * a.v.token + head * a.v.head;
+        const int32_t *const table = a.cache.table + (int64_t)b * a.cache.table_width;
+
+        // pages of 64 pieces of 16 tokens (16 tiles), one a lane
+        const auto pages_of = [&](int batch) {
+            const uint32_t token = ((uint32_t)batch * 64 + lane) * 16;       // (below 2^31 + 2^11)
+            int id = 0;
+            if (token < (uint32_t)job.held) id = table[token >> page_shift];
+            return id;
+        };
+        const auto scales_of = [&](int batch, int id, float &ks, float &vs) {
+            const bool there = ((uint32_t)batch * 64 + lane) * 16 < (uint32_t)job.held && id >= 0 && id < a.cache.pages;
+            ks = vs = 0.0f;
+            if (there) {
+                ks = a.cache.k_scales[(int64_t)id * a.heads + head];
+                vs = a.cache.v_scales[(int64_t)id * a.heads + head];
+            }
+        };
+        int page = 0, page_next = 0;
+        float ks_next = 0.0f, vs_next = 0.0f;
+        uintx4 code_k[kFetch], code_v[kFetch];
+        // the codes of tile t, from memory
+        const auto fetch = [&](int t) {
+            const int in = t & 15;
+            if (t != tile0 && in == 0) {
+                page = page_next;
+                page_next = pages_of((t >> 4) + 1);
+            }
+            if (in == 8) scales_of((t >> 4) + 1, page_next, ks_next, vs_next);
+            const int thread = afresh(threadIdx.x);
+#pragma unroll
+            for (int i = 0; i < kFetch; ++i) {
+                const int piece = (i * (64 / kFetch) + wave * (64 / kPieces)) / 16;      // of 16 tokens, the wavefront's
+                int id = __builtin_amdgcn_readlane(page, in * 4 + piece);
+                if (id < 0 || id >= a.cache.pages) id = 0;
+                const int slot = (t * kTokens + piece * 16) & ((1 << page_shift) - 1);
+                const int64_t place = ((((int64_t)id * a.heads + head) << page_shift) + slot) * DIM;
+                const int mine = thread / kPieces % 16 * DIM + thread % kPieces * 16;
+                code_k[i] = *(const uintx4 *)(a.cache.k + place + mine);
+                code_v[i] = *(const uintx4 *)(a.cache.v + place + mine);
+            }
+        };
+        // and into LDS
+        const auto convert = [&](int t, uint8_t *lds_k, uint8_t *lds_v) {
+            const int thread = afresh(threadIdx.x), code_row = thread / kPieces, code_unit = thread % kPieces;
+#pragma unroll
+            for (int i = 0; i < kFetch; ++i) {
+                const int r = i * (64 / kFetch) + code_row;
+                if (t * kTokens + r >= job.held) code_k[i] = code_v[i] = uintx4{0, 0, 0, 0};     // whatever the page holds there
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uintx2 k0 = sixteen<FP8, BF16>(code_k[i][2 * h]), k1 = sixteen<FP8, BF16>(code_k[i][2 * h + 1]);
+                    *(uintx4 *)(lds_k + r * kRow + ((2 * code_unit + h) ^ swizzle<DIM, true>(r & 31)) * 16) = uintx4{k0[0], k0[1], k1[0], k1[1]};
+                }
+                __builtin_amdgcn_sched_barrier(0);           // (no more registers at a time)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uintx2 v0 = sixteen<FP8, BF16>(code_v[i][2 * h]), v1 = sixteen<FP8, BF16>(code_v[i][2 * h + 1]);
+                    *(uintx4 *)(lds_v + r * kRow + ((2 * code_unit + h) ^ swizzle<DIM, false>(r & 15)) * 16) = uintx4{v0[0], v0[1], v1[0], v1[1]};
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        const auto bring = [&](int t, int to) {
+            if (t < cached) {
+                convert(t, tiles[to], tiles[to + 1]);
+                if (t + 1 < cached && t + 1 < tile1) fetch(t + 1);
+            } else {
+                const int t0 = (t - cached) * kTokens + 16 * wave;
+                const int mine = afresh(lane);
+                const Rows16<DIM, true> rows_k(mine, stride_k);
+                const Rows16<DIM, false> rows_v(mine, stride_v);
+                rows_k.load(rows16(k + (int64_t)t0 * stride_k, stride_k, n - t0, DIM), tiles[to] + wave * 16 * kRow);
+                rows_v.load(rows16(v + (int64_t)t0 * stride_v, stride_v, n - t0, DIM), tiles[to + 1] + wave * 16 * kRow);
+            }
+        };
+
+        floatx16 acc[kOut];
+#pragma unroll
+        for (int o = 0; o < kOut; ++o)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[o][r] = 0.0f;
+        float top = -FLT_MAX, peak = -FLT_MAX, total = 0.0f, unit = 1.0f, largest_unit = 0.0f;
+
+        floatx16 s[2];
+        uintx4 pf[4];
+        const auto scores = [&](const uint8_t *lds_k) {
+            const int mine = afresh(at_k);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[h][r] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < kSteps; ++j)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) s[h] = mma32<BF16>(*(const uintx4 *)(lds_k + (mine ^ (j << 5)) + h * 32 * kRow), qf[j], s[h]);
+        };
+        // tokens of the tile from `first` on, and before `sees`, are seen
+        const auto mask = [&](int first, int sees) {
+            first -= 4 * side;
+            sees -= 4 * side;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int t = h * 32 + 8 * (r / 4) + r % 4;
+                    if (t < first || t >= sees) s[h][r] = -__builtin_inff();
+                }
+        };
+        // The pieces of 16 tokens that the lanes have the scales of: what scores are multiplied by (powers of two), what is added to the
+        // exponents for the values' scales, and what sums of weights are multiplied by for that
+        float steep = 0.0f, raise = 0.0f, back = 0.0f;
+        const auto turn_to = [&](float key_scale, float value_scale) {
+            float widest = value_scale;
+#pragma unroll
+            for (int m = 1; m < 64; m <<= 1) widest = fmaxf(widest, __shfl_xor(widest, m));
+            widest = fmaxf(fminf(widest, 0x1p126f), FLT_MIN);
+            // the unit of the sums: the power of two at or below the largest scale, or kDeep of the largest unit so far
+            const float now = fmaxf(__builtin_amdgcn_ldexpf(1.0f, __builtin_amdgcn_frexp_expf(widest) - 1), fmaxf(largest_unit * kDeep, FLT_MIN));
+            if (now != unit) {
+                const float change = unit / now;
+#pragma unroll
+                for (int o = 0; o < kOut; ++o) acc[o] *= change;
+                unit = now;
+            }
+            largest_unit = fmaxf(largest_unit, now);
+            const float c = fmaxf(value_scale / unit, kFaint);
+            steep = fmaxf(factor * key_scale, FLT_MIN);
+            raise = __builtin_amdgcn_logf(c);            // log2
+            back = 1.0f / c;
+        };
+        const auto weights = [&](int piece) {
+            float fk[4], up[4];
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                fk[p] = lane_f(steep, piece + p);
+                up[p] = lane_f(raise, piece + p);
+            }
+            float most = -__builtin_inff();
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                float m = s[p / 2][8 * (p & 1)];
+#pragma unroll
+                for (int r = 1; r < 8; ++r) m = fmaxf(m, s[p / 2][8 * (p & 1) + r]);
+                most = fmaxf(most, __builtin_fmaf(m, fk[p], up[p]));
+            }
+            bool away;
+            if constexpr (BF16) {
+                away = most > top + kSlack<BF16>;
+            } else {
+                most = fmaxf(most, __shfl_xor(most, 32)) - kBias;
+                away = fabsf(most - top) > kSlack<BF16>;
+            }
+            if (__any(away)) {
+                if constexpr (BF16) most = fmaxf(most, __shfl_xor(most, 32));
+                // only rows that are away themselves: no row's bits depend on others
+                float now = most > top + kSlack<BF16> ? most : top;
+                if constexpr (!BF16) {
+                    now = fabsf(most - top) > kSlack<BF16> ? fmaxf(most, peak - kReach) : top;
+                    peak = fmaxf(peak, now);
+                }
+                const float shrink = __builtin_amdgcn_exp2f(top - now);
+                top = now;
+                total *= shrink;
+#pragma unroll
+                for (int o = 0; o < kOut; ++o) acc[o] *= shrink;
+            }
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                const float add = up[p] - top;
+                float part = 0.0f;
+#pragma unroll
+                for (int r = 0; r < 8; r += 2) {
+                    const float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[p / 2][8 * (p & 1) + r], fk[p], add));
+                    const float w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[p / 2][8 * (p & 1) + r + 1], fk[p], add));
+                    part += w0 + w1;
+                    pf[p][r / 2] = narrow2<BF16>(w0, w1);
+                }
+                total = __builtin_fmaf(part, lane_f(back, piece + p), total);
+            }
+        };
+        const auto add_values = [&](const uint8_t *lds_v) {
+            const int mine = afresh(at_v);
+#pragma unroll
+            for (int m = 0; m < 4; ++m)
+#pragma unroll
+                for (int o = 0; o < kOut; ++o) {
+                    const uint8_t *p = lds_v + (mine ^ (o << 6)) + m * 16 * kRow;
+                    const uintx2 lo = transposed(p), hi = transposed(p + 8 * kRow);
+                    acc[o] = mma32<BF16>(uintx4{lo[0], lo[1], hi[0], hi[1]}, pf[m], acc[o]);
+                }
+        };
+        // In a tile that not all rows see whole, an infinity or NaN among the new values would be NaN times the weight of 0 of those that do
+        // not.  Such values are added to the rows that see them, and taken out of the tile.
+        const auto not_finite = [](uint32_t w) { return (w & 0x7FFF7FFFu) + (BF16 ? 0x00800080u : 0x04000400u); };      // in the sign bits of w's halves
+        const auto finite_only = [&](uint32_t w) { return w & ~(((not_finite(w) & 0x80008000u) >> 15) * 0xFFFFu); };
+        const auto any_not_finite = [&](const uint8_t *lds_v) {
+            uint32_t any = 0;
+#pragma unroll 4
+            for (int i = 0; i < kTile / 1024; ++i) {
+                const uintx4 w = *(const uintx4 *)(lds_v + i * 1024 + lane * 16);
+                any |= not_finite(w[0]) | not_finite(w[1]) | not_finite(w[2]) | not_finite(w[3]);
+            }
+            return __any(any & 0x80008000u) != 0;
+        };
+        const auto add_not_finite = [&](const uint8_t *lds_v, int t0) {
+#pragma unroll 1
+            for (int t = 0; t < kTokens; ++t) {
+                const uint8_t *p = lds_v + t * kRow + side * 8;
+                const bool seen = t0 + t <= query && t0 + t >= skip;
+#pragma unroll
+                for (int o = 0; o < kOut; ++o)
+#pragma unroll
+                    for (int r = 0; r < 16; r += 4) {
+                        const uintx2 w = *(const uintx2 *)(p + ((o * 4 + r / 4) ^ swizzle<DIM, false>(t & 15)) * 16);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const uint32_t bits = i & 1 ? w[i / 2] >> 16 : w[i / 2] & 0xFFFFu;
+                            if (seen && (not_finite(bits) & 0x8000u)) acc[o][r + i] += widen<BF16>(bits);
+                        }
+                    }
+            }
+        };
+        const auto compute = [&](int t, int from) {
+            uint8_t *const lds_k = tiles[from], *const lds_v = tiles[from + 1];
+            const bool code = t < cached;
+            const int t0 = code ? t * kTokens : (t - cached) * kTokens;
+            const bool astray = !code && (t0 + kTokens - 1 > first_query || t0 < skip) && any_not_finite(lds_v);      // the same for all wavefronts
+            const bool sees = !idle && (code || t0 <= wave_last);
+            if (sees) {
+                scores(lds_k);
+                if (code ? t0 + kTokens > job.held : t0 + kTokens - 1 > wave_first || t0 < skip) mask(code ? 0 : skip - t0, (code ? job.held : query + 1) - t0);
+                weights((t & 15) * 4);
+            }
+            if (astray) {
+                if (sees) add_not_finite(lds_v, t0);
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll 1
+                for (int i = 0; i < kTile / 1024 / kWaves; ++i) {
+                    uintx4 *const place = (uintx4 *)(lds_v + (wave * (kTile / 1024 / kWaves) + i) * 1024 + lane * 16);
+                    const uintx4 w = *place;
+                    *place = uintx4{finite_only(w[0]), finite_only(w[1]), finite_only(w[2]), finite_only(w[3])};
+                }
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            }
+            if (sees) add_values(lds_v);
+        };
+
+        if (tile0 < cached) {
+            const int batch = tile0 >> 4;
+            page = pages_of(batch);
+            page_next = pages_of(batch + 1);
+            float ks, vs;
+            scales_of(batch, page, ks, vs);
+            scales_of(batch + 1, page_next, ks_next, vs_next);
+            turn_to(ks, vs);
+            fetch(tile0);
+        } else {
+            turn_to(1.0f, 1.0f);
+        }
+        bring(tile0, 0);
+        // the queries are here before the loop, where waiting for them would wait for the tiles that are loaded ahead
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j) asm volatile("" : "+v"(qf[j]));
+        arrived();
+        int from = 0;
+        for (int t = tile0; t < tile1; ++t, from ^= 2) {
+            if (t != tile0 && t <= cached && ((t & 15) == 0 || t == cached)) {
+                if (t < cached) turn_to(ks_next, vs_next);
+                else turn_to(1.0f, 1.0f);
+            }
+            if (t + 1 < tile1) bring(t + 1, from ^ 2);
+            compute(t, from);
+            arrived();
+        }
+
+        total += __shfl_xor(total, 32);
+        const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+        if (whole) {
+            // through LDS, where the tiles are done with, so that a wavefront stores whole rows (a lane has 4 elements of a row at a time)
+            uint8_t *const mine = &tiles[0][0] + wave * 32 * kOutRow;                     // neighbouring rows begin 4 banks apart
+#pragma unroll
+            for (int o = 0; o < kOut; ++o)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4)
+                    *(uintx2 *)(mine + col * kOutRow + (o * 32 + 2 * r + 4 * side) * 2) =
+                        uintx2{narrow2<BF16>(acc[o][r] * inv * unit, acc[o][r + 1] * inv * unit), narrow2<BF16>(acc[o][r + 2] * inv * unit, acc[o][r + 3] * inv * unit)};
+            constexpr int kLanes = DIM / 8;                  // of a row
+#pragma unroll
+            for (int i = 0; i < 32 * kLanes / 64; ++i) {
+                const int out_row = i * (64 / kLanes) + lane / kLanes, d = lane % kLanes * 8;
+                const uintx4 w = *(const uintx4 *)(mine + out_row * kOutRow + d * 2);
+                const int64_t r = row0 + out_row, q = r / group;
+                if (r < rows) *(uintx4 *)((uint16_t *)a.out.ptr + (job.off + q) * a.out.token + (head * group + (int)(r - q * group)) * a.out.head + d) = w;
+            }
+            __syncthreads();                                 // before the next item's tiles
+        } else if (!idle) {
+            // as the lanes have them: [place][wavefront][4 elements of each][lane]
+            const int64_t place = ((int64_t)range * 2 + (tile0 == 0)) * kWaves + wave, places = (int64_t)gridDim.x * 2 * kWaves;
+            floatx4 *const y = (floatx4 *)a.partial + place * (32 * DIM / 4);
+            const int mine = afresh(lane);
+#pragma unroll
+            for (int o = 0; o < kOut; ++o)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4)
+                    y[(o * 4 + r / 4) * 64 + mine] = floatx4{acc[o][r] * inv * unit, acc[o][r + 1] * inv * unit, acc[o][r + 2] * inv * unit, acc[o][r + 3] * inv * unit};
+            if (mine < 32) ((floatx2 *)(a.partial + places * (32 * DIM)))[place * 32 + mine] = floatx2{top, total};
+        }
+    }
+}
+
+// Joins what the ranges have of the items that were cut.  A workgroup has 32 of an item's elements (of all its rows), a wavefront 32 rows.  A range
+// has two places: 1 for an item that it begins and does not end, 0 for one that began before.
+template <int DIM, bool BF16>
+__global__ void __launch_bounds__(64 * kWaves) k_chunk_join(ChunkArgs a, int page_shift, int64_t slots)
+{
+    constexpr int kOut = DIM / 32;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, side = lane >> 5;
+    const uint64_t total_units = a.plan[0];
+    if (total_units == 0) return;
+    int64_t id = blockIdx.x;
+    const int o = (int)(id % kOut);
+    id /= kOut;
+    const int head = (int)(id % a.heads);
+    const int64_t slot = id / a.heads;
+    // the sequence with this slot: sequence b owns those from offsets[b] * group / 128 + b on
+    int lo = 0, hi = a.step.sequences - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if ((int64_t)a.step.offsets[mid] * a.group / kRows + mid <= slot) lo = mid;
+        else hi = mid - 1;
+    }
+    const int b = lo;
+    const Job job = job_of(a, a.step.offsets[b], a.step.offsets[b + 1], a.step.held[b], page_shift);
+    const int64_t block = slot - (job.off * a.group / kRows + b);
+    if (block < 0 || block >= job.blocks) return;
+    const int64_t rows = (int64_t)job.n * a.group, row0 = block * kRows + wave * 32, row = row0 + col;
+    if (row0 >= rows) return;
+    const Ranges ranges(total_units, a.workgroups);
+    const uint64_t item = a.plan[1 + b] + (uint64_t)head * job.total + units_before(job, block, a.group);
+    const uint64_t last_unit = a.plan[1 + b] + (uint64_t)head * job.total + units_before(job, block + 1, a.group) - 1;
+    const uint32_t first = ranges.of(item), last = ranges.of(last_unit);
+    if (first == last) return;                           // written already
+    const int64_t places = (int64_t)a.workgroups * 2 * kWaves;
+    const floatx4 *const x = (const floatx4 *)a.partial;
+    const floatx2 *const m = (const floatx2 *)(a.partial + places * (32 * DIM));
+    // the first range has it in its second place, the others in their first ones
+    const auto place = [&](uint32_t r) { return ((int64_t)r * 2 + (r == first)) * kWaves + wave; };
+    float best = -FLT_MAX;
+    for (uint32_t r = first; r <= last; ++r) best = fmaxf(best, m[place(r) * 32 + col][0]);
+    floatx4 sum[4];
+    float total = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (uint32_t r = first; r <= last; ++r) {
+        const floatx2 one = m[place(r) * 32 + col];
+        const float w = __builtin_amdgcn_exp2f(one[0] - best) * one[1];
+        total += w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const floatx4 y = x[place(r) * (32 * DIM / 4) + (o * 4 + i) * 64 + lane];
+            if (w != 0.0f) sum[i] += y * w;
+        }
+    }
+    if (row >= rows) return;
+    const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+    const int64_t q = row / a.group;
+    uint16_t *y = (uint16_t *)a.out.ptr + (job.off + q) * a.out.token + (head * a.group + (int)(row - q * a.group)) * a.out.head + o * 32 + 4 * side;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        *(uintx2 *)(y + 8 * i) = uintx2{narrow2<BF16>(sum[i][0] * inv, sum[i][1] * inv), narrow2<BF16>(sum[i][2] * inv, sum[i][3] * inv)};
+}
+
+int64_t slots_of(int64_t tokens, int group, int sequences) { return tokens * group / kRows + sequences; }
+
+template <int DIM, bool FP8, bool BF16>
+hipError_t chunk(const ChunkArgs &a, hipStream_t stream)
+{
+    const int shift = a.cache.page == 16 ? 4 : a.cache.page == 32 ? 5 : 6;
+    const int64_t slots = slots_of(a.step.tokens, a.group, a.step.sequences), joins = slots * a.heads * (DIM / 32);
+    if (!launchable(joins, 64 * kWaves)) return kTooLarge;               // before anything is
+    const hipError_t e = launch_many(k_chunk_attention<DIM, FP8, BF16>, a.workgroups, 64 * kWaves, stream, a, shift);
+    if (e != hipSuccess || a.workgroups == 1) return e;
+    return launch_many(k_chunk_join<DIM, BF16>, joins, 64 * kWaves, stream, a, shift, slots);
+}
+
+template <int DIM>
+hipError_t chunk_of(const ChunkArgs &a, hipStream_t stream)
+{
+    if (a.fp8) return a.bf16 ? chunk<DIM, true, true>(a, stream) : chunk<DIM, true, false>(a, stream);
+    return a.bf16 ? chunk<DIM, false, true>(a, stream) : chunk<DIM, false, false>(a, stream);
+}
+
+}  // namespace
+
+// Two workgroups for each of 256 compute units, or fewer where the announced lengths cannot make so many ranges
+int chunk_workgroups(int64_t tokens, int sequences, int heads, int group, int dim, int64_t longest)
+{
+    const double units = (double)slots_of(tokens, group, sequences) * heads * ((double)longest / kTokens + 2);
+    const double most = units / kLeast + 1;
+    return most < 512 ? (int)most : 512;
+}
+
+size_t chunk_workspace(int workgroups, int sequences, int dim)
+{
+    return ((size_t)sequences + 1 + 1) / 2 * 16 + (workgroups > 1 ? (size_t)workgroups * 2 * kRows * (dim + 2) * sizeof(float) : 0);
+}
+
+hipError_t launch_chunk_attention(const ChunkArgs &a, hipStream_t stream)
+{
+    return a.dim == 64 ? chunk_of<64>(a, stream) : chunk_of<128>(a, stream);
+}
+
+}  // namespace fc

@@ -13,63 +13,14 @@
 // Matrix instructions and the exponentials between them bound it, at a clock that falls under this load (1.5 to 1.7 GHz counted):
 // 16384 tokens, 16 heads, causal, bfloat16: 965 to 1036 us by card, 1.14 to 1.06 PFLOP/s, where a library's 16384^3 product reaches 1.31.
 // 11 ragged prompts, 8191 tokens, 40 heads, binary16: 129 to 136 us, where edges and what surrounds the loop weigh more.
-#include "fc_attn.hpp"
+#include "fc_attn_tiles.hpp"
 
 namespace fc {
 namespace {
 
-typedef short shortx4 __attribute__((ext_vector_type(4)));
-
 // in powers of two: how far a tile's largest score may be from the unit; where it is put; how far below the row's largest the unit may go
 template <bool BF16> constexpr float kSlack = BF16 ? 8.0f : 10.0f;
 constexpr float kBias = 5.0f, kReach = 60.0f;
-
-// what the number of a 16-byte unit is exchanged by in row t of a tile: 16 rows of K, read one unit each, and four of V, read 64 bytes
-// each, take every bank once
-template <int DIM, bool K> __device__ __forceinline__ int swizzle(int t)
-{
-    if (K) return DIM == 128 ? t & 15 : (t >> 1) & 7;
-    return DIM == 128 ? 4 * (t & 3) : 4 * ((t >> 1) & 1);
-}
-
-// buffer resource of 16 rows, of which [0, left) are there; everything else reads as zero
-__device__ __forceinline__ uintx4 rows16(const uint16_t *base, int stride, int left, int dim)
-{
-    const int last = left < 16 ? left - 1 : 15;
-    return resource(base, last < 0 ? 0u : (uint32_t)(last * stride + dim) * 2u);
-}
-
-// How a wavefront brings 16 rows of a tile to LDS, 1 KB at a time: where in memory each lane finds its 16 bytes
-template <int DIM, bool K>
-struct Rows16 {
-    static constexpr int kPieces = 16 * DIM * 2 / 1024;
-    int offset[kPieces];
-
-    __device__ __forceinline__ Rows16(int lane, int stride)
-    {
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const int at = i * 1024 + lane * 16, row = at / (2 * DIM), unit = at % (2 * DIM) / 16;
-            offset[i] = row * stride * 2 + (unit ^ swizzle<DIM, K>(row)) * 16;
-        }
-    }
-    __device__ __forceinline__ void load(uintx4 rsrc, const uint8_t *lds) const
-    {
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i) load_to_lds<false>(rsrc, offset[i], lds_address(lds) + i * 1024);
-    }
-};
-
-__device__ __forceinline__ uintx2 transposed(const uint8_t *p)
-{
-    return __builtin_bit_cast(uintx2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4 *)p));
-}
-
-template <int N>
-__device__ __forceinline__ void wait_vm()
-{
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
 
 // The sequence that has work unit u (see find_sequence), its first token and the next one's.  One read for 64 sequences instead of one
 // behind the other.

@@ -43,6 +43,7 @@ namespace {
     X(fc_allreduce_sim) X(fc_allreduce_sim_sym) X(fc_allreduce_sim_fp8) X(fc_allreduce_sim_cmeta)                    \
     X(fc_allreduce_sim_rot) X(fc_allreduce_sim_workspace_bytes)                                                      \
     X(fc_rotary) X(fc_cache_append) X(fc_cache_attention_workspace_bytes) X(fc_cache_attention) X(fc_prompt_attention) \
+    X(fc_chunk_attention_workspace_bytes) X(fc_chunk_attention)                                                      \
     X(fc_pages_fork) X(fc_pages_reserve_workspace_bytes) X(fc_pages_reserve) X(fc_pages_compact_workspace_bytes) X(fc_pages_compact)     \
     X(fc_cache_copy) X(fc_rms_norm) X(fc_rms_norm_quantize)
 
@@ -712,6 +713,52 @@ PyObject *prompt_attention(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     END_HANDLE_TH_ERRORS
 }
 
+// (q, k, v, cache, pages, offsets, held, longest, quantizer, scale, out, workspace)
+PyObject *chunk_attention(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    HANDLE_TH_ERRORS
+    if (n_args != 12 || !plain_context()) return fallback();
+    const int device = device_of(a[0]);
+    Activation q, k, v, y;
+    PagedStep s;
+    int64_t longest, quantizer;
+    float scale;
+    if (device < 0 || !activation(a[0], at::ScalarType::Undefined, device, q) || !activation(a[1], q.t->scalar_type(), device, k) ||
+        !activation(a[2], q.t->scalar_type(), device, v) || !v.like(k) || !s.take(a[3], a[4], a[5], a[6], device) || q.dim() != s.dim ||
+        k.dim() != s.dim || k.heads() != s.heads || k.tokens() != q.tokens() || q.heads() % s.heads != 0 || !integer(a[7], longest) ||
+        !integer(a[8], quantizer) || !softmax_scale(a[9], q.dim(), scale))
+        return fallback();
+    const int64_t tokens = q.tokens();
+    const int group = (int)(q.heads() / s.heads), type = type_code(q);
+    const size_t need = lib.fc_chunk_attention_workspace_bytes(tokens, (int)s.sequences, (int)s.heads, group, (int)s.dim, longest);
+    const at::Tensor *ws = nullptr;
+    if (a[11] != Py_None) {
+        ws = plain(a[11], at::kByte, device);
+        if (!ws || (size_t)ws->numel() < need) return fallback();
+    }
+    at::Tensor own, own_ws;
+    if (need == 0 || !result_rows(a[10], q, device, own, y)) return fallback();
+    if (!ws) {
+        own_ws = empty({(int64_t)need}, at::kByte, *q.t);
+        ws = &own_ws;
+    }
+    void *space = ws->data_ptr(), *stream = stream_of(device);
+    const size_t bytes = (size_t)ws->numel();
+    const void *kc = s.k->data_ptr(), *vc = s.v->data_ptr();
+    const float *ks = (const float *)s.ks->data_ptr(), *vs = (const float *)s.vs->data_ptr();
+    const int32_t *pages = (const int32_t *)s.pages->data_ptr(), *offsets = (const int32_t *)s.offsets->data_ptr(),
+                  *held = (const int32_t *)s.held->data_ptr();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = lib.fc_chunk_attention(q.ptr, q.token, q.head, k.ptr, k.token, k.head, v.ptr, v.token, v.head, tokens, (int)s.heads, group, (int)s.dim, type,
+                                (int)quantizer, kc, vc, ks, vs, s.count, (int)s.page, pages, (int)s.width, offsets, held, (int)s.sequences, longest,
+                                scale, y.ptr, y.token, y.head, space, bytes, stream);
+    Py_END_ALLOW_THREADS
+    if (!done(rc, "fc_chunk_attention")) return nullptr;
+    return wrapped(a[10], own);
+    END_HANDLE_TH_ERRORS
+}
+
 // ---- norm.py's calls ----
 
 // A [tokens, hidden] activation as the C ABI takes it
@@ -1067,7 +1114,7 @@ PyMethodDef methods[] = {
     FC_METHOD("allreduce_sim_rot", allreduce<kRot>),
     FC_METHOD("rotary", rotary), FC_METHOD("cache_append", cache_append), FC_METHOD("cache_attention", cache_attention),
     FC_METHOD("prompt_attention", prompt_attention),
-    FC_METHOD("rms_norm", rms_norm), FC_METHOD("rms_norm_quantize", rms_norm_quantize),
+    FC_METHOD("chunk_attention", chunk_attention), FC_METHOD("rms_norm", rms_norm), FC_METHOD("rms_norm_quantize", rms_norm_quantize),
     FC_METHOD("pages_fork", pages_fork), FC_METHOD("pages_reserve", pages_reserve), FC_METHOD("pages_compact", pages_compact),
     FC_METHOD("cache_copy", cache_copy),
     {nullptr, nullptr, 0, nullptr},

@@ -127,3 +127,29 @@ def test_calls_are_launched_up_to_what_the_runtime_takes():
             ("fc_pages_compact", [P, 1 << 12, 1 << 20, P, 8, P, P, P, P, P, P, 1 << 34, 0])]
     for call, (rc, seen) in zip(over, launched(*over)):
         assert rc == -4 and not seen, (call, rc, seen)
+
+
+def chunk(L, q=P, k=P, v=P, tokens=4, heads=2, group=2, dim=64, type=0, quantizer=1, cache=P, scales=P, pages=4, page=16, pt=P, width=2, offsets=P, held=P, sequences=1,
+          longest=64, scale=0.1, out=P, ws=P, bytes=1 << 40, vt=128):
+    return L.fc_chunk_attention(q, 256, 64, k, 128, 64, v, vt, 64, tokens, heads, group, dim, type, quantizer, cache, cache, scales, scales, pages, page, pt, width,
+                                offsets, held, sequences, longest, scale, out, 256, 64, ws, bytes, None)
+
+
+def test_chunk_attention_argument_checks(L):
+    assert chunk(L, type=2) == chunk(L, quantizer=0) == chunk(L, quantizer=3) == -8
+    assert chunk(L, dim=256) == chunk(L, dim=32) == chunk(L, heads=0) == chunk(L, group=0) == chunk(L, group=40000) == chunk(L, longest=0) == chunk(L, tokens=-1) == -4
+    assert chunk(L, page=8) == chunk(L, pages=0) == chunk(L, width=0) == chunk(L, sequences=0) == chunk(L, vt=1 << 25) == chunk(L, tokens=(1 << 31) - 1) == -4
+    assert chunk(L, scale=0.0) == chunk(L, scale=-1.0) == chunk(L, scale=float("nan")) == -4
+    for name in ("q", "k", "v", "cache", "scales", "pt", "offsets", "held", "out"):
+        assert chunk(L, **{name: None}) == -1, name
+    assert chunk(L, q=P + 2) == chunk(L, vt=12) == chunk(L, cache=P + 8) == chunk(L, ws=P + 4) == -5
+    need = L.fc_chunk_attention_workspace_bytes(4, 1, 2, 2, 64, 64)
+    assert need > 0 and need % 4 == 0
+    assert chunk(L, bytes=need - 1) == chunk(L, ws=None) == -6
+    assert chunk(L, tokens=0, q=None, k=None, v=None, out=None, cache=None, ws=None) == 0
+    for bad in ((4, 1, 2, 2, 256, 64), (4, 1, 0, 2, 64, 64), (-1, 1, 2, 2, 64, 64), (4, 1, 2, 2, 64, 0)):
+        assert L.fc_chunk_attention_workspace_bytes(*bad) == 0
+    # announced lengths are bounds, up to the largest that their types hold
+    for sequences, heads in ((256, 8), (1, 1), (65536, 64)):
+        needs = [L.fc_chunk_attention_workspace_bytes(1 << 20, sequences, heads, 8, 128, longest) for longest in (1 << 20, 1 << 26, (1 << 31) - 1)]
+        assert needs[0] > 0 and needs == [needs[0]] * 3
