@@ -13,12 +13,14 @@
 //   largest score up and down when that is kSlack away, and the largest is put at 2^kBias (kReach below the row's largest at most).
 // All work of the call, in units of a tile of 64 tokens for 128 rows, is cut into equal ranges, one a workgroup: contexts of any lengths
 // end together.  Rows that were cut are joined by a second kernel, from results that are normalised.
+#include <type_traits>
+
 #include "fc_attn_tiles.hpp"
 
 namespace fc {
 namespace {
 
-constexpr int kTokens = 64, kRows = 128, kWaves = 4;
+constexpr int kTokens = 64, kRows = 128, kWaves = 4, kAhead = 4;
 constexpr int kLeast = 2;               // units of a range
 template <bool BF16> constexpr float kSlack = BF16 ? 8.0f : 10.0f;
 constexpr float kBias = 4.0f, kReach = 36.0f;
@@ -101,7 +103,28 @@ __device__ __forceinline__ uintx2 sixteen(uint32_t w)
     else if constexpr (FP8)
         return uintx2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false)),
                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true))};
-    else return uintx2{narrow2<true>((float)(int8_t)w, (float)(int8_t)(w >> 8)), narrow2<true>((float)(int8_t)(w >> 16), (float)(int8_t)(w >> 24))};
+    else {
+        asm volatile("" : "+v"(w));                      // (one word after the other: the compiler would take all of a lane's together)
+        return uintx2{narrow2<true>((float)(int8_t)w, (float)(int8_t)(w >> 8)), narrow2<true>((float)(int8_t)(w >> 16), (float)(int8_t)(w >> 24))};
+    }
+}
+
+// N matrix instructions, AHEAD of which have their operands from LDS on the way: read(i) is the operand of the i-th, use(i, operand) executes it, and
+// beside(i) is other work of the wavefront that is issued while the matrix unit is at the i-th
+template <int N, int AHEAD, typename R, typename U, typename B>
+__device__ __forceinline__ void pipelined(const R &read, const U &use, const B &beside)
+{
+    uintx4 operand[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) operand[i] = read(i);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        __builtin_amdgcn_sched_barrier(0);
+        use(i, operand[i % AHEAD]);
+        if (i + AHEAD < N) operand[i % AHEAD] = read(i + AHEAD);
+        beside(i);
+    }
+    __builtin_amdgcn_sched_barrier(0);
 }
 
 template <int DIM, bool FP8, bool BF16>
@@ -226,63 +249,65 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_chunk_attention(ChunkArgs a,
                 vs = a.cache.v_scales[(int64_t)id * a.heads + head];
             }
         };
-        int page = 0, page_next = 0;
+        // where they are in the cache
+        const auto place_of = [&](int id) {
+            if (id < 0 || id >= a.cache.pages) id = 0;
+            return ((((uint64_t)id * a.heads + head) << page_shift) + (lane * 16 & ((1 << page_shift) - 1))) * DIM;
+        };
+        uint64_t place = 0;
+        int page_next = 0;
         float ks_next = 0.0f, vs_next = 0.0f;
         uintx4 code_k[kFetch], code_v[kFetch];
         // the codes of tile t, from memory
         const auto fetch = [&](int t) {
             const int in = t & 15;
             if (t != tile0 && in == 0) {
-                page = page_next;
+                place = place_of(page_next);
                 page_next = pages_of((t >> 4) + 1);
             }
             if (in == 8) scales_of((t >> 4) + 1, page_next, ks_next, vs_next);
-            const int thread = afresh(threadIdx.x);
+            const int thread = afresh(threadIdx.x), mine = thread / kPieces % 16 * DIM + thread % kPieces * 16;
 #pragma unroll
             for (int i = 0; i < kFetch; ++i) {
-                const int piece = (i * (64 / kFetch) + wave * (64 / kPieces)) / 16;      // of 16 tokens, the wavefront's
-                int id = __builtin_amdgcn_readlane(page, in * 4 + piece);
-                if (id < 0 || id >= a.cache.pages) id = 0;
-                const int slot = (t * kTokens + piece * 16) & ((1 << page_shift) - 1);
-                const int64_t place = ((((int64_t)id * a.heads + head) << page_shift) + slot) * DIM;
-                const int mine = thread / kPieces % 16 * DIM + thread % kPieces * 16;
-                code_k[i] = *(const uintx4 *)(a.cache.k + place + mine);
-                code_v[i] = *(const uintx4 *)(a.cache.v + place + mine);
+                const uint64_t at_page = lane_u64(place, in * 4 + (i * (64 / kFetch) + wave * (64 / kPieces)) / 16);       // the wavefront's piece
+                code_k[i] = *(const uintx4 *)(a.cache.k + at_page + mine);
+                code_v[i] = *(const uintx4 *)(a.cache.v + at_page + mine);
             }
         };
-        // and into LDS
-        const auto convert = [&](int t, uint8_t *lds_k, uint8_t *lds_v) {
-            const int thread = afresh(threadIdx.x), code_row = thread / kPieces, code_unit = thread % kPieces;
+        // and into LDS, 8 codes at a time
+        const auto clear_rest = [&](int t) {
+            if ((t + 1) * kTokens > job.held) {              // whatever the page holds beyond them
+                const int code_row = afresh(threadIdx.x) / kPieces;
 #pragma unroll
-            for (int i = 0; i < kFetch; ++i) {
-                const int r = i * (64 / kFetch) + code_row;
-                if (t * kTokens + r >= job.held) code_k[i] = code_v[i] = uintx4{0, 0, 0, 0};     // whatever the page holds there
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uintx2 k0 = sixteen<FP8, BF16>(code_k[i][2 * h]), k1 = sixteen<FP8, BF16>(code_k[i][2 * h + 1]);
-                    *(uintx4 *)(lds_k + r * kRow + ((2 * code_unit + h) ^ swizzle<DIM, true>(r & 31)) * 16) = uintx4{k0[0], k0[1], k1[0], k1[1]};
-                }
-                __builtin_amdgcn_sched_barrier(0);           // (no more registers at a time)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uintx2 v0 = sixteen<FP8, BF16>(code_v[i][2 * h]), v1 = sixteen<FP8, BF16>(code_v[i][2 * h + 1]);
-                    *(uintx4 *)(lds_v + r * kRow + ((2 * code_unit + h) ^ swizzle<DIM, false>(r & 15)) * 16) = uintx4{v0[0], v0[1], v1[0], v1[1]};
-                }
-                __builtin_amdgcn_sched_barrier(0);
+                for (int i = 0; i < kFetch; ++i)
+                    if (t * kTokens + i * (64 / kFetch) + code_row >= job.held) code_k[i] = code_v[i] = uintx4{0, 0, 0, 0};
             }
         };
-        const auto bring = [&](int t, int to) {
-            if (t < cached) {
-                convert(t, tiles[to], tiles[to + 1]);
-                if (t + 1 < cached && t + 1 < tile1) fetch(t + 1);
-            } else {
-                const int t0 = (t - cached) * kTokens + 16 * wave;
-                const int mine = afresh(lane);
-                const Rows16<DIM, true> rows_k(mine, stride_k);
-                const Rows16<DIM, false> rows_v(mine, stride_v);
-                rows_k.load(rows16(k + (int64_t)t0 * stride_k, stride_k, n - t0, DIM), tiles[to] + wave * 16 * kRow);
-                rows_v.load(rows16(v + (int64_t)t0 * stride_v, stride_v, n - t0, DIM), tiles[to + 1] + wave * 16 * kRow);
-            }
+        struct Places {
+            int k, v;
+        };
+        const auto code_places = [&](int to) {
+            const int thread = afresh(threadIdx.x), r = thread / kPieces, u = 2 * (thread % kPieces);
+            return Places{to * kTile + r * kRow + (u ^ swizzle<DIM, true>(r & 31)) * 16, (to + 1) * kTile + r * kRow + (u ^ swizzle<DIM, false>(r & 15)) * 16};
+        };
+        const auto convert = [&](int piece, const Places &at_lds) {
+            const int i = piece >> 2, h = piece & 1;
+            const uintx4 w = piece & 2 ? code_v[i] : code_k[i];
+            const uintx2 x = sixteen<FP8, BF16>(w[2 * h]), y = sixteen<FP8, BF16>(w[2 * h + 1]);
+            *(uintx4 *)(&tiles[0][0] + ((piece & 2 ? at_lds.v : at_lds.k) ^ (h << 4)) + i * (64 / kFetch) * kRow) = uintx4{x[0], x[1], y[0], y[1]};
+        };
+        const auto convert_all = [&](int to) {
+            const Places at_lds = code_places(to);
+#pragma unroll
+            for (int c = 0; c < 4 * kFetch; ++c) convert(c, at_lds);
+        };
+        // new tokens' tile t, straight to LDS
+        const auto load_new = [&](int t, int to) {
+            const int t0 = (t - cached) * kTokens + 16 * wave, mine = afresh(lane);
+            const Rows16<DIM, true> rows_k(mine, stride_k);
+            const Rows16<DIM, false> rows_v(mine, stride_v);
+            rows_k.load(rows16(k + (int64_t)t0 * stride_k, stride_k, n - t0, DIM), tiles[to] + wave * 16 * kRow);
+            rows_v.load(rows16(v + (int64_t)t0 * stride_v, stride_v, n - t0, DIM), tiles[to + 1] + wave * 16 * kRow);
         };
 
         floatx16 acc[kOut];
@@ -294,16 +319,21 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_chunk_attention(ChunkArgs a,
 
         floatx16 s[2];
         uintx4 pf[4];
-        const auto scores = [&](const uint8_t *lds_k) {
+        // convert_next: the next tile's codes are converted beside it
+        const auto scores = [&](const uint8_t *lds_k, auto convert_next, int to) {
             const int mine = afresh(at_k);
+            Places at_lds = {0, 0};
+            if constexpr (decltype(convert_next)::value) at_lds = code_places(to);
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[h][r] = 0.0f;
-#pragma unroll
-            for (int j = 0; j < kSteps; ++j)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) s[h] = mma32<BF16>(*(const uintx4 *)(lds_k + (mine ^ (j << 5)) + h * 32 * kRow), qf[j], s[h]);
+            pipelined<2 * kSteps, kAhead>([&](int i) { return *(const uintx4 *)(lds_k + (mine ^ (i / 2 << 5)) + (i & 1) * 32 * kRow); },
+                                          [&](int i, uintx4 x) { s[i & 1] = mma32<BF16>(x, qf[i / 2], s[i & 1]); },
+                                          [&](int i) {
+                                              if constexpr (decltype(convert_next)::value)
+                                                  if (i & 1) convert(i >> 1, at_lds);
+                                          });
         };
         // tokens of the tile from `first` on, and before `sees`, are seen
         const auto mask = [&](int first, int sees) {
@@ -339,7 +369,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_chunk_attention(ChunkArgs a,
             raise = __builtin_amdgcn_logf(c);            // log2
             back = 1.0f / c;
         };
-        const auto weights = [&](int piece) {
+        const auto raise_maxima = [&](int piece) {
             float fk[4], up[4];
 #pragma unroll
             for (int p = 0; p < 4; ++p) {
@@ -375,30 +405,33 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_chunk_attention(ChunkArgs a,
 #pragma unroll
                 for (int o = 0; o < kOut; ++o) acc[o] *= shrink;
             }
-#pragma unroll
-            for (int p = 0; p < 4; ++p) {
-                const float add = up[p] - top;
-                float part = 0.0f;
-#pragma unroll
-                for (int r = 0; r < 8; r += 2) {
-                    const float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[p / 2][8 * (p & 1) + r], fk[p], add));
-                    const float w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[p / 2][8 * (p & 1) + r + 1], fk[p], add));
-                    part += w0 + w1;
-                    pf[p][r / 2] = narrow2<BF16>(w0, w1);
-                }
-                total = __builtin_fmaf(part, lane_f(back, piece + p), total);
-            }
         };
-        const auto add_values = [&](const uint8_t *lds_v) {
+        // The weights of 16 tokens are made beside the products of the 16 before them
+        const auto add_values = [&](const uint8_t *lds_v, int piece) {
             const int mine = afresh(at_v);
+            float part = 0.0f;
+            const auto weigh = [&](int p, int pair) {
+                const float fk = lane_f(steep, piece + p), add = lane_f(raise, piece + p) - top;
+                const int r = 8 * (p & 1) + 2 * pair;
+                const float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[p / 2][r], fk, add)), w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[p / 2][r + 1], fk, add));
+                part = pair ? part + (w0 + w1) : w0 + w1;
+                pf[p][pair] = narrow2<BF16>(w0, w1);
+                if (pair == 3) total = __builtin_fmaf(part, lane_f(back, piece + p), total);
+            };
 #pragma unroll
-            for (int m = 0; m < 4; ++m)
-#pragma unroll
-                for (int o = 0; o < kOut; ++o) {
-                    const uint8_t *p = lds_v + (mine ^ (o << 6)) + m * 16 * kRow;
+            for (int pair = 0; pair < 4; ++pair) weigh(0, pair);
+            pipelined<4 * kOut, kAhead>(
+                [&](int i) {
+                    const uint8_t *p = lds_v + (mine ^ (i % kOut << 6)) + i / kOut * 16 * kRow;
                     const uintx2 lo = transposed(p), hi = transposed(p + 8 * kRow);
-                    acc[o] = mma32<BF16>(uintx4{lo[0], lo[1], hi[0], hi[1]}, pf[m], acc[o]);
-                }
+                    return uintx4{lo[0], lo[1], hi[0], hi[1]};
+                },
+                [&](int i, uintx4 x) { acc[i % kOut] = mma32<BF16>(x, pf[i / kOut], acc[i % kOut]); },
+                [&](int i) {
+                    if (i < 3 * kOut)
+#pragma unroll
+                        for (int pair = i % kOut * 4 / kOut; pair < (i % kOut + 1) * 4 / kOut; ++pair) weigh(i / kOut + 1, pair);
+                });
         };
         // In a tile that not all rows see whole, an infinity or NaN among the new values would be NaN times the weight of 0 of those that do
         // not.  Such values are added to the rows that see them, and taken out of the tile.
@@ -433,14 +466,23 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_chunk_attention(ChunkArgs a,
         };
         const auto compute = [&](int t, int from) {
             uint8_t *const lds_k = tiles[from], *const lds_v = tiles[from + 1];
-            const bool code = t < cached;
+            const bool code = t < cached, next = t + 1 < tile1, next_code = next && t + 1 < cached;
             const int t0 = code ? t * kTokens : (t - cached) * kTokens;
             const bool astray = !code && (t0 + kTokens - 1 > first_query || t0 < skip) && any_not_finite(lds_v);      // the same for all wavefronts
             const bool sees = !idle && (code || t0 <= wave_last);
+            if (next && !next_code) load_new(t + 1, from ^ 2);
+            if (next_code) clear_rest(t + 1);
+            if (!sees) {
+                if (next_code) convert_all(from ^ 2);
+            } else if (next_code) {
+                scores(lds_k, std::true_type(), from ^ 2);
+            } else {
+                scores(lds_k, std::false_type(), 0);
+            }
+            if (next_code && t + 2 < cached && t + 2 < tile1) fetch(t + 2);
             if (sees) {
-                scores(lds_k);
                 if (code ? t0 + kTokens > job.held : t0 + kTokens - 1 > wave_first || t0 < skip) mask(code ? 0 : skip - t0, (code ? job.held : query + 1) - t0);
-                weights((t & 15) * 4);
+                raise_maxima((t & 15) * 4);
             }
             if (astray) {
                 if (sees) add_not_finite(lds_v, t0);
@@ -453,22 +495,26 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_chunk_attention(ChunkArgs a,
                 }
                 asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
             }
-            if (sees) add_values(lds_v);
+            if (sees) add_values(lds_v, (t & 15) * 4);
         };
 
         if (tile0 < cached) {
             const int batch = tile0 >> 4;
-            page = pages_of(batch);
+            const int page = pages_of(batch);
+            place = place_of(page);
             page_next = pages_of(batch + 1);
             float ks, vs;
             scales_of(batch, page, ks, vs);
             scales_of(batch + 1, page_next, ks_next, vs_next);
             turn_to(ks, vs);
             fetch(tile0);
+            clear_rest(tile0);
+            convert_all(0);
+            if (tile0 + 1 < cached && tile0 + 1 < tile1) fetch(tile0 + 1);
         } else {
             turn_to(1.0f, 1.0f);
+            load_new(tile0, 0);
         }
-        bring(tile0, 0);
         // the queries are here before the loop, where waiting for them would wait for the tiles that are loaded ahead
 #pragma unroll
         for (int j = 0; j < kSteps; ++j) asm volatile("" : "+v"(qf[j]));
@@ -479,7 +525,6 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_chunk_attention(ChunkArgs a,
                 if (t < cached) turn_to(ks_next, vs_next);
                 else turn_to(1.0f, 1.0f);
             }
-            if (t + 1 < tile1) bring(t + 1, from ^ 2);
             compute(t, from);
             arrived();
         }
