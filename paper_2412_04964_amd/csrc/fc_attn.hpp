@@ -97,14 +97,15 @@ struct ChunkArgs {
     Rows q, k, v, out;
     Step step;
     Cache cache;
-    // of the items that more than one workgroup has a part of: [workgroups, 2, 128 rows] of normalised results, then maxima and weights
+    // of the items that more than one workgroup has a part of: [workgroups, 2, rows of a workgroup] of normalised results, then maxima and weights
     float *partial;
     uint64_t *plan;                                     // how many units there are, and where each sequence's begin
     float scale;
-    int heads, group, dim, fp8, bf16, workgroups;
+    int heads, group, dim, fp8, bf16;
+    int waves, workgroups;                              // chunk_plan's: wavefronts of a workgroup, with 32 rows each; ranges of the work
 };
-int chunk_workgroups(int64_t tokens, int sequences, int heads, int group, int dim, int64_t longest);
-size_t chunk_workspace(int workgroups, int sequences, int dim);
+void chunk_plan(int64_t tokens, int sequences, int heads, int group, int64_t longest, ChunkArgs *a);
+size_t chunk_workspace(const ChunkArgs &a, int sequences, int dim);
 hipError_t launch_chunk_attention(const ChunkArgs &a, hipStream_t stream);
 
 // The norm of rows [tokens, hidden]; strides in elements

@@ -260,7 +260,9 @@ int fc_prompt_attention(const void *q, int64_t q_token_stride, int64_t q_head_st
 size_t fc_chunk_attention_workspace_bytes(int64_t tokens, int sequences, int heads, int group, int dim, int64_t longest)
 {
     if (check_attention(tokens, sequences, heads, group, dim, 1, longest) != FC_OK || dim == 256) return 0;
-    return fc::chunk_workspace(fc::chunk_workgroups(tokens, sequences, heads, group, dim, longest), sequences, dim);
+    fc::ChunkArgs a;
+    fc::chunk_plan(tokens, sequences, heads, group, longest, &a);
+    return fc::chunk_workspace(a, sequences, dim);
 }
 
 int fc_chunk_attention(const void *q, int64_t q_token_stride, int64_t q_head_stride, const void *k, int64_t k_token_stride, int64_t k_head_stride,
@@ -288,8 +290,8 @@ int fc_chunk_attention(const void *q, int64_t q_token_stride, int64_t q_head_str
     const double tiles = (double)table_width * page / 64 + (double)tokens / 64 + 2, blocks = (double)tokens * group / 128 + sequences;
     if (tiles * blocks * heads >= 0x1p62) return FC_ERR_SHAPE;
     fc::ChunkArgs a;
-    a.workgroups = fc::chunk_workgroups(tokens, sequences, heads, group, dim, longest);
-    const size_t need = fc::chunk_workspace(a.workgroups, sequences, dim);
+    fc::chunk_plan(tokens, sequences, heads, group, longest, &a);
+    const size_t need = fc::chunk_workspace(a, sequences, dim);
     if (!workspace || workspace_bytes < need) return FC_ERR_WORKSPACE;
     if (!aligned16(workspace)) return FC_ERR_ALIGN;
     a.q = rows(q, q_token_stride, q_head_stride);

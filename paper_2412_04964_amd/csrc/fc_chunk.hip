@@ -20,27 +20,37 @@
 namespace fc {
 namespace {
 
-constexpr int kTokens = 64, kRows = 128, kWaves = 4, kAhead = 4;
+constexpr int kTokens = 64, kAhead = 6;
 constexpr int kLeast = 2;               // units of a range
+constexpr int rows_of(int waves) { return 32 * waves; }                  // of a workgroup
 template <bool BF16> constexpr float kSlack = BF16 ? 8.0f : 10.0f;
 constexpr float kBias = 4.0f, kReach = 36.0f;
 // how far below the largest unit so far the unit may go, and what a scale may be of it
 constexpr float kDeep = 0x1p-30f, kFaint = 0x1p-36f;
 
-// What there is to do for one sequence, for each key/value head: `blocks` of 128 rows, each over `cached` tiles and those new ones that it sees
+// What there is to do for one sequence, for each key/value head: `blocks` of a workgroup's rows, each over `cached` tiles and those new ones that it sees
 struct Job {
     int64_t off, blocks, total;                          // total: units of all blocks
     int n, held, skip, cached, fresh;                    // new tokens; tokens in the cache; new ones without a place; tiles of either kind
 };
 
-// units of new tokens of the first j blocks: block i - 1 sees the tokens before ceil(128 i / group), ceil(2 i / group) tiles of them
+// Units of new tokens of the first j blocks of ROWS: block i - 1 sees the tokens before ceil(ROWS i / group), so ceil(c i / group) tiles of them, c =
+// ROWS / 64.  Every `group` blocks that is c more, and in between one more from each i > k group / c on.
+template <int ROWS>
 __device__ __forceinline__ int64_t fresh_units(int64_t j, int group)
 {
-    const int64_t q = j / group;
-    const int r = (int)(j - q * group), over = r - group / 2;
-    return group * q * (q - 1) + q * (group + (group + 1) / 2) + 2 * q * r + r + (over > 0 ? over : 0);
+    constexpr int c = ROWS / kTokens;
+    const auto some = [&](int64_t r) {
+        int64_t sum = r;
+#pragma unroll
+        for (int k = 1; k < c; ++k) sum += r > k * group / c ? r - k * group / c : 0;
+        return sum;
+    };
+    const int64_t q = j / group, r = j - q * group;
+    return c * group * q * (q - 1) / 2 + q * some(group) + c * q * r + some(r);
 }
 
+template <int ROWS>
 __device__ __forceinline__ Job job_of(const ChunkArgs &a, int off, int next, int held, int page_shift)
 {
     Job j;
@@ -51,12 +61,16 @@ __device__ __forceinline__ Job job_of(const ChunkArgs &a, int off, int next, int
     j.skip = held < 0 ? -(held + 1) < j.n ? -held : j.n : 0;
     j.cached = (int)(((int64_t)j.held + kTokens - 1) / kTokens);
     j.fresh = (int)(((int64_t)j.n + kTokens - 1) / kTokens);
-    j.blocks = ((int64_t)j.n * a.group + kRows - 1) / kRows;
-    j.total = j.blocks ? (j.blocks - 1) * j.cached + fresh_units(j.blocks - 1, a.group) + j.cached + j.fresh : 0;
+    j.blocks = ((int64_t)j.n * a.group + ROWS - 1) / ROWS;
+    j.total = j.blocks ? (j.blocks - 1) * j.cached + fresh_units<ROWS>(j.blocks - 1, a.group) + j.cached + j.fresh : 0;
     return j;
 }
 
-__device__ __forceinline__ int64_t units_before(const Job &j, int64_t block, int group) { return block >= j.blocks ? j.total : block * j.cached + fresh_units(block, group); }
+template <int ROWS>
+__device__ __forceinline__ int64_t units_before(const Job &j, int64_t block, int group)
+{
+    return block >= j.blocks ? j.total : block * j.cached + fresh_units<ROWS>(block, group);
+}
 
 // The units of all sequences, one behind the other, cut into ranges that differ by one unit at most; fewer of them where they would have
 // less than kLeast units
@@ -109,32 +123,34 @@ __device__ __forceinline__ uintx2 sixteen(uint32_t w)
     }
 }
 
-// N matrix instructions, AHEAD of which have their operands from LDS on the way: read(i) is the operand of the i-th, use(i, operand) executes it, and
-// beside(i) is other work of the wavefront that is issued while the matrix unit is at the i-th
-template <int N, int AHEAD, typename R, typename U, typename B>
-__device__ __forceinline__ void pipelined(const R &read, const U &use, const B &beside)
+// N matrix instructions whose operands come from LDS: the first AHEAD of them are in `operand`, read(i) is the i-th, and later(j) does what follows
+// behind the last read; use(i, operand) executes an instruction, and beside(i) is other work of the wavefront that is issued while the
+// matrix unit is at it
+template <int N, int AHEAD, typename R, typename L, typename U, typename B>
+__device__ __forceinline__ void pipelined(uintx4 (&operand)[AHEAD], const R &read, const L &later, const U &use, const B &beside)
 {
-    uintx4 operand[AHEAD];
-#pragma unroll
-    for (int i = 0; i < AHEAD; ++i) operand[i] = read(i);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         __builtin_amdgcn_sched_barrier(0);
         use(i, operand[i % AHEAD]);
         if (i + AHEAD < N) operand[i % AHEAD] = read(i + AHEAD);
+        else later(i + AHEAD - N);
         beside(i);
     }
     __builtin_amdgcn_sched_barrier(0);
 }
 
-template <int DIM, bool FP8, bool BF16>
-__global__ void __launch_bounds__(64 * kWaves, 2) k_chunk_attention(ChunkArgs a, int page_shift)
+// W wavefronts have 32 rows each and share the tiles.  Three tiles are in LDS: while one is worked on, the next is whole, and the codes of the one
+// behind that are converted; a barrier in the middle of a tile's work is all that they need.
+template <int DIM, bool FP8, bool BF16, int W>
+__global__ void __launch_bounds__(64 * W, W == 8 ? 2 : 1) k_chunk_attention(ChunkArgs a, int page_shift)
 {
-    constexpr int kSteps = DIM / 16, kOut = DIM / 32, kRow = 2 * DIM, kTile = kTokens * kRow;
+    constexpr int kSteps = DIM / 16, kOut = DIM / 32, kRow = 2 * DIM, kTile = kTokens * kRow, kRows = rows_of(W);
     constexpr int kOutRow = kRow + 16;
-    constexpr int kFetch = DIM / 64, kPieces = DIM / 16;                 // loads of a tile's K or V codes; lanes of a token
-    __shared__ __attribute__((aligned(1024))) uint8_t tiles[4][kTile];
-    static_assert(sizeof(tiles) >= kWaves * 32 * kOutRow, "the results fit the tiles");
+    // A lane loads 16 codes at a time: kLoads of a tile, the first half of them K and the others V (with one load, half of the wavefronts have K)
+    constexpr int kLoads = DIM / (8 * W), kEach = kLoads > 1 ? kLoads / 2 : 1, kPieces = DIM / 16, kRound = kTokens / kEach;
+    __shared__ __attribute__((aligned(1024))) uint8_t tiles[4][2][kTile];       // K and V
+    static_assert(sizeof(tiles) >= W * 32 * kOutRow, "the results fit the tiles");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, side = lane >> 5;
     const int sequences = a.step.sequences, group = a.group;
 
@@ -147,7 +163,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_chunk_attention(ChunkArgs a,
             off = a.step.offsets[c + lane];
             next = a.step.offsets[c + lane + 1];
             held = a.step.held[c + lane];
-            sum += (uint64_t)job_of(a, off, next, held, page_shift).total * a.heads;
+            sum += (uint64_t)job_of<kRows>(a, off, next, held, page_shift).total * a.heads;
             astray |= off < 0 || next < off || next > a.step.tokens;
         }
     // (units of offsets that do not ascend may be more than 64 bits count: none of them is done)
@@ -167,7 +183,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_chunk_attention(ChunkArgs a,
             off = a.step.offsets[c + lane];
             next = a.step.offsets[c + lane + 1];
             held = a.step.held[c + lane];
-            work = (uint64_t)job_of(a, off, next, held, page_shift).total * a.heads;
+            work = (uint64_t)job_of<kRows>(a, off, next, held, page_shift).total * a.heads;
         }
         const uint64_t upto = run + running_sum(work, lane);
         if (blockIdx.x == 0 && wave == 0 && c + lane < sequences) a.plan[1 + c + lane] = upto - work;
@@ -183,7 +199,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_chunk_attention(ChunkArgs a,
 
     // ---- places that do not change ----
     const int stride_k = (int)a.k.token, stride_v = (int)a.v.token;
-    // (Addresses that are a few operations away from the lane's number are made where they are used: the loop has no registers for them.)
+    // (What is a few operations away from the lane's number is made where it is used: the loop has no registers for it.)
     const auto afresh = [](int v) {
         asm volatile("" : "+v"(v));
         return v;
@@ -192,10 +208,11 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_chunk_attention(ChunkArgs a,
     const int v_row = 4 * side + (lane & 15) / 4;
     const int at_v = v_row * kRow + ((((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) ^ swizzle<DIM, false>(v_row)) * 16 + (lane & 1) * 8;
     const float factor = a.scale * 1.4426950408889634f;      // scores in powers of two
-    const auto arrived = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+    const int half = kLoads == 1 ? wave / (W / 2) : 0, code_wave = kLoads == 1 ? wave % (W / 2) : wave;        // half: 1 for wavefronts that have V only
+    const auto code_thread = [&] { return afresh(kLoads == 1 ? threadIdx.x % (32 * W) : threadIdx.x); };
 
     while (at < end) {
-        const Job job = job_of(a, a.step.offsets[b], a.step.offsets[b + 1], a.step.held[b], page_shift);
+        const Job job = job_of<kRows>(a, a.step.offsets[b], a.step.offsets[b + 1], a.step.held[b], page_shift);
         const uint64_t work = (uint64_t)job.total * a.heads;
         if (at >= begins + work) {
             begins += work;
@@ -208,41 +225,39 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_chunk_attention(ChunkArgs a,
         int64_t lo = 0, hi = job.blocks - 1;
         while (lo < hi) {
             const int64_t mid = (lo + hi + 1) >> 1;
-            if (units_before(job, mid, group) <= within) lo = mid;
+            if (units_before<kRows>(job, mid, group) <= within) lo = mid;
             else hi = mid - 1;
         }
-        const int64_t block = lo, before = units_before(job, block, group);
-        const int units = (int)(units_before(job, block + 1, group) - before);
+        const int64_t block = lo, before = units_before<kRows>(job, block, group);
+        const int units = (int)(units_before<kRows>(job, block + 1, group) - before);
         const int tile0 = (int)(within - before);
         const int tile1 = end - at < (uint64_t)(units - tile0) ? tile0 + (int)(end - at) : units;
         at += tile1 - tile0;
         const bool whole = tile0 == 0 && tile1 == units;
-        const int64_t rows = (int64_t)job.n * group, row0 = block * kRows + wave * 32, row = row0 + col;
-        const int n = job.n, cached = job.cached, skip = job.skip;
+        const int64_t rows = (int64_t)job.n * group, row0 = block * kRows + wave * 32;
+        const int n = job.n, held = job.held, cached = job.cached, skip = job.skip, codes_end = cached < tile1 ? cached : tile1;
         const bool idle = row0 >= rows;                  // this wavefront has no rows
-        const int query = (int)((row < rows ? row : rows - 1) / group), query_head = head * group + (int)((row < rows ? row : rows - 1) - (int64_t)query * group);
-        const int first_query = (int)(block * kRows / group);                    // of the workgroup
-        const int wave_first = (int)((row0 < rows ? row0 : rows - 1) / group), wave_last = (int)((row0 + 31 < rows ? row0 + 31 : rows - 1) / group);
 
+        int query;
         uintx4 qf[kSteps];
         {
-            const uint16_t *q = (const uint16_t *)a.q.ptr + (job.off + query) * a.q.token + query_head * a.q.head + side * 8;
+            const int64_t row = row0 + col < rows ? row0 + col : rows - 1;
+            query = (int)(row / group);
+            const uint16_t *q = (const uint16_t *)a.q.ptr + (job.off + query) * a.q.token + (head * group + (int)(row - (int64_t)query * group)) * a.q.head + side * 8;
 #pragma unroll
             for (int j = 0; j < kSteps; ++j) qf[j] = *(const uintx4 *)(q + 16 * j);
         }
-        const uint16_t *k = (const uint16_t *)a.k.ptr + job.off * a.k.token + head * a.k.head;
-        const uint16_t *v = (const uint16_t *)a.v.ptr + job.off * a.v.token + head * a.v.head;
         const int32_t *const table = a.cache.table + (int64_t)b * a.cache.table_width;
 
         // pages of 64 pieces of 16 tokens (16 tiles), one a lane
         const auto pages_of = [&](int batch) {
-            const uint32_t token = ((uint32_t)batch * 64 + lane) * 16;       // (below 2^31 + 2^11)
+            const uint32_t token = ((uint32_t)batch * 64 + afresh(lane)) * 16;       // (below 2^31 + 2^11)
             int id = 0;
-            if (token < (uint32_t)job.held) id = table[token >> page_shift];
+            if (token < (uint32_t)held) id = table[token >> page_shift];
             return id;
         };
         const auto scales_of = [&](int batch, int id, float &ks, float &vs) {
-            const bool there = ((uint32_t)batch * 64 + lane) * 16 < (uint32_t)job.held && id >= 0 && id < a.cache.pages;
+            const bool there = ((uint32_t)batch * 64 + afresh(lane)) * 16 < (uint32_t)held && id >= 0 && id < a.cache.pages;
             ks = vs = 0.0f;
             if (there) {
                 ks = a.cache.k_scales[(int64_t)id * a.heads + head];
@@ -252,12 +267,14 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_chunk_attention(ChunkArgs a,
         // where they are in the cache
         const auto place_of = [&](int id) {
             if (id < 0 || id >= a.cache.pages) id = 0;
-            return ((((uint64_t)id * a.heads + head) << page_shift) + (lane * 16 & ((1 << page_shift) - 1))) * DIM;
+            return ((((uint64_t)id * a.heads + head) << page_shift) + (afresh(lane) * 16 & ((1 << page_shift) - 1))) * DIM;
         };
         uint64_t place = 0;
         int page_next = 0;
         float ks_next = 0.0f, vs_next = 0.0f;
-        uintx4 code_k[kFetch], code_v[kFetch];
+        struct Codes {
+            uintx4 w[kLoads];
+        };
         // the codes of tile t, from memory
         const auto fetch = [&](int t) {
             const int in = t & 15;
@@ -266,48 +283,59 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_chunk_attention(ChunkArgs a,
                 page_next = pages_of((t >> 4) + 1);
             }
             if (in == 8) scales_of((t >> 4) + 1, page_next, ks_next, vs_next);
-            const int thread = afresh(threadIdx.x), mine = thread / kPieces % 16 * DIM + thread % kPieces * 16;
+            const int thread = code_thread(), mine = thread / kPieces % 16 * DIM + thread % kPieces * 16;
+            Codes c;
 #pragma unroll
-            for (int i = 0; i < kFetch; ++i) {
-                const uint64_t at_page = lane_u64(place, in * 4 + (i * (64 / kFetch) + wave * (64 / kPieces)) / 16);       // the wavefront's piece
-                code_k[i] = *(const uintx4 *)(a.cache.k + at_page + mine);
-                code_v[i] = *(const uintx4 *)(a.cache.v + at_page + mine);
+            for (int i = 0; i < kEach; ++i) {
+                const uint64_t at_page = lane_u64(place, in * 4 + (i * kRound + code_wave * (64 / kPieces)) / 16);       // the wavefront's piece
+                if constexpr (kLoads == 1) {
+                    c.w[0] = *(const uintx4 *)((half ? a.cache.v : a.cache.k) + at_page + mine);
+                } else {
+                    c.w[i] = *(const uintx4 *)(a.cache.k + at_page + mine);
+                    c.w[kEach + i] = *(const uintx4 *)(a.cache.v + at_page + mine);
+                }
             }
+            return c;
         };
-        // and into LDS, 8 codes at a time
-        const auto clear_rest = [&](int t) {
-            if ((t + 1) * kTokens > job.held) {              // whatever the page holds beyond them
-                const int code_row = afresh(threadIdx.x) / kPieces;
+        // and into LDS, 8 codes at a time: half a load
+        const auto clear_rest = [&](Codes &c, int t) {
+            if ((t + 1) * kTokens > held) {                  // whatever the page holds beyond them
+                const int code_row = code_thread() / kPieces;
 #pragma unroll
-                for (int i = 0; i < kFetch; ++i)
-                    if (t * kTokens + i * (64 / kFetch) + code_row >= job.held) code_k[i] = code_v[i] = uintx4{0, 0, 0, 0};
+                for (int i = 0; i < kLoads; ++i)
+                    if (t * kTokens + i % kEach * kRound + code_row >= held) c.w[i] = uintx4{0, 0, 0, 0};
             }
         };
         struct Places {
             int k, v;
         };
-        const auto code_places = [&](int to) {
-            const int thread = afresh(threadIdx.x), r = thread / kPieces, u = 2 * (thread % kPieces);
-            return Places{to * kTile + r * kRow + (u ^ swizzle<DIM, true>(r & 31)) * 16, (to + 1) * kTile + r * kRow + (u ^ swizzle<DIM, false>(r & 15)) * 16};
+        const Places places = [&] {
+            const int thread = code_thread(), r = thread / kPieces, u = 2 * (thread % kPieces);
+            const int k = r * kRow + (u ^ swizzle<DIM, true>(r & 31)) * 16, v = r * kRow + (u ^ swizzle<DIM, false>(r & 15)) * 16 + kTile;
+            return kLoads == 1 ? Places{half ? v : k, 0} : Places{k, v};
+        }();
+        const auto convert = [&](const Codes &c, int piece, uint8_t *to, const Places &at_lds) {
+            const int i = piece >> 1, h = piece & 1;
+            const uintx2 x = sixteen<FP8, BF16>(c.w[i][2 * h]), y = sixteen<FP8, BF16>(c.w[i][2 * h + 1]);
+            *(uintx4 *)(to + ((i >= kEach ? at_lds.v : at_lds.k) ^ (h << 4)) + i % kEach * kRound * kRow) = uintx4{x[0], x[1], y[0], y[1]};
         };
-        const auto convert = [&](int piece, const Places &at_lds) {
-            const int i = piece >> 2, h = piece & 1;
-            const uintx4 w = piece & 2 ? code_v[i] : code_k[i];
-            const uintx2 x = sixteen<FP8, BF16>(w[2 * h]), y = sixteen<FP8, BF16>(w[2 * h + 1]);
-            *(uintx4 *)(&tiles[0][0] + ((piece & 2 ? at_lds.v : at_lds.k) ^ (h << 4)) + i * (64 / kFetch) * kRow) = uintx4{x[0], x[1], y[0], y[1]};
-        };
-        const auto convert_all = [&](int to) {
-            const Places at_lds = code_places(to);
+        const auto convert_all = [&](const Codes &c, uint8_t *to) {
 #pragma unroll
-            for (int c = 0; c < 4 * kFetch; ++c) convert(c, at_lds);
+            for (int piece = 0; piece < 2 * kLoads; ++piece) convert(c, piece, to, places);
         };
-        // new tokens' tile t, straight to LDS
-        const auto load_new = [&](int t, int to) {
-            const int t0 = (t - cached) * kTokens + 16 * wave, mine = afresh(lane);
-            const Rows16<DIM, true> rows_k(mine, stride_k);
-            const Rows16<DIM, false> rows_v(mine, stride_v);
-            rows_k.load(rows16(k + (int64_t)t0 * stride_k, stride_k, n - t0, DIM), tiles[to] + wave * 16 * kRow);
-            rows_v.load(rows16(v + (int64_t)t0 * stride_v, stride_v, n - t0, DIM), tiles[to + 1] + wave * 16 * kRow);
+        // new tokens' tile t, straight to LDS: 16 rows of K and of V a wavefront, or with eight of either
+        const auto load_new = [&](int t, uint8_t *to) {
+            const int16_t *const k = (const int16_t *)a.k.ptr + job.off * a.k.token + head * a.k.head;
+            const int16_t *const v = (const int16_t *)a.v.ptr + job.off * a.v.token + head * a.v.head;
+            const int part = wave & 3, t0 = (t - cached) * kTokens + 16 * part, mine = afresh(lane);
+            if (W == 4 || wave < 4) {
+                const Rows16<DIM, true> rows_k(mine, stride_k);
+                rows_k.load(rows16((const uint16_t *)k + (int64_t)t0 * stride_k, stride_k, n - t0, DIM), to + part * 16 * kRow);
+            }
+            if (W == 4 || wave >= 4) {
+                const Rows16<DIM, false> rows_v(mine, stride_v);
+                rows_v.load(rows16((const uint16_t *)v + (int64_t)t0 * stride_v, stride_v, n - t0, DIM), to + kTile + part * 16 * kRow);
+            }
         };
 
         floatx16 acc[kOut];
@@ -319,26 +347,27 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_chunk_attention(ChunkArgs a,
 
         floatx16 s[2];
         uintx4 pf[4];
-        // convert_next: the next tile's codes are converted beside it
-        const auto scores = [&](const uint8_t *lds_k, auto convert_next, int to) {
-            const int mine = afresh(at_k);
-            Places at_lds = {0, 0};
-            if constexpr (decltype(convert_next)::value) at_lds = code_places(to);
+        // Operands that are on their way from LDS: V's while the last products with K are made, the next tile's K's beside the last ones with V
+        uintx4 kf[kAhead], vf[kAhead];
+        const auto read_k = [&](const uint8_t *tile, int i) { return *(const uintx4 *)(tile + (at_k ^ (i / 2 << 5)) + (i & 1) * 32 * kRow); };
+        const auto read_v = [&](const uint8_t *tile, int i) {
+            const uint8_t *p = tile + kTile + (at_v ^ (i % kOut << 6)) + i / kOut * 16 * kRow;
+            const uintx2 lo = transposed(p), hi = transposed(p + 8 * kRow);
+            return uintx4{lo[0], lo[1], hi[0], hi[1]};
+        };
+        const auto scores = [&](const uint8_t *tile) {
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[h][r] = 0.0f;
-            pipelined<2 * kSteps, kAhead>([&](int i) { return *(const uintx4 *)(lds_k + (mine ^ (i / 2 << 5)) + (i & 1) * 32 * kRow); },
-                                          [&](int i, uintx4 x) { s[i & 1] = mma32<BF16>(x, qf[i / 2], s[i & 1]); },
-                                          [&](int i) {
-                                              if constexpr (decltype(convert_next)::value)
-                                                  if (i & 1) convert(i >> 1, at_lds);
-                                          });
+            pipelined<2 * kSteps>(kf, [&](int i) { return read_k(tile, i); }, [&](int j) { vf[j] = read_v(tile, j); },
+                                  [&](int i, uintx4 x) { s[i & 1] = mma32<BF16>(x, qf[i / 2], s[i & 1]); }, [](int) {});
         };
         // tokens of the tile from `first` on, and before `sees`, are seen
         const auto mask = [&](int first, int sees) {
-            first -= 4 * side;
-            sees -= 4 * side;
+            const int before = 4 * afresh(side);
+            first -= before;
+            sees -= before;
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -370,19 +399,13 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_chunk_attention(ChunkArgs a,
             back = 1.0f / c;
         };
         const auto raise_maxima = [&](int piece) {
-            float fk[4], up[4];
-#pragma unroll
-            for (int p = 0; p < 4; ++p) {
-                fk[p] = lane_f(steep, piece + p);
-                up[p] = lane_f(raise, piece + p);
-            }
             float most = -__builtin_inff();
 #pragma unroll
             for (int p = 0; p < 4; ++p) {
                 float m = s[p / 2][8 * (p & 1)];
 #pragma unroll
                 for (int r = 1; r < 8; ++r) m = fmaxf(m, s[p / 2][8 * (p & 1) + r]);
-                most = fmaxf(most, __builtin_fmaf(m, fk[p], up[p]));
+                most = fmaxf(most, __builtin_fmaf(m, lane_f(steep, piece + p), lane_f(raise, piece + p)));
             }
             bool away;
             if constexpr (BF16) {
@@ -406,9 +429,9 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_chunk_attention(ChunkArgs a,
                 for (int o = 0; o < kOut; ++o) acc[o] *= shrink;
             }
         };
-        // The weights of 16 tokens are made beside the products of the 16 before them
-        const auto add_values = [&](const uint8_t *lds_v, int piece) {
-            const int mine = afresh(at_v);
+        // The weights of 16 tokens are made beside the products of the 16 before them, and beside the last products the codes of the tile after
+        // the next one are converted
+        const auto add_values = [&](const uint8_t *tile, const uint8_t *behind, int piece, auto convert_codes, const Codes &c, uint8_t *to) {
             float part = 0.0f;
             const auto weigh = [&](int p, int pair) {
                 const float fk = lane_f(steep, piece + p), add = lane_f(raise, piece + p) - top;
@@ -420,18 +443,18 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_chunk_attention(ChunkArgs a,
             };
 #pragma unroll
             for (int pair = 0; pair < 4; ++pair) weigh(0, pair);
-            pipelined<4 * kOut, kAhead>(
-                [&](int i) {
-                    const uint8_t *p = lds_v + (mine ^ (i % kOut << 6)) + i / kOut * 16 * kRow;
-                    const uintx2 lo = transposed(p), hi = transposed(p + 8 * kRow);
-                    return uintx4{lo[0], lo[1], hi[0], hi[1]};
-                },
-                [&](int i, uintx4 x) { acc[i % kOut] = mma32<BF16>(x, pf[i / kOut], acc[i % kOut]); },
-                [&](int i) {
-                    if (i < 3 * kOut)
+            pipelined<4 * kOut>(vf, [&](int i) { return read_v(tile, i); }, [&](int j) { kf[j] = read_k(behind, j); },
+                                [&](int i, uintx4 x) { acc[i % kOut] = mma32<BF16>(x, pf[i / kOut], acc[i % kOut]); },
+                                [&](int i) {
+                                    // beside each instruction 4 / kOut pairs of weights, or, for the last 16 tokens, 2 kLoads / kOut halves of loads
+                                    if (i < 3 * kOut) {
 #pragma unroll
-                        for (int pair = i % kOut * 4 / kOut; pair < (i % kOut + 1) * 4 / kOut; ++pair) weigh(i / kOut + 1, pair);
-                });
+                                        for (int j = i % kOut * 4 / kOut; j < (i % kOut + 1) * 4 / kOut; ++j) weigh(i / kOut + 1, j);
+                                    } else if constexpr (decltype(convert_codes)::value) {
+#pragma unroll
+                                        for (int j = (i - 3 * kOut) * 2 * kLoads / kOut; j < (i - 3 * kOut + 1) * 2 * kLoads / kOut; ++j) convert(c, j, to, places);
+                                    }
+                                });
         };
         // In a tile that not all rows see whole, an infinity or NaN among the new values would be NaN times the weight of 0 of those that do
         // not.  Such values are added to the rows that see them, and taken out of the tile.
@@ -439,17 +462,19 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_chunk_attention(ChunkArgs a,
         const auto finite_only = [&](uint32_t w) { return w & ~(((not_finite(w) & 0x80008000u) >> 15) * 0xFFFFu); };
         const auto any_not_finite = [&](const uint8_t *lds_v) {
             uint32_t any = 0;
+            const int mine = afresh(lane);
 #pragma unroll 4
             for (int i = 0; i < kTile / 1024; ++i) {
-                const uintx4 w = *(const uintx4 *)(lds_v + i * 1024 + lane * 16);
+                const uintx4 w = *(const uintx4 *)(lds_v + i * 1024 + mine * 16);
                 any |= not_finite(w[0]) | not_finite(w[1]) | not_finite(w[2]) | not_finite(w[3]);
             }
             return __any(any & 0x80008000u) != 0;
         };
         const auto add_not_finite = [&](const uint8_t *lds_v, int t0) {
+            const int my_side = afresh(side);
 #pragma unroll 1
             for (int t = 0; t < kTokens; ++t) {
-                const uint8_t *p = lds_v + t * kRow + side * 8;
+                const uint8_t *p = lds_v + t * kRow + my_side * 8;
                 const bool seen = t0 + t <= query && t0 + t >= skip;
 #pragma unroll
                 for (int o = 0; o < kOut; ++o)
@@ -464,94 +489,125 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_chunk_attention(ChunkArgs a,
                     }
             }
         };
-        const auto compute = [&](int t, int from) {
-            uint8_t *const lds_k = tiles[from], *const lds_v = tiles[from + 1];
-            const bool code = t < cached, next = t + 1 < tile1, next_code = next && t + 1 < cached;
-            const int t0 = code ? t * kTokens : (t - cached) * kTokens;
-            const bool astray = !code && (t0 + kTokens - 1 > first_query || t0 < skip) && any_not_finite(lds_v);      // the same for all wavefronts
-            const bool sees = !idle && (code || t0 <= wave_last);
-            if (next && !next_code) load_new(t + 1, from ^ 2);
-            if (next_code) clear_rest(t + 1);
-            if (!sees) {
-                if (next_code) convert_all(from ^ 2);
-            } else if (next_code) {
-                scores(lds_k, std::true_type(), from ^ 2);
-            } else {
-                scores(lds_k, std::false_type(), 0);
-            }
-            if (next_code && t + 2 < cached && t + 2 < tile1) fetch(t + 2);
-            if (sees) {
-                if (code ? t0 + kTokens > job.held : t0 + kTokens - 1 > wave_first || t0 < skip) mask(code ? 0 : skip - t0, (code ? job.held : query + 1) - t0);
-                raise_maxima((t & 15) * 4);
-            }
-            if (astray) {
-                if (sees) add_not_finite(lds_v, t0);
-                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-#pragma unroll 1
-                for (int i = 0; i < kTile / 1024 / kWaves; ++i) {
-                    uintx4 *const place = (uintx4 *)(lds_v + (wave * (kTile / 1024 / kWaves) + i) * 1024 + lane * 16);
-                    const uintx4 w = *place;
-                    *place = uintx4{finite_only(w[0]), finite_only(w[1]), finite_only(w[2]), finite_only(w[3])};
-                }
-                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            }
-            if (sees) add_values(lds_v, (t & 15) * 4);
-        };
 
+        // ---- the tiles ----
+        // everything that this wavefront has written to LDS, or (loads) sent there straight from memory, is there, and the others' too
+        const auto arrived = [](bool loads) {
+            if (loads) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        };
+        uint8_t *now = &tiles[0][0][0], *next = &tiles[1][0][0], *after = &tiles[2][0][0];
+        Codes codes = {};
+        const auto pass_on = [&] {
+            uint8_t *const free = now;
+            now = next;
+            next = after;
+            after = free;
+        };
         if (tile0 < cached) {
-            const int batch = tile0 >> 4;
-            const int page = pages_of(batch);
+            const int batch = tile0 >> 4, page = pages_of(batch);
             place = place_of(page);
             page_next = pages_of(batch + 1);
             float ks, vs;
+            Codes first = fetch(tile0);
             scales_of(batch, page, ks, vs);
-            scales_of(batch + 1, page_next, ks_next, vs_next);
+            scales_of(batch + 1, page_next, ks_next, vs_next);     // (before the next fetch may go on to that batch)
+            if (tile0 + 1 < codes_end) codes = fetch(tile0 + 1);
             turn_to(ks, vs);
-            fetch(tile0);
-            clear_rest(tile0);
-            convert_all(0);
-            if (tile0 + 1 < cached && tile0 + 1 < tile1) fetch(tile0 + 1);
+            clear_rest(first, tile0);
+            convert_all(first, now);
+            if (tile0 + 1 < codes_end) {
+                clear_rest(codes, tile0 + 1);
+                convert_all(codes, next);
+                if (tile0 + 2 < codes_end) codes = fetch(tile0 + 2);
+            }
         } else {
             turn_to(1.0f, 1.0f);
-            load_new(tile0, 0);
+            load_new(tile0, now);
         }
-        // the queries are here before the loop, where waiting for them would wait for the tiles that are loaded ahead
+        if (tile0 + 1 < tile1 && tile0 + 1 >= cached) load_new(tile0 + 1, next);
+        // the queries are here before the loop, where waiting for them would wait for what is loaded ahead
 #pragma unroll
         for (int j = 0; j < kSteps; ++j) asm volatile("" : "+v"(qf[j]));
-        arrived();
-        int from = 0;
-        for (int t = tile0; t < tile1; ++t, from ^= 2) {
-            if (t != tile0 && t <= cached && ((t & 15) == 0 || t == cached)) {
-                if (t < cached) turn_to(ks_next, vs_next);
-                else turn_to(1.0f, 1.0f);
+        arrived(true);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) kf[j] = read_k(now, j);
+        int t = tile0;
+        for (; t < codes_end; ++t) {
+            if ((t & 15) == 0 && t != tile0) turn_to(ks_next, vs_next);
+            if (!idle) scores(now);
+            // the next tile is whole, and the one before this one is done with
+            arrived(t + 1 >= cached);
+            // (where there are no more codes the last ones go to a tile that nobody reads: one form of the products is enough)
+            uint8_t *const to = t + 2 < codes_end ? after : &tiles[3][0][0];
+            if (t + 2 < codes_end) clear_rest(codes, t + 2);
+            else if (t + 2 < tile1) load_new(t + 2, after);
+            if (!idle) {
+                if ((t + 1) * kTokens > held) mask(0, held - t * kTokens);
+                raise_maxima((t & 15) * 4);
+                add_values(now, next, (t & 15) * 4, std::true_type(), codes, to);
+            } else {
+                convert_all(codes, to);
             }
-            compute(t, from);
-            arrived();
+            if (t + 3 < codes_end) codes = fetch(t + 3);
+            pass_on();
+        }
+        if (t < tile1 && t != tile0) turn_to(1.0f, 1.0f);
+        const int first_query = (int)(block * kRows / group);                    // of the workgroup
+        const int wave_first = (int)((row0 < rows ? row0 : rows - 1) / group), wave_last = (int)((row0 + 32 <= rows ? row0 + 31 : rows - 1) / group);
+        for (; t < tile1; ++t) {
+            const int t0 = (t - cached) * kTokens;
+            const bool sees = !idle && t0 <= wave_last;
+            if (sees) scores(now);
+            arrived(true);
+            if (t + 2 < tile1) load_new(t + 2, after);
+            if (sees) {
+                if (t0 + kTokens - 1 > wave_first || t0 < skip) mask(skip - t0, query + 1 - t0);
+                raise_maxima(0);
+            }
+            if ((t0 + kTokens - 1 > first_query || t0 < skip) && any_not_finite(now + kTile)) {           // the same for all wavefronts
+                uint8_t *const lds_v = now + kTile;
+                const int mine = afresh(lane);
+                if (sees) add_not_finite(lds_v, t0);
+                arrived(false);
+#pragma unroll 1
+                for (int i = 0; i < kTile / 1024 / W; ++i) {
+                    uintx4 *const place = (uintx4 *)(lds_v + (wave * (kTile / 1024 / W) + i) * 1024 + mine * 16);
+                    const uintx4 w = *place;
+                    *place = uintx4{finite_only(w[0]), finite_only(w[1]), finite_only(w[2]), finite_only(w[3])};
+                }
+                arrived(false);
+#pragma unroll
+                for (int j = 0; j < kAhead; ++j) vf[j] = read_v(now, j);
+            }
+            if (sees) add_values(now, next, 0, std::false_type(), codes, after);
+            pass_on();
         }
 
         total += __shfl_xor(total, 32);
         const float inv = total == 0.0f ? 0.0f : 1.0f / total;
         if (whole) {
             // through LDS, where the tiles are done with, so that a wavefront stores whole rows (a lane has 4 elements of a row at a time)
-            uint8_t *const mine = &tiles[0][0] + wave * 32 * kOutRow;                     // neighbouring rows begin 4 banks apart
+            __syncthreads();
+            const int here = afresh(lane), col = here & 31, side = here >> 5;
+            uint8_t *const mine = &tiles[0][0][0] + wave * 32 * kOutRow;                  // neighbouring rows begin 4 banks apart
+            constexpr int kLanes = DIM / 8;                  // of a row
 #pragma unroll
             for (int o = 0; o < kOut; ++o)
 #pragma unroll
                 for (int r = 0; r < 16; r += 4)
                     *(uintx2 *)(mine + col * kOutRow + (o * 32 + 2 * r + 4 * side) * 2) =
                         uintx2{narrow2<BF16>(acc[o][r] * inv * unit, acc[o][r + 1] * inv * unit), narrow2<BF16>(acc[o][r + 2] * inv * unit, acc[o][r + 3] * inv * unit)};
-            constexpr int kLanes = DIM / 8;                  // of a row
 #pragma unroll
             for (int i = 0; i < 32 * kLanes / 64; ++i) {
-                const int out_row = i * (64 / kLanes) + lane / kLanes, d = lane % kLanes * 8;
+                const int out_row = i * (64 / kLanes) + here / kLanes, d = here % kLanes * 8;
                 const uintx4 w = *(const uintx4 *)(mine + out_row * kOutRow + d * 2);
                 const int64_t r = row0 + out_row, q = r / group;
                 if (r < rows) *(uintx4 *)((uint16_t *)a.out.ptr + (job.off + q) * a.out.token + (head * group + (int)(r - q * group)) * a.out.head + d) = w;
             }
-            __syncthreads();                                 // before the next item's tiles
         } else if (!idle) {
             // as the lanes have them: [place][wavefront][4 elements of each][lane]
-            const int64_t place = ((int64_t)range * 2 + (tile0 == 0)) * kWaves + wave, places = (int64_t)gridDim.x * 2 * kWaves;
+            const int64_t place = ((int64_t)range * 2 + (tile0 == 0)) * W + wave, places = (int64_t)gridDim.x * 2 * W;
             floatx4 *const y = (floatx4 *)a.partial + place * (32 * DIM / 4);
             const int mine = afresh(lane);
 #pragma unroll
@@ -561,15 +617,16 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_chunk_attention(ChunkArgs a,
                     y[(o * 4 + r / 4) * 64 + mine] = floatx4{acc[o][r] * inv * unit, acc[o][r + 1] * inv * unit, acc[o][r + 2] * inv * unit, acc[o][r + 3] * inv * unit};
             if (mine < 32) ((floatx2 *)(a.partial + places * (32 * DIM)))[place * 32 + mine] = floatx2{top, total};
         }
+        __syncthreads();                                     // before the next item's tiles
     }
 }
 
 // Joins what the ranges have of the items that were cut.  A workgroup has 32 of an item's elements (of all its rows), a wavefront 32 rows.  A range
 // has two places: 1 for an item that it begins and does not end, 0 for one that began before.
-template <int DIM, bool BF16>
-__global__ void __launch_bounds__(64 * kWaves) k_chunk_join(ChunkArgs a, int page_shift, int64_t slots)
+template <int DIM, bool BF16, int W>
+__global__ void __launch_bounds__(64 * W) k_chunk_join(ChunkArgs a, int page_shift)
 {
-    constexpr int kOut = DIM / 32;
+    constexpr int kOut = DIM / 32, kRows = rows_of(W);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, side = lane >> 5;
     const uint64_t total_units = a.plan[0];
     if (total_units == 0) return;
@@ -578,7 +635,7 @@ __global__ void __launch_bounds__(64 * kWaves) k_chunk_join(ChunkArgs a, int pag
     id /= kOut;
     const int head = (int)(id % a.heads);
     const int64_t slot = id / a.heads;
-    // the sequence with this slot: sequence b owns those from offsets[b] * group / 128 + b on
+    // the sequence with this slot: sequence b owns those from offsets[b] * group / kRows + b on
     int lo = 0, hi = a.step.sequences - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
@@ -586,21 +643,21 @@ __global__ void __launch_bounds__(64 * kWaves) k_chunk_join(ChunkArgs a, int pag
         else hi = mid - 1;
     }
     const int b = lo;
-    const Job job = job_of(a, a.step.offsets[b], a.step.offsets[b + 1], a.step.held[b], page_shift);
+    const Job job = job_of<kRows>(a, a.step.offsets[b], a.step.offsets[b + 1], a.step.held[b], page_shift);
     const int64_t block = slot - (job.off * a.group / kRows + b);
     if (block < 0 || block >= job.blocks) return;
     const int64_t rows = (int64_t)job.n * a.group, row0 = block * kRows + wave * 32, row = row0 + col;
     if (row0 >= rows) return;
     const Ranges ranges(total_units, a.workgroups);
-    const uint64_t item = a.plan[1 + b] + (uint64_t)head * job.total + units_before(job, block, a.group);
-    const uint64_t last_unit = a.plan[1 + b] + (uint64_t)head * job.total + units_before(job, block + 1, a.group) - 1;
+    const uint64_t item = a.plan[1 + b] + (uint64_t)head * job.total + units_before<kRows>(job, block, a.group);
+    const uint64_t last_unit = a.plan[1 + b] + (uint64_t)head * job.total + units_before<kRows>(job, block + 1, a.group) - 1;
     const uint32_t first = ranges.of(item), last = ranges.of(last_unit);
     if (first == last) return;                           // written already
-    const int64_t places = (int64_t)a.workgroups * 2 * kWaves;
+    const int64_t places = (int64_t)a.workgroups * 2 * W;
     const floatx4 *const x = (const floatx4 *)a.partial;
     const floatx2 *const m = (const floatx2 *)(a.partial + places * (32 * DIM));
     // the first range has it in its second place, the others in their first ones
-    const auto place = [&](uint32_t r) { return ((int64_t)r * 2 + (r == first)) * kWaves + wave; };
+    const auto place = [&](uint32_t r) { return ((int64_t)r * 2 + (r == first)) * W + wave; };
     float best = -FLT_MAX;
     for (uint32_t r = first; r <= last; ++r) best = fmaxf(best, m[place(r) * 32 + col][0]);
     floatx4 sum[4];
@@ -626,39 +683,46 @@ __global__ void __launch_bounds__(64 * kWaves) k_chunk_join(ChunkArgs a, int pag
         *(uintx2 *)(y + 8 * i) = uintx2{narrow2<BF16>(sum[i][0] * inv, sum[i][1] * inv), narrow2<BF16>(sum[i][2] * inv, sum[i][3] * inv)};
 }
 
-int64_t slots_of(int64_t tokens, int group, int sequences) { return tokens * group / kRows + sequences; }
+int64_t slots_of(int64_t tokens, int group, int sequences, int waves) { return tokens * group / rows_of(waves) + sequences; }
 
-template <int DIM, bool FP8, bool BF16>
+template <int DIM, bool FP8, bool BF16, int W>
 hipError_t chunk(const ChunkArgs &a, hipStream_t stream)
 {
     const int shift = a.cache.page == 16 ? 4 : a.cache.page == 32 ? 5 : 6;
-    const int64_t slots = slots_of(a.step.tokens, a.group, a.step.sequences), joins = slots * a.heads * (DIM / 32);
-    if (!launchable(joins, 64 * kWaves)) return kTooLarge;               // before anything is
-    const hipError_t e = launch_many(k_chunk_attention<DIM, FP8, BF16>, a.workgroups, 64 * kWaves, stream, a, shift);
+    const int64_t joins = slots_of(a.step.tokens, a.group, a.step.sequences, W) * a.heads * (DIM / 32);
+    if (!launchable(joins, 64 * W)) return kTooLarge;           // before anything is
+    const hipError_t e = launch_many(k_chunk_attention<DIM, FP8, BF16, W>, a.workgroups, 64 * W, stream, a, shift);
     if (e != hipSuccess || a.workgroups == 1) return e;
-    return launch_many(k_chunk_join<DIM, BF16>, joins, 64 * kWaves, stream, a, shift, slots);
+    return launch_many(k_chunk_join<DIM, BF16, W>, joins, 64 * W, stream, a, shift);
+}
+
+template <int DIM, bool FP8, bool BF16>
+hipError_t chunk_of(const ChunkArgs &a, hipStream_t stream)
+{
+    return a.waves == 8 ? chunk<DIM, FP8, BF16, 8>(a, stream) : chunk<DIM, FP8, BF16, 4>(a, stream);
 }
 
 template <int DIM>
 hipError_t chunk_of(const ChunkArgs &a, hipStream_t stream)
 {
-    if (a.fp8) return a.bf16 ? chunk<DIM, true, true>(a, stream) : chunk<DIM, true, false>(a, stream);
-    return a.bf16 ? chunk<DIM, false, true>(a, stream) : chunk<DIM, false, false>(a, stream);
+    if (a.fp8) return a.bf16 ? chunk_of<DIM, true, true>(a, stream) : chunk_of<DIM, true, false>(a, stream);
+    return a.bf16 ? chunk_of<DIM, false, true>(a, stream) : chunk_of<DIM, false, false>(a, stream);
 }
 
 }  // namespace
 
-// Two workgroups for each of 256 compute units, or fewer where the announced lengths cannot make so many ranges
-int chunk_workgroups(int64_t tokens, int sequences, int heads, int group, int dim, int64_t longest)
+void chunk_plan(int64_t tokens, int sequences, int heads, int group, int64_t longest, ChunkArgs *a)
 {
-    const double units = (double)slots_of(tokens, group, sequences) * heads * ((double)longest / kTokens + 2);
+    a->waves = (double)tokens * group >= 192.0 * sequences ? 8 : 4;
+    // a workgroup for each of 256 compute units, or fewer where the announced lengths cannot make so many ranges
+    const double units = (double)slots_of(tokens, group, sequences, a->waves) * heads * ((double)longest / kTokens + 2);
     const double most = units / kLeast + 1;
-    return most < 512 ? (int)most : 512;
+    a->workgroups = most < 256 ? (int)most : 256;
 }
 
-size_t chunk_workspace(int workgroups, int sequences, int dim)
+size_t chunk_workspace(const ChunkArgs &a, int sequences, int dim)
 {
-    return ((size_t)sequences + 1 + 1) / 2 * 16 + (workgroups > 1 ? (size_t)workgroups * 2 * kRows * (dim + 2) * sizeof(float) : 0);
+    return ((size_t)sequences + 1 + 1) / 2 * 16 + (a.workgroups > 1 ? (size_t)a.workgroups * 2 * rows_of(a.waves) * (dim + 2) * sizeof(float) : 0);
 }
 
 hipError_t launch_chunk_attention(const ChunkArgs &a, hipStream_t stream)
