@@ -286,9 +286,10 @@ int fc_chunk_attention(const void *q, int64_t q_token_stride, int64_t q_head_str
     // 32-bit offsets in a tile, and tokens of a sequence
     if (tokens > kMaxTokens - 1024) return FC_ERR_SHAPE;
     if (k_token_stride >= 1 << 25 || v_token_stride >= 1 << 25 || k_token_stride < 0 || v_token_stride < 0) return FC_ERR_SHAPE;
-    // units of work are counted in 64 bits, whatever the arrays say
-    const double tiles = (double)table_width * page / 64 + (double)tokens / 64 + 2, blocks = (double)tokens * group / 128 + sequences;
-    if (tiles * blocks * heads >= 0x1p62) return FC_ERR_SHAPE;
+    // rows of a key/value head are counted in 32 bits, and units of work in 64, whatever the arrays say
+    if (tokens * group > kMaxTokens - 1024) return FC_ERR_SHAPE;
+    const double tiles = (double)table_width * page / 64 + (double)tokens / 64 + 16, blocks = (double)tokens * group / 128 + sequences;
+    if (tiles * blocks * heads >= 0x1p62 || blocks * heads * 4 >= 2147483648.0) return FC_ERR_SHAPE;
     fc::ChunkArgs a;
     fc::chunk_plan(tokens, sequences, heads, group, longest, &a);
     const size_t need = fc::chunk_workspace(a, sequences, dim);

@@ -22,32 +22,34 @@ namespace {
 
 constexpr int kTokens = 64, kAhead = 6;
 constexpr int kLeast = 2;               // units of a range
+constexpr int kBegin = 3;               // units that what surrounds an item's tiles counts for
 constexpr int rows_of(int waves) { return 32 * waves; }                  // of a workgroup
 template <bool BF16> constexpr float kSlack = BF16 ? 8.0f : 10.0f;
 constexpr float kBias = 4.0f, kReach = 36.0f;
 // how far below the largest unit so far the unit may go, and what a scale may be of it
 constexpr float kDeep = 0x1p-30f, kFaint = 0x1p-36f;
 
-// What there is to do for one sequence, for each key/value head: `blocks` of a workgroup's rows, each over `cached` tiles and those new ones that it sees
+// What there is to do for one sequence, for each key/value head: `blocks` of a workgroup's rows, each over `cached` tiles and those new ones that it
+// sees, and kBegin units for what surrounds them
 struct Job {
-    int64_t off, blocks, total;                          // total: units of all blocks
-    int n, held, skip, cached, fresh;                    // new tokens; tokens in the cache; new ones without a place; tiles of either kind
+    int64_t off, total;                                  // total: units of all blocks
+    int blocks, n, held, skip, cached, fresh;            // new tokens; tokens in the cache; new ones without a place; tiles of either kind
 };
 
 // Units of new tokens of the first j blocks of ROWS: block i - 1 sees the tokens before ceil(ROWS i / group), so ceil(c i / group) tiles of them, c =
 // ROWS / 64.  Every `group` blocks that is c more, and in between one more from each i > k group / c on.
 template <int ROWS>
-__device__ __forceinline__ int64_t fresh_units(int64_t j, int group)
+__device__ __forceinline__ int64_t fresh_units(int j, int group)
 {
     constexpr int c = ROWS / kTokens;
-    const auto some = [&](int64_t r) {
-        int64_t sum = r;
+    const auto some = [&](int r) {
+        int sum = r;
 #pragma unroll
         for (int k = 1; k < c; ++k) sum += r > k * group / c ? r - k * group / c : 0;
         return sum;
     };
-    const int64_t q = j / group, r = j - q * group;
-    return c * group * q * (q - 1) / 2 + q * some(group) + c * q * r + some(r);
+    const int q = (int)((uint32_t)j / (uint32_t)group), r = j - q * group;
+    return (int64_t)(c * group) * ((int64_t)q * (q - 1) / 2) + (int64_t)q * some(group) + (int64_t)(c * r) * q + some(r);
 }
 
 template <int ROWS>
@@ -59,18 +61,33 @@ __device__ __forceinline__ Job job_of(const ChunkArgs &a, int off, int next, int
     const int64_t room = (int64_t)a.cache.table_width << page_shift;
     j.held = held < 0 ? 0 : held < room ? held : (int)room;
     j.skip = held < 0 ? -(held + 1) < j.n ? -held : j.n : 0;
-    j.cached = (int)(((int64_t)j.held + kTokens - 1) / kTokens);
-    j.fresh = (int)(((int64_t)j.n + kTokens - 1) / kTokens);
-    j.blocks = ((int64_t)j.n * a.group + ROWS - 1) / ROWS;
-    j.total = j.blocks ? (j.blocks - 1) * j.cached + fresh_units<ROWS>(j.blocks - 1, a.group) + j.cached + j.fresh : 0;
+    j.cached = (int)(((uint32_t)j.held + kTokens - 1) / kTokens);
+    j.fresh = (int)(((uint32_t)j.n + kTokens - 1) / kTokens);
+    j.blocks = (int)(((uint32_t)j.n * (uint32_t)a.group + ROWS - 1) / ROWS);             // (tokens * group is below 2^31)
+    j.total = j.blocks ? (int64_t)j.blocks * (j.cached + kBegin) + fresh_units<ROWS>(j.blocks - 1, a.group) + j.fresh : 0;
     return j;
 }
 
 template <int ROWS>
-__device__ __forceinline__ int64_t units_before(const Job &j, int64_t block, int group)
+__device__ __forceinline__ int64_t units_before(const Job &j, int block, int group)
 {
-    return block >= j.blocks ? j.total : block * j.cached + fresh_units<ROWS>(block, group);
+    return block >= j.blocks ? j.total : (int64_t)block * (j.cached + kBegin) + fresh_units<ROWS>(block, group);
 }
+
+// the block that has unit u: a guess by the square that its sum nearly is, and the one or two beside it
+template <int ROWS>
+__device__ __forceinline__ int block_of(const Job &j, int64_t u, int group)
+{
+    const float slope = (float)(ROWS / kTokens) / (float)group, flat = (float)(j.cached + kBegin) + 0.5f * slope, x = (float)u;
+    int block = (int)__builtin_amdgcn_readfirstlane((int)(2.0f * x / (flat + __builtin_sqrtf(flat * flat + 2.0f * slope * x))));
+    if (block > j.blocks - 1) block = j.blocks - 1;
+    while (block > 0 && units_before<ROWS>(j, block, group) > u) --block;
+    while (block < j.blocks - 1 && units_before<ROWS>(j, block + 1, group) <= u) ++block;
+    return block;
+}
+
+// a / b, where both are mostly small
+__device__ __forceinline__ uint64_t quotient(uint64_t a, uint64_t b) { return (a | b) >> 32 ? a / b : (uint32_t)a / (uint32_t)b; }
 
 // The units of all sequences, one behind the other, cut into ranges that differ by one unit at most; fewer of them where they would have
 // less than kLeast units
@@ -81,14 +98,14 @@ struct Ranges {
     {
         const uint64_t most = (total + kLeast - 1) / kLeast;
         count = most < workgroups ? (uint32_t)most : workgroups;
-        each = count ? total / count : 0;
+        each = count ? quotient(total, count) : 0;
         longer = (uint32_t)(total - count * each);
     }
     __device__ __forceinline__ uint64_t begin(uint32_t r) const { return r * each + (r < longer ? r : longer); }
     __device__ __forceinline__ uint32_t of(uint64_t unit) const
     {
         const uint64_t split = longer * (each + 1);
-        return (uint32_t)(unit < split ? unit / (each + 1) : longer + (unit - split) / each);
+        return (uint32_t)(unit < split ? quotient(unit, each + 1) : longer + quotient(unit - split, each));
     }
 };
 
@@ -220,30 +237,26 @@ __global__ void __launch_bounds__(64 * W, W == 8 ? 2 : 1) k_chunk_attention(Chun
             continue;
         }
         // ---- the item: a head, a block of rows, and its tiles [tile0, tile1) ----
-        const int head = (int)((at - begins) / job.total);
+        const int head = (int)quotient(at - begins, job.total);
         const int64_t within = (int64_t)(at - begins) - head * job.total;
-        int64_t lo = 0, hi = job.blocks - 1;
-        while (lo < hi) {
-            const int64_t mid = (lo + hi + 1) >> 1;
-            if (units_before<kRows>(job, mid, group) <= within) lo = mid;
-            else hi = mid - 1;
-        }
-        const int64_t block = lo, before = units_before<kRows>(job, block, group);
-        const int units = (int)(units_before<kRows>(job, block + 1, group) - before);
-        const int tile0 = (int)(within - before);
-        const int tile1 = end - at < (uint64_t)(units - tile0) ? tile0 + (int)(end - at) : units;
-        at += tile1 - tile0;
-        const bool whole = tile0 == 0 && tile1 == units;
-        const int64_t rows = (int64_t)job.n * group, row0 = block * kRows + wave * 32;
+        const int block = block_of<kRows>(job, within, group);
+        const int64_t before = units_before<kRows>(job, block, group);
+        const int units = (int)(units_before<kRows>(job, block + 1, group) - before), unit0 = (int)(within - before);
+        const int unit1 = end - at < (uint64_t)(units - unit0) ? unit0 + (int)(end - at) : units;
+        at += unit1 - unit0;
+        const int tile0 = unit0 < kBegin ? 0 : unit0 - kBegin, tile1 = unit1 - kBegin;
+        if (tile1 <= tile0) continue;                    // none of its tiles
+        const bool whole = tile0 == 0 && tile1 == units - kBegin;
+        const int rows = job.n * group, row0 = block * kRows + wave * 32;
         const int n = job.n, held = job.held, cached = job.cached, skip = job.skip, codes_end = cached < tile1 ? cached : tile1;
         const bool idle = row0 >= rows;                  // this wavefront has no rows
 
         int query;
         uintx4 qf[kSteps];
         {
-            const int64_t row = row0 + col < rows ? row0 + col : rows - 1;
-            query = (int)(row / group);
-            const uint16_t *q = (const uint16_t *)a.q.ptr + (job.off + query) * a.q.token + (head * group + (int)(row - (int64_t)query * group)) * a.q.head + side * 8;
+            const int row = row0 + col < rows ? row0 + col : rows - 1;
+            query = (int)((uint32_t)row / (uint32_t)group);
+            const uint16_t *q = (const uint16_t *)a.q.ptr + (job.off + query) * a.q.token + (head * group + (row - query * group)) * a.q.head + side * 8;
 #pragma unroll
             for (int j = 0; j < kSteps; ++j) qf[j] = *(const uintx4 *)(q + 16 * j);
         }
@@ -553,8 +566,8 @@ __global__ void __launch_bounds__(64 * W, W == 8 ? 2 : 1) k_chunk_attention(Chun
             pass_on();
         }
         if (t < tile1 && t != tile0) turn_to(1.0f, 1.0f);
-        const int first_query = (int)(block * kRows / group);                    // of the workgroup
-        const int wave_first = (int)((row0 < rows ? row0 : rows - 1) / group), wave_last = (int)((row0 + 32 <= rows ? row0 + 31 : rows - 1) / group);
+        const int first_query = (int)((uint32_t)(block * kRows) / (uint32_t)group);      // of the workgroup
+        const int wave_first = (int)((uint32_t)(row0 < rows ? row0 : rows - 1) / (uint32_t)group), wave_last = (int)((uint32_t)(row0 + 31 < rows ? row0 + 31 : rows - 1) / (uint32_t)group);
         for (; t < tile1; ++t) {
             const int t0 = (t - cached) * kTokens;
             const bool sees = !idle && t0 <= wave_last;
@@ -602,8 +615,8 @@ __global__ void __launch_bounds__(64 * W, W == 8 ? 2 : 1) k_chunk_attention(Chun
             for (int i = 0; i < 32 * kLanes / 64; ++i) {
                 const int out_row = i * (64 / kLanes) + here / kLanes, d = here % kLanes * 8;
                 const uintx4 w = *(const uintx4 *)(mine + out_row * kOutRow + d * 2);
-                const int64_t r = row0 + out_row, q = r / group;
-                if (r < rows) *(uintx4 *)((uint16_t *)a.out.ptr + (job.off + q) * a.out.token + (head * group + (int)(r - q * group)) * a.out.head + d) = w;
+                const int r = row0 + out_row, q = (int)((uint32_t)r / (uint32_t)group);
+                if (r < rows) *(uintx4 *)((uint16_t *)a.out.ptr + (job.off + q) * a.out.token + (head * group + (r - q * group)) * a.out.head + d) = w;
             }
         } else if (!idle) {
             // as the lanes have them: [place][wavefront][4 elements of each][lane]
@@ -630,28 +643,26 @@ __global__ void __launch_bounds__(64 * W) k_chunk_join(ChunkArgs a, int page_shi
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, side = lane >> 5;
     const uint64_t total_units = a.plan[0];
     if (total_units == 0) return;
-    int64_t id = blockIdx.x;
-    const int o = (int)(id % kOut);
+    uint32_t id = blockIdx.x;
+    const int o = id % kOut;
     id /= kOut;
-    const int head = (int)(id % a.heads);
-    const int64_t slot = id / a.heads;
+    const int slot = id / (uint32_t)a.heads, head = id - slot * a.heads;
     // the sequence with this slot: sequence b owns those from offsets[b] * group / kRows + b on
     int lo = 0, hi = a.step.sequences - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if ((int64_t)a.step.offsets[mid] * a.group / kRows + mid <= slot) lo = mid;
+        if (a.step.offsets[mid] * a.group / kRows + mid <= slot) lo = mid;
         else hi = mid - 1;
     }
     const int b = lo;
     const Job job = job_of<kRows>(a, a.step.offsets[b], a.step.offsets[b + 1], a.step.held[b], page_shift);
-    const int64_t block = slot - (job.off * a.group / kRows + b);
+    const int block = slot - ((int)job.off * a.group / kRows + b);
     if (block < 0 || block >= job.blocks) return;
-    const int64_t rows = (int64_t)job.n * a.group, row0 = block * kRows + wave * 32, row = row0 + col;
+    const int rows = job.n * a.group, row0 = block * kRows + wave * 32, row = row0 + col;
     if (row0 >= rows) return;
     const Ranges ranges(total_units, a.workgroups);
-    const uint64_t item = a.plan[1 + b] + (uint64_t)head * job.total + units_before<kRows>(job, block, a.group);
-    const uint64_t last_unit = a.plan[1 + b] + (uint64_t)head * job.total + units_before<kRows>(job, block + 1, a.group) - 1;
-    const uint32_t first = ranges.of(item), last = ranges.of(last_unit);
+    const uint64_t item = a.plan[1 + b] + (uint64_t)head * job.total;
+    const uint32_t first = ranges.of(item + units_before<kRows>(job, block, a.group) + kBegin), last = ranges.of(item + units_before<kRows>(job, block + 1, a.group) - 1);
     if (first == last) return;                           // written already
     const int64_t places = (int64_t)a.workgroups * 2 * W;
     const floatx4 *const x = (const floatx4 *)a.partial;
@@ -659,25 +670,36 @@ __global__ void __launch_bounds__(64 * W) k_chunk_join(ChunkArgs a, int page_shi
     // the first range has it in its second place, the others in their first ones
     const auto place = [&](uint32_t r) { return ((int64_t)r * 2 + (r == first)) * W + wave; };
     float best = -FLT_MAX;
+#pragma unroll 4
     for (uint32_t r = first; r <= last; ++r) best = fmaxf(best, m[place(r) * 32 + col][0]);
     floatx4 sum[4];
     float total = 0.0f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) sum[i] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-    for (uint32_t r = first; r <= last; ++r) {
-        const floatx2 one = m[place(r) * 32 + col];
-        const float w = __builtin_amdgcn_exp2f(one[0] - best) * one[1];
-        total += w;
+    for (uint32_t r0 = first; r0 <= last; r0 += 4) {
+        // four pieces on their way at a time; those behind the last one are it again, and count for nothing
+        floatx4 y[4][4];
+        floatx2 one[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const floatx4 y = x[place(r) * (32 * DIM / 4) + (o * 4 + i) * 64 + lane];
-            if (w != 0.0f) sum[i] += y * w;
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t r = r0 + k < last ? r0 + k : last;
+            one[k] = m[place(r) * 32 + col];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[k][i] = x[place(r) * (32 * DIM / 4) + (o * 4 + i) * 64 + lane];
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float w = r0 + k <= last ? __builtin_amdgcn_exp2f(one[k][0] - best) * one[k][1] : 0.0f;
+            total += w;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (w != 0.0f) sum[i] += y[k][i] * w;
         }
     }
     if (row >= rows) return;
     const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-    const int64_t q = row / a.group;
-    uint16_t *y = (uint16_t *)a.out.ptr + (job.off + q) * a.out.token + (head * a.group + (int)(row - q * a.group)) * a.out.head + o * 32 + 4 * side;
+    const int q = (int)((uint32_t)row / (uint32_t)a.group);
+    uint16_t *y = (uint16_t *)a.out.ptr + (job.off + q) * a.out.token + (head * a.group + (row - q * a.group)) * a.out.head + o * 32 + 4 * side;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         *(uintx2 *)(y + 8 * i) = uintx2{narrow2<BF16>(sum[i][0] * inv, sum[i][1] * inv), narrow2<BF16>(sum[i][2] * inv, sum[i][3] * inv)};
@@ -715,7 +737,7 @@ void chunk_plan(int64_t tokens, int sequences, int heads, int group, int64_t lon
 {
     a->waves = (double)tokens * group >= 192.0 * sequences ? 8 : 4;
     // a workgroup for each of 256 compute units, or fewer where the announced lengths cannot make so many ranges
-    const double units = (double)slots_of(tokens, group, sequences, a->waves) * heads * ((double)longest / kTokens + 2);
+    const double units = (double)slots_of(tokens, group, sequences, a->waves) * heads * ((double)longest / kTokens + 2 + kBegin);
     const double most = units / kLeast + 1;
     a->workgroups = most < 256 ? (int)most : 256;
 }
