@@ -404,8 +404,8 @@ FC_API int fc_prompt_attention(const void *q, int64_t q_token_stride, int64_t q_
  * 8 bits; binary16 11 bits for what is less than 2^8 below the largest of 64 tokens, absolutely 2^-15 of that one at least.  Pages whose value scale
  * is 2^-36 of the largest among 1024 neighbouring tokens and less are taken as if it were that.  Sums must fit fp32 as there.
  * What the pages hold beyond the held tokens has no influence, and no bit of a row depends on later tokens, infinities and NaN included.
- * longest: the most tokens, held and new, of a sequence; it only sizes the launch.
- * workspace: fc_chunk_attention_workspace_bytes(...) bytes, 16-byte aligned, contents unspecified.
+ * longest: the most tokens, held and new, of a sequence; it only sizes the launch.  tokens * group is below 2^31 - 1024.
+ * workspace: fc_chunk_attention_workspace_bytes(...) bytes, 16-byte aligned, contents unspecified; may be NULL if that is 0.
  */
 FC_API size_t fc_chunk_attention_workspace_bytes(int64_t tokens, int sequences, int heads, int group, int dim, int64_t longest);
 FC_API int fc_chunk_attention(const void *q, int64_t q_token_stride, int64_t q_head_stride, const void *k, int64_t k_token_stride,

@@ -92,6 +92,12 @@ struct PromptArgs {
 };
 hipError_t launch_prompt_attention(const PromptArgs &a, hipStream_t stream);
 
+// An item of the work below that begins in one range and ends in another: in how many it lies (0: there is none), its sequence's first token, its
+// head, and its first row and the number of rows of its sequence
+struct ChunkCut {
+    int pieces, off, head, row, rows, pad[3];
+};
+
 // Attention of the step's new tokens, which are at hand in 16 bits, over what their sequences hold in the cache and over themselves
 struct ChunkArgs {
     Rows q, k, v, out;
@@ -99,13 +105,13 @@ struct ChunkArgs {
     Cache cache;
     // of the items that more than one workgroup has a part of: [workgroups, 2, rows of a workgroup] of normalised results, then maxima and weights
     float *partial;
-    uint64_t *plan;                                     // how many units there are, and where each sequence's begin
+    ChunkCut *cuts;                                     // [workgroups]: what each range begins and does not end
     float scale;
     int heads, group, dim, fp8, bf16;
-    int waves, workgroups;                              // chunk_plan's: wavefronts of a workgroup, with 32 rows each; ranges of the work
+    int waves, by_item, workgroups;                     // chunk_plan's: wavefronts of a workgroup, with 32 rows each; whether each item has a workgroup; or ranges of the work
 };
 void chunk_plan(int64_t tokens, int sequences, int heads, int group, int64_t longest, ChunkArgs *a);
-size_t chunk_workspace(const ChunkArgs &a, int sequences, int dim);
+size_t chunk_workspace(const ChunkArgs &a, int dim);
 hipError_t launch_chunk_attention(const ChunkArgs &a, hipStream_t stream);
 
 // The norm of rows [tokens, hidden]; strides in elements

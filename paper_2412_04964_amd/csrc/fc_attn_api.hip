@@ -262,7 +262,7 @@ size_t fc_chunk_attention_workspace_bytes(int64_t tokens, int sequences, int hea
     if (check_attention(tokens, sequences, heads, group, dim, 1, longest) != FC_OK || dim == 256) return 0;
     fc::ChunkArgs a;
     fc::chunk_plan(tokens, sequences, heads, group, longest, &a);
-    return fc::chunk_workspace(a, sequences, dim);
+    return fc::chunk_workspace(a, dim);
 }
 
 int fc_chunk_attention(const void *q, int64_t q_token_stride, int64_t q_head_stride, const void *k, int64_t k_token_stride, int64_t k_head_stride,
@@ -292,9 +292,9 @@ int fc_chunk_attention(const void *q, int64_t q_token_stride, int64_t q_head_str
     if (tiles * blocks * heads >= 0x1p62 || blocks * heads * 4 >= 2147483648.0) return FC_ERR_SHAPE;
     fc::ChunkArgs a;
     fc::chunk_plan(tokens, sequences, heads, group, longest, &a);
-    const size_t need = fc::chunk_workspace(a, sequences, dim);
-    if (!workspace || workspace_bytes < need) return FC_ERR_WORKSPACE;
-    if (!aligned16(workspace)) return FC_ERR_ALIGN;
+    const size_t need = fc::chunk_workspace(a, dim);
+    if (need && (!workspace || workspace_bytes < need)) return FC_ERR_WORKSPACE;
+    if (need && !aligned16(workspace)) return FC_ERR_ALIGN;
     a.q = rows(q, q_token_stride, q_head_stride);
     a.k = rows(k, k_token_stride, k_head_stride);
     a.v = rows(v, v_token_stride, v_head_stride);
@@ -302,8 +302,8 @@ int fc_chunk_attention(const void *q, int64_t q_token_stride, int64_t q_head_str
     a.step = {offsets, held, sequences, tokens};
     a.cache = {static_cast<uint8_t *>(const_cast<void *>(k_cache)), static_cast<uint8_t *>(const_cast<void *>(v_cache)),
                const_cast<float *>(k_scales), const_cast<float *>(v_scales), page_table, pages, page, table_width};
-    a.plan = static_cast<uint64_t *>(workspace);        // the partials behind it, on a 16-byte boundary
-    a.partial = reinterpret_cast<float *>(static_cast<char *>(workspace) + ((size_t)sequences + 2) / 2 * 16);
+    a.cuts = static_cast<fc::ChunkCut *>(workspace);    // the partials behind it, on a 16-byte boundary
+    a.partial = reinterpret_cast<float *>(a.cuts + a.workgroups);
     a.scale = scale;
     a.heads = heads;
     a.group = group;

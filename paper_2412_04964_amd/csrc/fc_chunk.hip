@@ -20,8 +20,9 @@
 namespace fc {
 namespace {
 
-constexpr int kTokens = 64, kAhead = 6;
+constexpr int kTokens = 64;
 constexpr int kLeast = 2;               // units of a range
+constexpr int kShort = 12;              // tiles of an item up to which it is not cut
 constexpr int kBegin = 3;               // units that what surrounds an item's tiles counts for
 constexpr int rows_of(int waves) { return 32 * waves; }                  // of a workgroup
 template <bool BF16> constexpr float kSlack = BF16 ? 8.0f : 10.0f;
@@ -94,13 +95,16 @@ __device__ __forceinline__ uint64_t quotient(uint64_t a, uint64_t b) { return (a
 struct Ranges {
     uint64_t each;
     uint32_t count, longer;                              // the first `longer` of them have one more than `each`
-    __device__ __forceinline__ Ranges(uint64_t total, uint32_t workgroups)
+    static __device__ __forceinline__ Ranges of_all(uint64_t total, uint32_t workgroups)
     {
+        Ranges r(0, 0);
         const uint64_t most = (total + kLeast - 1) / kLeast;
-        count = most < workgroups ? (uint32_t)most : workgroups;
-        each = count ? quotient(total, count) : 0;
-        longer = (uint32_t)(total - count * each);
+        r.count = most < workgroups ? (uint32_t)most : workgroups;
+        r.each = r.count ? quotient(total, r.count) : 0;
+        r.longer = (uint32_t)(total - r.count * r.each);
+        return r;
     }
+    __device__ __forceinline__ Ranges(uint64_t each_, uint32_t longer_) : each(each_), count(0), longer(longer_) {}
     __device__ __forceinline__ uint64_t begin(uint32_t r) const { return r * each + (r < longer ? r : longer); }
     __device__ __forceinline__ uint32_t of(uint64_t unit) const
     {
@@ -125,6 +129,30 @@ __device__ __forceinline__ uint64_t lane_u64(uint64_t v, int lane)
     return (uint64_t)hi << 32 | lo;
 }
 __device__ __forceinline__ float lane_f(float v, int lane) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane)); }
+
+// Where a call gives a workgroup each item: the item of workgroup `id`, in the units of its sequence
+struct Item {
+    bool there;
+    int b;
+    uint64_t begin, end;
+};
+template <int ROWS>
+__device__ __forceinline__ Item item_of(const ChunkArgs &a, uint32_t id, int page_shift)
+{
+    const int slot = id / (uint32_t)a.heads, head = id - slot * a.heads;
+    // sequence b owns the slots from offsets[b] * group / ROWS + b on (these starts leave every sequence room enough, and need nothing but the offsets)
+    int lo = 0, hi = a.step.sequences - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if ((int64_t)a.step.offsets[mid] * a.group / ROWS + mid <= slot) lo = mid;
+        else hi = mid - 1;
+    }
+    const Job job = job_of<ROWS>(a, a.step.offsets[lo], a.step.offsets[lo + 1], a.step.held[lo], page_shift);
+    const int64_t block = slot - (job.off * a.group / ROWS + lo);
+    if (block < 0 || block >= job.blocks) return {false, 0, 0, 0};
+    const uint64_t begin = (uint64_t)head * job.total;
+    return {true, lo, begin + units_before<ROWS>(job, (int)block, a.group), begin + units_before<ROWS>(job, (int)block + 1, a.group)};
+}
 
 // 4 codes of a word -> two words of 16-bit values, which hold either kind exactly
 template <bool FP8, bool BF16>
@@ -164,6 +192,7 @@ __global__ void __launch_bounds__(64 * W, W == 8 ? 2 : 1) k_chunk_attention(Chun
 {
     constexpr int kSteps = DIM / 16, kOut = DIM / 32, kRow = 2 * DIM, kTile = kTokens * kRow, kRows = rows_of(W);
     constexpr int kOutRow = kRow + 16;
+    constexpr int kAhead = FP8 || BF16 ? 6 : 5;         // operands on their way; one more would not fit the registers
     // A lane loads 16 codes at a time: kLoads of a tile, the first half of them K and the others V (with one load, half of the wavefronts have K)
     constexpr int kLoads = DIM / (8 * W), kEach = kLoads > 1 ? kLoads / 2 : 1, kPieces = DIM / 16, kRound = kTokens / kEach;
     __shared__ __attribute__((aligned(1024))) uint8_t tiles[4][2][kTile];       // K and V
@@ -171,48 +200,72 @@ __global__ void __launch_bounds__(64 * W, W == 8 ? 2 : 1) k_chunk_attention(Chun
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, side = lane >> 5;
     const int sequences = a.step.sequences, group = a.group;
 
-    // ---- this workgroup's range ----
-    uint64_t sum = 0;
-    bool astray = false;
-    int off = 0, next = 0, held = 0;
-    for (int c = 0; c < sequences; c += 64)
-        if (c + lane < sequences) {
-            off = a.step.offsets[c + lane];
-            next = a.step.offsets[c + lane + 1];
-            held = a.step.held[c + lane];
-            sum += (uint64_t)job_of<kRows>(a, off, next, held, page_shift).total * a.heads;
-            astray |= off < 0 || next < off || next > a.step.tokens;
-        }
-    // (units of offsets that do not ascend may be more than 64 bits count: none of them is done)
-    const uint64_t total_units = __any(astray) ? 0 : lane_u64(running_sum(sum, lane), 63);
-    const Ranges ranges(total_units, gridDim.x);
-    if (blockIdx.x == 0 && threadIdx.x == 0) a.plan[0] = total_units;
-    if (blockIdx.x >= ranges.count) return;
-    // workgroups go to the 8 XCDs in turn: an XCD gets neighbouring ranges, whose K and V its L2 then holds
-    const uint32_t range = ranges.count % 8 == 0 ? (blockIdx.x & 7) * (ranges.count / 8) + (blockIdx.x >> 3) : blockIdx.x;
-    uint64_t at = ranges.begin(range);
-    const uint64_t end = ranges.begin(range + 1);
+    // ---- this workgroup's range of all work, or its item ----
+    // (What is needed between items only is kept in LDS: the loop over tiles has no registers for it.)
+    __shared__ uint64_t kept[4];                         // where this range ends, where the sequence's units begin; each and longer of Ranges
+    uint64_t at, first_end, first_begins = 0, each = 0;
+    uint32_t range = 0, longer = 0;
+    bool cut = false;                                    // an item begins here and goes on behind this range
     int b = -1;
-    uint64_t begins = 0, run = 0;
-    for (int c = 0; c < sequences; c += 64) {
-        uint64_t work = 0;
-        if (c + lane < sequences) {
-            off = a.step.offsets[c + lane];
-            next = a.step.offsets[c + lane + 1];
-            held = a.step.held[c + lane];
-            work = (uint64_t)job_of<kRows>(a, off, next, held, page_shift).total * a.heads;
+    if (a.by_item) {
+        const Item item = item_of<kRows>(a, blockIdx.x, page_shift);
+        if (!item.there) return;
+        b = item.b;
+        at = item.begin;
+        first_end = item.end;
+    } else {
+        uint64_t sum = 0;
+        bool astray = false;
+        int off = 0, next = 0, held = 0;
+        for (int c = 0; c < sequences; c += 64)
+            if (c + lane < sequences) {
+                off = a.step.offsets[c + lane];
+                next = a.step.offsets[c + lane + 1];
+                held = a.step.held[c + lane];
+                sum += (uint64_t)job_of<kRows>(a, off, next, held, page_shift).total * a.heads;
+                astray |= off < 0 || next < off || next > a.step.tokens;
+            }
+        // (units of offsets that do not ascend may be more than 64 bits count: none of them is done)
+        const uint64_t total_units = __any(astray) ? 0 : lane_u64(running_sum(sum, lane), 63);
+        const Ranges ranges = Ranges::of_all(total_units, gridDim.x);
+        if (blockIdx.x >= ranges.count) {
+            if (threadIdx.x == 0) a.cuts[blockIdx.x].pieces = 0;
+            return;
         }
-        const uint64_t upto = run + running_sum(work, lane);
-        if (blockIdx.x == 0 && wave == 0 && c + lane < sequences) a.plan[1 + c + lane] = upto - work;
-        const uint64_t past = __ballot(upto > at);
-        if (b < 0 && past) {
-            const int l = __builtin_ctzll(past);
-            b = c + l;
-            begins = lane_u64(upto - work, l);
-            if (blockIdx.x) break;                       // the first one writes where every sequence begins
+        // workgroups go to the 8 XCDs in turn: an XCD gets neighbouring ranges, whose K and V its L2 then holds
+        range = ranges.count % 8 == 0 ? (blockIdx.x & 7) * (ranges.count / 8) + (blockIdx.x >> 3) : blockIdx.x;
+        at = ranges.begin(range);
+        first_end = ranges.begin(range + 1);
+        each = ranges.each;
+        longer = ranges.longer;
+        uint64_t run = 0;
+        for (int c = 0; c < sequences; c += 64) {
+            uint64_t work = 0;
+            if (c + lane < sequences) {
+                off = a.step.offsets[c + lane];
+                next = a.step.offsets[c + lane + 1];
+                held = a.step.held[c + lane];
+                work = (uint64_t)job_of<kRows>(a, off, next, held, page_shift).total * a.heads;
+            }
+            const uint64_t upto = run + running_sum(work, lane);
+            const uint64_t past = __ballot(upto > at);
+            if (past) {
+                const int l = __builtin_ctzll(past);
+                b = c + l;
+                first_begins = lane_u64(upto - work, l);
+                break;
+            }
+            run = lane_u64(upto, 63);
         }
-        run = lane_u64(upto, 63);
     }
+
+    if (threadIdx.x == 0) {
+        kept[0] = first_end;
+        kept[1] = first_begins;
+        kept[2] = each;
+        kept[3] = longer;
+    }
+    __syncthreads();
 
     // ---- places that do not change ----
     const int stride_k = (int)a.k.token, stride_v = (int)a.v.token;
@@ -228,11 +281,15 @@ __global__ void __launch_bounds__(64 * W, W == 8 ? 2 : 1) k_chunk_attention(Chun
     const int half = kLoads == 1 ? wave / (W / 2) : 0, code_wave = kLoads == 1 ? wave % (W / 2) : wave;        // half: 1 for wavefronts that have V only
     const auto code_thread = [&] { return afresh(kLoads == 1 ? threadIdx.x % (32 * W) : threadIdx.x); };
 
-    while (at < end) {
+    while (true) {
+        const uint64_t end = lane_u64(kept[0], 0), begins = lane_u64(kept[1], 0);
+        if (at >= end) break;
         const Job job = job_of<kRows>(a, a.step.offsets[b], a.step.offsets[b + 1], a.step.held[b], page_shift);
         const uint64_t work = (uint64_t)job.total * a.heads;
         if (at >= begins + work) {
-            begins += work;
+            __syncthreads();                             // all have read it
+            if (threadIdx.x == 0) kept[1] = begins + work;
+            __syncthreads();
             ++b;
             continue;
         }
@@ -248,6 +305,13 @@ __global__ void __launch_bounds__(64 * W, W == 8 ? 2 : 1) k_chunk_attention(Chun
         if (tile1 <= tile0) continue;                    // none of its tiles
         const bool whole = tile0 == 0 && tile1 == units - kBegin;
         const int rows = job.n * group, row0 = block * kRows + wave * 32;
+        if (tile0 == 0 && !whole) {
+            cut = true;
+            if (threadIdx.x == 0) {
+                const uint32_t last = Ranges(kept[2], (uint32_t)kept[3]).of(begins + (uint64_t)head * job.total + before + units - 1);
+                a.cuts[range] = {(int)(last - range) + 1, (int)job.off, head, block * kRows, rows, {0, 0, 0}};
+            }
+        }
         const int n = job.n, held = job.held, cached = job.cached, skip = job.skip, codes_end = cached < tile1 ? cached : tile1;
         const bool idle = row0 >= rows;                  // this wavefront has no rows
 
@@ -618,52 +682,38 @@ __global__ void __launch_bounds__(64 * W, W == 8 ? 2 : 1) k_chunk_attention(Chun
                 const int r = row0 + out_row, q = (int)((uint32_t)r / (uint32_t)group);
                 if (r < rows) *(uintx4 *)((uint16_t *)a.out.ptr + (job.off + q) * a.out.token + (head * group + (r - q * group)) * a.out.head + d) = w;
             }
-        } else if (!idle) {
+        } else {
             // as the lanes have them: [place][wavefront][4 elements of each][lane]
             const int64_t place = ((int64_t)range * 2 + (tile0 == 0)) * W + wave, places = (int64_t)gridDim.x * 2 * W;
             floatx4 *const y = (floatx4 *)a.partial + place * (32 * DIM / 4);
             const int mine = afresh(lane);
+            if (!idle)
 #pragma unroll
             for (int o = 0; o < kOut; ++o)
 #pragma unroll
                 for (int r = 0; r < 16; r += 4)
                     y[(o * 4 + r / 4) * 64 + mine] = floatx4{acc[o][r] * inv * unit, acc[o][r + 1] * inv * unit, acc[o][r + 2] * inv * unit, acc[o][r + 3] * inv * unit};
-            if (mine < 32) ((floatx2 *)(a.partial + places * (32 * DIM)))[place * 32 + mine] = floatx2{top, total};
+            if (!idle && mine < 32) ((floatx2 *)(a.partial + places * (32 * DIM)))[place * 32 + mine] = floatx2{top, total};
         }
         __syncthreads();                                     // before the next item's tiles
     }
+    if (!a.by_item && !cut && threadIdx.x == 0) a.cuts[range].pieces = 0;
 }
 
-// Joins what the ranges have of the items that were cut.  A workgroup has 32 of an item's elements (of all its rows), a wavefront 32 rows.  A range
-// has two places: 1 for an item that it begins and does not end, 0 for one that began before.
+// Joins what the ranges have of the items that were cut: a wavefront has 32 elements of 32 rows of the item that begins in range `first` and goes on
+// behind it.  A range has two places: 1 for an item that it begins and does not end, 0 for one that began before.
 template <int DIM, bool BF16, int W>
-__global__ void __launch_bounds__(64 * W) k_chunk_join(ChunkArgs a, int page_shift)
+__global__ void __launch_bounds__(256) k_chunk_join(ChunkArgs a)
 {
-    constexpr int kOut = DIM / 32, kRows = rows_of(W);
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, side = lane >> 5;
-    const uint64_t total_units = a.plan[0];
-    if (total_units == 0) return;
-    uint32_t id = blockIdx.x;
-    const int o = id % kOut;
-    id /= kOut;
-    const int slot = id / (uint32_t)a.heads, head = id - slot * a.heads;
-    // the sequence with this slot: sequence b owns those from offsets[b] * group / kRows + b on
-    int lo = 0, hi = a.step.sequences - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (a.step.offsets[mid] * a.group / kRows + mid <= slot) lo = mid;
-        else hi = mid - 1;
-    }
-    const int b = lo;
-    const Job job = job_of<kRows>(a, a.step.offsets[b], a.step.offsets[b + 1], a.step.held[b], page_shift);
-    const int block = slot - ((int)job.off * a.group / kRows + b);
-    if (block < 0 || block >= job.blocks) return;
-    const int rows = job.n * a.group, row0 = block * kRows + wave * 32, row = row0 + col;
+    constexpr int kOut = DIM / 32;
+    const int lane = threadIdx.x & 63, col = lane & 31, side = lane >> 5;
+    const uint32_t id = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), first = id / (W * kOut);
+    const int wave = id % W, o = id / W % kOut;
+    const ChunkCut cut = a.cuts[first];
+    if (cut.pieces == 0) return;
+    const uint32_t last = first + cut.pieces - 1;
+    const int rows = cut.rows, row0 = cut.row + wave * 32, row = row0 + col, head = cut.head;
     if (row0 >= rows) return;
-    const Ranges ranges(total_units, a.workgroups);
-    const uint64_t item = a.plan[1 + b] + (uint64_t)head * job.total;
-    const uint32_t first = ranges.of(item + units_before<kRows>(job, block, a.group) + kBegin), last = ranges.of(item + units_before<kRows>(job, block + 1, a.group) - 1);
-    if (first == last) return;                           // written already
     const int64_t places = (int64_t)a.workgroups * 2 * W;
     const floatx4 *const x = (const floatx4 *)a.partial;
     const floatx2 *const m = (const floatx2 *)(a.partial + places * (32 * DIM));
@@ -699,7 +749,7 @@ __global__ void __launch_bounds__(64 * W) k_chunk_join(ChunkArgs a, int page_shi
     if (row >= rows) return;
     const float inv = total == 0.0f ? 0.0f : 1.0f / total;
     const int q = (int)((uint32_t)row / (uint32_t)a.group);
-    uint16_t *y = (uint16_t *)a.out.ptr + (job.off + q) * a.out.token + (head * a.group + (row - q * a.group)) * a.out.head + o * 32 + 4 * side;
+    uint16_t *y = (uint16_t *)a.out.ptr + (int64_t)(cut.off + q) * a.out.token + (int64_t)(head * a.group + (row - q * a.group)) * a.out.head + o * 32 + 4 * side;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         *(uintx2 *)(y + 8 * i) = uintx2{narrow2<BF16>(sum[i][0] * inv, sum[i][1] * inv), narrow2<BF16>(sum[i][2] * inv, sum[i][3] * inv)};
@@ -711,11 +761,10 @@ template <int DIM, bool FP8, bool BF16, int W>
 hipError_t chunk(const ChunkArgs &a, hipStream_t stream)
 {
     const int shift = a.cache.page == 16 ? 4 : a.cache.page == 32 ? 5 : 6;
-    const int64_t joins = slots_of(a.step.tokens, a.group, a.step.sequences, W) * a.heads * (DIM / 32);
-    if (!launchable(joins, 64 * W)) return kTooLarge;           // before anything is
-    const hipError_t e = launch_many(k_chunk_attention<DIM, FP8, BF16, W>, a.workgroups, 64 * W, stream, a, shift);
-    if (e != hipSuccess || a.workgroups == 1) return e;
-    return launch_many(k_chunk_join<DIM, BF16, W>, joins, 64 * W, stream, a, shift);
+    const int64_t grid = a.by_item ? slots_of(a.step.tokens, a.group, a.step.sequences, W) * a.heads : a.workgroups;
+    const hipError_t e = launch_many(k_chunk_attention<DIM, FP8, BF16, W>, grid, 64 * W, stream, a, shift);
+    if (e != hipSuccess || a.by_item || a.workgroups == 1) return e;
+    return launch_many(k_chunk_join<DIM, BF16, W>, ((int64_t)a.workgroups - 1) * W * (DIM / 32) / 4, 256, stream, a);
 }
 
 template <int DIM, bool FP8, bool BF16>
@@ -736,15 +785,17 @@ hipError_t chunk_of(const ChunkArgs &a, hipStream_t stream)
 void chunk_plan(int64_t tokens, int sequences, int heads, int group, int64_t longest, ChunkArgs *a)
 {
     a->waves = (double)tokens * group >= 192.0 * sequences ? 8 : 4;
-    // a workgroup for each of 256 compute units, or fewer where the announced lengths cannot make so many ranges
-    const double units = (double)slots_of(tokens, group, sequences, a->waves) * heads * ((double)longest / kTokens + 2 + kBegin);
-    const double most = units / kLeast + 1;
-    a->workgroups = most < 256 ? (int)most : 256;
+    // Short contexts: a workgroup for each item, and nothing to join
+    const double tiles = (double)longest / kTokens + 2, slots = (double)slots_of(tokens, group, sequences, a->waves);
+    a->by_item = tiles <= kShort && slots * heads * 512 < 4294967296.0;
+    // else one for each of 256 compute units, or fewer where the announced lengths cannot make so many ranges
+    const double most = slots * heads * (tiles + kBegin) / kLeast + 1;
+    a->workgroups = a->by_item ? 0 : most < 256 ? (int)most : 256;
 }
 
-size_t chunk_workspace(const ChunkArgs &a, int sequences, int dim)
+size_t chunk_workspace(const ChunkArgs &a, int dim)
 {
-    return ((size_t)sequences + 1 + 1) / 2 * 16 + (a.workgroups > 1 ? (size_t)a.workgroups * 2 * rows_of(a.waves) * (dim + 2) * sizeof(float) : 0);
+    return (size_t)a.workgroups * (sizeof(ChunkCut) + (a.workgroups > 1 ? 2 * rows_of(a.waves) * (dim + 2) * sizeof(float) : 0));
 }
 
 hipError_t launch_chunk_attention(const ChunkArgs &a, hipStream_t stream)

@@ -737,13 +737,13 @@ PyObject *chunk_attention(PyObject *, PyObject *const *a, Py_ssize_t n_args)
         if (!ws || (size_t)ws->numel() < need) return fallback();
     }
     at::Tensor own, own_ws;
-    if (need == 0 || !result_rows(a[10], q, device, own, y)) return fallback();
-    if (!ws) {
+    if (!result_rows(a[10], q, device, own, y)) return fallback();
+    if (need && !ws) {
         own_ws = empty({(int64_t)need}, at::kByte, *q.t);
         ws = &own_ws;
     }
-    void *space = ws->data_ptr(), *stream = stream_of(device);
-    const size_t bytes = (size_t)ws->numel();
+    void *space = ws ? ws->data_ptr() : nullptr, *stream = stream_of(device);
+    const size_t bytes = ws ? (size_t)ws->numel() : 0;
     const void *kc = s.k->data_ptr(), *vc = s.v->data_ptr();
     const float *ks = (const float *)s.ks->data_ptr(), *vs = (const float *)s.vs->data_ptr();
     const int32_t *pages = (const int32_t *)s.pages->data_ptr(), *offsets = (const int32_t *)s.offsets->data_ptr(),

@@ -144,9 +144,11 @@ def test_chunk_attention_matches_its_definition(fc, dtype, quantizer, case):
     *shape, longest = STEPS[case]
     print("chunk", dtype, quantizer, STEPS[case][:6], flush=True)
     s = Step(*shape, dtype, quantizer, case)
-    got = s.call(fc) if longest is None else s.call(fc, longest=longest)
-    check(got, *s.exact())
-    assert same(got, s.call(fc) if longest is None else s.call(fc, longest=longest))
+    want = s.exact()
+    for announced in (s.longest, 1 << 20, 1) if longest is None else (longest,):        # items cut or not
+        got = s.call(fc, longest=announced)
+        check(got, *want)
+        assert same(got, s.call(fc, longest=announced))
     if case in (2, 7):                                   # another softmax scale
         check(s.call(fc, scale=0.5), *s.exact(0.5))
 
@@ -274,9 +276,12 @@ def test_strides_results_and_guards(fc):
     fc.chunk_attention(q, k, v, s.cache, table, offsets + 2, held, s.longest, SYM, out=got)
     assert same(got[2:162], want) and bool((got[:2] == 7).all()) and bool((got[162:] == 7).all())
     # a workspace of exactly the bytes that are asked for, and nothing written behind it
-    need = fc.chunk_attention_workspace_bytes(160, 3, 2, 3, 128, s.longest)
-    space = torch.full((need + 64,), 99, dtype=torch.uint8, device="cuda")
-    assert same(s.call(fc, workspace=space[:need]), want) and bool((space[need:] == 99).all())
+    for longest in (s.longest, 5000):
+        need = fc.chunk_attention_workspace_bytes(160, 3, 2, 3, 128, longest)
+        space = torch.full((need + 64,), 99, dtype=torch.uint8, device="cuda")
+        got = s.call(fc, longest=longest)
+        check(got, *s.exact())
+        assert same(s.call(fc, longest=longest, workspace=space[:need]), got) and bool((space[need:] == 99).all())
 
 
 def test_index_arrays_that_make_no_sense_touch_nothing_else(fc):
@@ -286,9 +291,10 @@ def test_index_arrays_that_make_no_sense_touch_nothing_else(fc):
     for offsets, held, pages in (([0, 60, 50], s.held, table), ([0, 50, 111], s.held, table), ([-5, 50, 110], s.held, table), ([0, 1 << 30, 110], s.held, table),
                                  ([0, 50, 110], [1 << 30, 2147483647], table), ([0, 50, 110], [-2147483648, -1], table), ([0, 50, 110], s.held, table * 0 + 99999),
                                  ([0, 50, 110], s.held, table * 0 - 99999), ([0, 0, 110], [5, 40], table)):
-        print("indexes", offsets, held, flush=True)
-        fc.chunk_attention(s.q, s.k, s.v, s.cache, pages, ints(offsets), ints(held), 400, SYM, out=big[10:120])
-        torch.cuda.synchronize()
+        for longest in (400, 1 << 20):
+            print("indexes", offsets, held, longest, flush=True)
+            fc.chunk_attention(s.q, s.k, s.v, s.cache, pages, ints(offsets), ints(held), longest, SYM, out=big[10:120])
+            torch.cuda.synchronize()
         assert bool((big[:10] == 3).all()) and bool((big[120:] == 3).all())
     assert same(s.call(fc), s.call(fc))
 
@@ -341,7 +347,8 @@ def test_graphs_streams_and_the_native_call(fc):
     s = Step(2, 4, 128, 16, [500, 70], [33, 100], BF16, FP8, 15)
     want = s.call(fc)
     table, offsets, held = s.table.cuda(), offsets_of(s.new), ints(s.held)
-    args = (s.q, s.k, s.v, s.cache, table, offsets, held, s.longest, FP8)
+    args = (s.q, s.k, s.v, s.cache, table, offsets, held, 5000, FP8)          # (announced as long enough to be cut)
+    want = s.call(fc, longest=5000)
     native = fc.binding._calls()
     assert native.chunk_attention(*args, None, None, None) is not None
     fc.binding._native = fc.binding._NoNativeCalls()
@@ -349,7 +356,7 @@ def test_graphs_streams_and_the_native_call(fc):
         assert same(fc.chunk_attention(*args), want)
     finally:
         fc.binding._native = native
-    need = fc.chunk_attention_workspace_bytes(133, 2, 2, 4, 128, s.longest)
+    need = fc.chunk_attention_workspace_bytes(133, 2, 2, 4, 128, 5000)
     space = torch.empty(need, dtype=torch.uint8, device="cuda")
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
@@ -388,9 +395,11 @@ def test_empty_calls_and_refusals(fc):
     for at, bad in ((1, s.k[:-1]), (2, s.v[:, :1]), (0, s.q[:, :3]), (0, s.q[..., :32]), (4, table[:0]), (6, held[:0]), (3, s.cache[:3])):
         with pytest.raises((ValueError, fc.FcError)):
             fc.chunk_attention(*args[:at], bad, *args[at + 1:])
-    for more in (dict(quantizer=0), dict(quantizer=3), dict(scale=0.0), dict(scale=float("inf")), dict(workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))):
+    for more in (dict(quantizer=0), dict(quantizer=3), dict(scale=0.0), dict(scale=float("inf"))):
         with pytest.raises(fc.FcError):
             fc.chunk_attention(*args, **more)
+    with pytest.raises(fc.FcError):
+        fc.chunk_attention(*args[:7], 100000, workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))
     with pytest.raises(fc.FcError):
         fc.chunk_attention(*args[:7], 0)
     with pytest.raises(ValueError):

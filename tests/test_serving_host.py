@@ -138,14 +138,14 @@ def chunk(L, q=P, k=P, v=P, tokens=4, heads=2, group=2, dim=64, type=0, quantize
 def test_chunk_attention_argument_checks(L):
     assert chunk(L, type=2) == chunk(L, quantizer=0) == chunk(L, quantizer=3) == -8
     assert chunk(L, dim=256) == chunk(L, dim=32) == chunk(L, heads=0) == chunk(L, group=0) == chunk(L, group=40000) == chunk(L, longest=0) == chunk(L, tokens=-1) == -4
-    assert chunk(L, page=8) == chunk(L, pages=0) == chunk(L, width=0) == chunk(L, sequences=0) == chunk(L, vt=1 << 25) == chunk(L, tokens=(1 << 31) - 1) == -4
+    assert chunk(L, page=8) == chunk(L, pages=0) == chunk(L, width=0) == chunk(L, sequences=0) == chunk(L, vt=1 << 25) == chunk(L, tokens=(1 << 31) - 1) == chunk(L, tokens=1 << 30) == -4
     assert chunk(L, scale=0.0) == chunk(L, scale=-1.0) == chunk(L, scale=float("nan")) == -4
     for name in ("q", "k", "v", "cache", "scales", "pt", "offsets", "held", "out"):
         assert chunk(L, **{name: None}) == -1, name
-    assert chunk(L, q=P + 2) == chunk(L, vt=12) == chunk(L, cache=P + 8) == chunk(L, ws=P + 4) == -5
-    need = L.fc_chunk_attention_workspace_bytes(4, 1, 2, 2, 64, 64)
+    assert chunk(L, q=P + 2) == chunk(L, vt=12) == chunk(L, cache=P + 8) == -5
+    need = L.fc_chunk_attention_workspace_bytes(4, 1, 2, 2, 64, 100000)
     assert need > 0 and need % 4 == 0
-    assert chunk(L, bytes=need - 1) == chunk(L, ws=None) == -6
+    assert chunk(L, longest=100000, bytes=need - 1) == chunk(L, longest=100000, ws=None) == -6 and chunk(L, longest=100000, ws=P + 4) == -5
     assert chunk(L, tokens=0, q=None, k=None, v=None, out=None, cache=None, ws=None) == 0
     for bad in ((4, 1, 2, 2, 256, 64), (4, 1, 0, 2, 64, 64), (-1, 1, 2, 2, 64, 64), (4, 1, 2, 2, 64, 0)):
         assert L.fc_chunk_attention_workspace_bytes(*bad) == 0
