@@ -8,6 +8,11 @@
 namespace fc {
 namespace {
 
+typedef int intx4 __attribute__((ext_vector_type(4)));
+struct __attribute__((packed, aligned(4))) intx4_as_int {        // on any 4-byte boundary
+    intx4 v;
+};
+
 // entries of a row that hold tokens
 __device__ __forceinline__ int64_t filled_slots(int64_t held, int page_shift) { return held > 0 ? (held + (1 << page_shift) - 1) >> page_shift : 0; }
 
@@ -46,6 +51,8 @@ __global__ void __launch_bounds__(256) k_pages_fork(ForkArgs a, int page_shift)
         if (by && id >= 0 && id < a.pages) atomicAdd(&a.uses[id], by);
     }
 }
+
+constexpr int kSegments = 8;                             // of a pool that every workgroup counts itself
 
 // sums of the lanes up to this one
 __device__ __forceinline__ int upto(int v, int lane)
@@ -90,72 +97,85 @@ __device__ __forceinline__ Slots slots_of(const ReserveArgs &a, int b, int page_
     return {(int)first, (int)(last - first) + 1, (begin & ((1 << page_shift) - 1)) != 0};
 }
 
-// One workgroup for the step.  While it runs, source[b] is the partly filled page that sequence b writes to, or -1, and target[b] where its
-// fresh pages begin among all.
+// One workgroup for the step: a lane has a sequence, the first 1024 of them from beginning to end.  While it runs, source[b] is the partly filled
+// page that sequence b writes to, or -1, and target[b] where its fresh pages begin among all (~ that: and it copies).
+// Bound by reads that depend on each other and by the walk through `uses` up to the last page that is needed (16 counts a lane at a time): 4 sequences
+// 5 us, 241 of which half part with a page, in a pool of 20000, 10 us.
 __global__ void __launch_bounds__(1024) k_pages_reserve(ReserveArgs a, int page_shift)
 {
     __shared__ int sums[16];
-    __shared__ int staged[1024];
+    __shared__ __attribute__((aligned(16))) int staged[1024];
     const auto none = [&](int id) { return id < 0 || id >= a.pages; };
-    for (int b = threadIdx.x; b < a.sequences; b += 1024) {
+    Slots own = {0, 0, false};
+    int own_page = -1, own_id = -1;                      // of the first slot: what the table has there; the page if it is partly filled
+    const auto look = [&](int b) {
         const Slots s = slots_of(a, b, page_shift);
-        int mine = -1;
-        if (s.count && s.partial) {
-            mine = a.table[(int64_t)b * a.width + s.first];
-            if (none(mine)) mine = -1;
+        const int id = s.count ? a.table[(int64_t)b * a.width + s.first] : -1;
+        if (b < 1024) {
+            own = s;
+            own_page = id;
+            own_id = s.partial && !none(id) ? id : -1;
         }
-        a.source[b] = mine;
-    }
+        return s.partial && !none(id) ? id : -1;
+    };
+    for (int b = threadIdx.x; b < a.sequences; b += 1024) a.source[b] = look(b);
     __syncthreads();
     // who copies, and how many fresh pages each sequence takes
     int needed = 0;
     for (int c = 0; c < a.sequences; c += 1024) {
         const int b = c + threadIdx.x;
         const bool here = b < a.sequences;
-        const int mine = here ? a.source[b] : -1, users = mine >= 0 ? a.uses[mine] : 0;
+        const int mine = !here ? -1 : c ? a.source[b] : own_id, users = mine >= 0 ? a.uses[mine] : 0;
         int writers = 0, later = 0;
-        for (int d = 0; d < a.sequences; d += 1024) {
-            __syncthreads();
-            staged[threadIdx.x] = d + threadIdx.x < a.sequences ? a.source[d + threadIdx.x] : -1;
-            __syncthreads();
-            if (users > 1) {
-                const int n = a.sequences - d < 1024 ? a.sequences - d : 1024;
-                for (int i = 0; i < n; ++i) {
-                    const bool same = staged[i] == mine;
-                    writers += same;
-                    later += same && d + i > b;
+        if (__syncthreads_or(users > 1)) {
+            for (int d = 0; d < a.sequences; d += 1024) {
+                __syncthreads();
+                staged[threadIdx.x] = d + threadIdx.x < a.sequences ? d ? a.source[d + threadIdx.x] : own_id : -1;
+                __syncthreads();
+                if (users > 1) {
+                    const int n = a.sequences - d < 1024 ? a.sequences - d : 1024;
+#pragma unroll 4
+                    for (int i = 0; i < n; i += 4) {     // (behind the last sequence there is no page)
+                        const intx4 four = *(const intx4 *)&staged[i];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            writers += four[j] == mine;
+                            later += four[j] == mine && d + i + j > b;
+                        }
+                    }
                 }
             }
         }
         const bool copies = users > 1 && (later || writers < users);
         int want = copies;
         if (here) {
-            const Slots s = slots_of(a, b, page_shift);
-            for (int i = 0; i < s.count; ++i) want += none(a.table[(int64_t)b * a.width + s.first + i]);
+            const Slots s = c ? slots_of(a, b, page_shift) : own;
+            if (c == 0) want += s.count && none(own_page);
+            for (int i = c == 0; i < s.count; ++i) want += none(a.table[(int64_t)b * a.width + s.first + i]);
         }
         int all;
         const int start = needed + before(want, sums, &all);
-        if (here) a.target[b] = copies ? ~start : start;  // (who does not copy has a start of 0 or more)
+        if (here) a.target[b] = copies ? ~start : start;
         needed += all;
     }
     // the lowest free pages
     int found = 0;
-    for (int64_t p0 = 0; p0 < a.pages && found < needed; p0 += 4096) {
-        const int64_t p = p0 + 4 * threadIdx.x;
-        bool free[4];
-        int mine = 0, all;
+    for (int64_t p0 = 0; p0 < a.pages && found < needed; p0 += 16384) {
+        const int64_t p = p0 + 16 * threadIdx.x;
+        uint32_t free = 0;
+        if (p + 16 <= a.pages) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            free[i] = p + i < a.pages && a.uses[p + i] == 0;
-            mine += free[i];
-        }
-        int at = found + before(mine, sums, &all);
+            for (int i = 0; i < 4; ++i) {
+                const intx4 u = ((const intx4_as_int *)(a.uses + p))[i].v;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (free[i]) {
-                if (at < needed) a.fresh[at] = (int)(p + i);
-                ++at;
+                for (int j = 0; j < 4; ++j) free |= (u[j] == 0) << (4 * i + j);
             }
+        } else {
+            for (int i = 0; i < 16; ++i) free |= (p + i < a.pages && a.uses[p + i] == 0) << i;
+        }
+        int all;
+        int at = found + before(__builtin_popcount(free), sums, &all);
+        for (; free && at < needed; free &= free - 1) a.fresh[at++] = (int)p + __builtin_ctz(free);
         found += all;
     }
     __syncthreads();
@@ -165,76 +185,97 @@ __global__ void __launch_bounds__(1024) k_pages_reserve(ReserveArgs a, int page_
         const bool copies = mark < 0 && found >= needed;
         int at = mark < 0 ? ~mark : mark;
         int target = -1;
-        if (found >= needed) {
-            const Slots s = slots_of(a, b, page_shift);
+        if (found >= needed && needed) {
+            const Slots s = b < 1024 ? own : slots_of(a, b, page_shift);
             int32_t *row = a.table + (int64_t)b * a.width + s.first;
             for (int i = 0; i < s.count; ++i) {
                 const bool copy = copies && i == 0;
-                if (!copy && !none(row[i])) continue;
+                if (!copy && !none(b < 1024 && i == 0 ? own_page : row[i])) continue;
                 const int id = a.fresh[at++];
                 row[i] = id;
                 a.uses[id] = 1;
                 if (copy) target = id;
             }
-            if (copies) atomicAdd(&a.uses[a.source[b]], -1);
+            if (copies) atomicAdd(&a.uses[b < 1024 ? own_id : a.source[b]], -1);
         }
         a.target[b] = target;
         if (!copies) a.source[b] = -1;
     }
 }
 
-// used pages of each segment
-__global__ void __launch_bounds__(256) k_pages_count(CompactArgs a)
+// used ones among 4 pages from p on
+__device__ __forceinline__ int used4(const CompactArgs &a, int64_t p, int (&use)[4])
 {
-    __shared__ int total;
-    if (threadIdx.x == 0) total = 0;
-    __syncthreads();
-    int n = 0;
-    for (int i = threadIdx.x; i < kSegment; i += 256) {
-        const int64_t p = (int64_t)blockIdx.x * kSegment + i;
-        n += p < a.pages && a.uses[p] > 0;
+    if (p + 4 <= a.pages) {
+        const intx4 u = ((const intx4_as_int *)(a.uses + p))->v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) use[i] = u[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) use[i] = p + i < a.pages ? a.uses[p + i] : 0;
     }
-    if (n) atomicAdd(&total, n);
-    __syncthreads();
-    if (threadIdx.x == 0) a.counts[blockIdx.x] = total;
+    return (use[0] > 0) + (use[1] > 0) + (use[2] > 0) + (use[3] > 0);
 }
 
-// Each segment's free pages below U (the pages in use) and used ones from U on, as the k-th of all
+// used pages of each segment
+__global__ void __launch_bounds__(1024) k_pages_count(CompactArgs a)
+{
+    __shared__ int sums[16];
+    int use[4], n;
+    before(used4(a, (int64_t)blockIdx.x * kSegment + 4 * threadIdx.x, use), sums, &n);
+    if (threadIdx.x == 0) a.counts[blockIdx.x] = n;
+}
+
+// Each segment's free pages below U (the pages in use) and used ones from U on, as the k-th of all.  COUNTED: the segments' used pages are known; in
+// a small pool every workgroup counts them all itself.
+template <bool COUNTED>
 __global__ void __launch_bounds__(1024) k_pages_pair(CompactArgs a, int segments)
 {
     __shared__ int sums[16];
+    __shared__ int used[COUNTED ? 1 : kSegments];
     const int64_t p0 = (int64_t)blockIdx.x * kSegment;
+    int use[4], n;
+    if constexpr (!COUNTED) {
+        if (threadIdx.x < kSegments) used[threadIdx.x] = 0;
+        __syncthreads();
+        // (all reads are on their way before the first sum)
+        int mine[kSegments];
+#pragma unroll
+        for (int i = 0; i < kSegments; ++i) mine[i] = used4(a, (int64_t)i * kSegment + 4 * threadIdx.x, use);
+#pragma unroll
+        for (int i = 0; i < kSegments; ++i) {
+            if (i >= segments) break;
+            const int all = __builtin_amdgcn_readlane(upto(mine[i], threadIdx.x & 63), 63);
+            if ((threadIdx.x & 63) == 0) atomicAdd(&used[i], all);
+        }
+        __syncthreads();
+    }
+    const auto count = [&](int i) { return COUNTED ? a.counts[i] : used[i]; };
     int earlier = 0, all = 0;                            // used pages before this segment; all of them
     {
-        int mine = 0, rest = 0, n;
+        int mine = 0, rest = 0;
         for (int i = threadIdx.x; i < segments; i += 1024) {
-            const int c = a.counts[i];
+            const int c = count(i);
             mine += i < (int)blockIdx.x ? c : 0;
             rest += c;
         }
-        before(mine, sums, &n);
-        earlier = n;
-        before(rest, sums, &n);
-        all = n;
+        before(mine, sums, &earlier);
+        before(rest, sums, &all);
     }
     // used pages before page U
     int below = 0;
     {
-        const int segment = all / kSegment;
-        int mine = 0, n;
-        for (int i = threadIdx.x; i < segment; i += 1024) mine += a.counts[i];
-        for (int i = threadIdx.x; i < all % kSegment; i += 1024) mine += a.uses[(int64_t)segment * kSegment + i] > 0;
-        before(mine, sums, &n);
-        below = n;
+        const int segment = all / kSegment, rest = all - segment * kSegment - 4 * (int)threadIdx.x;      // of the last segment, from this lane's on
+        int mine = 0;
+        for (int i = threadIdx.x; i < segment; i += 1024) mine += count(i);
+        used4(a, (int64_t)segment * kSegment + 4 * threadIdx.x, use);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mine += i < rest && use[i] > 0;
+        before(mine, sums, &below);
     }
     const int moves = all - below;
     const int64_t p = p0 + 4 * threadIdx.x;
-    int use[4], mine = 0, n;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        use[i] = p + i < a.pages ? a.uses[p + i] : 0;
-        mine += use[i] > 0;
-    }
+    const int mine = used4(a, p, use);
     int at = earlier + before(mine, sums, &n);           // used pages before this lane's
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -276,6 +317,9 @@ __global__ void __launch_bounds__(256) k_pages_move(CompactArgs a)
 
 constexpr int64_t kCopy = 16384;                         // bytes of each cache that a workgroup copies
 
+// Memory bounds it: 5000 pages of 8 heads of 16 tokens of 128, 329 MB read and written, 58 us, 5.7 TB/s.  Every lane's reads are on their way
+// before it writes.  STREAM: more than the memory-side cache holds; a few pages are read again soon.
+template <bool STREAM>
 __global__ void __launch_bounds__(256) k_cache_copy(CopyArgs a, int parts)
 {
     const int64_t pair = blockIdx.x / parts;
@@ -283,12 +327,26 @@ __global__ void __launch_bounds__(256) k_cache_copy(CopyArgs a, int parts)
     const int64_t from = a.source[pair], to = a.target[pair];
     if (from < 0 || to < 0 || from >= a.pages || to >= a.pages || from == to) return;
     const int64_t left = a.bytes - part * kCopy;
-    for (int64_t i = threadIdx.x * 16; i < kCopy && i < left; i += 256 * 16) {
-        const int64_t at = part * kCopy + i;
-        const uintx4 k = *(const uintx4 *)(a.k + from * a.bytes + at), v = *(const uintx4 *)(a.v + from * a.bytes + at);
-        *(uintx4 *)(a.k + to * a.bytes + at) = k;
-        *(uintx4 *)(a.v + to * a.bytes + at) = v;
-    }
+    constexpr int kEach = kCopy / (256 * 16);
+    const int64_t at = part * kCopy + threadIdx.x * 16;
+    uintx4 k[kEach], v[kEach];
+    const auto load = [](const uint8_t *p) { return STREAM ? __builtin_nontemporal_load((const uintx4 *)p) : *(const uintx4 *)p; };
+    const auto store = [](uintx4 w, uint8_t *p) {
+        if constexpr (STREAM) __builtin_nontemporal_store(w, (uintx4 *)p);
+        else *(uintx4 *)p = w;
+    };
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+        if (threadIdx.x * 16 + i * 4096 < left) {
+            k[i] = load(a.k + from * a.bytes + at + i * 4096);
+            v[i] = load(a.v + from * a.bytes + at + i * 4096);
+        }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+        if (threadIdx.x * 16 + i * 4096 < left) {
+            store(k[i], a.k + to * a.bytes + at + i * 4096);
+            store(v[i], a.v + to * a.bytes + at + i * 4096);
+        }
     if (part == 0)
         for (int h = threadIdx.x; h < a.heads; h += 256) {
             a.k_scales[to * a.heads + h] = a.k_scales[from * a.heads + h];
@@ -314,8 +372,13 @@ hipError_t launch_pages_compact(const CompactArgs &a, hipStream_t stream)
 {
     const int64_t segments = (a.pages + kSegment - 1) / kSegment, most = a.entries > a.pages / 2 ? a.entries : a.pages / 2;
     if (!launchable((most + 255) / 256, 256)) return kTooLarge;        // before anything is
-    hipError_t e = launch_many(k_pages_count, segments, 256, stream, a);
-    if (e == hipSuccess) e = launch_many(k_pages_pair, segments, 1024, stream, a, (int)segments);
+    hipError_t e = hipSuccess;
+    if (segments <= kSegments) {
+        e = launch_many(k_pages_pair<false>, segments, 1024, stream, a, (int)segments);
+    } else {
+        e = launch_many(k_pages_count, segments, 1024, stream, a);
+        if (e == hipSuccess) e = launch_many(k_pages_pair<true>, segments, 1024, stream, a, (int)segments);
+    }
     if (e == hipSuccess && most) e = launch_many(k_pages_move, (most + 255) / 256, 256, stream, a);
     return e;
 }
@@ -323,7 +386,8 @@ hipError_t launch_pages_compact(const CompactArgs &a, hipStream_t stream)
 hipError_t launch_cache_copy(const CopyArgs &a, hipStream_t stream)
 {
     const int64_t parts = (a.bytes + kCopy - 1) / kCopy;
-    return a.count > (int64_t)1 << 32 ? kTooLarge : launch_many(k_cache_copy, a.count * parts, 256, stream, a, (int)parts);
+    if (beyond_cache((double)a.count * a.bytes * 2)) return launch_many(k_cache_copy<true>, a.count * parts, 256, stream, a, (int)parts);
+    return launch_many(k_cache_copy<false>, a.count * parts, 256, stream, a, (int)parts);
 }
 
 }  // namespace fc

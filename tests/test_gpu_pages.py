@@ -233,6 +233,19 @@ def test_compact(fc, pages, sequences, width):
         assert all(torch.equal(a, b) for a, b in zip(out, got))
 
 
+@pytest.mark.parametrize("pages", [5, 4095, 4096, 20011, 32768, 32769, 70001])
+def test_compact_pools_of_any_fill(fc, pages):
+    for fill in (0.02, 0.5, 0.97, 1.0):
+        rng = random.Random(pages)
+        uses = [rng.randint(1, 3) if rng.random() < fill else rng.choice([0, 0, -2]) for _ in range(pages)]
+        table = [[rng.randrange(-2, pages + 2) for _ in range(37)] for _ in range(11)]
+        want = compact([[p if 0 <= p < pages and uses[p] > 0 else -5 for p in row] for row in table], uses)
+        got = fc.pages_compact(ints(table), ints(uses))
+        assert got[4].item() == want[4] and got[1].tolist() == want[1] and got[2].tolist() == want[2] and got[3].tolist() == want[3]
+        for row, mine, old in zip(got[0].tolist(), want[0], table):
+            assert row == [m if m != -5 else p for m, p in zip(mine, old)]        # entries that name no page in use stay
+
+
 def cache_of(pages, heads, page, dim, seed):
     g = torch.Generator().manual_seed(seed)
     codes = [torch.randint(0, 256, (pages, heads, page, dim), dtype=torch.uint8, generator=g).cuda() for _ in range(2)]
