@@ -52,34 +52,34 @@ __global__ void __launch_bounds__(256) k_pages_fork(ForkArgs a, int page_shift)
     }
 }
 
-constexpr int kSegments = 8;                             // of a pool that every workgroup counts itself
+constexpr int kFew = 4096;                               // fresh pages that are listed in LDS
+constexpr int kSegments = 8;                             // of a pool that every workgroup counts itself (20000 pages: 6.8 us, with counts ahead 5 + 4.5)
 
-// sums of the lanes up to this one
-__device__ __forceinline__ int upto(int v, int lane)
+// Sums of the lanes up to this one: within 16 lanes, then from the last lane of the 16 before, then from the last of the first 32
+__device__ __forceinline__ int upto(int v)
 {
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-        const int u = __shfl_up(v, m);
-        if (lane >= m) v += u;
-    }
-    return v;
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);
+    return v + __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
 }
 
-// Sum of `v` over the lanes of a workgroup of 16 wavefronts before this one, and over all.  Two barriers.
-__device__ __forceinline__ int before(int v, int (&sums)[16], int *all)
+// Sum of `v` over the lanes of a workgroup of 16 wavefronts before this one, and over all; a second value's sum over all.  Two barriers.
+__device__ __forceinline__ int before(int v, int (&sums)[2][16], int *all, int other = 0, int *others = nullptr)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, run = upto(v, lane);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), run = upto(v), more = others ? upto(other) : 0;
     __syncthreads();
-    if (lane == 63) sums[wave] = run;
-    __syncthreads();
-    int base = 0, total = 0;
-#pragma unroll
-    for (int w = 0; w < 16; ++w) {
-        if (w < wave) base += sums[w];
-        total += sums[w];
+    if (lane == 63) {
+        sums[0][wave] = run;
+        if (others) sums[1][wave] = more;
     }
-    *all = total;
-    return base + run - v;
+    __syncthreads();
+    const int mine = upto(sums[0][lane & 15]);           // (of the 16, in every 16 lanes; the first ones count)
+    *all = __builtin_amdgcn_readlane(mine, 15);
+    if (others) *others = __builtin_amdgcn_readlane(upto(sums[1][lane & 15]), 15);
+    return (wave ? __builtin_amdgcn_readlane(mine, wave - 1) : 0) + run - v;
 }
 
 // The slots of a sequence's table row that its new tokens go to
@@ -100,12 +100,29 @@ __device__ __forceinline__ Slots slots_of(const ReserveArgs &a, int b, int page_
 // One workgroup for the step: a lane has a sequence, the first 1024 of them from beginning to end.  While it runs, source[b] is the partly filled
 // page that sequence b writes to, or -1, and target[b] where its fresh pages begin among all (~ that: and it copies).
 // Bound by reads that depend on each other and by the walk through `uses` up to the last page that is needed (16 counts a lane at a time): 4 sequences
-// 5 us, 241 of which half part with a page, in a pool of 20000, 10 us.
+// 6.4 us, 241 of which half part with a page, in a pool of 20000, 12.8 us.
 __global__ void __launch_bounds__(1024) k_pages_reserve(ReserveArgs a, int page_shift)
 {
-    __shared__ int sums[16];
+    __shared__ int sums[2][16];
     __shared__ __attribute__((aligned(16))) int staged[1024];
+    __shared__ int few[kFew];                            // the fresh pages, if they are few
     const auto none = [&](int id) { return id < 0 || id >= a.pages; };
+    // free ones among the 16 pages from p on
+    const auto free_of = [&](int64_t p) {
+        uint32_t free = 0;
+        if (p + 16 <= a.pages) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const intx4 u = ((const intx4_as_int *)(a.uses + p))[i].v;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) free |= (u[j] == 0) << (4 * i + j);
+            }
+        } else {
+            for (int i = 0; i < 16; ++i) free |= (p + i < a.pages && a.uses[p + i] == 0) << i;
+        }
+        return free;
+    };
+    uint32_t free_next = free_of(16 * threadIdx.x);      // (on its way while the rest is found out)
     Slots own = {0, 0, false};
     int own_page = -1, own_id = -1;                      // of the first slot: what the table has there; the page if it is partly filled
     const auto look = [&](int b) {
@@ -159,23 +176,14 @@ __global__ void __launch_bounds__(1024) k_pages_reserve(ReserveArgs a, int page_
         needed += all;
     }
     // the lowest free pages
+    int *const fresh = needed <= kFew ? few : a.fresh;
     int found = 0;
     for (int64_t p0 = 0; p0 < a.pages && found < needed; p0 += 16384) {
-        const int64_t p = p0 + 16 * threadIdx.x;
-        uint32_t free = 0;
-        if (p + 16 <= a.pages) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const intx4 u = ((const intx4_as_int *)(a.uses + p))[i].v;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) free |= (u[j] == 0) << (4 * i + j);
-            }
-        } else {
-            for (int i = 0; i < 16; ++i) free |= (p + i < a.pages && a.uses[p + i] == 0) << i;
-        }
+        uint32_t free = free_next;
+        free_next = free_of(p0 + 16384 + 16 * threadIdx.x);
         int all;
         int at = found + before(__builtin_popcount(free), sums, &all);
-        for (; free && at < needed; free &= free - 1) a.fresh[at++] = (int)p + __builtin_ctz(free);
+        for (; free && at < needed; free &= free - 1) fresh[at++] = (int)p0 + 16 * threadIdx.x + __builtin_ctz(free);
         found += all;
     }
     __syncthreads();
@@ -191,7 +199,7 @@ __global__ void __launch_bounds__(1024) k_pages_reserve(ReserveArgs a, int page_
             for (int i = 0; i < s.count; ++i) {
                 const bool copy = copies && i == 0;
                 if (!copy && !none(b < 1024 && i == 0 ? own_page : row[i])) continue;
-                const int id = a.fresh[at++];
+                const int id = fresh[at++];
                 row[i] = id;
                 a.uses[id] = 1;
                 if (copy) target = id;
@@ -220,7 +228,7 @@ __device__ __forceinline__ int used4(const CompactArgs &a, int64_t p, int (&use)
 // used pages of each segment
 __global__ void __launch_bounds__(1024) k_pages_count(CompactArgs a)
 {
-    __shared__ int sums[16];
+    __shared__ int sums[2][16];
     int use[4], n;
     before(used4(a, (int64_t)blockIdx.x * kSegment + 4 * threadIdx.x, use), sums, &n);
     if (threadIdx.x == 0) a.counts[blockIdx.x] = n;
@@ -231,52 +239,41 @@ __global__ void __launch_bounds__(1024) k_pages_count(CompactArgs a)
 template <bool COUNTED>
 __global__ void __launch_bounds__(1024) k_pages_pair(CompactArgs a, int segments)
 {
-    __shared__ int sums[16];
-    __shared__ int used[COUNTED ? 1 : kSegments];
+    __shared__ int sums[2][16];
     const int64_t p0 = (int64_t)blockIdx.x * kSegment;
-    int use[4], n;
+    int use[4], earlier, all, below, n;                  // used pages before this segment, all of them, and those before page U
     if constexpr (!COUNTED) {
-        if (threadIdx.x < kSegments) used[threadIdx.x] = 0;
-        __syncthreads();
-        // (all reads are on their way before the first sum)
-        int mine[kSegments];
-#pragma unroll
-        for (int i = 0; i < kSegments; ++i) mine[i] = used4(a, (int64_t)i * kSegment + 4 * threadIdx.x, use);
+        uint32_t used = 0;                               // 4 bits for this lane's pages of each segment
 #pragma unroll
         for (int i = 0; i < kSegments; ++i) {
-            if (i >= segments) break;
-            const int all = __builtin_amdgcn_readlane(upto(mine[i], threadIdx.x & 63), 63);
-            if ((threadIdx.x & 63) == 0) atomicAdd(&used[i], all);
+            used4(a, (int64_t)i * kSegment + 4 * threadIdx.x, use);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) used |= (uint32_t)(use[j] > 0) << (4 * i + j);
         }
-        __syncthreads();
-    }
-    const auto count = [&](int i) { return COUNTED ? a.counts[i] : used[i]; };
-    int earlier = 0, all = 0;                            // used pages before this segment; all of them
-    {
-        int mine = 0, rest = 0;
-        for (int i = threadIdx.x; i < segments; i += 1024) {
-            const int c = count(i);
-            mine += i < (int)blockIdx.x ? c : 0;
-            rest += c;
-        }
-        before(mine, sums, &earlier);
-        before(rest, sums, &all);
-    }
-    // used pages before page U
-    int below = 0;
-    {
+        const auto bits = [](int n) { return n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1; };
+        before(__builtin_popcount(used & bits(4 * blockIdx.x)), sums, &earlier, __builtin_popcount(used), &all);
         const int segment = all / kSegment, rest = all - segment * kSegment - 4 * (int)threadIdx.x;      // of the last segment, from this lane's on
-        int mine = 0;
-        for (int i = threadIdx.x; i < segment; i += 1024) mine += count(i);
+        n = __builtin_popcount(used & bits(4 * segment + (rest < 0 ? 0 : rest > 4 ? 4 : rest)));
+    } else {
+        int mine = 0, sum = 0;
+        for (int i = threadIdx.x; i < segments; i += 1024) {
+            const int c = a.counts[i];
+            mine += i < (int)blockIdx.x ? c : 0;
+            sum += c;
+        }
+        before(mine, sums, &earlier, sum, &all);
+        const int segment = all / kSegment, rest = all - segment * kSegment - 4 * (int)threadIdx.x;
+        n = 0;
+        for (int i = threadIdx.x; i < segment; i += 1024) n += a.counts[i];
         used4(a, (int64_t)segment * kSegment + 4 * threadIdx.x, use);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) mine += i < rest && use[i] > 0;
-        before(mine, sums, &below);
+        for (int i = 0; i < 4; ++i) n += i < rest && use[i] > 0;
     }
-    const int moves = all - below;
     const int64_t p = p0 + 4 * threadIdx.x;
     const int mine = used4(a, p, use);
-    int at = earlier + before(mine, sums, &n);           // used pages before this lane's
+    int all_here;
+    int at = before(mine, sums, &all_here, n, &below) + earlier;         // used pages before this lane's
+    const int moves = all - below;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         if (p + i >= a.pages) break;
