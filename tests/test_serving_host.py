@@ -93,7 +93,7 @@ import ctypes, json, sys
 ctypes.CDLL(sys.argv[1], ctypes.RTLD_GLOBAL)
 L = ctypes.CDLL(sys.argv[2])
 for name, args in json.load(sys.stdin):
-    print("R", getattr(L, name)(*[ctypes.c_double(a) if isinstance(a, float) else ctypes.c_int64(a) for a in args]), flush=True)
+    print("R", getattr(L, name)(*[{float: ctypes.c_double, str: lambda a: ctypes.c_float(float(a)), int: ctypes.c_int64}[type(a)](a) for a in args]), flush=True)
 """
 
 
@@ -153,3 +153,34 @@ def test_chunk_attention_argument_checks(L):
     for sequences, heads in ((256, 8), (1, 1), (65536, 64)):
         needs = [L.fc_chunk_attention_workspace_bytes(1 << 20, sequences, heads, 8, 128, longest) for longest in (1 << 20, 1 << 26, (1 << 31) - 1)]
         assert needs[0] > 0 and needs == [needs[0]] * 3
+
+
+def chunk_call(tokens, heads, group, dim, sequences, longest, ws=1 << 40, scale="0.125"):
+    row = heads * group * dim
+    return "fc_chunk_attention", [P, row, dim, P, heads * dim, dim, P, heads * dim, dim, tokens, heads, group, dim, 0, 1, P, P, P, P, 1 << 20, 16, P, 1 << 20, P, P,
+                                  sequences, longest, scale, P, row, dim, P, ws, 0]
+
+
+def test_chunk_attention_launches(L):
+    """One kernel where no sequence is long, and the join behind it where items may be cut; workgroups of 4 wavefronts where a sequence has few rows"""
+    calls = [chunk_call(4, 2, 4, 64, 2, 600), chunk_call(400, 2, 4, 64, 2, 600), chunk_call(4, 2, 4, 64, 2, 6000), chunk_call(4000, 8, 4, 128, 2, 600000),
+             chunk_call((1 << 31) - 1025, 1, 1, 128, 1, (1 << 31) - 1025), chunk_call(1, 32, 1, 64, 1 << 20, 64), chunk_call(1, 1, 1, 64, 1, 1 << 30)]
+    names = []
+    for call, (rc, seen) in zip(calls, launched(*calls)):
+        assert rc == 0 and len(seen) in (1, 2), (call, rc, seen)
+        names.append([k for k, _, _ in seen])
+        assert all(grid * block < 1 << 32 for _, grid, block in seen), seen
+        lanes = [block for k, _, block in seen]
+        assert lanes[0] == (512 if call[1][9] * call[1][11] >= 192 * call[1][25] else 256)
+    assert [len(n) for n in names] == [1, 1, 2, 2, 2, 2, 2], names       # (the last but one: short, but 2^25 workgroups of 256 lanes are too many)
+    assert all("k_chunk_attention" in n[0] for n in names) and all("k_chunk_join" in n[1] for n in names if len(n) == 2)
+    # what a plan needs is what the entry point asks for
+    for call in calls:
+        a = call[1]
+        need = L.fc_chunk_attention_workspace_bytes(a[9], a[25], a[10], a[11], a[12], a[26])
+        less = list(a)
+        less[32] = need - 1
+        enough = list(a)
+        enough[32] = need
+        results = launched(*([(call[0], less)] if need else []), (call[0], enough))
+        assert [rc for rc, _ in results] == ([-6] if need else []) + [0], (a, need, results)
