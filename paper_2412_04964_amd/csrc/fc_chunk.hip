@@ -69,6 +69,14 @@ __device__ __forceinline__ Job job_of(const ChunkArgs &a, int off, int next, int
     return j;
 }
 
+// units of a block
+template <int ROWS>
+__device__ __forceinline__ int units_of(const Job &j, int block, int group)
+{
+    constexpr int c = ROWS / kTokens;
+    return j.cached + kBegin + (block == j.blocks - 1 ? j.fresh : (int)(((uint32_t)c * ((uint32_t)block + 1) + group - 1) / (uint32_t)group));
+}
+
 template <int ROWS>
 __device__ __forceinline__ int64_t units_before(const Job &j, int block, int group)
 {
@@ -113,14 +121,43 @@ struct Ranges {
     }
 };
 
-__device__ __forceinline__ uint64_t running_sum(uint64_t v, int lane)
+// v of the lane that CTRL names, 0 where it names none or the lane's row of 16 is not one of ROWS
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint64_t moved(uint64_t v)
 {
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-        const uint64_t u = __shfl_up(v, m);
-        if (lane >= m) v += u;
-    }
-    return v;
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (uint32_t)v, CTRL, ROWS, 0xF, ROWS == 0xF);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (uint32_t)(v >> 32), CTRL, ROWS, 0xF, ROWS == 0xF);
+    return (uint64_t)hi << 32 | lo;
+}
+// Sums of the lanes up to this one: within 16 lanes, then from the last lane of the 16 before, then from the last of the first 32
+__device__ __forceinline__ uint64_t running_sum(uint64_t v)
+{
+    v += moved<0x111, 0xF>(v);
+    v += moved<0x112, 0xF>(v);
+    v += moved<0x114, 0xF>(v);
+    v += moved<0x118, 0xF>(v);
+    v += moved<0x142, 0xA>(v);
+    return v + moved<0x143, 0xC>(v);
+}
+
+// largest of a lane and the one 16 or 32 away in the pairs of rows that change places
+template <int FAR>
+__device__ __forceinline__ float max_across(float v)
+{
+    const uint32_t x = __builtin_bit_cast(uint32_t, v);
+    const auto r = FAR == 32 ? __builtin_amdgcn_permlane32_swap(x, x, false, false) : __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    const uint32_t a = r[0], b = r[1];                   // (a bit cast of an element itself takes the first one's bits)
+    return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+}
+template <int CTRL>
+__device__ __forceinline__ float max_with(float v)
+{
+    return fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true)));
+}
+// largest of all lanes: of 16 by pairs, then mirrored in 8 and in 16
+__device__ __forceinline__ float max_of_all(float v)
+{
+    return max_across<32>(max_across<16>(max_with<0x140>(max_with<0x141>(max_with<0x4E>(max_with<0xB1>(v))))));
 }
 
 __device__ __forceinline__ uint64_t lane_u64(uint64_t v, int lane)
@@ -130,11 +167,9 @@ __device__ __forceinline__ uint64_t lane_u64(uint64_t v, int lane)
 }
 __device__ __forceinline__ float lane_f(float v, int lane) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane)); }
 
-// Where a call gives a workgroup each item: the item of workgroup `id`, in the units of its sequence
+// Where a call gives a workgroup each item: the item of workgroup `id`; units: 0 if it has none
 struct Item {
-    bool there;
-    int b;
-    uint64_t begin, end;
+    int b, head, block, units;
 };
 template <int ROWS>
 __device__ __forceinline__ Item item_of(const ChunkArgs &a, uint32_t id, int page_shift)
@@ -149,23 +184,20 @@ __device__ __forceinline__ Item item_of(const ChunkArgs &a, uint32_t id, int pag
     }
     const Job job = job_of<ROWS>(a, a.step.offsets[lo], a.step.offsets[lo + 1], a.step.held[lo], page_shift);
     const int64_t block = slot - (job.off * a.group / ROWS + lo);
-    if (block < 0 || block >= job.blocks) return {false, 0, 0, 0};
-    const uint64_t begin = (uint64_t)head * job.total;
-    return {true, lo, begin + units_before<ROWS>(job, (int)block, a.group), begin + units_before<ROWS>(job, (int)block + 1, a.group)};
+    if (block < 0 || block >= job.blocks) return {0, 0, 0, 0};
+    return {lo, head, (int)block, units_of<ROWS>(job, (int)block, a.group)};
 }
 
 // 4 codes of a word -> two words of 16-bit values, which hold either kind exactly
 template <bool FP8, bool BF16>
 __device__ __forceinline__ uintx2 sixteen(uint32_t w)
 {
+    asm volatile("" : "+v"(w));                          // (where it stands: the compiler would take all of a lane's together, and wait for them, far ahead)
     if constexpr (!BF16) return halves<FP8>(w);
     else if constexpr (FP8)
         return uintx2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false)),
                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true))};
-    else {
-        asm volatile("" : "+v"(w));                      // (one word after the other: the compiler would take all of a lane's together)
-        return uintx2{narrow2<true>((float)(int8_t)w, (float)(int8_t)(w >> 8)), narrow2<true>((float)(int8_t)(w >> 16), (float)(int8_t)(w >> 24))};
-    }
+    else return uintx2{narrow2<true>((float)(int8_t)w, (float)(int8_t)(w >> 8)), narrow2<true>((float)(int8_t)(w >> 16), (float)(int8_t)(w >> 24))};
 }
 
 // N matrix instructions whose operands come from LDS: the first AHEAD of them are in `operand`, read(i) is the i-th, and later(j) does what follows
@@ -202,17 +234,18 @@ __global__ void __launch_bounds__(64 * W, W == 8 ? 2 : 1) k_chunk_attention(Chun
 
     // ---- this workgroup's range of all work, or its item ----
     // (What is needed between items only is kept in LDS: the loop over tiles has no registers for it.)
-    __shared__ uint64_t kept[4];                         // where this range ends, where the sequence's units begin; each and longer of Ranges
-    uint64_t at, first_end, first_begins = 0, each = 0;
+    __shared__ uint64_t kept[3];                         // where this range ends; each and longer of Ranges
+    uint64_t at = 0, last_end = 0, each = 0;
     uint32_t range = 0, longer = 0;
     bool cut = false;                                    // an item begins here and goes on behind this range
-    int b = -1;
+    int b = -1, head = 0, block = 0, first_unit = 0;     // the next item, and its first unit here
     if (a.by_item) {
         const Item item = item_of<kRows>(a, blockIdx.x, page_shift);
-        if (!item.there) return;
+        if (item.units == 0) return;
         b = item.b;
-        at = item.begin;
-        first_end = item.end;
+        head = item.head;
+        block = item.block;
+        last_end = item.units;
     } else {
         uint64_t sum = 0;
         bool astray = false;
@@ -225,8 +258,9 @@ __global__ void __launch_bounds__(64 * W, W == 8 ? 2 : 1) k_chunk_attention(Chun
                 sum += (uint64_t)job_of<kRows>(a, off, next, held, page_shift).total * a.heads;
                 astray |= off < 0 || next < off || next > a.step.tokens;
             }
+        const uint64_t all = running_sum(sum);
         // (units of offsets that do not ascend may be more than 64 bits count: none of them is done)
-        const uint64_t total_units = __any(astray) ? 0 : lane_u64(running_sum(sum, lane), 63);
+        const uint64_t total_units = __any(astray) ? 0 : lane_u64(all, 63);
         const Ranges ranges = Ranges::of_all(total_units, gridDim.x);
         if (blockIdx.x >= ranges.count) {
             if (threadIdx.x == 0) a.cuts[blockIdx.x].pieces = 0;
@@ -235,24 +269,32 @@ __global__ void __launch_bounds__(64 * W, W == 8 ? 2 : 1) k_chunk_attention(Chun
         // workgroups go to the 8 XCDs in turn: an XCD gets neighbouring ranges, whose K and V its L2 then holds
         range = ranges.count % 8 == 0 ? (blockIdx.x & 7) * (ranges.count / 8) + (blockIdx.x >> 3) : blockIdx.x;
         at = ranges.begin(range);
-        first_end = ranges.begin(range + 1);
+        last_end = ranges.begin(range + 1);
         each = ranges.each;
         longer = ranges.longer;
         uint64_t run = 0;
         for (int c = 0; c < sequences; c += 64) {
-            uint64_t work = 0;
-            if (c + lane < sequences) {
-                off = a.step.offsets[c + lane];
-                next = a.step.offsets[c + lane + 1];
-                held = a.step.held[c + lane];
-                work = (uint64_t)job_of<kRows>(a, off, next, held, page_shift).total * a.heads;
+            uint64_t work = sum, upto = all;
+            if (sequences > 64) {
+                work = 0;
+                if (c + lane < sequences) {
+                    off = a.step.offsets[c + lane];
+                    next = a.step.offsets[c + lane + 1];
+                    held = a.step.held[c + lane];
+                    work = (uint64_t)job_of<kRows>(a, off, next, held, page_shift).total * a.heads;
+                }
+                upto = run + running_sum(work);
             }
-            const uint64_t upto = run + running_sum(work, lane);
             const uint64_t past = __ballot(upto > at);
             if (past) {
                 const int l = __builtin_ctzll(past);
                 b = c + l;
-                first_begins = lane_u64(upto - work, l);
+                const Job job = job_of<kRows>(a, __builtin_amdgcn_readlane(off, l), __builtin_amdgcn_readlane(next, l), __builtin_amdgcn_readlane(held, l), page_shift);
+                const uint64_t within = at - lane_u64(upto - work, l);
+                head = (int)quotient(within, job.total);
+                const int64_t of_head = (int64_t)within - head * job.total;
+                block = block_of<kRows>(job, of_head, group);
+                first_unit = (int)(of_head - units_before<kRows>(job, block, group));
                 break;
             }
             run = lane_u64(upto, 63);
@@ -260,10 +302,9 @@ __global__ void __launch_bounds__(64 * W, W == 8 ? 2 : 1) k_chunk_attention(Chun
     }
 
     if (threadIdx.x == 0) {
-        kept[0] = first_end;
-        kept[1] = first_begins;
-        kept[2] = each;
-        kept[3] = longer;
+        kept[0] = last_end;
+        kept[1] = each;
+        kept[2] = longer;
     }
     __syncthreads();
 
@@ -282,34 +323,33 @@ __global__ void __launch_bounds__(64 * W, W == 8 ? 2 : 1) k_chunk_attention(Chun
     const auto code_thread = [&] { return afresh(kLoads == 1 ? threadIdx.x % (32 * W) : threadIdx.x); };
 
     while (true) {
-        const uint64_t end = lane_u64(kept[0], 0), begins = lane_u64(kept[1], 0);
+        const uint64_t end = lane_u64(kept[0], 0);
         if (at >= end) break;
         const Job job = job_of<kRows>(a, a.step.offsets[b], a.step.offsets[b + 1], a.step.held[b], page_shift);
-        const uint64_t work = (uint64_t)job.total * a.heads;
-        if (at >= begins + work) {
-            __syncthreads();                             // all have read it
-            if (threadIdx.x == 0) kept[1] = begins + work;
-            __syncthreads();
-            ++b;
+        if (block >= job.blocks) {                       // the next head, or sequence
+            block = 0;
+            if (job.blocks == 0 || ++head == a.heads) {
+                head = 0;
+                ++b;
+            }
             continue;
         }
         // ---- the item: a head, a block of rows, and its tiles [tile0, tile1) ----
-        const int head = (int)quotient(at - begins, job.total);
-        const int64_t within = (int64_t)(at - begins) - head * job.total;
-        const int block = block_of<kRows>(job, within, group);
-        const int64_t before = units_before<kRows>(job, block, group);
-        const int units = (int)(units_before<kRows>(job, block + 1, group) - before), unit0 = (int)(within - before);
+        const int block_row = block * kRows, units = units_of<kRows>(job, block, group), unit0 = first_unit;
+        const uint64_t item = at - unit0;                // its first unit
         const int unit1 = end - at < (uint64_t)(units - unit0) ? unit0 + (int)(end - at) : units;
         at += unit1 - unit0;
+        ++block;
+        first_unit = 0;
         const int tile0 = unit0 < kBegin ? 0 : unit0 - kBegin, tile1 = unit1 - kBegin;
         if (tile1 <= tile0) continue;                    // none of its tiles
         const bool whole = tile0 == 0 && tile1 == units - kBegin;
-        const int rows = job.n * group, row0 = block * kRows + wave * 32;
+        const int rows = job.n * group, row0 = block_row + wave * 32;
         if (tile0 == 0 && !whole) {
             cut = true;
             if (threadIdx.x == 0) {
-                const uint32_t last = Ranges(kept[2], (uint32_t)kept[3]).of(begins + (uint64_t)head * job.total + before + units - 1);
-                a.cuts[range] = {(int)(last - range) + 1, (int)job.off, head, block * kRows, rows, {0, 0, 0}};
+                const uint32_t last = Ranges(kept[1], (uint32_t)kept[2]).of(item + units - 1);
+                a.cuts[range] = {(int)(last - range) + 1, (int)job.off, head, block_row, rows, {0, 0, 0}};
             }
         }
         const int n = job.n, held = job.held, cached = job.cached, skip = job.skip, codes_end = cached < tile1 ? cached : tile1;
@@ -457,10 +497,7 @@ __global__ void __launch_bounds__(64 * W, W == 8 ? 2 : 1) k_chunk_attention(Chun
         // exponents for the values' scales, and what sums of weights are multiplied by for that
         float steep = 0.0f, raise = 0.0f, back = 0.0f;
         const auto turn_to = [&](float key_scale, float value_scale) {
-            float widest = value_scale;
-#pragma unroll
-            for (int m = 1; m < 64; m <<= 1) widest = fmaxf(widest, __shfl_xor(widest, m));
-            widest = fmaxf(fminf(widest, 0x1p126f), FLT_MIN);
+            const float widest = fmaxf(fminf(max_of_all(value_scale), 0x1p126f), FLT_MIN);
             // the unit of the sums: the power of two at or below the largest scale, or kDeep of the largest unit so far
             const float now = fmaxf(__builtin_amdgcn_ldexpf(1.0f, __builtin_amdgcn_frexp_expf(widest) - 1), fmaxf(largest_unit * kDeep, FLT_MIN));
             if (now != unit) {
@@ -488,11 +525,11 @@ __global__ void __launch_bounds__(64 * W, W == 8 ? 2 : 1) k_chunk_attention(Chun
             if constexpr (BF16) {
                 away = most > top + kSlack<BF16>;
             } else {
-                most = fmaxf(most, __shfl_xor(most, 32)) - kBias;
+                most = max_across<32>(most) - kBias;
                 away = fabsf(most - top) > kSlack<BF16>;
             }
             if (__any(away)) {
-                if constexpr (BF16) most = fmaxf(most, __shfl_xor(most, 32));
+                if constexpr (BF16) most = max_across<32>(most);
                 // only rows that are away themselves: no row's bits depend on others
                 float now = most > top + kSlack<BF16> ? most : top;
                 if constexpr (!BF16) {
@@ -630,7 +667,7 @@ __global__ void __launch_bounds__(64 * W, W == 8 ? 2 : 1) k_chunk_attention(Chun
             pass_on();
         }
         if (t < tile1 && t != tile0) turn_to(1.0f, 1.0f);
-        const int first_query = (int)((uint32_t)(block * kRows) / (uint32_t)group);      // of the workgroup
+        const int first_query = (int)((uint32_t)block_row / (uint32_t)group);      // of the workgroup
         const int wave_first = (int)((uint32_t)(row0 < rows ? row0 : rows - 1) / (uint32_t)group), wave_last = (int)((uint32_t)(row0 + 31 < rows ? row0 + 31 : rows - 1) / (uint32_t)group);
         for (; t < tile1; ++t) {
             const int t0 = (t - cached) * kTokens;
@@ -700,59 +737,58 @@ __global__ void __launch_bounds__(64 * W, W == 8 ? 2 : 1) k_chunk_attention(Chun
     if (!a.by_item && !cut && threadIdx.x == 0) a.cuts[range].pieces = 0;
 }
 
-// Joins what the ranges have of the items that were cut: a wavefront has 32 elements of 32 rows of the item that begins in range `first` and goes on
+// Joins what the ranges have of the items that were cut: a wavefront has 8 elements of 32 rows of the item that begins in range `first` and goes on
 // behind it.  A range has two places: 1 for an item that it begins and does not end, 0 for one that began before.
 template <int DIM, bool BF16, int W>
 __global__ void __launch_bounds__(256) k_chunk_join(ChunkArgs a)
 {
-    constexpr int kOut = DIM / 32;
+    constexpr int kEighths = DIM / 8;
     const int lane = threadIdx.x & 63, col = lane & 31, side = lane >> 5;
-    const uint32_t id = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), first = id / (W * kOut);
-    const int wave = id % W, o = id / W % kOut;
+    const uint32_t id = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), first = id / (W * kEighths);
+    const int wave = id / kEighths % W, eighth = id % kEighths;
     const ChunkCut cut = a.cuts[first];
     if (cut.pieces == 0) return;
-    const uint32_t last = first + cut.pieces - 1;
     const int rows = cut.rows, row0 = cut.row + wave * 32, row = row0 + col, head = cut.head;
     if (row0 >= rows) return;
     const int64_t places = (int64_t)a.workgroups * 2 * W;
-    const floatx4 *const x = (const floatx4 *)a.partial;
-    const floatx2 *const m = (const floatx2 *)(a.partial + places * (32 * DIM));
-    // the first range has it in its second place, the others in their first ones
-    const auto place = [&](uint32_t r) { return ((int64_t)r * 2 + (r == first)) * W + wave; };
-    float best = -FLT_MAX;
-#pragma unroll 4
-    for (uint32_t r = first; r <= last; ++r) best = fmaxf(best, m[place(r) * 32 + col][0]);
-    floatx4 sum[4];
-    float total = 0.0f;
+    const floatx4 *const x = (const floatx4 *)a.partial + eighth * 64 + lane;
+    const floatx2 *const m = (const floatx2 *)(a.partial + places * (32 * DIM)) + col;
+    float best = -FLT_MAX, total = 0.0f;
+    floatx4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+    // N pieces on their way at a time; those behind the last one are it again, and count for nothing
+    const auto add = [&](auto pieces, int r0) {
+        constexpr int N = decltype(pieces)::value;
+        floatx4 y[N];
+        floatx2 one[N];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sum[i] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-    for (uint32_t r0 = first; r0 <= last; r0 += 4) {
-        // four pieces on their way at a time; those behind the last one are it again, and count for nothing
-        floatx4 y[4][4];
-        floatx2 one[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const uint32_t r = r0 + k < last ? r0 + k : last;
-            one[k] = m[place(r) * 32 + col];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) y[k][i] = x[place(r) * (32 * DIM / 4) + (o * 4 + i) * 64 + lane];
+        for (int k = 0; k < N; ++k) {
+            const int r = r0 + k < cut.pieces ? r0 + k : cut.pieces - 1;
+            const int64_t place = ((int64_t)(first + r) * 2 + (r == 0)) * W + wave;      // (the first range has it in its second place)
+            one[k] = m[place * 32];
+            y[k] = x[place * (32 * DIM / 4)];
         }
+        float now = best;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const float w = r0 + k <= last ? __builtin_amdgcn_exp2f(one[k][0] - best) * one[k][1] : 0.0f;
+        for (int k = 0; k < N; ++k) now = fmaxf(now, one[k][0]);
+        const float shrink = __builtin_amdgcn_exp2f(best - now);
+        best = now;
+        total *= shrink;
+        sum *= shrink;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const float w = r0 + k < cut.pieces ? __builtin_amdgcn_exp2f(one[k][0] - best) * one[k][1] : 0.0f;
             total += w;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (w != 0.0f) sum[i] += y[k][i] * w;
+            if (w != 0.0f) sum += y[k] * w;
         }
-    }
+    };
+    if (cut.pieces <= 2) add(std::integral_constant<int, 2>(), 0);
+    else
+        for (int r = 0; r < cut.pieces; r += 8) add(std::integral_constant<int, 8>(), r);
     if (row >= rows) return;
     const float inv = total == 0.0f ? 0.0f : 1.0f / total;
     const int q = (int)((uint32_t)row / (uint32_t)a.group);
-    uint16_t *y = (uint16_t *)a.out.ptr + (int64_t)(cut.off + q) * a.out.token + (int64_t)(head * a.group + (row - q * a.group)) * a.out.head + o * 32 + 4 * side;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        *(uintx2 *)(y + 8 * i) = uintx2{narrow2<BF16>(sum[i][0] * inv, sum[i][1] * inv), narrow2<BF16>(sum[i][2] * inv, sum[i][3] * inv)};
+    *(uintx2 *)((uint16_t *)a.out.ptr + (int64_t)(cut.off + q) * a.out.token + (int64_t)(head * a.group + (row - q * a.group)) * a.out.head + 8 * eighth + 4 * side) =
+        uintx2{narrow2<BF16>(sum[0] * inv, sum[1] * inv), narrow2<BF16>(sum[2] * inv, sum[3] * inv)};
 }
 
 int64_t slots_of(int64_t tokens, int group, int sequences, int waves) { return tokens * group / rows_of(waves) + sequences; }
@@ -764,7 +800,7 @@ hipError_t chunk(const ChunkArgs &a, hipStream_t stream)
     const int64_t grid = a.by_item ? slots_of(a.step.tokens, a.group, a.step.sequences, W) * a.heads : a.workgroups;
     const hipError_t e = launch_many(k_chunk_attention<DIM, FP8, BF16, W>, grid, 64 * W, stream, a, shift);
     if (e != hipSuccess || a.by_item || a.workgroups == 1) return e;
-    return launch_many(k_chunk_join<DIM, BF16, W>, ((int64_t)a.workgroups - 1) * W * (DIM / 32) / 4, 256, stream, a);
+    return launch_many(k_chunk_join<DIM, BF16, W>, ((int64_t)a.workgroups - 1) * W * (DIM / 8) / 4, 256, stream, a);
 }
 
 template <int DIM, bool FP8, bool BF16>
