@@ -13,6 +13,7 @@
 //   largest score up and down when that is kSlack away, and the largest is put at 2^kBias (kReach below the row's largest at most).
 // All work of the call, in units of a tile of 64 tokens for 128 rows, is cut into equal ranges, one a workgroup: contexts of any lengths
 // end together.  Rows that were cut are joined by a second kernel, from results that are normalised.
+#include <cmath>
 #include <type_traits>
 
 #include "fc_attn_tiles.hpp"
@@ -21,9 +22,12 @@ namespace fc {
 namespace {
 
 constexpr int kTokens = 64;
+constexpr int kRanges = 256;            // one for each compute unit
 constexpr int kLeast = 2;               // units of a range
-constexpr int kShort = 12;              // tiles of an item up to which it is not cut
-constexpr int kBegin = 3;               // units that what surrounds an item's tiles counts for
+constexpr int kShort = 12;              // tiles of an item that need not be cut: sequences may be far shorter than announced
+constexpr int kBegin = 3;               // units that what surrounds an item's tiles counts for (the batch below with 2, 3, 4, 6: 281, 270, 274, 276 us)
+constexpr double kUnits = 4.5;          // of a range, from which on workgroups have eight wavefronts
+constexpr double kJoined = 4.0;         // units that the join counts for
 constexpr int rows_of(int waves) { return 32 * waves; }                  // of a workgroup
 template <bool BF16> constexpr float kSlack = BF16 ? 8.0f : 10.0f;
 constexpr float kBias = 4.0f, kReach = 36.0f;
@@ -818,15 +822,22 @@ hipError_t chunk_of(const ChunkArgs &a, hipStream_t stream)
 
 }  // namespace
 
+// Times in what follows: keys and values of 8 heads of 128 in E4M3, bfloat16, 4 query heads each.
 void chunk_plan(int64_t tokens, int sequences, int heads, int group, int64_t longest, ChunkArgs *a)
 {
-    a->waves = (double)tokens * group >= 192.0 * sequences ? 8 : 4;
-    // Short contexts: a workgroup for each item, and nothing to join
-    const double tiles = (double)longest / kTokens + 2, slots = (double)slots_of(tokens, group, sequences, a->waves);
-    a->by_item = tiles <= kShort && slots * heads * 512 < 4294967296.0;
+    const double all_rows = (double)tokens * group, tiles = (double)longest / kTokens + 2;
+    const auto items = [&](int waves) { return std::fmax(sequences, all_rows / rows_of(waves) + 0.5 * sequences) * heads; };
+    const auto units = [&](int waves) { return items(waves) * (tiles + kBegin) / kRanges; };             // of a range
+    // Eight wavefronts convert a tile's codes for twice the rows; four leave more ranges to share the rows.  One sequence over 4000 tokens, 8 / 4 wavefronts:
+    // 160 rows 33.3 / 28.7 us, 256 34.2 / 31.4, 384 35.5 / 36.0, 512 38.6 / 38.8; eight over 1000 to 2000 tokens: 64 rows each 27.6 / 29.0, 256 42.2 / 47.4
+    a->waves = units(8) >= kUnits ? 8 : 4;
+    // Short contexts: a workgroup for each item, and nothing to join, unless ranges would end that much sooner.  By items / by ranges: 2 items of 3 tiles
+    // 12.5 / 16.3 us, of 6 20.1 / 16.7, of 11 28.7 / 17.5; about 190 items of 6 tiles 31.0 / 38.1, of 11 42.0 / 41.6
+    const double slots = (double)slots_of(tokens, group, sequences, a->waves);
+    a->by_item = tiles <= kShort && tiles * std::ceil(items(a->waves) / kRanges) <= units(a->waves) + kJoined && slots * heads * 512 < 4294967296.0;
     // else one for each of 256 compute units, or fewer where the announced lengths cannot make so many ranges
     const double most = slots * heads * (tiles + kBegin) / kLeast + 1;
-    a->workgroups = a->by_item ? 0 : most < 256 ? (int)most : 256;
+    a->workgroups = a->by_item ? 0 : most < kRanges ? (int)most : kRanges;
 }
 
 size_t chunk_workspace(const ChunkArgs &a, int dim)

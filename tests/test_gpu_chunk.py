@@ -134,6 +134,8 @@ STEPS = [
     (1, 200, 64, 16, [100], [9], None),                               # more query heads than a workgroup has rows
     (2, 2, 64, 16, [40] * 150, [1 + b % 3 for b in range(150)], None),         # more sequences than lanes
     (1, 8, 128, 16, [30000], [7], None),                              # few rows over a long context
+    (8, 8, 64, 16, [100, 0, 333, 64, 1, 500], [200, 150, 33, 257, 1, 259], None),        # many items
+    (8, 8, 128, 32, [0, 70, 333, 64, 1, 500], [200, 150, 33, 257, 1, 259], None),
 ]
 
 
@@ -145,7 +147,7 @@ def test_chunk_attention_matches_its_definition(fc, dtype, quantizer, case):
     print("chunk", dtype, quantizer, STEPS[case][:6], flush=True)
     s = Step(*shape, dtype, quantizer, case)
     want = s.exact()
-    for announced in (s.longest, 1 << 20, 1) if longest is None else (longest,):        # items cut or not
+    for announced in (s.longest, 3000, 1 << 20, 1) if longest is None else (longest,):        # items cut or not, workgroups of four or eight wavefronts
         got = s.call(fc, longest=announced)
         check(got, *want)
         assert same(got, s.call(fc, longest=announced))

@@ -74,43 +74,47 @@ def test_samples_on_shared_pages_answer_as_samples_with_pages_of_their_own(fc, d
         return z[:, :heads * group], z[:, heads * group:heads * (group + 1)], z[:, heads * (group + 1):], z[:, :heads * (group + 1)]
 
     def serve(shared):
-        """outputs of all pieces of the prompts, and of each step for all samples"""
-        copies = 1 if shared else samples
-        xs = [x for x in prompts for _ in range(copies)]
+        """outputs of the prompts, and of each step for all samples"""
         pool = rows * width
         shape = (pool, heads, page, dim)
         cache = (torch.full(shape, 0xFF, dtype=torch.uint8, device="cuda"), torch.full(shape, 0xFF, dtype=torch.uint8, device="cuda"),
                  torch.full(shape[:2], float("nan"), device="cuda"), torch.full(shape[:2], float("nan"), device="cuda"))
-        pages, uses = torch.full((len(xs), width), -1, dtype=torch.int32, device="cuda"), torch.zeros(pool, dtype=torch.int32, device="cuda")
-        outputs, begin = [[] for _ in xs], 0
+        uses = torch.zeros(pool, dtype=torch.int32, device="cuda")
 
-        def room(offsets, held):
+        def room(pages, offsets, held):
             source, target, lacking = fc.pages_reserve(pages, held, uses, offsets, page)
             assert int(lacking) == 0
             fc.cache_copy(cache, source, target)
 
-        while begin < max(lengths):
-            parts = [x[begin:begin + piece] for x in xs]
-            offsets = ints([0] + [len(p) for p in parts]).cumsum(0).int()
-            held = ints([min(begin, len(x)) for x in xs])
-            positions = torch.cat([torch.arange(len(p), dtype=torch.int32, device="cuda") + begin for p in parts])
-            room(offsets, held)
-            q, k, v, turned = qkv(parts)
-            fc.rotary(turned, table, positions, out=turned)
-            o = fc.chunk_attention(q, k, v, cache, pages, offsets, held, max(lengths), quantizer)
-            fc.cache_append(k, v, cache, pages, offsets, held, piece, quantizer)
-            at = 0
-            for i, p in enumerate(parts):
-                outputs[i].append(o[at:at + len(p)])
-                at += len(p)
-            begin += piece
-        outputs = [torch.cat(o) for o in outputs]
+        def take_prompts():
+            """(how a step's work is cut depends on all of its sequences: every copy is taken in the same company)"""
+            pages = torch.full((len(prompts), width), -1, dtype=torch.int32, device="cuda")
+            outputs, begin = [[] for _ in prompts], 0
+            while begin < max(lengths):
+                parts = [x[begin:begin + piece] for x in prompts]
+                offsets = ints([0] + [len(p) for p in parts]).cumsum(0).int()
+                held = ints([min(begin, n) for n in lengths])
+                positions = torch.cat([torch.arange(len(p), dtype=torch.int32, device="cuda") + begin for p in parts])
+                room(pages, offsets, held)
+                q, k, v, turned = qkv(parts)
+                fc.rotary(turned, table, positions, out=turned)
+                o = fc.chunk_attention(q, k, v, cache, pages, offsets, held, max(lengths), quantizer)
+                fc.cache_append(k, v, cache, pages, offsets, held, piece, quantizer)
+                for out, part in zip(outputs, o.split([len(p) for p in parts])):
+                    out.append(part)
+                begin += piece
+            return pages, [torch.cat(o) for o in outputs]
+
         if shared:
+            pages, outputs = take_prompts()
             outputs = [o for o in outputs for _ in range(samples)]
-            parents = ints([b for b in range(len(xs)) for _ in range(samples)])
+            parents = ints([b for b in range(len(prompts)) for _ in range(samples)])
             pages, held = fc.pages_fork(pages, ints(lengths), uses, parents, page)
         else:
-            held = ints([len(x) for x in xs])
+            taken = [take_prompts() for _ in range(samples)]
+            pages = torch.stack([pages for pages, _ in taken], 1).view(rows, width)
+            outputs = [outputs[b] for b in range(len(prompts)) for _, outputs in taken]
+            held = ints([n for n in lengths for _ in range(samples)])
         offsets, out = ints(list(range(rows + 1))), []
         for i in range(steps):
             if shared and i in (5, 20):
@@ -119,7 +123,7 @@ def test_samples_on_shared_pages_answer_as_samples_with_pages_of_their_own(fc, d
                 # as many pages as the tokens need: full pages of the prompts are there once, what follows them once a sample
                 need = sum(n // page + samples * (-(-(n + i) // page) - n // page) for n in lengths)
                 assert int(used) == need and int((uses > 0).sum()) == need and bool((uses[:need] > 0).all())
-            room(offsets, held)
+            room(pages, offsets, held)
             q, k, v, _ = qkv([tokens[i]])
             fc.rotary(q, table, held, out=q)
             fc.cache_append(k, v, cache, pages, offsets, held, 1, quantizer, table)
