@@ -3,16 +3,26 @@
 //
 // Query i of a sequence that held L tokens before the step sees the L cached ones, k = sk ck and v = sv cv with the scales of their page
 // and head, and the new tokens j <= i:  o = sum_t softmax_t(scale q . k_t) v_t.
-// The rows of a key/value head are the queries times the query heads that share it.  A workgroup has 128 of them, 32 a wavefront, and takes 64
-// tokens at a time, first the cached ones, then the new.  As over prompts a wavefront forms S^T = K Q^T with 32 x 32 x 16 matrix instructions,
+// The rows of a key/value head are the queries times the query heads that share it.  A workgroup has 256 of them (or 128), 32 a wavefront, and takes
+// 64 tokens at a time, first the cached ones, then the new.  As over prompts a wavefront forms S^T = K Q^T with 32 x 32 x 16 matrix instructions,
 // which leaves a lane with weights of the very tokens that it needs as operand of O^T = V^T P^T: scores and weights stay in registers.
 //   Both kinds of codes are exact in binary16 and in bfloat16: a tile's codes are converted once, on their way to LDS, for the workgroup's rows.
 //   sk multiplies scores.  sv would multiply weights; it goes into their exponents instead, w = 2^(s - top + log2(sv / unit)), and what sums
 //   of weights then have too much is divided out once for 16 tokens.  The unit of the sums is a power of two, common to the workgroup.
 //   The unit of a row's weights is its running maximum.  Binary16 has not the range for all that are lower: there it follows a tile's
 //   largest score up and down when that is kSlack away, and the largest is put at 2^kBias (kReach below the row's largest at most).
-// All work of the call, in units of a tile of 64 tokens for 128 rows, is cut into equal ranges, one a workgroup: contexts of any lengths
+// All work of the call, in units of a tile of 64 tokens for a workgroup's rows, is cut into equal ranges, one a workgroup: contexts of any lengths
 // end together.  Rows that were cut are joined by a second kernel, from results that are normalised.
+//   What bounds it.  2048 tokens over 65531, 16 query heads over 2 of 128 in E4M3, bfloat16: 1.10 ms, 1.02 PFLOP/s, where a product of 16384^3
+//   reaches 1.36: the power that the card has, for the time stays where it is when waits are added to the loop (1.76 GHz, the matrix
+//   units busy 41% of it; with 10% more cycles 1.94 GHz and as long).  A tile takes 4900 cycles, of which 2048 are the matrix units',
+//   and 2570 of vector instructions are beside them.  512 tokens over 8191: 59 us, of which 11 are the join's (it reads 34 MB that others wrote),
+//   8 the way to the first product and 34 the tiles.  Nine sequences of 4099 tokens over up to 4000 in signed codes, binary16, 8 heads of 4:
+//   239 us, 14 of them the join's and about 6 for the beginning and the end of each of three items.  17 tokens over 129: 17 us, one workgroup a
+//   head, where the code itself is on its way from memory.
+//   Taken one after the other: operands ahead of their products (1.59 -> 1.42 ms for the first of these), eight wavefronts over three tiles (1.14, the
+//   batch 452 -> 420 us), what surrounds an item counted as work (420 -> 270), items without a division, lanes without LDS (270 -> 240).  Two halves of
+//   a workgroup half a tile apart, one at products and one at weights, took as long on the first and 10% longer on the others.
 #include <cmath>
 #include <type_traits>
 
@@ -228,7 +238,7 @@ __global__ void __launch_bounds__(64 * W, W == 8 ? 2 : 1) k_chunk_attention(Chun
 {
     constexpr int kSteps = DIM / 16, kOut = DIM / 32, kRow = 2 * DIM, kTile = kTokens * kRow, kRows = rows_of(W);
     constexpr int kOutRow = kRow + 16;
-    constexpr int kAhead = FP8 || BF16 ? 6 : 5;         // operands on their way; one more would not fit the registers
+    constexpr int kAhead = FP8 || BF16 ? 6 : 5;         // operands on their way (4: 1152 us where 6 takes 1138); with signed codes and binary16 6 are no faster
     // A lane loads 16 codes at a time: kLoads of a tile, the first half of them K and the others V (with one load, half of the wavefronts have K)
     constexpr int kLoads = DIM / (8 * W), kEach = kLoads > 1 ? kLoads / 2 : 1, kPieces = DIM / 16, kRound = kTokens / kEach;
     __shared__ __attribute__((aligned(1024))) uint8_t tiles[4][2][kTile];       // K and V
