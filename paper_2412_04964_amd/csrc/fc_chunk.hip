@@ -18,8 +18,8 @@
 //   units busy 41% of it; with 10% more cycles 1.94 GHz and as long).  A tile takes 4900 cycles, of which 2048 are the matrix units',
 //   and 2570 of vector instructions are beside them.  512 tokens over 8191: 59 us, of which 11 are the join's (it reads 34 MB that others wrote),
 //   8 the way to the first product and 34 the tiles.  Nine sequences of 4099 tokens over up to 4000 in signed codes, binary16, 8 heads of 4:
-//   239 us, 14 of them the join's and about 6 for the beginning and the end of each of three items.  17 tokens over 129: 17 us, one workgroup a
-//   head, where the code itself is on its way from memory.
+//   239 us, 14 of them the join's and about 6 for the beginning and the end of each of three items.  17 tokens over 129: 17 us, in
+//   eight workgroups and the join as in one workgroup a head; much of it waits for the code itself, which every launch fetches anew.
 //   Taken one after the other: operands ahead of their products (1.59 -> 1.42 ms for the first of these), eight wavefronts over three tiles (1.14, the
 //   batch 452 -> 420 us), what surrounds an item counted as work (420 -> 270), items without a division, lanes without LDS (270 -> 240).  Two halves of
 //   a workgroup half a tile apart, one at products and one at weights, took as long on the first and 10% longer on the others.
