@@ -437,7 +437,8 @@ FC_API int fc_pages_fork(const int32_t *page_table, const int32_t *held, int seq
  * a partly filled page that is named elsewhere too gives way to a fresh one, into which fc_cache_copy copies it: source[b] -> target[b]
  * (int32 [sequences], -1 and -1 where there is nothing to copy).  If all rows that name such a page write to it, the last one keeps it.
  * Fresh pages are the lowest-numbered free ones, handed out by row, then slot; uses follows.  Slots beyond table_width are left out.
- * lacking: int32 [1], how many free pages are missing; if that is not 0, table and uses are as they were and nothing is to be copied.
+ * lacking: int32 [1], how many free pages are missing; if that is not 0, table and uses are as they were and nothing is to be copied.  So it is,
+ * with lacking 0, where offsets do not ascend from 0 or more.
  * workspace: fc_pages_reserve_workspace_bytes(pages) bytes, 16-byte aligned, contents unspecified.
  */
 FC_API size_t fc_pages_reserve_workspace_bytes(int64_t pages);

@@ -135,8 +135,16 @@ __global__ void __launch_bounds__(1024) k_pages_reserve(ReserveArgs a, int page_
         }
         return s.partial && !none(id) ? id : -1;
     };
-    for (int b = threadIdx.x; b < a.sequences; b += 1024) a.source[b] = look(b);
-    __syncthreads();
+    bool astray = false;                                 // offsets that do not ascend may ask for more pages than 32 bits count: none of them gets any
+    for (int b = threadIdx.x; b < a.sequences; b += 1024) {
+        astray |= a.offsets[b] < 0 || a.offsets[b + 1] < a.offsets[b];
+        a.source[b] = look(b);
+    }
+    if (__syncthreads_or(astray)) {
+        for (int b = threadIdx.x; b < a.sequences; b += 1024) a.source[b] = a.target[b] = -1;
+        if (threadIdx.x == 0) *a.lacking = 0;
+        return;
+    }
     // who copies, and how many fresh pages each sequence takes
     int needed = 0;
     for (int c = 0; c < a.sequences; c += 1024) {

@@ -204,6 +204,26 @@ def test_reserve_all_or_nothing(fc):
     assert [x.tolist() for x in out] == [[-1] * 3, [-1] * 3, [0]] and t.tolist() == table and got.tolist() == uses
 
 
+@pytest.mark.parametrize("offsets", [[0, 40, 20, 60], [-1, 5, 6, 7], [0, 1 << 30, 5, 1 << 30], [7, 6, 5, 4], [0, 3, 4, -(1 << 31)]])
+def test_offsets_that_do_not_ascend_reserve_nothing(fc, offsets):
+    """A row whose own tokens would need pages among them: what all rows need together may be more than 32 bits count"""
+    table, held, uses = [[0, 1, -1, -1], [0, 1, -1, -1], [2, -1, -1, -1]], [20, 20, 3], [2, 2, 1, 0, 0, 0, 0, 0]
+    t, u = ints(table), ints(uses)
+    source, target, lacking = fc.pages_reserve(t, ints(held), u, ints(offsets), 16)
+    assert t.tolist() == table and u.tolist() == uses and lacking.tolist() == [0]
+    assert source.tolist() == [-1, -1, -1] == target.tolist()
+
+
+def test_reserve_more_rows_than_lanes_with_offsets_astray(fc):
+    rows = 2500
+    table = torch.full((rows, 2), -1, dtype=torch.int32, device="cuda")
+    offsets = torch.arange(rows + 1, dtype=torch.int32, device="cuda")
+    offsets[2400] = 7                                    # (below the one before it)
+    uses = torch.zeros(4096, dtype=torch.int32, device="cuda")
+    source, target, lacking = fc.pages_reserve(table, torch.zeros(rows, dtype=torch.int32, device="cuda"), uses, offsets, 16)
+    assert bool((table == -1).all()) and bool((uses == 0).all()) and bool((source == -1).all()) and bool((target == -1).all()) and int(lacking) == 0
+
+
 def test_the_last_of_all_writers_keeps_a_page(fc):
     # three users: all write, two of them write, one writes
     for new, copied in (([1, 1, 1], [0, 1]), ([1, 0, 1], [0, 2]), ([0, 1, 0], [1])):
