@@ -155,9 +155,10 @@ def test_chunk_attention_matches_its_definition(fc, dtype, quantizer, case):
         check(s.call(fc, scale=0.5), *s.exact(0.5))
 
 
+@pytest.mark.parametrize("announced", [None, 1 << 20])                 # workgroups of four wavefronts, and of eight
 @pytest.mark.parametrize("dtype", [F16, BF16])
 @pytest.mark.parametrize("quantizer", [SYM, FP8])
-def test_pages_of_very_different_scales(fc, dtype, quantizer):
+def test_pages_of_very_different_scales(fc, announced, dtype, quantizer):
     # key scales change what is seen, value scales what it counts for; a page of zeros under the least scale counts in the sum of weights
     s = Step(2, 4, 128, 16, [600, 1200], [40, 70], dtype, quantizer, 3)
     g = gen(9)
@@ -169,19 +170,20 @@ def test_pages_of_very_different_scales(fc, dtype, quantizer):
         s.cache[0][id] = 0
         s.cache[1][id] = 0
         ks[id] = vs[id] = torch.finfo(torch.float32).tiny
-    check(s.call(fc), *s.exact())
+    check(s.call(fc, longest=announced or s.longest), *s.exact())
     # values far below and far above: float32 has the range for their sums (float16 results have not)
     if dtype == BF16:
         for factor in (2.0 ** -60, 2.0 ** 60):
             t = Step(1, 2, 64, 16, [500], [30], dtype, quantizer, 4)
             t.cache[3].mul_(factor)
             t.v.mul_(factor)
-            check(t.call(fc), *t.exact())
+            check(t.call(fc, longest=announced or t.longest), *t.exact())
 
 
+@pytest.mark.parametrize("announced", [None, 1 << 20])                 # workgroups of four wavefronts, and of eight
 @pytest.mark.parametrize("dtype", [F16, BF16])
 @pytest.mark.parametrize("heads,group,dim,held,new", [(1, 4, 128, [700], [100]), (2, 1, 64, [0, 5000], [200, 3])])
-def test_one_token_far_above_the_rest(fc, dtype, heads, group, dim, held, new):
+def test_one_token_far_above_the_rest(fc, announced, dtype, heads, group, dim, held, new):
     # a peak in the cache or among the new tokens; the weights beside it, 2^-20 of it and less, have to be right where the peak's value is zero
     for place in ("cached", "new"):
         s = Step(heads, group, dim, 16, held, new, dtype, SYM, 5)
@@ -197,14 +199,15 @@ def test_one_token_far_above_the_rest(fc, dtype, heads, group, dim, held, new):
             s.k[off + 1] = 40 / dim ** 0.5
             s.v[off + 1] = 0
         want, weight, tiles = s.exact()
-        check(s.call(fc), want, weight, tiles)
+        check(s.call(fc, longest=announced or s.longest), want, weight, tiles)
 
 
+@pytest.mark.parametrize("announced", [None, 1 << 20])                 # workgroups of four wavefronts, and of eight
 @pytest.mark.parametrize("dtype", [F16, BF16])
 @pytest.mark.parametrize("heads,group,dim,held,new", [(2, 4, 128, [100, 0], [70, 200]), (1, 1, 64, [0], [300]), (1, 8, 128, [-3, 1000], [60, 17])])
-def test_no_bit_of_a_row_depends_on_later_tokens(fc, dtype, heads, group, dim, held, new):
+def test_no_bit_of_a_row_depends_on_later_tokens(fc, announced, dtype, heads, group, dim, held, new):
     s = Step(heads, group, dim, 16, held, new, dtype, FP8, 6)
-    plain = s.call(fc)
+    plain = s.call(fc, longest=announced or s.longest)
     check(plain, *s.exact())
     off = 0
     for b, n in enumerate(new):
@@ -212,7 +215,7 @@ def test_no_bit_of_a_row_depends_on_later_tokens(fc, dtype, heads, group, dim, h
         for at, value in ((n - 1, float("nan")), (n // 2, float("inf")), (n // 2, -60000.0), (first, float("nan"))):
             k, v = s.k.clone(), s.v.clone()
             s.k[off + at:off + n], s.v[off + at:off + n] = value, value
-            got = s.call(fc)
+            got = s.call(fc, longest=announced or s.longest)
             rows = list(range(off, off + at)) + list(range(0, off)) + list(range(off + n, sum(new)))
             assert same(got[rows], plain[rows]), (b, at, value)
             if value == float("inf"):                    # a weight above zero of an infinity, and scores of either sign
@@ -222,31 +225,33 @@ def test_no_bit_of_a_row_depends_on_later_tokens(fc, dtype, heads, group, dim, h
         # tokens without a place
         k, v = s.k.clone(), s.v.clone()
         s.k[off:off + first], s.v[off:off + first] = float("nan"), float("-inf")
-        assert same(s.call(fc), plain) and not plain[off:off + first].any()
+        assert same(s.call(fc, longest=announced or s.longest), plain) and not plain[off:off + first].any()
         s.k.copy_(k)
         s.v.copy_(v)
         off += n
     # values alone: the weights are finite, so an infinity is the result of all that see it, and only theirs
     v = s.v.clone()
     s.v[new[0] // 2, 0, 3] = float("inf")
-    got = s.call(fc)
+    got = s.call(fc, longest=announced or s.longest)
     want = plain.clone()
     want[new[0] // 2:new[0], :group, 3] = float("inf")
     assert same(got, want)
     s.v.copy_(v)
 
 
-def test_nan_in_the_cache_is_seen_by_its_own_rows_only(fc):
+@pytest.mark.parametrize("announced", [None, 1 << 20])                 # workgroups of four wavefronts, and of eight
+def test_nan_in_the_cache_is_seen_by_its_own_rows_only(fc, announced):
     s = Step(2, 4, 128, 16, [100, 200], [30, 40], F16, FP8, 7)
-    plain = s.call(fc)
+    plain = s.call(fc, longest=announced or s.longest)
     s.cache[1][int(s.table[1, 3]), 1, 4, 9] = 0x7F
-    got = s.call(fc)
+    got = s.call(fc, longest=announced or s.longest)
     assert torch.isnan(got[30:, 4:, 9]).all()
     got[30:, 4:, 9] = plain[30:, 4:, 9]
     assert same(got, plain)
 
 
-def test_weights_of_a_flat_tail(fc):
+@pytest.mark.parametrize("announced", [None, 1 << 20])                 # workgroups of four wavefronts, and of eight
+def test_weights_of_a_flat_tail(fc, announced):
     # a cached peak of weight ~1 whose value is zero, and thousands of equal tokens 2^-14 below it, whose values add up to what counts
     s = Step(1, 1, 128, 64, [40000], [3], F16, SYM, 8)
     s.cache[0].zero_()
@@ -257,7 +262,7 @@ def test_weights_of_a_flat_tail(fc):
     s.k.zero_()
     s.v.zero_()
     s.k[:] = 14 * 0.6931471805599453 / 128 ** 0.5
-    check(s.call(fc), *s.exact())
+    check(s.call(fc, longest=announced or s.longest), *s.exact())
 
 
 def test_strides_results_and_guards(fc):
