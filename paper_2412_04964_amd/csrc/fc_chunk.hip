@@ -334,7 +334,7 @@ __global__ void __launch_bounds__(64 * W, W == 8 ? 2 : 1) k_chunk_attention(Chun
     const int at_v = v_row * kRow + ((((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) ^ swizzle<DIM, false>(v_row)) * 16 + (lane & 1) * 8;
     const float factor = a.scale * 1.4426950408889634f;      // scores in powers of two
     const int half = kLoads == 1 ? wave / (W / 2) : 0, code_wave = kLoads == 1 ? wave % (W / 2) : wave;        // half: 1 for wavefronts that have V only
-    const auto code_thread = [&] { return afresh(kLoads == 1 ? threadIdx.x % (32 * W) : threadIdx.x); };
+    const auto code_thread = [&] { return (uint32_t)afresh(kLoads == 1 ? threadIdx.x % (32 * W) : threadIdx.x); };
 
     while (true) {
         const uint64_t end = lane_u64(kept[0], 0);
@@ -409,12 +409,9 @@ __global__ void __launch_bounds__(64 * W, W == 8 ? 2 : 1) k_chunk_attention(Chun
         // the codes of tile t, from memory
         const auto fetch = [&](int t) {
             const int in = t & 15;
-            if (t != tile0 && in == 0) {
-                place = place_of(page_next);
-                page_next = pages_of((t >> 4) + 1);
-            }
-            if (in == 8) scales_of((t >> 4) + 1, page_next, ks_next, vs_next);
-            const int thread = code_thread(), mine = thread / kPieces % 16 * DIM + thread % kPieces * 16;
+            const bool turns = t != tile0 && in == 0;
+            if (turns) place = place_of(page_next);
+            const uint32_t thread = code_thread(), mine = thread / kPieces % 16 * DIM + thread % kPieces * 16;
             Codes c;
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
@@ -426,12 +423,15 @@ __global__ void __launch_bounds__(64 * W, W == 8 ? 2 : 1) k_chunk_attention(Chun
                     c.w[kEach + i] = *(const uintx4 *)(a.cache.v + at_page + mine);
                 }
             }
+            // (behind the codes: nothing waits for these until the next codes are there)
+            if (turns) page_next = pages_of((t >> 4) + 1);
+            if (in == 8) scales_of((t >> 4) + 1, page_next, ks_next, vs_next);
             return c;
         };
         // and into LDS, 8 codes at a time: half a load
         const auto clear_rest = [&](Codes &c, int t) {
             if ((t + 1) * kTokens > held) {                  // whatever the page holds beyond them
-                const int code_row = code_thread() / kPieces;
+                const int code_row = (int)(code_thread() / kPieces);
 #pragma unroll
                 for (int i = 0; i < kLoads; ++i)
                     if (t * kTokens + i % kEach * kRound + code_row >= held) c.w[i] = uintx4{0, 0, 0, 0};
@@ -441,7 +441,7 @@ __global__ void __launch_bounds__(64 * W, W == 8 ? 2 : 1) k_chunk_attention(Chun
             int k, v;
         };
         const Places places = [&] {
-            const int thread = code_thread(), r = thread / kPieces, u = 2 * (thread % kPieces);
+            const int thread = (int)code_thread(), r = (uint32_t)thread / kPieces, u = 2 * ((uint32_t)thread % kPieces);
             const int k = r * kRow + (u ^ swizzle<DIM, true>(r & 31)) * 16, v = r * kRow + (u ^ swizzle<DIM, false>(r & 15)) * 16 + kTile;
             return kLoads == 1 ? Places{half ? v : k, 0} : Places{k, v};
         }();
@@ -677,6 +677,8 @@ __global__ void __launch_bounds__(64 * W, W == 8 ? 2 : 1) k_chunk_attention(Chun
             } else {
                 convert_all(codes, to);
             }
+            // (all that was loaded ahead is here by now; said here, where it costs nothing, and not between the next loads)
+            asm volatile("" : "+v"(page_next), "+v"(ks_next), "+v"(vs_next));
             if (t + 3 < codes_end) codes = fetch(t + 3);
             pass_on();
         }
