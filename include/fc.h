@@ -401,8 +401,10 @@ FC_API int fc_prompt_attention(const void *q, int64_t q_token_stride, int64_t q_
  * q, out: [tokens, heads * group, dim]; k, v: [tokens, heads, dim], keys turned; dim in {64, 128}; token strides of k and v below 2^25.  The
  * new tokens need not be in the cache, which is only read: fc_cache_append may come before or after.  Otherwise as fc_cache_attention.
  * Products are of `type`, sums in fp32.  Weights, times the scales of their pages where the values are codes, are rounded to `type`: bfloat16
- * 8 bits; binary16 11 bits for what is less than 2^8 below the largest of 64 tokens, absolutely 2^-15 of that one at least.  Pages whose value scale
- * is 2^-36 of the largest among 1024 neighbouring tokens and less are taken as if it were that.  Sums must fit fp32 as there.
+ * 8 bits; binary16 11 bits for what is less than 2^8 below the largest of 64 tokens, absolutely 2^-15 of that one at least.  Sums must fit fp32 as there.
+ * bfloat16: value scales may lie as far apart as fp32 has them (values below 2^-126 may count as 0).  binary16: the value scales of a sequence, and 1 for
+ * its new tokens, lie within 2^56 of each other, pages of zeros alone aside (those that fc_cache_append makes of binary16 values, and 1, within 2^43); a
+ * lower one may be taken for a higher.
  * What the pages hold beyond the held tokens has no influence, and no bit of a row depends on later tokens, infinities and NaN included.
  * longest: the most tokens, held and new, of a sequence; it only sizes the launch.  tokens * group is below 2^31 - 1024.
  * workspace: fc_chunk_attention_workspace_bytes(...) bytes, 16-byte aligned, contents unspecified; may be NULL if that is 0.

@@ -7,8 +7,10 @@
 // 64 tokens at a time, first the cached ones, then the new.  As over prompts a wavefront forms S^T = K Q^T with 32 x 32 x 16 matrix instructions,
 // which leaves a lane with weights of the very tokens that it needs as operand of O^T = V^T P^T: scores and weights stay in registers.
 //   Both kinds of codes are exact in binary16 and in bfloat16: a tile's codes are converted once, on their way to LDS, for the workgroup's rows.
-//   sk multiplies scores.  sv would multiply weights; it goes into their exponents instead, w = 2^(s - top + log2(sv / unit)), and what sums
-//   of weights then have too much is divided out once for 16 tokens.  The unit of the sums is a power of two, common to the workgroup.
+//   sk multiplies scores.  sv would multiply weights; it goes into their exponents instead, w = 2^(s - top + log2 c), and what sums
+//   of weights then have too much is divided out once for 16 tokens.  In bfloat16 c is the part of sv in [1, 2): its power of two multiplies
+//   the codes on their way to LDS, which hold it exactly (8 bits, and the exponents of fp32), so that scales of any size stand beside each
+//   other.  Binary16 has not the exponents: c is sv / unit, where the unit of the sums is a power of two, common to the workgroup.
 //   The unit of a row's weights is its running maximum.  Binary16 has not the range for all that are lower: there it follows a tile's
 //   largest score up and down when that is kSlack away, and the largest is put at 2^kBias (kReach below the row's largest at most).
 // All work of the call, in units of a tile of 64 tokens for a workgroup's rows, is cut into equal ranges, one a workgroup: contexts of any lengths
@@ -41,8 +43,11 @@ constexpr double kJoined = 4.0;         // units that the join counts for
 constexpr int rows_of(int waves) { return 32 * waves; }                  // of a workgroup
 template <bool BF16> constexpr float kSlack = BF16 ? 8.0f : 10.0f;
 constexpr float kBias = 4.0f, kReach = 36.0f;
-// how far below the largest unit so far the unit may go, and what a scale may be of it
-constexpr float kDeep = 0x1p-30f, kFaint = 0x1p-36f;
+// Binary16: how far below the largest unit so far the unit may go, and what a scale may be of it.  What fc_cache_append makes of binary16 values is
+// between 2^-33 and 2^10 (2^-24 / 448 and 65504 / 127), or the least scale over zeros, so that neither limit is met there.  Both keep the
+// sums in range: sums of values grow by 1 / kDeep where the unit falls, from 2^(kBias + kSlack + 9) a token at most; the weight of a token whose
+// scale is kFaint of the unit counts up to 2^(kReach + kSlack) / kFaint = 2^102, of which fp32 has room for 2^25.
+constexpr float kDeep = 0x1p-42f, kFaint = 0x1p-56f;
 
 // What there is to do for one sequence, for each key/value head: `blocks` of a workgroup's rows, each over `cached` tiles and those new ones that it
 // sees, and kBegin units for what surrounds them
@@ -202,16 +207,18 @@ __device__ __forceinline__ Item item_of(const ChunkArgs &a, uint32_t id, int pag
     return {lo, head, (int)block, units_of<ROWS>(job, (int)block, a.group)};
 }
 
-// 4 codes of a word -> two words of 16-bit values, which hold either kind exactly
+// 4 codes of a word -> two words of 16-bit values, which hold either kind exactly; bfloat16: times a power of two
 template <bool FP8, bool BF16>
-__device__ __forceinline__ uintx2 sixteen(uint32_t w)
+__device__ __forceinline__ uintx2 sixteen(uint32_t w, float power)
 {
     asm volatile("" : "+v"(w));                          // (where it stands: the compiler would take all of a lane's together, and wait for them, far ahead)
     if constexpr (!BF16) return halves<FP8>(w);
     else if constexpr (FP8)
-        return uintx2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false)),
-                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true))};
-    else return uintx2{narrow2<true>((float)(int8_t)w, (float)(int8_t)(w >> 8)), narrow2<true>((float)(int8_t)(w >> 16), (float)(int8_t)(w >> 24))};
+        return uintx2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, power, false)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, power, true))};
+    else
+        return uintx2{narrow2<true>((float)(int8_t)w * power, (float)(int8_t)(w >> 8) * power),
+                      narrow2<true>((float)(int8_t)(w >> 16) * power, (float)(int8_t)(w >> 24) * power)};
 }
 
 // N matrix instructions whose operands come from LDS: the first AHEAD of them are in `operand`, read(i) is the i-th, and later(j) does what follows
@@ -405,14 +412,22 @@ __global__ void __launch_bounds__(64 * W, W == 8 ? 2 : 1) k_chunk_attention(Chun
         float ks_next = 0.0f, vs_next = 0.0f;
         struct Codes {
             uintx4 w[kLoads];
+            float power[kEach];                          // bfloat16: what multiplies V's
+        };
+        // of a scale, the power of two at or below it
+        const auto power_of = [](float scale) { return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, scale) & 0x7F800000u); };
+        // (of tile t, whose pieces' are in the lanes of `powers`; one piece for each of a wavefront's rows of codes)
+        const auto raise_codes = [&](Codes &c, int t, float powers) {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i)
+                c.power[i] = BF16 && (kLoads > 1 || half) ? lane_f(powers, (t & 15) * 4 + (i * kRound + code_wave * (64 / kPieces)) / 16) : 1.0f;
         };
         // the codes of tile t, from memory
-        const auto fetch = [&](int t) {
+        const auto fetch = [&](Codes &c, int t) {
             const int in = t & 15;
             const bool turns = t != tile0 && in == 0;
             if (turns) place = place_of(page_next);
             const uint32_t thread = code_thread(), mine = thread / kPieces % 16 * DIM + thread % kPieces * 16;
-            Codes c;
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
                 const uint64_t at_page = lane_u64(place, in * 4 + (i * kRound + code_wave * (64 / kPieces)) / 16);       // the wavefront's piece
@@ -426,7 +441,6 @@ __global__ void __launch_bounds__(64 * W, W == 8 ? 2 : 1) k_chunk_attention(Chun
             // (behind the codes: nothing waits for these until the next codes are there)
             if (turns) page_next = pages_of((t >> 4) + 1);
             if (in == 8) scales_of((t >> 4) + 1, page_next, ks_next, vs_next);
-            return c;
         };
         // and into LDS, 8 codes at a time: half a load
         const auto clear_rest = [&](Codes &c, int t) {
@@ -447,7 +461,8 @@ __global__ void __launch_bounds__(64 * W, W == 8 ? 2 : 1) k_chunk_attention(Chun
         }();
         const auto convert = [&](const Codes &c, int piece, uint8_t *to, const Places &at_lds) {
             const int i = piece >> 1, h = piece & 1;
-            const uintx2 x = sixteen<FP8, BF16>(c.w[i][2 * h]), y = sixteen<FP8, BF16>(c.w[i][2 * h + 1]);
+            const float power = kLoads == 1 ? c.power[0] : i >= kEach ? c.power[i % kEach] : 1.0f;
+            const uintx2 x = sixteen<FP8, BF16>(c.w[i][2 * h], power), y = sixteen<FP8, BF16>(c.w[i][2 * h + 1], power);
             *(uintx4 *)(to + ((i >= kEach ? at_lds.v : at_lds.k) ^ (h << 4)) + i % kEach * kRound * kRow) = uintx4{x[0], x[1], y[0], y[1]};
         };
         const auto convert_all = [&](const Codes &c, uint8_t *to) {
@@ -509,19 +524,25 @@ __global__ void __launch_bounds__(64 * W, W == 8 ? 2 : 1) k_chunk_attention(Chun
         };
         // The pieces of 16 tokens that the lanes have the scales of: what scores are multiplied by (powers of two), what is added to the
         // exponents for the values' scales, and what sums of weights are multiplied by for that
-        float steep = 0.0f, raise = 0.0f, back = 0.0f;
+        float steep = 0.0f, raise = 0.0f, back = 0.0f, powers = 0.0f;
         const auto turn_to = [&](float key_scale, float value_scale) {
-            const float widest = fmaxf(fminf(max_of_all(value_scale), 0x1p126f), FLT_MIN);
-            // the unit of the sums: the power of two at or below the largest scale, or kDeep of the largest unit so far
-            const float now = fmaxf(__builtin_amdgcn_ldexpf(1.0f, __builtin_amdgcn_frexp_expf(widest) - 1), fmaxf(largest_unit * kDeep, FLT_MIN));
-            if (now != unit) {
-                const float change = unit / now;
+            float c;
+            if constexpr (BF16) {
+                powers = power_of(value_scale);
+                c = __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, value_scale) & 0x7FFFFFu) | 0x3F800000u);
+            } else {
+                const float widest = fmaxf(fminf(max_of_all(value_scale), 0x1p126f), FLT_MIN);
+                // the unit of the sums: the power of two at or below the largest scale, or kDeep of the largest unit so far
+                const float now = fmaxf(__builtin_amdgcn_ldexpf(1.0f, __builtin_amdgcn_frexp_expf(widest) - 1), fmaxf(largest_unit * kDeep, FLT_MIN));
+                if (now != unit) {
+                    const float change = unit / now;
 #pragma unroll
-                for (int o = 0; o < kOut; ++o) acc[o] *= change;
-                unit = now;
+                    for (int o = 0; o < kOut; ++o) acc[o] *= change;
+                    unit = now;
+                }
+                largest_unit = fmaxf(largest_unit, now);
+                c = fmaxf(value_scale / unit, kFaint);
             }
-            largest_unit = fmaxf(largest_unit, now);
-            const float c = fmaxf(value_scale / unit, kFaint);
             steep = fmaxf(factor * key_scale, FLT_MIN);
             raise = __builtin_amdgcn_logf(c);            // log2
             back = 1.0f / c;
@@ -632,22 +653,30 @@ __global__ void __launch_bounds__(64 * W, W == 8 ? 2 : 1) k_chunk_attention(Chun
             next = after;
             after = free;
         };
+        // the powers of tile t's batch, where `batch` is the one that was turned to: it, or the next one
+        const auto powers_at = [&](int t, int batch) { return t >> 4 == batch ? powers : power_of(vs_next); };
         if (tile0 < cached) {
             const int batch = tile0 >> 4, page = pages_of(batch);
             place = place_of(page);
             page_next = pages_of(batch + 1);
             float ks, vs;
-            Codes first = fetch(tile0);
+            Codes first;
+            fetch(first, tile0);
             scales_of(batch, page, ks, vs);
             scales_of(batch + 1, page_next, ks_next, vs_next);     // (before the next fetch may go on to that batch)
-            if (tile0 + 1 < codes_end) codes = fetch(tile0 + 1);
+            if (tile0 + 1 < codes_end) fetch(codes, tile0 + 1);
             turn_to(ks, vs);
             clear_rest(first, tile0);
+            raise_codes(first, tile0, powers);
             convert_all(first, now);
             if (tile0 + 1 < codes_end) {
                 clear_rest(codes, tile0 + 1);
+                raise_codes(codes, tile0 + 1, powers_at(tile0 + 1, batch));
                 convert_all(codes, next);
-                if (tile0 + 2 < codes_end) codes = fetch(tile0 + 2);
+                if (tile0 + 2 < codes_end) {
+                    raise_codes(codes, tile0 + 2, powers_at(tile0 + 2, batch));
+                    fetch(codes, tile0 + 2);
+                }
             }
         } else {
             turn_to(1.0f, 1.0f);
@@ -679,7 +708,10 @@ __global__ void __launch_bounds__(64 * W, W == 8 ? 2 : 1) k_chunk_attention(Chun
             }
             // (all that was loaded ahead is here by now; said here, where it costs nothing, and not between the next loads)
             asm volatile("" : "+v"(page_next), "+v"(ks_next), "+v"(vs_next));
-            if (t + 3 < codes_end) codes = fetch(t + 3);
+            if (t + 3 < codes_end) {
+                raise_codes(codes, t + 3, powers_at(t + 3, t >> 4));
+                fetch(codes, t + 3);
+            }
             pass_on();
         }
         if (t < tile1 && t != tile0) turn_to(1.0f, 1.0f);
