@@ -471,7 +471,8 @@ FC_API int fc_cache_copy(void *k_cache, void *v_cache, float *k_scales, float *v
  *
  * x, residual, sum, y: 16-bit rows [tokens, hidden], dense but for the row stride (elements, a multiple of 8), 16-byte aligned; hidden a multiple
  * of 8 up to 32768.  residual may be NULL (nothing is added), sum too (x + residual is not kept).  weight [hidden]: of weight_type, which is
- * type or FC_TYPE_F32.  eps positive and finite.  sum and y may be x or residual where their strides are equal; otherwise nothing overlaps.
+ * type or FC_TYPE_F32.  eps positive and finite.  sum and y may be x or residual where their strides are equal; otherwise no result overlaps what is
+ * read, or another (the Python calls refuse what does; rows may lie between other rows).
  * Results are bit-identical, except where two correctly rounded 64-bit sums of the squares differ, to
  *     h   = x + residual                          fp32;  sum = h rounded to the type
  *     d   = fp32(1 / sqrt(sum of h * h / hidden + eps))          squares, sum, divides and root in 64 bits

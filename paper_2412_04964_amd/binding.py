@@ -238,6 +238,38 @@ def _shape(t, want, what: str):
     return t
 
 
+def _meet(a, b) -> bool:
+    """Whether two tensors, of up to three axes of which the last is dense, have a byte in common: exactly, so that views of one buffer whose
+    rows lie between each other's pass.  (At once for tensors whose spans are apart; one division where their row strides are equal.)"""
+    if not a.numel() or not b.numel():
+        return False
+    sides = []
+    for t in (a, b):
+        n = t.element_size()
+        axes = [((t.stride(i) if t.shape[i] > 1 else 0) * n, t.shape[i]) for i in range(t.dim() - 1)]
+        rows = axes[0] if axes else (0, 1)
+        parts = axes[1] if len(axes) > 1 else (0, 1)
+        sides.append((t.data_ptr(), rows, parts, t.shape[-1] * n, t.data_ptr() + sum(s * (k - 1) for s, k in axes) + t.shape[-1] * n))
+    (at, (s, n), (ps, pn), w, end), (at2, (s2, n2), (ps2, pn2), w2, end2) = sides
+    if end <= at2 or end2 <= at:
+        return False
+    # parts are heads: every one of a's with every one of b's
+    for d in {at2 + j * ps2 - at - i * ps for i in range(pn) for j in range(pn2)}:
+        if s == s2 or n == 1 or n2 == 1:
+            # rows i of a and j of b are d + j s2 - i s apart, which has to be in (-w2, w)
+            stride, low, high = (s2, 0, n2 - 1) if n == 1 else (s, 1 - n, 0) if n2 == 1 else (s, 1 - n, n2 - 1)
+            k = min(max(-((d + w2 - 1) // stride), low), high) if stride else 0        # the first that is not before them
+            if -w2 < d + k * stride < w:
+                return True
+        else:
+            torch = _torch()
+            i = d - s * torch.arange(n)
+            k = (-((i + w2 - 1) // s2)).clamp(0, n2 - 1) if s2 else torch.zeros_like(i)
+            if bool(((i + k * s2 > -w2) & (i + k * s2 < w)).any()):
+                return True
+    return False
+
+
 def _sources(t, what: str):
     """[N, tokens, bytes-or-groups] stacked on the source axis, each source's slab dense"""
     if t.dim() != 3:

@@ -759,6 +759,22 @@ PyObject *chunk_attention(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     END_HANDLE_TH_ERRORS
 }
 
+// Whether rows lie apart for all that their strides tell: `extent` bytes of every row, rows `stride` bytes apart.  (Where this does not see it, the
+// Python path decides exactly.)
+struct Extent {
+    const void *ptr;
+    int64_t stride, extent, rows;
+    int64_t span() const { return stride * (rows - 1) + extent; }
+};
+bool rows_apart(const Extent &a, const Extent &b)
+{
+    const int64_t from = reinterpret_cast<intptr_t>(b.ptr) - reinterpret_cast<intptr_t>(a.ptr);
+    if (from >= a.span() || -from >= b.span()) return true;
+    if (a.stride != b.stride || a.stride <= 0 || a.rows != b.rows) return false;
+    const int64_t within = (from % a.stride + a.stride) % a.stride;
+    return within >= a.extent && a.stride - within >= b.extent;
+}
+
 // ---- norm.py's calls ----
 
 // A [tokens, hidden] activation as the C ABI takes it
@@ -798,6 +814,13 @@ bool row_result(PyObject *out, const Row &like, int device, at::Tensor &own, Row
     return row(out, like.t, device, r) && (r.t->size(0) == 1 || r.stride >= r.t->size(1));
 }
 
+// a result and what is read: apart, or the same rows
+bool apart_or_same(const Row &y, const Row &x)
+{
+    const int64_t rows = x.t->size(0), width = x.t->size(1) * 2;
+    return (y.ptr == x.ptr && y.stride == x.stride) || rows_apart({y.ptr, y.stride * 2, width, rows}, {x.ptr, x.stride * 2, width, rows});
+}
+
 struct Norm {
     Row x, r;
     const at::Tensor *weight = nullptr;
@@ -822,6 +845,19 @@ struct Norm {
         hidden = (int)x.t->size(1);
         return pr == Py_None ? sum_out == Py_None : row(pr, x.t, device, r);
     }
+    Extent weights() const { return {weight->data_ptr(), 0, (int64_t)weight->nbytes(), 1}; }
+    // of the caller's result (norm.py refuses what does not hold)
+    bool apart_from(const Row &y) const
+    {
+        return apart_or_same(y, x) && (!r.t || apart_or_same(y, r)) && rows_apart({y.ptr, y.stride * 2, (int64_t)hidden * 2, tokens}, weights());
+    }
+    // dense results, that are no rows of x's
+    bool apart_from(const at::Tensor &t) const
+    {
+        const Extent e{t.data_ptr(), 0, (int64_t)t.nbytes(), 1};
+        const auto rows = [&](const Row &y) { return rows_apart(e, {y.ptr, 0, 2 * (y.stride * (tokens - 1) + hidden), 1}); };
+        return rows(x) && (!r.t || rows(r)) && rows_apart(e, weights());
+    }
 };
 
 // (x, weight, eps, residual, out, sum_out)
@@ -834,7 +870,9 @@ PyObject *rms_norm(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     Row y, sum;
     if (!n.take(a[0], a[1], a[2], a[3], a[5], device)) return fallback();
     at::Tensor own, own_sum;
-    if (!row_result(a[4], n.x, device, own, y) || (n.r.t && !row_result(a[5], n.x, device, own_sum, sum)) || sum.ptr == y.ptr) return fallback();
+    if (!row_result(a[4], n.x, device, own, y) || (n.r.t && !row_result(a[5], n.x, device, own_sum, sum))) return fallback();
+    if ((a[4] != Py_None && !n.apart_from(y)) || (a[5] != Py_None && !n.apart_from(sum))) return fallback();
+    if (a[4] != Py_None && a[5] != Py_None && ((sum.ptr == y.ptr && sum.stride == y.stride) || !apart_or_same(sum, y))) return fallback();
     void *stream = stream_of(device);
     const void *weight = n.weight->data_ptr();
     int rc;
@@ -863,8 +901,14 @@ PyObject *rms_norm_quantize(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     if (a[6] != Py_None && !c.take(a[6], 2, n.tokens, n.hidden, group, 8, at::kFloat, device, false)) return fallback();
     at::Tensor own_sum;
     if (n.r.t && !row_result(a[7], n.x, device, own_sum, sum)) return fallback();
+    if (a[7] != Py_None && !n.apart_from(sum)) return fallback();
+    if (a[6] != Py_None) {
+        const Extent codes{c.ptr(0), 0, (int64_t)c.t[0]->nbytes(), 1}, scales{c.ptr(1), 0, (int64_t)c.t[1]->nbytes(), 1};
+        const Extent sums{sum.ptr, 0, sum.t ? 2 * (sum.stride * (n.tokens - 1) + n.hidden) : 0, 1};
+        if (!n.apart_from(*c.t[0]) || !n.apart_from(*c.t[1]) || !rows_apart(codes, scales)) return fallback();
+        if (a[7] != Py_None && (!rows_apart(codes, sums) || !rows_apart(scales, sums))) return fallback();
+    }
     if (a[6] == Py_None) c.allocate(2, n.tokens, n.hidden, group, 8, at::kFloat, *n.x.t);
-    if (sum.ptr == c.ptr(0)) return fallback();
     void *stream = stream_of(device), *codes = c.ptr(0);
     float *scales = (float *)c.ptr(1);
     const void *weight = n.weight->data_ptr();

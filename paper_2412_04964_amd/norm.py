@@ -9,7 +9,7 @@ from __future__ import annotations
 
 from . import binding
 from .attention import _type
-from .binding import QUANTIZER_SYM, _check, _coded_outputs, _dev, _shape, _stream, _torch
+from .binding import QUANTIZER_SYM, _check, _coded_outputs, _dev, _meet, _shape, _stream, _torch
 
 _F32 = 2                                                 # FC_TYPE_F32
 
@@ -75,20 +75,29 @@ def _inputs(x, weight, residual, sum_out):
     return kind, (residual.data_ptr(), _stride(residual)), _result(sum_out, x, "sum_out")
 
 
-def _apart(total, *results):
-    if total is not None and any(r.numel() and r.data_ptr() == total.data_ptr() for r in results):
-        raise ValueError("the sum and the norm need tensors of their own")
+def _apart(results, x, residual, weight):
+    """results, (what, tensor, whether it may be x or residual), overlap neither each other nor what is read: workgroups take the rows in any order"""
+    for i, (what, t, in_place) in enumerate(results):
+        for other, u in (("x", x), ("residual", residual), ("weight", weight)):
+            if u is None or not _meet(t, u):
+                continue
+            if not (in_place and other != "weight" and t.data_ptr() == u.data_ptr() and _stride(t) == _stride(u)):
+                raise ValueError("%s must not overlap %s%s" % (what, other, ", unless it has the same rows" if in_place and other != "weight" else ""))
+        for other, u, _ in results[:i]:
+            if _meet(t, u):
+                raise ValueError("%s and %s need memory of their own" % (other, what))
 
 
 def rms_norm(x, weight, eps: float = 1e-5, residual=None, out=None, sum_out=None):
     """fc_rms_norm: y, the norm of x's rows times weight (of x's type or float32, [hidden]).  With a residual: (y, sum), the norm of
-    x + residual and that sum, which the next layer's residual is.  out and sum_out may be x or residual."""
+    x + residual and that sum, which the next layer's residual is.  out and sum_out may be x or residual, row for row; what overlaps
+    otherwise is refused."""
     done = (binding._native or binding._calls()).rms_norm(x, weight, eps, residual, out, sum_out)
     if done is not None:
         return done
     kind, other, total = _inputs(x, weight, residual, sum_out)
     y = _result(out, x, "out")
-    _apart(total, y)
+    _apart([(what, t, True) for what, t in (("out", out), ("sum_out", sum_out)) if t is not None], x, residual, weight)
     _check(binding.lib().fc_rms_norm(x.data_ptr(), _stride(x), *other, weight.data_ptr(), kind, x.shape[0], x.shape[1], eps, _type(x, "x"),
                                      *((None, 0) if total is None else (total.data_ptr(), _stride(total))), y.data_ptr(), _stride(y), _stream()),
            "fc_rms_norm")
@@ -108,7 +117,8 @@ def rms_norm_quantize(x, weight, eps: float = 1e-5, group: int = 128, quantizer:
     if group < 1 or hidden % group or (group != hidden and (group < 32 or group > 16384 or group & (group - 1))):
         raise binding.FcError(-3, "fc_rms_norm_quantize")
     codes, scales = _coded_outputs(x.device, tokens, hidden, group, 8, out, [(torch.float32, "scales")])
-    _apart(total, codes)
+    _apart([("codes (out)", codes, False), ("scales (out)", scales, False)] * (out is not None) + [("sum_out", total, True)] * (sum_out is not None), x, residual,
+           weight)
     _check(binding.lib().fc_rms_norm_quantize(x.data_ptr(), _stride(x), *other, weight.data_ptr(), kind, tokens, hidden, eps, _type(x, "x"), group,
                                               quantizer, *((None, 0) if total is None else (total.data_ptr(), _stride(total))), codes.data_ptr(),
                                               scales.data_ptr(), _stream()), "fc_rms_norm_quantize")

@@ -1,0 +1,72 @@
+"""Results that lie over what a call reads, or over each other, are refused; those in place, and views of one buffer whose rows lie between each other's,
+are not."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+F16 = torch.float16
+
+
+@pytest.fixture(scope="module")
+def fc():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests selected but no GPU is visible")
+    import paper_2412_04964_amd as m
+    m.lib()
+    return m
+
+
+@pytest.fixture(params=["native", "python"])
+def path(request, fc):
+    native = fc.binding._calls()
+    fc.binding._native = native if request.param == "native" else fc.binding._NoNativeCalls()
+    yield request.param
+    fc.binding._native = native
+
+
+def test_norms(fc, path):
+    g = torch.Generator().manual_seed(1)
+    buf = torch.randn((3, 12, 1024), generator=g).half().cuda()
+    w = (1 + 0.1 * torch.randn(512, generator=g)).half().cuda()
+    x, r = buf[0, 1:7, :512], buf[1, 1:7, :512]
+    first = fc.rms_norm(x.clone(), w, residual=r.clone())
+    coded = fc.rms_norm_quantize(x.clone(), w, 1e-5, 64, fc.QUANTIZER_SYM, residual=r.clone())
+    before = buf.clone()
+    dense = buf[2].view(-1)
+    over = dense[:3072].view(6, 512)
+    bad = [
+        dict(out=buf[0, 2:8, :512]), dict(out=buf[0, :6, :512]), dict(out=buf[0, 1:7, 8:520]), dict(out=buf[0, 1:7, 256:768]),       # x, some rows or elements on
+        dict(sum_out=buf[0, 2:8, :512]), dict(sum_out=buf[1, 2:8, :512]), dict(out=buf[1, 1:7, 504:1016]),
+        dict(out=buf[2, 0:6, :512], sum_out=buf[2, 3:9, :512]), dict(out=buf[2, 0:6, :512], sum_out=buf[2, 0:6, :512]),
+        dict(out=buf[2, 0:6, :512], sum_out=buf[2, 0:6, 256:768]), dict(out=over, sum_out=buf[2, 0:6, :512]),                       # rows of other strides
+        dict(out=buf[0].view(-1)[1024:1024 + 3072].view(6, 512)),                                                                     # x's start, another stride
+    ]
+    for more in bad:
+        with pytest.raises(ValueError):
+            fc.rms_norm(x, w, residual=r, **more)
+    # the weight
+    base = buf[2].view(-1)
+    with pytest.raises(ValueError):
+        fc.rms_norm(x, base[512:1024], out=buf[2, 0:6, :512].as_strided((6, 512), (512, 1)))
+    # codes and scales
+    bytes_ = buf.view(torch.uint8).view(-1)
+    at = (x.data_ptr() - buf.data_ptr())
+    fresh_codes, fresh_scales = torch.empty((6, 512), dtype=torch.uint8, device="cuda"), torch.empty((6, 8), device="cuda")
+    mixed = torch.empty(4096, dtype=torch.uint8, device="cuda")
+    for out, more in (((bytes_[at:at + 3072].view(6, 512), fresh_scales), {}), ((bytes_[at + 2048:at + 2048 + 3072].view(6, 512), fresh_scales), {}),
+                      ((fresh_codes, bytes_[at:at + 192].view(torch.float32).view(6, 8)), {}), ((mixed[:3072].view(6, 512), mixed[3056:3248].view(torch.float32).view(6, 8)), {}),
+                      ((bytes_[-3072:].view(6, 512), fresh_scales), dict(sum_out=buf[2, 6:12, 512:]))):
+        with pytest.raises(ValueError):
+            fc.rms_norm_quantize(x, w, 1e-5, 64, fc.QUANTIZER_SYM, residual=r, out=out, **more)
+    assert torch.equal(buf, before)
+    # rows between rows, and in place
+    got = fc.rms_norm(x, w, residual=r, out=buf[0, 1:7, 512:], sum_out=buf[1, 1:7, 512:])
+    assert all(torch.equal(a, b) for a, b in zip(got, first))
+    got = fc.rms_norm_quantize(x, w, 1e-5, 64, fc.QUANTIZER_SYM, residual=r, out=(mixed[:3072].view(6, 512), mixed[3072:3264].view(torch.float32).view(6, 8)), sum_out=buf[0, 1:7, 512:])
+    assert all(torch.equal(a, b) for a, b in zip((*got[0:2], got[2]), coded))
+    assert torch.equal(fc.rms_norm(x[:1], w, out=x[:1]), fc.rms_norm(before[0, 1:2, :512], w))
+    x.copy_(before[0, 1:7, :512])
+    got = fc.rms_norm(x, w, residual=r, out=x, sum_out=r)
+    assert got[0] is x and all(torch.equal(a, b) for a, b in zip(got, first))
