@@ -16,7 +16,7 @@ from __future__ import annotations
 import math
 
 from . import binding
-from .binding import QUANTIZER_SYM, FcError, _check, _dev, _shape, _stream, _torch
+from .binding import QUANTIZER_SYM, FcError, _check, _dev, _meet, _shape, _stream, _torch
 
 _TYPES = None
 
@@ -282,7 +282,7 @@ def chunk_attention_workspace_bytes(tokens: int, sequences: int, heads: int, gro
 def chunk_attention(q, k, v, cache, pages, offsets, held, longest: int, quantizer: int = QUANTIZER_SYM, scale=None, out=None, workspace=None):
     """fc_chunk_attention: a prompt that is taken in pieces.  q [tokens, query heads, dim] over the held tokens of every sequence in the cache and
     over the new ones up to itself, whose k, v [tokens, heads, dim] (keys turned) need not be in the cache.  longest: the most tokens,
-    held and new, that a sequence has.  scale: dim^-0.5 unless given."""
+    held and new, that a sequence has.  scale: dim^-0.5 unless given.  out may be q, row for row; what overlaps otherwise is refused."""
     done = (binding._native or binding._calls()).chunk_attention(q, k, v, cache, pages, offsets, held, longest, quantizer, scale, out, workspace)
     if done is not None:
         return done
@@ -298,11 +298,19 @@ def chunk_attention(q, k, v, cache, pages, offsets, held, longest: int, quantize
     group = _group(q, heads, "cache")
     y = _out_rows(out, q, tuple(q.shape))
     need = chunk_attention_workspace_bytes(tokens, sequences, heads, group, dim, longest)
+    dense = zip(("k_cache", "v_cache", "k_scales", "v_scales", "pages", "offsets", "held"), (*cache, pages, offsets, held))
+    read = [("q", q), ("k", k), ("v", v)] + [(name, t.view(-1)) for name, t in dense]
+    for name, t in read if out is not None else ():
+        if _meet(y, t) and not (name == "q" and y.data_ptr() == q.data_ptr() and _strides(y) == _strides(q)):
+            raise ValueError("out must not overlap %s%s" % (name, ", unless it has the same rows" if name == "q" else ""))
     if workspace is None:
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-    _dev(workspace, torch.uint8, "workspace")
-    if workspace.numel() < need:
+    elif _dev(workspace, torch.uint8, "workspace").numel() < need:
         raise FcError(-6, "fc_chunk_attention")
+    else:
+        for name, t in read + [("out", y)]:
+            if _meet(workspace.view(-1), t):
+                raise ValueError("workspace must not overlap %s" % name)
     _check(binding.lib().fc_chunk_attention(
         q.data_ptr(), *_strides(q), k.data_ptr(), *_strides(k), v.data_ptr(), *_strides(v), tokens, heads, group, dim, _type(q, "q"), quantizer,
         cache[0].data_ptr(), cache[1].data_ptr(), cache[2].data_ptr(), cache[3].data_ptr(), count, page, pages.data_ptr(), width,

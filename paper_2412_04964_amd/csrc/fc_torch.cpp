@@ -570,6 +570,32 @@ struct PagedStep {
     }
 };
 
+// Whether rows lie apart for all that their strides tell: `extent` bytes of every row, rows `stride` bytes apart.  (Where this does not see it, the
+// Python path decides exactly.)
+struct Extent {
+    const void *ptr;
+    int64_t stride, extent, rows;
+    int64_t span() const { return stride * (rows - 1) + extent; }
+};
+bool rows_apart(const Extent &a, const Extent &b)
+{
+    if (a.extent == 0 || b.extent == 0) return true;
+    const int64_t from = reinterpret_cast<intptr_t>(b.ptr) - reinterpret_cast<intptr_t>(a.ptr);
+    if (from >= a.span() || -from >= b.span()) return true;
+    if (a.stride != b.stride || a.stride <= 0 || a.rows != b.rows) return false;
+    const int64_t within = (from % a.stride + a.stride) % a.stride;
+    return within >= a.extent && a.stride - within >= b.extent;
+}
+
+Extent extent_of(const Activation &a) { return {a.ptr, a.token * 2, (a.head * (a.heads() - 1) + a.dim()) * 2, a.tokens()}; }
+Extent extent_of(const at::Tensor &t) { return {t.data_ptr(), 0, (int64_t)t.nbytes(), 1}; }      // a dense one
+
+bool apart(const at::Tensor &a, const at::Tensor &b)
+{
+    const char *pa = (const char *)a.data_ptr(), *pb = (const char *)b.data_ptr();
+    return a.numel() == 0 || b.numel() == 0 || pa + a.nbytes() <= pb || pb + b.nbytes() <= pa;
+}
+
 bool table_of(const at::Tensor *t) { return t && t->dim() == 2 && t->size(1) <= 4096; }
 
 // (x, table, positions, interleaved, inverse, out)
@@ -738,6 +764,14 @@ PyObject *chunk_attention(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     }
     at::Tensor own, own_ws;
     if (!result_rows(a[10], q, device, own, y)) return fallback();
+    const auto clear = [&](const Extent &e, bool also_q) {          // (attention.py refuses what is not)
+        bool ok = (!also_q || rows_apart(e, extent_of(q))) && rows_apart(e, extent_of(k)) && rows_apart(e, extent_of(v));
+        for (const at::Tensor *read : {s.k, s.v, s.ks, s.vs, s.pages, s.offsets, s.held}) ok = ok && rows_apart(e, extent_of(*read));
+        return ok;
+    };
+    const bool over_q = y.ptr == q.ptr && y.token == q.token && y.head == q.head;
+    if (a[10] != Py_None && !clear(extent_of(y), !over_q)) return fallback();
+    if (ws && (!clear(extent_of(*ws), true) || !rows_apart(extent_of(*ws), extent_of(y)))) return fallback();
     if (need && !ws) {
         own_ws = empty({(int64_t)need}, at::kByte, *q.t);
         ws = &own_ws;
@@ -757,22 +791,6 @@ PyObject *chunk_attention(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     if (!done(rc, "fc_chunk_attention")) return nullptr;
     return wrapped(a[10], own);
     END_HANDLE_TH_ERRORS
-}
-
-// Whether rows lie apart for all that their strides tell: `extent` bytes of every row, rows `stride` bytes apart.  (Where this does not see it, the
-// Python path decides exactly.)
-struct Extent {
-    const void *ptr;
-    int64_t stride, extent, rows;
-    int64_t span() const { return stride * (rows - 1) + extent; }
-};
-bool rows_apart(const Extent &a, const Extent &b)
-{
-    const int64_t from = reinterpret_cast<intptr_t>(b.ptr) - reinterpret_cast<intptr_t>(a.ptr);
-    if (from >= a.span() || -from >= b.span()) return true;
-    if (a.stride != b.stride || a.stride <= 0 || a.rows != b.rows) return false;
-    const int64_t within = (from % a.stride + a.stride) % a.stride;
-    return within >= a.extent && a.stride - within >= b.extent;
 }
 
 // ---- norm.py's calls ----
@@ -845,18 +863,17 @@ struct Norm {
         hidden = (int)x.t->size(1);
         return pr == Py_None ? sum_out == Py_None : row(pr, x.t, device, r);
     }
-    Extent weights() const { return {weight->data_ptr(), 0, (int64_t)weight->nbytes(), 1}; }
     // of the caller's result (norm.py refuses what does not hold)
     bool apart_from(const Row &y) const
     {
-        return apart_or_same(y, x) && (!r.t || apart_or_same(y, r)) && rows_apart({y.ptr, y.stride * 2, (int64_t)hidden * 2, tokens}, weights());
+        return apart_or_same(y, x) && (!r.t || apart_or_same(y, r)) && rows_apart({y.ptr, y.stride * 2, (int64_t)hidden * 2, tokens}, extent_of(*weight));
     }
     // dense results, that are no rows of x's
     bool apart_from(const at::Tensor &t) const
     {
-        const Extent e{t.data_ptr(), 0, (int64_t)t.nbytes(), 1};
+        const Extent e = extent_of(t);
         const auto rows = [&](const Row &y) { return rows_apart(e, {y.ptr, 0, 2 * (y.stride * (tokens - 1) + hidden), 1}); };
-        return rows(x) && (!r.t || rows(r)) && rows_apart(e, weights());
+        return rows(x) && (!r.t || rows(r)) && rows_apart(e, extent_of(*weight));
     }
 };
 
@@ -903,7 +920,7 @@ PyObject *rms_norm_quantize(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     if (n.r.t && !row_result(a[7], n.x, device, own_sum, sum)) return fallback();
     if (a[7] != Py_None && !n.apart_from(sum)) return fallback();
     if (a[6] != Py_None) {
-        const Extent codes{c.ptr(0), 0, (int64_t)c.t[0]->nbytes(), 1}, scales{c.ptr(1), 0, (int64_t)c.t[1]->nbytes(), 1};
+        const Extent codes = extent_of(*c.t[0]), scales = extent_of(*c.t[1]);
         const Extent sums{sum.ptr, 0, sum.t ? 2 * (sum.stride * (n.tokens - 1) + n.hidden) : 0, 1};
         if (!n.apart_from(*c.t[0]) || !n.apart_from(*c.t[1]) || !rows_apart(codes, scales)) return fallback();
         if (a[7] != Py_None && (!rows_apart(codes, sums) || !rows_apart(scales, sums))) return fallback();
@@ -972,12 +989,6 @@ struct Ints {
         return r;
     }
 };
-
-bool apart(const at::Tensor &a, const at::Tensor &b)
-{
-    const char *pa = (const char *)a.data_ptr(), *pb = (const char *)b.data_ptr();
-    return a.numel() == 0 || b.numel() == 0 || pa + a.nbytes() <= pb || pb + b.nbytes() <= pa;
-}
 
 // (pages, held, uses, parents, page, out)
 PyObject *pages_fork(PyObject *, PyObject *const *a, Py_ssize_t n_args)

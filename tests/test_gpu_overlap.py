@@ -70,3 +70,32 @@ def test_norms(fc, path):
     x.copy_(before[0, 1:7, :512])
     got = fc.rms_norm(x, w, residual=r, out=x, sum_out=r)
     assert got[0] is x and all(torch.equal(a, b) for a, b in zip(got, first))
+
+
+def test_chunk_attention(fc, path):
+    from test_gpu_chunk import BF16, SYM, Step, ints, offsets_of, same
+    for longest in (None, 5000):                         # items whole, and cut into ranges
+        s = Step(2, 2, 128, 16, [500, 30], [40, 100], BF16, SYM, 1)
+        joint = torch.zeros((145, 12, 128), dtype=BF16, device="cuda")       # queries 4, keys 2, values 2, and room
+        q, k, v = joint[2:142, :4], joint[2:142, 4:6], joint[2:142, 6:8]
+        q.copy_(s.q), k.copy_(s.k), v.copy_(s.v)
+        args = (q, k, v, s.cache, s.table.cuda(), offsets_of(s.new), ints(s.held), longest or s.longest, SYM)
+        want = s.call(fc, longest=longest or s.longest)
+        need = fc.chunk_attention_workspace_bytes(140, 2, 2, 2, 128, longest or s.longest)
+        before = joint.clone()
+        codes = s.cache[0].view(-1)
+        assert codes.numel() > 140 * 4 * 128 * 2 + 16
+        for out in (joint[2:142, 4:8], joint[2:142, 3:7], joint[2:142, 1:5], joint[3:143, :4], joint[1:141, 6:10], joint[2:142, 7:11],
+                    joint.view(-1)[8 * 1536:8 * 1536 + 140 * 512].view(140, 4, 128), codes[:140 * 4 * 128 * 2].view(BF16).view(140, 4, 128)):
+            with pytest.raises(ValueError):
+                fc.chunk_attention(*args, out=out)
+        big = torch.zeros(need + (1 << 20), dtype=torch.uint8, device="cuda")
+        y = big[:140 * 1024].view(BF16).view(140, 4, 128)
+        if need:
+            for space, out in ((big, y), (joint.view(-1).view(torch.uint8), None), (codes, None)):
+                with pytest.raises((ValueError, fc.FcError)):
+                    fc.chunk_attention(*args, out=out, workspace=space)
+        assert torch.equal(joint, before)
+        assert same(fc.chunk_attention(*args, out=joint[2:142, 8:12]), want)          # beside the others
+        assert same(fc.chunk_attention(*args, out=y, workspace=big[1 << 19:]), want)
+        assert fc.chunk_attention(*args, out=q) is q and same(q, want)
