@@ -425,7 +425,8 @@ FC_API int fc_chunk_attention(const void *q, int64_t q_token_stride, int64_t q_h
  * page_table, held: as above.  uses: int32 [pages], in how many rows of the table a page is named; 0 is a free page.  An entry outside
  * [0, pages) is no page.  A page that is not full of a sequence's tokens, and those reserved beyond them, are not shared but as
  * fc_pages_fork leaves them.  Everything is decided on the device, in whole numbers that do not depend on the order of execution.  Where a
- * model has a cache for each layer, tables and counts are common to them and fc_cache_copy is called for each.
+ * model has a cache for each layer, tables and counts are common to them and fc_cache_copy is called for each.  Arrays that a call writes, its
+ * workspace among them, overlap nothing else of it but where this says so (the Python calls refuse what does).
  *
  * fc_pages_fork makes the table of the next step: its row b is what row parents[b] of the old one holds, the first ceil(held / page)
  * entries, and -1 behind them; a parent outside [0, sequences) gives an empty row (held 0).  So rows are kept, copied (they share their

@@ -590,12 +590,6 @@ bool rows_apart(const Extent &a, const Extent &b)
 Extent extent_of(const Activation &a) { return {a.ptr, a.token * 2, (a.head * (a.heads() - 1) + a.dim()) * 2, a.tokens()}; }
 Extent extent_of(const at::Tensor &t) { return {t.data_ptr(), 0, (int64_t)t.nbytes(), 1}; }      // a dense one
 
-bool apart(const at::Tensor &a, const at::Tensor &b)
-{
-    const char *pa = (const char *)a.data_ptr(), *pb = (const char *)b.data_ptr();
-    return a.numel() == 0 || b.numel() == 0 || pa + a.nbytes() <= pb || pb + b.nbytes() <= pa;
-}
-
 bool table_of(const at::Tensor *t) { return t && t->dim() == 2 && t->size(1) <= 4096; }
 
 // (x, table, positions, interleaved, inverse, out)
@@ -990,6 +984,24 @@ struct Ints {
     }
 };
 
+bool apart(const at::Tensor &a, const at::Tensor &b)
+{
+    const char *pa = (const char *)a.data_ptr(), *pb = (const char *)b.data_ptr();
+    return a.numel() == 0 || b.numel() == 0 || pa + a.nbytes() <= pb || pb + b.nbytes() <= pa;
+}
+
+// Dense tensors: no two that are written have a byte in common, and none has with one that is read.  (pages.py refuses what does.)
+bool all_apart(std::initializer_list<const at::Tensor *> written, std::initializer_list<const at::Tensor *> read)
+{
+    for (auto w = written.begin(); w != written.end(); ++w) {
+        for (auto o = written.begin(); o != w; ++o)
+            if (!apart(**w, **o)) return false;
+        for (const at::Tensor *r : read)
+            if (!apart(**w, *r)) return false;
+    }
+    return true;
+}
+
 // (pages, held, uses, parents, page, out)
 PyObject *pages_fork(PyObject *, PyObject *const *a, Py_ssize_t n_args)
 {
@@ -1006,11 +1018,7 @@ PyObject *pages_fork(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     const int64_t rows = parents->size(0), width = table->size(1), count = uses->size(0);
     Ints<2> out;
     if (!held || !out.take(a[5], {{{rows, width}, {rows, -1}}}, *table, device)) return fallback();
-    if (out.given) {
-        for (const at::Tensor *old : {table, held, uses, parents})
-            if (!apart(*out.t[0], *old) || !apart(*out.t[1], *old)) return fallback();
-        if (!apart(*out.t[0], *out.t[1])) return fallback();
-    }
+    if (out.given && !all_apart({uses, out.t[0], out.t[1]}, {table, held, parents})) return fallback();
     const int sequences = (int)table->size(0);
     const int32_t *pt = (const int32_t *)table->data_ptr(), *ph = (const int32_t *)held->data_ptr(), *pp = (const int32_t *)parents->data_ptr();
     int32_t *pu = (int32_t *)uses->data_ptr(), *nt = out.ptr(0), *nh = out.ptr(1);
@@ -1054,6 +1062,7 @@ PyObject *pages_reserve(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     const at::Tensor *ws = space(a[6], lib.fc_pages_reserve_workspace_bytes(count), *table, device, own);
     Ints<3> out;
     if (!ws || !out.take(a[5], {{{sequences, -1}, {sequences, -1}, {1, -1}}}, *table, device)) return fallback();
+    if ((out.given || a[6] != Py_None) && !all_apart({table, uses, out.t[0], out.t[1], out.t[2], ws}, {held, offsets})) return fallback();
     int32_t *pt = (int32_t *)table->data_ptr(), *pu = (int32_t *)uses->data_ptr(), *source = out.ptr(0), *target = out.ptr(1), *lacking = out.ptr(2);
     const int32_t *ph = (const int32_t *)held->data_ptr(), *po = (const int32_t *)offsets->data_ptr();
     void *stream = stream_of(device), *pw = ws->data_ptr();
@@ -1083,7 +1092,9 @@ PyObject *pages_compact(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     const at::Tensor *ws = space(a[3], lib.fc_pages_compact_workspace_bytes(count), *table, device, own);
     Ints<5> out;
     if (!ws || !out.take(a[2], {{{sequences, width}, {count, -1}, {count / 2, -1}, {count / 2, -1}, {1, -1}}}, *table, device)) return fallback();
-    if (out.given && ((out.ptr(0) != table->data_ptr() && !apart(*out.t[0], *table)) || !apart(*out.t[1], *uses))) return fallback();
+    // (the table may be written in place)
+    if ((out.given || a[3] != Py_None) && !all_apart({out.t[0], out.t[1], out.t[2], out.t[3], out.t[4], ws}, {uses, out.ptr(0) == table->data_ptr() ? uses : table}))
+        return fallback();
     const int32_t *pt = (const int32_t *)table->data_ptr(), *pu = (const int32_t *)uses->data_ptr();
     int32_t *nt = out.ptr(0), *nu = out.ptr(1), *source = out.ptr(2), *target = out.ptr(3), *used = out.ptr(4);
     void *stream = stream_of(device), *pw = ws->data_ptr();

@@ -16,7 +16,7 @@ from __future__ import annotations
 
 from . import binding
 from .attention import _cache, _index
-from .binding import FcError, _check, _dev, _stream, _torch
+from .binding import FcError, _check, _dev, _meet, _stream, _torch
 
 
 def _table(pages, what="pages"):
@@ -44,10 +44,12 @@ def _results(out, shapes, like):
     return tuple(_index(t, name + " (out)", shape) for t, (name, shape) in zip(out, shapes))
 
 
-def _apart(a, b, what):
-    """a and b share no byte"""
-    if a.numel() and b.numel() and a.data_ptr() < b.data_ptr() + 4 * b.numel() and b.data_ptr() < a.data_ptr() + 4 * a.numel():
-        raise ValueError("%s must not overlap" % what)
+def _apart(written, read=()):
+    """no two (name, tensor) of `written` have a byte in common, and none has with one of `read`"""
+    for i, (name, t) in enumerate(written):
+        for other, u in (*written[:i], *read):
+            if _meet(t.view(-1), u.view(-1)):
+                raise ValueError("%s and %s must not overlap" % (name, other))
 
 
 def _space(workspace, need, like, what):
@@ -73,10 +75,8 @@ def pages_fork(pages, held, uses, parents, page: int, out=None):
         raise ValueError("parents must be int32 [rows], got shape %s" % (tuple(parents.shape),))
     rows = parents.shape[0]
     table, now = _results(out, [("pages", (rows, width)), ("held", (rows,))], pages)
-    for new in (table, now):
-        for old in (pages, held, uses, parents):
-            _apart(new, old, "old and new tables")
-    _apart(table, now, "old and new tables")
+    if out is not None:
+        _apart([("uses", uses), ("the new table", table), ("the new held", now)], [("pages", pages), ("held", held), ("parents", parents)])
     _check(binding.lib().fc_pages_fork(pages.data_ptr(), held.data_ptr(), sequences, width, page, uses.data_ptr(), count, parents.data_ptr(), rows,
                                        table.data_ptr(), now.data_ptr(), _stream()), "fc_pages_fork")
     return table, now
@@ -95,7 +95,11 @@ def pages_reserve(pages, held, uses, offsets, page: int, out=None, workspace=Non
     count = _count(uses)
     source, target, lacking = _results(out, [("source", (sequences,)), ("target", (sequences,)), ("lacking", (1,))], pages)
     L = binding.lib()
+    given = out is not None or workspace is not None
     workspace = _space(workspace, int(L.fc_pages_reserve_workspace_bytes(count)), pages, "fc_pages_reserve")
+    if given:
+        _apart([("pages", pages), ("uses", uses), ("source", source), ("target", target), ("lacking", lacking), ("workspace", workspace)],
+               [("held", held), ("offsets", offsets)])
     _check(L.fc_pages_reserve(pages.data_ptr(), held.data_ptr(), offsets.data_ptr(), sequences, width, page, uses.data_ptr(), count, source.data_ptr(),
                               target.data_ptr(), lacking.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream()), "fc_pages_reserve")
     return source, target, lacking
@@ -111,11 +115,12 @@ def pages_compact(pages, uses, out=None, workspace=None):
     sequences, width = _table(pages)
     count = _count(uses)
     results = _results(out, [("pages", (sequences, width)), ("uses", (count,)), ("source", (count // 2,)), ("target", (count // 2,)), ("used", (1,))], pages)
-    if results[0].data_ptr() != pages.data_ptr():
-        _apart(results[0], pages, "old and new tables")
-    _apart(results[1], uses, "old and new counts")
     L = binding.lib()
+    given = out is not None or workspace is not None
     workspace = _space(workspace, int(L.fc_pages_compact_workspace_bytes(count)), pages, "fc_pages_compact")
+    if given:
+        written = [*zip(("the new table", "the new counts", "source", "target", "used"), results), ("workspace", workspace)]
+        _apart(written, [("uses", uses)] + ([("pages", pages)] if results[0].data_ptr() != pages.data_ptr() else []))
     _check(L.fc_pages_compact(pages.data_ptr(), sequences, width, uses.data_ptr(), count, *[t.data_ptr() for t in results], workspace.data_ptr(),
                               workspace.numel(), _stream()), "fc_pages_compact")
     return results

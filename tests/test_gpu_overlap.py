@@ -99,3 +99,41 @@ def test_chunk_attention(fc, path):
         assert same(fc.chunk_attention(*args, out=joint[2:142, 8:12]), want)          # beside the others
         assert same(fc.chunk_attention(*args, out=y, workspace=big[1 << 19:]), want)
         assert fc.chunk_attention(*args, out=q) is q and same(q, want)
+
+
+def test_pages(fc, path):
+    def ints(values):
+        return torch.tensor(values, dtype=torch.int32, device="cuda")
+
+    pages, held, uses, offsets, parents = ints([[0, -1], [1, 2]]), ints([3, 20]), ints([1, 1, 1, 0, 0, 0, 0, 0]), ints([0, 15, 17]), ints([1, 0])
+    room = torch.zeros(64, dtype=torch.int32, device="cuda")
+    base = [t.clone() for t in (pages, held, uses, offsets, parents)]
+    part = lambda at, *shape: room[at:at + (shape[0] * (shape[1] if len(shape) > 1 else 1))].view(shape)      # noqa: E731
+    new = (part(0, 2, 2), part(4, 2))
+    for out in ((pages, new[1]), (new[0], held), (new[0], parents), (new[0], part(3, 2)), (uses[:4].view(2, 2), new[1])):
+        with pytest.raises(ValueError):
+            fc.pages_fork(pages, held, uses, parents, 16, out=out)
+    s, t, lack, space = part(0, 2), part(2, 2), part(4, 1), room[8:16].view(torch.uint8)
+    for out, work in (((s, s, lack), None), ((s, part(1, 2), lack), None), ((s, t, part(3, 1)), None), ((held, t, lack), None), ((s, uses[2:4], lack), None),
+                      ((s, t, offsets[:1]), None), ((s, pages[0], lack), None), ((s, t, lack), room[2:16].view(torch.uint8)), (None, uses.view(torch.uint8)),
+                      (None, torch.cat([room, room]).view(torch.uint8)[:8])):
+        with pytest.raises((ValueError, fc.FcError)):
+            fc.pages_reserve(pages, held, uses, offsets, 16, out=out, workspace=work)
+    five = (part(0, 2, 2), part(4, 8), part(12, 4), part(16, 4), part(20, 1))
+    space = room[24:40].view(torch.uint8)
+    for at, bad in ((0, uses[:4].view(2, 2)), (1, uses), (2, five[3]), (3, five[1][4:]), (4, uses[:1]), (2, pages.view(-1)), (4, pages.view(-1)[:1])):
+        with pytest.raises(ValueError):
+            fc.pages_compact(pages, uses, out=(*five[:at], bad, *five[at + 1:]))
+    for work in (room[16:32].view(torch.uint8), pages.view(torch.uint8).view(-1)[:16], uses.view(torch.uint8)):
+        with pytest.raises((ValueError, fc.FcError)):
+            fc.pages_compact(pages, uses, out=five, workspace=work)
+    assert all(torch.equal(a, b) for a, b in zip((pages, held, uses, offsets, parents), base)) and not room.any()
+    # what lies side by side passes, and the table of a compaction in place
+    fc.pages_fork(pages, held, uses, parents, 16, out=new)
+    assert new[0].tolist() == [[1, 2], [0, -1]] and new[1].tolist() == [20, 3] and uses.tolist() == [1, 1, 1, 0, 0, 0, 0, 0]
+    fc.pages_reserve(pages, held, uses, offsets, 16, out=(s, t, lack), workspace=space)
+    assert pages.tolist() == [[0, 3], [1, 2]] and lack.item() == 0 and uses.tolist() == [1, 1, 1, 1, 0, 0, 0, 0]
+    uses[0] = 0
+    pages[0, 0] = -1
+    got = fc.pages_compact(pages, uses, out=(pages, *five[1:]), workspace=space)
+    assert pages.tolist() == [[-1, 0], [1, 2]] and got[4].item() == 3 and got[1].tolist() == [1, 1, 1, 0, 0, 0, 0, 0]
