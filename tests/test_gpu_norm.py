@@ -264,3 +264,33 @@ def test_empty_calls_and_refusals(fc):
             fc.rms_norm(t[0], t[1], residual=t[2])
         with torch.no_grad():
             assert same(fc.rms_norm(t[0], t[1], residual=t[2])[0], fc.rms_norm(x, w, residual=r)[0])
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("wide_weight", [False, True])
+@pytest.mark.parametrize("tokens,hidden,groups", [(65543, 512, (64, 512)), (4099, 8192, (128, 8192)), (6561, 5120, (1024, 5120)), (2053, 16384, (64, 16384))])
+def test_more_than_the_caches_hold_equals_pieces_of_it(fc, dtype, wide_weight, tokens, hidden, groups):
+    """134 MB of rows and more are read and written past the caches, with one, two and four units a lane: the bits are those of 1000 rows at a time,
+    and of the formula"""
+    assert tokens * hidden * 4 > 1 << 27
+    x, r, w = inputs(tokens, hidden, dtype, hidden + 3)
+    w = w if wide_weight else w.to(dtype)
+    at = [0, 1, tokens // 2, tokens - 1]
+    y, h = normed(x[at], w, 1e-5, r[at])
+    cx, cr, cw = x.cuda(), r.cuda(), w.cuda()
+    print("norm past the caches", dtype, wide_weight, tokens, hidden, flush=True)
+    got, total = fc.rms_norm(cx, cw, 1e-5, residual=cr)
+    alone = fc.rms_norm(cx, cw, 1e-5)
+    assert same(got[at], y.to(dtype)) and same(total[at], h.to(dtype)) and same(alone[at], normed(x[at], w, 1e-5)[0].to(dtype))
+    parts = [slice(i, min(i + 1000, tokens)) for i in range(0, tokens, 1000)]
+    for p in parts:
+        a, b = fc.rms_norm(cx[p], cw, 1e-5, residual=cr[p])
+        assert torch.equal(a, got[p]) and torch.equal(b, total[p]) and torch.equal(fc.rms_norm(cx[p], cw, 1e-5), alone[p])
+    for quantizer in (SYM, FP8):
+        for group in groups:
+            codes, scales, sums = fc.rms_norm_quantize(cx, cw, 1e-5, group, quantizer, residual=cr)
+            want = coded(y, group, quantizer)
+            assert same(codes[at], want[0]) and same(scales[at], want[1]) and torch.equal(sums, total)
+            for p in parts:
+                a, b, _ = fc.rms_norm_quantize(cx[p], cw, 1e-5, group, quantizer, residual=cr[p])
+                assert torch.equal(a, codes[p]) and torch.equal(b, scales[p])

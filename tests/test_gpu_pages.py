@@ -373,3 +373,49 @@ def test_refusals(fc):
         with pytest.raises(fc.FcError):
             bad()
     assert t.tolist() == [[0, -1], [1, 2]] and u.tolist() == [1, 1, 1, 0]
+
+
+@pytest.mark.parametrize("needed", [[4096], [4097], [9001], [1, 4094], [1, 4096], [2000, 0, 2096, 1], [3000, 2999, 4000]])
+@pytest.mark.parametrize("lack", [0, 1])
+def test_reserve_lists_many_pages_in_the_workspace(fc, needed, lack):
+    """More fresh pages than are listed in LDS (4096), for one row and for several, the last ones of which also part with a shared page"""
+    page, pages, width, n = 16, 20011, max(needed) + 2, len(needed)
+    shared = pages - 1                                   # partly filled, of all rows but the first, and of one that is not in this step
+    table = [[shared if b else -1] + [-1] * (width - 1) for b in range(n)]
+    held = [5 if b else 0 for b in range(n)]
+    # a row with a partly filled page copies it: one of the pages that it needs
+    new = [(k - 1) * page + 11 if b and k else k * page for b, k in enumerate(needed)]
+    offsets = [sum(new[:b]) for b in range(n + 1)]
+    total = sum(needed)
+    rng = random.Random(total)
+    free = set(rng.sample(range(pages - 1), total - lack))
+    uses = [0 if p in free else 1 for p in range(pages)]
+    uses[shared] = n
+    want = reserve(table, held, uses, offsets, page)
+    assert want[4] == lack
+    need = fc.lib().fc_pages_reserve_workspace_bytes(pages)
+    space = torch.full((need + 4096,), 99, dtype=torch.uint8, device="cuda")
+    t, u = ints(table), ints(uses)
+    print("reserve many", needed, lack, flush=True)
+    source, target, lacking = fc.pages_reserve(t, ints(held), u, ints(offsets), page, workspace=space[:need])
+    assert lacking.tolist() == [lack] and bool((space[need:] == 99).all())
+    assert t.tolist() == want[0] and u.tolist() == want[1] and source.tolist() == want[2] and target.tolist() == want[3]
+
+
+@pytest.mark.parametrize("heads,page,dim,pages", [(5, 32, 128, 7000), (1, 16, 64, 140000), (8, 16, 128, 9000)])
+def test_copy_of_more_than_the_caches_hold(fc, heads, page, dim, pages):
+    """134 MB and more are copied past the caches; pages whose last 16 KB are not whole, pages smaller than that, and pairs that name no page"""
+    cache = cache_of(pages, heads, page, dim, pages)
+    half = pages // 2
+    g = torch.Generator().manual_seed(3)
+    source, target = torch.randint(0, half, (half,), generator=g), half + torch.randperm(half, generator=g)
+    for at, s, t in ((0, -1, half), (half // 2, 3, -1), (half - 1, pages, half + 1), (7, 1, pages)):
+        source[at], target[at] = s, t
+    assert half * heads * page * dim * 2 > 1 << 27
+    there = (source >= 0) & (source < half) & (target >= 0) & (target < pages)
+    want = [c.clone() for c in cache]
+    for c in want:
+        c[target[there].cuda()] = c[source[there].cuda()]
+    print("copy", heads, page, dim, pages, flush=True)
+    fc.cache_copy(cache, source.to(torch.int32).cuda(), target.to(torch.int32).cuda())
+    assert all(torch.equal(a, b) for a, b in zip(cache, want))
