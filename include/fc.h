@@ -406,8 +406,10 @@ FC_API int fc_prompt_attention(const void *q, int64_t q_token_stride, int64_t q_
  * its new tokens, lie within 2^56 of each other, pages of zeros alone aside (those that fc_cache_append makes of binary16 values, and 1, within 2^43); a
  * lower one may be taken for a higher.
  * What the pages hold beyond the held tokens has no influence, and no bit of a row depends on later tokens, infinities and NaN included.
- * longest: the most tokens, held and new, of a sequence; it only sizes the launch.  tokens * group is below 2^31 - 1024.  out may be q where their
- * strides are equal, and otherwise overlaps nothing that is read (the Python call refuses what does; rows may lie between other rows).
+ * longest: the most tokens, held and new, of a sequence; it sizes the launch and the workspace, and sequences beyond it are computed all the same.  The
+ * order of sums, and so the last bits of a row, depend on it and on the other sequences of the call; the same call gives the same bits.
+ * tokens * group is below 2^31 - 1024.  out may be q where their strides are equal, and otherwise overlaps nothing that is read (the Python call refuses
+ * what does; rows may lie between other rows).
  * workspace: fc_chunk_attention_workspace_bytes(...) bytes, 16-byte aligned, contents unspecified; may be NULL if that is 0.
  */
 FC_API size_t fc_chunk_attention_workspace_bytes(int64_t tokens, int sequences, int heads, int group, int dim, int64_t longest);

@@ -13,14 +13,16 @@
 //   other.  Binary16 has not the exponents: c is sv / unit, where the unit of the sums is a power of two, common to the workgroup.
 //   The unit of a row's weights is its running maximum.  Binary16 has not the range for all that are lower: there it follows a tile's
 //   largest score up and down when that is kSlack away, and the largest is put at 2^kBias (kReach below the row's largest at most).
+//   Weights are rounded to the type before the products with V, as over prompts: the matrix instructions take both operands in 16 bits, and a
+//   second product for the bits that are cut off would make them half as many again.  The sum that divides them is of the unrounded ones.
 // All work of the call, in units of a tile of 64 tokens for a workgroup's rows, is cut into equal ranges, one a workgroup: contexts of any lengths
 // end together.  Rows that were cut are joined by a second kernel, from results that are normalised.
-//   What bounds it.  2048 tokens over 65531, 16 query heads over 2 of 128 in E4M3, bfloat16: 1.10 ms, 1.02 PFLOP/s, where a product of 16384^3
-//   reaches 1.36: the power that the card has, for the time stays where it is when waits are added to the loop (1.76 GHz, the matrix
-//   units busy 41% of it; with 10% more cycles 1.94 GHz and as long).  A tile takes 4900 cycles, of which 2048 are the matrix units',
-//   and 2570 of vector instructions are beside them.  512 tokens over 8191: 59 us, of which 11 are the join's (it reads 34 MB that others wrote),
-//   8 the way to the first product and 34 the tiles.  Nine sequences of 4099 tokens over up to 4000 in signed codes, binary16, 8 heads of 4:
-//   239 us, 14 of them the join's and about 6 for the beginning and the end of each of three items.  17 tokens over 129: 17 us, in
+//   What bounds it.  2048 tokens over 65531, 16 query heads over 2 of 128 in E4M3, bfloat16: 1.09 to 1.17 ms by card, 1.02 PFLOP/s, where a product
+//   of 16384^3 reaches 1.36.  A tile takes 4580 cycles (2.25 GHz), which is the sum of 2048 of the matrix units and 2500 of vector instructions: the two
+//   wavefronts of a SIMD are mostly at the same of both.  512 tokens over 8191: 60 us, of which 43 are a range's (7.5 the way to the first tile, 35 the
+//   16.6 tiles and their end, 2.3 GHz), 10 the join's (34 MB that others wrote, 3.3 TB/s) and the rest the launches'; the first calls after a pause 68, at 1.95
+//   GHz.  Nine sequences of 4099 tokens over up to 4000 in signed codes, binary16, 8 heads of 4: 232 to 253 us, 13 of them the join's; a tile with
+//   what surrounds the three items of a range 5300 cycles, 1920 of the matrix units and 2890 of vector instructions.  17 tokens over 129: 17 us, in
 //   eight workgroups and the join as in one workgroup a head; much of it waits for the code itself, which every launch fetches anew.
 //   Taken one after the other: operands ahead of their products (1.59 -> 1.42 ms for the first of these), eight wavefronts over three tiles (1.14, the
 //   batch 452 -> 420 us), what surrounds an item counted as work (420 -> 270), items without a division, lanes without LDS (270 -> 240).  Two halves of

@@ -3,11 +3,12 @@
 //     h = x + r,  d = fp32(1 / sqrt(sum h^2 / hidden + eps)),  y = (h d) w
 //     codes: s = max|y| / top over a group (1 if that is below FLT_MIN),  code = round(y (1 / s))
 // in fp32 with IEEE divides, each operation rounded to nearest even; the sum of squares, the division and the root are in 64 bits.  A
-// square of an fp32 number has 48 bits, so the sum of a row is exact but for its last few bits and d does not depend on the order: one
-// definition for all forms of the launch, and codes next to a border are the same in each.
+// square of an fp32 number has 48 bits, so the sum of a row is exact but for its last few bits, and d does not depend on the order but where two
+// such sums lie on either side of a border between fp32 numbers: nearly one definition for all forms of the launch.
 // A workgroup has a row, from its first read to the last store, in registers; wavefronts add up in LDS, once for the sum and, with scales that
-// they share, once for the largest value.  Memory bounds it: 8192 rows of 8192 with a residual, 537 MB, 87.5 us, 6.1 TB/s; 16383 rows of 5120 into
-// E4M3 with a scale a token, 587 MB, 107 us, 5.5 TB/s, where the two joins of a row weigh.  One token is bound by the call: 8 x 8192 4.4 us.
+// they share, once for the largest value.  Memory bounds it: 8192 rows of 8192 with a residual, 537 MB, 88 us, 6.1 TB/s; 16383 rows of 5120 into
+// E4M3 with a scale a token, 587 MB, 101 to 104 us, 5.8 to 5.6 TB/s, where the two joins of a row weigh.  Few tokens are bound by the call: 8 x 8192
+// 4.9 us, of which the kernel takes 3.5.
 #include "fc_attn.hpp"
 
 namespace fc {
